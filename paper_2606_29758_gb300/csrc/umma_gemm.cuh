@@ -41,6 +41,7 @@ struct Sched {
   int num_units;  // m_blocks * splits
   int num_kb;     // ceil(K / 64)
   int clear;      // this launch opens a library call: it zeroes the status words
+  int first;      // k blocks (Pair::kSumK) or m blocks (Pair::kTwoM) of the first of two operand sets
 
   __device__ __forceinline__ void unit(int u, int& m_blk, int& split, int& n0, int& n1) const {
     const int per_band = band_m * splits;
@@ -105,20 +106,42 @@ constexpr size_t gemm_smem_bytes() {   // + alignment slack
   return sizeof(GemmSmemT<HALVES, EpiWarps<Epi>::value, Epi::kStageBytes>) + 1024;
 }
 
+// Products with two operand sets in one launch:
+//   kTwoB  D1 = A B1^T and D2 = A B2^T side by side: a tile is 128 columns of each (columns 0..127 and 128..255 of
+//          the accumulator), and the epilogue gets the same 32-column slice of both (a gate and what it gates)
+//   kSumK  D = A1 B1^T + A2 B2^T: the K loop runs over the first set's k blocks, then over the second's
+//   kTwoM  D1 = A1 B^T and D2 = A2 B^T below each other, each with an output of its own: m blocks from
+//          Sched::first on belong to the second
+enum Pair { kNoPair = 0, kTwoB = 1, kSumK = 2, kTwoM = 3 };
+
+// An epilogue with kOwnStore stages and stores its slices itself: chunk_own() gets the slice (with kTwoB those of
+// both products), what load_ahead() loaded beside the accumulator, the warp's staging buffer and its count of
+// stores, the row of its lane 0 and the output maps.
+template <class Epi, class = void>
+struct OwnStore {
+  static constexpr bool value = false;
+};
+template <class Epi>
+struct OwnStore<Epi, decltype(static_cast<void>(Epi::kOwnStore))> {
+  static constexpr bool value = Epi::kOwnStore;
+};
+
 // tmC: the output map of epilogues that store through TMA (unused by the others). An epilogue's
 // begin_unit / end_unit see the unit's split index times the column groups (1 with 4 epilogue
 // warps, 2 with 8) plus the thread's column group.
-template <bool A_MN, bool B_MN, class Epi, int HALVES = 1>
-__global__ void __launch_bounds__(64 + 32 * EpiWarps<Epi>::value, 1)
-    umma_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                     const __grid_constant__ CUtensorMap tmC, const Sched sched, const typename Epi::Params ep,
-                     uint32_t* status, uint64_t timeout_ns) {
+template <bool A_MN, bool B_MN, class Epi, int HALVES, int PAIR>
+__device__ __forceinline__ void umma_gemm_body(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC,
+                                               const CUtensorMap& tmA2, const CUtensorMap& tmB2,
+                                               const CUtensorMap& tmC2, const CUtensorMap& tmC3, const Sched& sched,
+                                               const typename Epi::Params& ep, uint32_t* status, uint64_t timeout_ns) {
+  static_assert(PAIR != kTwoB || (!B_MN && OwnStore<Epi>::value), "two B operands: K-major, epilogue of its own");
+  constexpr int TN = PAIR == kTwoB ? kBN / 2 : kBN;   // output columns per tile
   using Cfg = GemmCfg<HALVES>;
   constexpr int S = Cfg::kStagesH;
   constexpr int NB = Cfg::kAccBufs;
   constexpr int EW = EpiWarps<Epi>::value;
   constexpr int G = EW / 4;                 // column groups per TMEM lane quarter
-  constexpr int CPG = (kBN / 32) / G;       // 32-column chunks per group
+  constexpr int CPG = (TN / 32) / G;        // 32-column chunks per group
   using Smem = GemmSmemT<HALVES, EW, Epi::kStageBytes>;
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -169,18 +192,25 @@ __global__ void __launch_bounds__(64 + 32 * EpiWarps<Epi>::value, 1)
             const uint32_t ph = (kc / S) & 1u;
             if (!mbar_wait(&sm.empty[s], ph ^ 1u, timeout_ns, abort)) { ok = false; break; }
             mbar_arrive_expect_tx(&sm.full[s], Cfg::kABytes + kTileBBytes);
-            const int m0 = m_blk * Cfg::kRows, nn0 = nb * kBN, k0 = kb * kBK;
+            const bool second = (PAIR == kSumK && kb >= sched.first) || (PAIR == kTwoM && m_blk >= sched.first);
+            const CUtensorMap* const mapA = second ? &tmA2 : &tmA;
+            const CUtensorMap* const mapB = PAIR == kSumK && second ? &tmB2 : &tmB;
+            const int m0 = (PAIR == kTwoM && second ? m_blk - sched.first : m_blk) * Cfg::kRows, nn0 = nb * TN;
+            const int k0 = (PAIR == kSumK && second ? kb - sched.first : kb) * kBK;
             if (A_MN) {
               for (int i = 0; i < Cfg::kRows / 64; ++i)
-                tma_load_2d(sm.a[s] + i * (kBK * 128), &tmA, &sm.full[s], m0 + i * 64, k0);
+                tma_load_2d(sm.a[s] + i * (kBK * 128), mapA, &sm.full[s], m0 + i * 64, k0);
             } else {
-              tma_load_2d(sm.a[s], &tmA, &sm.full[s], k0, m0);   // box of kRows rows
+              tma_load_2d(sm.a[s], mapA, &sm.full[s], k0, m0);   // box of kRows rows
             }
-            if (B_MN) {
-              for (int i = 0; i < kBN / 64; ++i)
-                tma_load_2d(sm.b[s] + i * (kBK * 128), &tmB, &sm.full[s], nn0 + i * 64, k0);
-            } else {
+            if (PAIR == kTwoB) {   // boxes of 128 rows
               tma_load_2d(sm.b[s], &tmB, &sm.full[s], k0, nn0);
+              tma_load_2d(sm.b[s] + kTileBBytes / 2, &tmB2, &sm.full[s], k0, nn0);
+            } else if (B_MN) {
+              for (int i = 0; i < kBN / 64; ++i)
+                tma_load_2d(sm.b[s] + i * (kBK * 128), mapB, &sm.full[s], nn0 + i * 64, k0);
+            } else {
+              tma_load_2d(sm.b[s], mapB, &sm.full[s], k0, nn0);
             }
           }
         }
@@ -285,11 +315,15 @@ __global__ void __launch_bounds__(64 + 32 * EpiWarps<Epi>::value, 1)
     const int grp = ew >> 2;                    // column group: chunks [grp * CPG, grp * CPG + CPG)
     const int row_in_tile = quad * 32 + lane;
     typename Epi::State st[HALVES];             // a thread owns row r of each half
+    [[maybe_unused]] uint32_t stored = 0;       // slices this warp has stored (OwnStore)
     uint32_t tile = 0;
     bool ok = true;
     for (int u = blockIdx.x; ok && u < sched.num_units; u += gridDim.x) {
       int m_blk, split, n0, n1;
       sched.unit(u, m_blk, split, n0, n1);
+      const bool second = PAIR == kTwoM && m_blk >= sched.first;
+      const CUtensorMap* const mapC = second ? &tmC2 : &tmC;
+      if (second) m_blk -= sched.first;
       const int row0 = m_blk * Cfg::kRows + row_in_tile;
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) Epi::begin_unit(ep, st[h], row0 + h * kBM, split * G + grp);
@@ -328,10 +362,28 @@ __global__ void __launch_bounds__(64 + 32 * EpiWarps<Epi>::value, 1)
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                  Epi::store(ep, &tmC, buf, col0, m_blk * Cfg::kRows + h * kBM + quad * 32);
+                  Epi::store(ep, mapC, buf, col0, m_blk * Cfg::kRows + h * kBM + quad * 32);
                   bulk_commit_group();
                 }
               }
+            }
+          } else if constexpr (OwnStore<Epi>::value) {
+#pragma unroll 1
+            for (int c = grp * CPG; c < grp * CPG + CPG; ++c) {
+              uint32_t r[32], r2[PAIR == kTwoB ? 32 : 1];
+              const int col0 = nb * TN + c * 32;
+              typename Epi::Ahead ahead;
+              Epi::load_ahead(ep, row, col0, ahead);
+              tmem_ld32(t_row + c * 32, r);
+              if constexpr (PAIR == kTwoB) tmem_ld32(t_row + TN + c * 32, r2);
+              tmem_ld_wait();
+              if (c == grp * CPG + CPG - 1) {
+                tc_fence_before();
+                mbar_arrive(&sm.tempty[HALVES == 2 ? h : acc]);
+              }
+              if (col0 < Epi::cols(ep))
+                Epi::chunk_own(ep, row, col0, r, r2, ahead, sm.stage[ew], stored, lane,
+                               m_blk * Cfg::kRows + h * kBM + quad * 32, &tmC, &tmC2, &tmC3);
             }
           } else {
 #pragma unroll 1
@@ -356,7 +408,7 @@ __global__ void __launch_bounds__(64 + 32 * EpiWarps<Epi>::value, 1)
                   fence_proxy_async_smem();
                   __syncwarp();
                   if (lane == 0) {
-                    Epi::store(ep, &tmC, buf, col0, m_blk * Cfg::kRows + h * kBM + quad * 32);
+                    Epi::store(ep, mapC, buf, col0, m_blk * Cfg::kRows + h * kBM + quad * 32);
                     bulk_commit_group();
                   }
                 }
@@ -386,6 +438,25 @@ __global__ void __launch_bounds__(64 + 32 * EpiWarps<Epi>::value, 1)
     tc_fence_after();
     tmem_dealloc(tmem_base, kTmemCols);
   }
+}
+
+template <bool A_MN, bool B_MN, class Epi, int HALVES = 1>
+__global__ void __launch_bounds__(64 + 32 * EpiWarps<Epi>::value, 1)
+    umma_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                     const __grid_constant__ CUtensorMap tmC, const Sched sched, const typename Epi::Params ep,
+                     uint32_t* status, uint64_t timeout_ns) {
+  umma_gemm_body<A_MN, B_MN, Epi, HALVES, kNoPair>(tmA, tmB, tmC, tmA, tmB, tmC, tmC, sched, ep, status, timeout_ns);
+}
+
+// The same with a second operand set (Pair), or an epilogue that writes up to three outputs.
+template <bool A_MN, bool B_MN, class Epi, int HALVES, int PAIR>
+__global__ void __launch_bounds__(64 + 32 * EpiWarps<Epi>::value, 1)
+    umma_gemm_two_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                         const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmA2,
+                         const __grid_constant__ CUtensorMap tmB2, const __grid_constant__ CUtensorMap tmC2,
+                         const __grid_constant__ CUtensorMap tmC3, const Sched sched, const typename Epi::Params ep,
+                         uint32_t* status, uint64_t timeout_ns) {
+  umma_gemm_body<A_MN, B_MN, Epi, HALVES, PAIR>(tmA, tmB, tmC, tmA2, tmB2, tmC2, tmC3, sched, ep, status, timeout_ns);
 }
 
 // =============================================================================================
