@@ -441,6 +441,113 @@ int ps_lmhead_ppo_fwd_noalloc(int64_t N, int d, int V, int dtype, const void* Hp
                               double* loss, float* lse, float* logp, float* ratio, float* coef,
                               float* row_loss, ps_stream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Row-wise operators of a policy block over packed rows: what carries dH from the head into
+ * the policy's body and prepares its rows for the head. The paper has no counterpart (its
+ * policies are ordinary transformers); rows are those of ps_pack_prefixes, and row_traj and
+ * row_pos are its outputs. Row pitches (ld*) are in elements; every row of a tensor-core
+ * operand and of the q/k rows starts on a 16-byte boundary.
+ *
+ * ps_gated_ffn_fwd / ps_gated_ffn_bwd -- the gated feed-forward block.
+ *
+ *   G = X Wg^T, U = X Wu^T, A = s(G) U, Y = A Wd^T;  s(x) = x / (1 + e^-x) (PS_ACT_SILU) or
+ *   x Phi(x) with the normal distribution function Phi (PS_ACT_GELU);
+ *   dA = dY Wd, dU = dA s(G), dG = dA U s'(G), dX = dG Wg + dU Wu, dWg = dG^T X,
+ *   dWu = dU^T X, dWd = dY^T A.
+ * X, Y, dY [N][d] bf16, Wg, Wu [F][d] and Wd [d][F] bf16, contiguous (the halves of one
+ * [2F][d] buffer will do); f32 accumulation. A, dG and dU are rounded to bf16 between the
+ * products. PS_DTYPE_F32 returns PS_ERR_UNSUPPORTED.
+ * store: NULL (no backward follows; A lies in the workspace), or ps_gated_ffn_store_size(N, F)
+ *   bytes, 16-byte aligned, that the forward fills and the backward of the same N, F, X and
+ *   weights consumes: A [N][F] bf16, then, each from the next 256-byte boundary, P = U s'(G)
+ *   and Q = s(G) [N][F] f16, relative to a power of two per row and 32 columns, and their
+ *   exponents [ceil(F/32)][N] (6.1 bytes per row and column of F). The backward overwrites P
+ *   and Q with dG and dU (bf16): one backward per forward; calling it twice on one store is
+ *   an error the library cannot see. Too small: PS_ERR_WORKSPACE.
+ * Backward outputs: dX [N][d], dWg, dWu [F][d], dWd [d][F], in dx_dtype and dw_dtype (bf16:
+ *   rounded once from the f32 sums; f32). NULL skips dX, dWd, or dWg with dWu. Flags:
+ *   PS_DW_ACCUMULATE and PS_DH_ACCUMULATE (dX) add to what the buffers hold, f32 only (a sum
+ *   over calls in bf16 would lose its small terms: PS_ERR_UNSUPPORTED). N = 0 zeroes dW.
+ * Limits: d, F >= 8 and multiples of 8, 0 <= N <= 2^30, 16-byte aligned pointers, pitches a
+ *   multiple of 16 bytes.
+ * ------------------------------------------------------------------------- */
+enum { PS_ACT_SILU = 0, PS_ACT_GELU = 1 };
+size_t ps_gated_ffn_store_size(int64_t N, int F);
+size_t ps_gated_ffn_fwd_workspace_size(int64_t N, int F, int with_store);
+int ps_gated_ffn_fwd(int64_t N, int d, int F, int dtype, int act, const void* X, int64_t ldx,
+                     const void* Wg, const void* Wu, const void* Wd, void* Y, int64_t ldy,
+                     void* store, size_t store_bytes, void* ws, size_t ws_bytes, ps_stream_t stream);
+size_t ps_gated_ffn_bwd_workspace_size(void);
+int ps_gated_ffn_bwd(int64_t N, int d, int F, int dtype, const void* dY, int64_t lddy,
+                     const void* X, int64_t ldx, const void* Wg, const void* Wu, const void* Wd,
+                     void* store, size_t store_bytes, void* dX, int64_t lddx, int dx_dtype,
+                     void* dWg, void* dWu, void* dWd, int dw_dtype, int flags,
+                     void* ws, size_t ws_bytes, ps_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * ps_qk_norm_rope_fwd / ps_qk_norm_rope_bwd -- root-mean-square norms of queries and keys per
+ * head and the rotary positions, in one pass.
+ *
+ *   n = x r g, r = (mean over the head of x^2 + eps)^(-1/2), g the gain (gq, gk; NULL: 1);
+ *   the first R of a head's D dims are turned in pairs by the angle of the row's position:
+ *   (a, b) -> (a cos - b sin, a sin + b cos), pair i = dims (i, i + R/2) (PS_ROPE_HALF) or
+ *   (2i, 2i + 1) (PS_ROPE_EVEN), cos and sin from table[pos - pos_base][i].
+ *   Backward: dn = the turn back of dy, dg = sum over rows and heads of dn x r,
+ *   dx = r (g dn - x r^2 mean(g dn x)).
+ * q [N][Hq][D], k [N][Hk][D] (row pitches ldq, ldk, so they may lie in one projection's rows;
+ *   bf16 or f32, outputs and gains alike), pos [N] int32 (row_pos with pos_base = 1), table
+ *   [T][R/2][2] f32 (ps_rope_table). A position outside [pos_base, pos_base + T) sets
+ *   PS_DEV_BAD_LENGTH and gives NaN in the row's rotated dims (forward) or in the row's
+ *   gradients and the gain gradients (backward). R = 0: norms only, pos and table not read.
+ *   Hq or Hk may be 0 (that side's pointers are not read). Outputs may be the inputs (same
+ *   pointer and pitch), else must not overlap them.
+ * Backward: dq_out, dk_out are the gradients of the outputs, q, k the forward's inputs; dq, dk
+ *   in their type; dgq, dgk [D] f32 or NULL (PS_DW_ACCUMULATE adds to them; summed in a fixed
+ *   order, reruns are bit-identical). N = 0 zeroes dgq and dgk.
+ * Workspace: 256 bytes for the forward and for a backward without gain gradients, else
+ *   ps_qk_norm_rope_workspace_size(D).
+ * Limits: 16 <= D <= 512, D and R multiples of 16, 0 <= R <= D, Hq, Hk <= 65536, eps >= 0,
+ *   16-byte aligned pointers and pitches.
+ * ps_rope_table: table[t][i] = (cos, sin) of t theta^(-2i/R), in f64 and rounded once;
+ *   16 <= R <= 512, a multiple of 16; 16-byte aligned; no workspace.
+ * ------------------------------------------------------------------------- */
+enum { PS_ROPE_HALF = 0, PS_ROPE_EVEN = 1 };
+int ps_rope_table(int T, int R, double theta, float* table, ps_stream_t stream);
+size_t ps_qk_norm_rope_workspace_size(int D);
+int ps_qk_norm_rope_fwd(int64_t N, int Hq, int Hk, int D, int R, int dtype, int layout,
+                        const void* q, int64_t ldq, const void* k, int64_t ldk,
+                        const void* gq, const void* gk, double eps, const int32_t* pos,
+                        int pos_base, int T, const float* table, void* q_out, int64_t ldqo,
+                        void* k_out, int64_t ldko, void* ws, size_t ws_bytes, ps_stream_t stream);
+int ps_qk_norm_rope_bwd(int64_t N, int Hq, int Hk, int D, int R, int dtype, int layout,
+                        const void* dq_out, int64_t lddqo, const void* dk_out, int64_t lddko,
+                        const void* q, int64_t ldq, const void* k, int64_t ldk,
+                        const void* gq, const void* gk, double eps, const int32_t* pos,
+                        int pos_base, int T, const float* table, void* dq, int64_t lddq,
+                        void* dk, int64_t lddk, float* dgq, float* dgk, int flags,
+                        void* ws, size_t ws_bytes, ps_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * ps_dropout_rows -- dropout of a branch's rows, added to the residual rows.
+ *
+ *   y[i][c] = res[i][c] + (u(i, c) >= K ? x[i][c] 2^16 / (2^16 - K) : 0),  K = floor(2^16 p + 1/2)
+ * (res NULL: 0). u(i, c) are 16 bits of Philox4x32-10 with key (seed's low word, its high word) and
+ * counter (site 2^16 + c / 8, row_pos[i], traj_base + row_traj[i] mod 2^32, step): of its four
+ * output words, the low (even) or high (odd) half of word (c mod 8) / 2. So p is held as K / 2^16, and
+ * kept values are scaled by exactly its survival's inverse; no mask is stored; and a token's mask depends
+ * on its completion, position, step and site (the branch or layer), not on the cutoffs, the packing or
+ * the shard. The backward is the same call on dy without res (the residual's gradient is dy
+ * itself). A dropped value counts as 0 whatever it is (NaN and infinities too).
+ * x, res, y [N][d] bf16 or f32, any pitch >= d and any alignment of whole elements (16-byte rows
+ * of whole blocks of 8 are fastest); y may be x or res (same pointer and pitch). row_traj, row_pos
+ * [N] int32 as from ps_pack_prefixes. 0 <= p < 1 (K = 2^16 is refused), 0 <= step, traj_base < 2^32,
+ * 0 <= site < 2^16, 1 <= d <= 2^19. No workspace; asynchronous on `stream`.
+ * ------------------------------------------------------------------------- */
+int ps_dropout_rows(int64_t N, int d, int dtype, const void* x, int64_t ldx, const void* res,
+                    int64_t ldr, const int32_t* row_traj, const int32_t* row_pos,
+                    int64_t traj_base, double p, uint64_t seed, uint64_t step, int site,
+                    void* y, int64_t ldy, ps_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,6 +21,8 @@ Modules, in the order of the update pass:
             binarisation of continuous rewards (Appendix G), the budgeted monotone
             design with its cap (Section 3.3, Appendix F), the Section 4 variants,
             and the integer masses the sampler takes.
+  block     row-wise operators of a policy block over packed rows (the gated feed-forward
+            block, norms of queries and keys with rotary positions, dropout), from their formulas.
 
 Every function is pinned by the tests in tests/test_oracle_*.py against facts
 fixed by the paper or by mathematics (finite differences, exact enumeration of

@@ -38,8 +38,13 @@ EXPORTS = [
     "ps_lmhead_score_proxy_workspace_size", "ps_lmhead_score_proxy",
     "ps_design_cutoffs_workspace_size", "ps_design_cutoffs",
     "ps_reward_uncertainty_workspace_size", "ps_reward_uncertainty", "ps_binarize_rewards",
+    "ps_gated_ffn_store_size", "ps_gated_ffn_fwd_workspace_size", "ps_gated_ffn_fwd",
+    "ps_gated_ffn_bwd_workspace_size", "ps_gated_ffn_bwd",
+    "ps_rope_table", "ps_qk_norm_rope_workspace_size", "ps_qk_norm_rope_fwd", "ps_qk_norm_rope_bwd", "ps_dropout_rows",
 ]
 PS_DESIGN_OPTIMIZED, PS_DESIGN_HEURISTIC, PS_DESIGN_UNIFORM, PS_DESIGN_TIME_PRIOR, PS_DESIGN_FIXED = range(5)
+PS_ACT_SILU, PS_ACT_GELU = 0, 1
+PS_ROPE_HALF, PS_ROPE_EVEN = 0, 1
 
 
 __all__ = EXPORTS + [
@@ -49,7 +54,7 @@ __all__ = EXPORTS + [
     "PS_DTYPE_BF16", "PS_DTYPE_F32", "PS_ADV_CENTERED", "PS_ADV_GROUP_NORM", "PS_DW_OVERWRITE",
     "PS_DW_ACCUMULATE", "PS_DH_ACCUMULATE", "PS_DEV_BAD_PMF", "PS_DEV_BAD_LENGTH", "PS_DEV_CAPACITY", "PS_DEV_BAD_TOKEN",
     "PS_DEV_TIMEOUT", "PS_DEV_NONFINITE", "PS_DESIGN_OPTIMIZED", "PS_DESIGN_HEURISTIC", "PS_DESIGN_UNIFORM",
-    "PS_DESIGN_TIME_PRIOR", "PS_DESIGN_FIXED",
+    "PS_DESIGN_TIME_PRIOR", "PS_DESIGN_FIXED", "PS_ACT_SILU", "PS_ACT_GELU", "PS_ROPE_HALF", "PS_ROPE_EVEN",
 ]
 
 
@@ -110,6 +115,22 @@ _SIGS = {
     "ps_design_cutoffs": (_i32, [_i32, _i32, _i32, _vp, _vp, _vp, _f64, _i32, _f64, _vp, _vp, _vp, _sz, _vp]),
     "ps_lmhead_ppo_fwd_noalloc": (_i32, [_i64, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _f64, _f64,
                                          _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "ps_gated_ffn_store_size": (_sz, [_i64, _i32]),
+    "ps_gated_ffn_fwd_workspace_size": (_sz, [_i64, _i32, _i32]),
+    "ps_gated_ffn_fwd": (_i32, [_i64, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _sz, _vp, _sz,
+                                _vp]),
+    "ps_gated_ffn_bwd_workspace_size": (_sz, []),
+    "ps_gated_ffn_bwd": (_i32, [_i64, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _sz, _vp, _i64, _i32,
+                                _vp, _vp, _vp, _i32, _i32, _vp, _sz, _vp]),
+    "ps_rope_table": (_i32, [_i32, _i32, _f64, _vp, _vp]),
+    "ps_qk_norm_rope_workspace_size": (_sz, [_i32]),
+    "ps_qk_norm_rope_fwd": (_i32, [_i64, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _f64, _vp,
+                                   _i32, _i32, _vp, _vp, _i64, _vp, _i64, _vp, _sz, _vp]),
+    "ps_qk_norm_rope_bwd": (_i32, [_i64, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64,
+                                   _vp, _vp, _f64, _vp, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _sz,
+                                   _vp]),
+    "ps_dropout_rows": (_i32, [_i64, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _f64, _u64, _u64, _i32, _vp,
+                               _i64, _vp]),
 }
 
 
@@ -361,6 +382,73 @@ def ps_lmhead_ppo_bwd_vocab_shard_from_store(N, d, Vs, v0, V, dtype, Hpk, W_shar
                                                         _nbytes(store), _ptr(dH), _ptr(dW_shard), flags, _ptr(ws),
                                                         _nbytes(ws), _stream(stream))
     _check(rc, "ps_lmhead_ppo_bwd_vocab_shard_from_store")
+
+
+def _ld(t) -> int:
+    """Row pitch of a 2-D tensor in elements (0 for None; a single row's stride says nothing)."""
+    return 0 if t is None else t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def ps_gated_ffn_store_size(N: int, F: int) -> int:
+    return lib().ps_gated_ffn_store_size(N, F)
+
+
+def ps_gated_ffn_fwd_workspace_size(N: int, F: int, with_store: bool) -> int:
+    return lib().ps_gated_ffn_fwd_workspace_size(N, F, int(with_store))
+
+
+def ps_gated_ffn_fwd(N, d, F, dtype, act, X, Wg, Wu, Wd, Y, store, ws, stream=None):
+    """X and Y: 2-D tensors whose row pitch is taken from the tensor."""
+    rc = lib().ps_gated_ffn_fwd(N, d, F, dtype, act, _ptr(X), _ld(X), _ptr(Wg), _ptr(Wu), _ptr(Wd), _ptr(Y), _ld(Y),
+                                _ptr(store), 0 if store is None else _nbytes(store), _ptr(ws), _nbytes(ws),
+                                _stream(stream))
+    _check(rc, "ps_gated_ffn_fwd")
+
+
+def ps_gated_ffn_bwd_workspace_size() -> int:
+    return lib().ps_gated_ffn_bwd_workspace_size()
+
+
+def ps_gated_ffn_bwd(N, d, F, dtype, dY, X, Wg, Wu, Wd, store, dX, dx_dtype, dWg, dWu, dWd, dw_dtype, flags, ws,
+                     stream=None):
+    rc = lib().ps_gated_ffn_bwd(N, d, F, dtype, _ptr(dY), _ld(dY), _ptr(X), _ld(X), _ptr(Wg), _ptr(Wu), _ptr(Wd),
+                                _ptr(store), 0 if store is None else _nbytes(store), _ptr(dX), _ld(dX), dx_dtype,
+                                _ptr(dWg), _ptr(dWu), _ptr(dWd), dw_dtype, flags, _ptr(ws), _nbytes(ws),
+                                _stream(stream))
+    _check(rc, "ps_gated_ffn_bwd")
+
+
+def ps_rope_table(T: int, R: int, theta: float, table, stream=None):
+    rc = lib().ps_rope_table(T, R, float(theta), _ptr(table), _stream(stream))
+    _check(rc, "ps_rope_table")
+
+
+def ps_qk_norm_rope_workspace_size(D: int) -> int:
+    return lib().ps_qk_norm_rope_workspace_size(D)
+
+
+def ps_qk_norm_rope_fwd(N, Hq, Hk, D, R, dtype, layout, q, k, gq, gk, eps, pos, pos_base, T, table, q_out, k_out, ws,
+                        stream=None):
+    rc = lib().ps_qk_norm_rope_fwd(N, Hq, Hk, D, R, dtype, layout, _ptr(q), _ld(q), _ptr(k), _ld(k), _ptr(gq), _ptr(gk),
+                                   eps, _ptr(pos), pos_base, T, _ptr(table), _ptr(q_out), _ld(q_out), _ptr(k_out),
+                                   _ld(k_out), _ptr(ws), _nbytes(ws), _stream(stream))
+    _check(rc, "ps_qk_norm_rope_fwd")
+
+
+def ps_qk_norm_rope_bwd(N, Hq, Hk, D, R, dtype, layout, dq_out, dk_out, q, k, gq, gk, eps, pos, pos_base, T, table, dq,
+                        dk, dgq, dgk, flags, ws, stream=None):
+    rc = lib().ps_qk_norm_rope_bwd(N, Hq, Hk, D, R, dtype, layout, _ptr(dq_out), _ld(dq_out), _ptr(dk_out), _ld(dk_out),
+                                   _ptr(q), _ld(q), _ptr(k), _ld(k), _ptr(gq), _ptr(gk), eps, _ptr(pos), pos_base, T,
+                                   _ptr(table), _ptr(dq), _ld(dq), _ptr(dk), _ld(dk), _ptr(dgq), _ptr(dgk), flags,
+                                   _ptr(ws), _nbytes(ws), _stream(stream))
+    _check(rc, "ps_qk_norm_rope_bwd")
+
+
+def ps_dropout_rows(N, d, dtype, x, res, row_traj, row_pos, traj_base, p, seed, step, site, y, stream=None):
+    rc = lib().ps_dropout_rows(N, d, dtype, _ptr(x), _ld(x), _ptr(res), _ld(res), _ptr(row_traj), _ptr(row_pos),
+                               traj_base, float(p), seed & (2**64 - 1), step & (2**64 - 1), site, _ptr(y), _ld(y),
+                               _stream(stream))
+    _check(rc, "ps_dropout_rows")
 
 
 def ps_diag_gemm_bf16(M, N, K, a_mn_major, b_mn_major, A, lda, B, ldb, C, ldc, accumulate, ws, variant=0,

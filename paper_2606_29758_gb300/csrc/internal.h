@@ -9,6 +9,7 @@ namespace psk {
 int num_sms_current();
 int device_is_sm103();
 int refused(int rc, void* ws, cudaStream_t s);   // rc, the workspace's status zeroed: an error before a call's first kernel
+int check_ws(const void* ws, size_t ws_bytes, size_t need);   // PS_OK or PS_ERR_WORKSPACE
 
 // Forward GEMM with the online-logsumexp epilogue. part: [splits * fwd_partials_per_split_bf16()][N]
 // (max2, sum) pairs (max in log2 units); ztok: [N] chosen-token logit, written only for rows whose token id minus

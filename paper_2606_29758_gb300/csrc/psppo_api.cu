@@ -33,7 +33,7 @@ int device_is_sm103() {
   return major == 10 && minor == 3;
 }
 
-static int check_ws(const void* ws, size_t ws_bytes, size_t need) {
+int check_ws(const void* ws, size_t ws_bytes, size_t need) {
   if (ws == nullptr || (reinterpret_cast<uintptr_t>(ws) & 255)) return PS_ERR_WORKSPACE;
   return ws_bytes < need ? PS_ERR_WORKSPACE : PS_OK;
 }
