@@ -15,23 +15,41 @@ import torch
 from . import _binding as B
 
 
-def _rows(name: str, t: torch.Tensor, n: Optional[int], cols: int, dtype: torch.dtype) -> torch.Tensor:
-    """A 2-D tensor of n rows (any number: None) whose elements lie side by side, checked before its pointer is taken."""
-    if t.dim() != 2 or t.shape[1] != cols or (n is not None and t.shape[0] != n):
-        raise ValueError(f"{name}: need [{'N' if n is None else n}][{cols}], got {tuple(t.shape)}")
-    if t.dtype != dtype:
-        raise TypeError(f"{name}: need {dtype}, got {t.dtype}")
-    if cols > 1 and t.numel() > 0 and t.stride(1) != 1:
-        raise ValueError(f"{name}: the elements of a row must lie side by side (stride {t.stride(1)})")
-    return t
+# The checks below run before a pointer is taken; together with the library's own they are most of a small call's host
+# time, so each is one comparison of what a right call has, and the reason is looked for only after it fails.
+def _pitch(name: str, t: torch.Tensor, n: int, cols: int, dtype: torch.dtype) -> int:
+    """The row pitch of a tensor of n rows of cols elements that lie side by side."""
+    st = t.stride()
+    if t.shape != (n, cols) or t.dtype is not dtype or not t.is_cuda or (st[1] != 1 and cols > 1 and n > 0):
+        if t.dim() != 2 or t.shape != (n, cols):
+            raise ValueError(f"{name}: need [{n}][{cols}], got {tuple(t.shape)}")
+        if t.dtype is not dtype:
+            raise TypeError(f"{name}: need {dtype}, got {t.dtype}")
+        if not t.is_cuda:
+            raise ValueError(f"{name}: not on a GPU ({t.device})")
+        raise ValueError(f"{name}: the elements of a row must lie side by side (stride {st[1]})")
+    return st[0] if n > 1 else cols      # (a single row's stride says nothing)
 
 
-def _whole(name: str, t: torch.Tensor, shape, dtype: torch.dtype) -> torch.Tensor:
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name}: need a contiguous {tuple(shape)}, got {tuple(t.shape)}")
-    if t.dtype != dtype:
-        raise TypeError(f"{name}: need {dtype}, got {t.dtype}")
-    return t
+def _whole(name: str, t: torch.Tensor, shape, dtype: torch.dtype) -> int:
+    """The address of a contiguous tensor."""
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        if t.dtype is not dtype:
+            raise TypeError(f"{name}: need {dtype}, got {t.dtype}")
+        if not t.is_cuda:
+            raise ValueError(f"{name}: not on a GPU ({t.device})")
+        raise ValueError(f"{name}: need a contiguous {tuple(shape)}, got {tuple(t.shape)}, strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _row_count(name: str, t: torch.Tensor, most: int) -> int:
+    if t.dim() != 2 or t.shape[0] > most:
+        raise ValueError(f"{name}: {tuple(t.shape)}, built for {most} rows")
+    return t.shape[0]
+
+
+def _first(t: torch.Tensor, n: int) -> torch.Tensor:
+    return t if t.shape[0] == n else t[:n]
 
 
 def _status(what: str, ws):
@@ -57,10 +75,13 @@ class GatedFFN:
     def __init__(self, shape: FFNShape, device: str = "cuda"):
         s = shape
         self.s, self.device = s, device
+        L = B.lib()
+        self._fwd, self._bwd = L.ps_gated_ffn_fwd, L.ps_gated_ffn_bwd
         bf16 = dict(dtype=torch.bfloat16, device=device)
         u8 = dict(dtype=torch.uint8, device=device)   # zeroed: a status word never written reads clear
         self.Y = torch.empty(s.rows, s.d, **bf16)
         self.ws_fwd = torch.zeros(B.ps_gated_ffn_fwd_workspace_size(s.rows, s.F, s.train), **u8)
+        self._fwd_tail = (None, 0, self.ws_fwd.data_ptr(), self.ws_fwd.numel())
         self.store = self.ws_bwd = None
         self.stored = -1              # rows of the last forward, until its backward has used the store
         if s.train:
@@ -69,37 +90,41 @@ class GatedFFN:
             self.dX = torch.empty(s.rows, s.d, dtype=s.dx_dtype, device=device)
             self.dWg, self.dWu = (torch.empty(s.F, s.d, dtype=s.dw_dtype, device=device) for _ in range(2))
             self.dWd = torch.empty(s.d, s.F, dtype=s.dw_dtype, device=device)
-            self._dx, self._dw = (B.dtype_code(t) for t in (self.dX, self.dWd))
+            kept = (self.store.data_ptr(), self.store.numel())
+            self._fwd_tail = kept + self._fwd_tail[2:]
+            self._bwd_tail = kept + (self.dX.data_ptr(), s.d, B.dtype_code(self.dX), self.dWg.data_ptr(),
+                                     self.dWu.data_ptr(), self.dWd.data_ptr(), B.dtype_code(self.dWd))
+            self._bwd_ws = (self.ws_bwd.data_ptr(), self.ws_bwd.numel())
+        self._w1, self._w2 = (s.F, s.d), (s.d, s.F)
 
-    def _inputs(self, X, Wg, Wu, Wd) -> int:
-        s, t = self.s, torch.bfloat16
-        _rows("X", X, None, s.d, t)
-        if X.shape[0] > s.rows:
-            raise ValueError(f"X: {X.shape[0]} rows, built for {s.rows}")
-        _whole("Wg", Wg, (s.F, s.d), t)
-        _whole("Wu", Wu, (s.F, s.d), t)
-        _whole("Wd", Wd, (s.d, s.F), t)
-        return X.shape[0]
+    def _inputs(self, X, Wg, Wu, Wd):
+        N, t = _row_count("X", X, self.s.rows), torch.bfloat16
+        return (N, X.data_ptr(), _pitch("X", X, N, self.s.d, t), _whole("Wg", Wg, self._w1, t),
+                _whole("Wu", Wu, self._w1, t), _whole("Wd", Wd, self._w2, t))
 
     def forward(self, X, Wg, Wu, Wd, out=None):
         """Y [N][d] (in `out` if given)."""
-        s, N = self.s, self._inputs(X, Wg, Wu, Wd)
-        Y = self.Y[:N] if out is None else _rows("out", out, N, s.d, torch.bfloat16)
-        B.ps_gated_ffn_fwd(N, s.d, s.F, B.PS_DTYPE_BF16, s.act, X, Wg, Wu, Wd, Y, self.store, self.ws_fwd)
+        s = self.s
+        N, *inputs = self._inputs(X, Wg, Wu, Wd)
+        Y = _first(self.Y, N) if out is None else out
+        rc = self._fwd(N, s.d, s.F, B.PS_DTYPE_BF16, s.act, *inputs, Y.data_ptr(),
+                       s.d if out is None else _pitch("out", out, N, s.d, torch.bfloat16), *self._fwd_tail, B._stream())
+        B._check(rc, "ps_gated_ffn_fwd")
         self.stored = N if s.train else -1
         return Y
 
     def backward(self, dY, X, Wg, Wu, Wd, dw_accumulate: bool = False):
         """(dX, dWg, dWu, dWd) of the last forward, which must have been given the same X and weights: one
         backward per forward (it turns the store into dG and dU in place)."""
-        s, N = self.s, self._inputs(X, Wg, Wu, Wd)
+        s = self.s
+        N, *inputs = self._inputs(X, Wg, Wu, Wd)
         if self.stored != N:
             raise RuntimeError("backward needs a forward of the same rows before it (train=True, one backward each)")
-        _rows("dY", dY, N, s.d, torch.bfloat16)
-        B.ps_gated_ffn_bwd(N, s.d, s.F, B.PS_DTYPE_BF16, dY, X, Wg, Wu, Wd, self.store, self.dX[:N], self._dx, self.dWg,
-                           self.dWu, self.dWd, self._dw, B.PS_DW_ACCUMULATE if dw_accumulate else 0, self.ws_bwd)
+        rc = self._bwd(N, s.d, s.F, B.PS_DTYPE_BF16, dY.data_ptr(), _pitch("dY", dY, N, s.d, torch.bfloat16), *inputs,
+                       *self._bwd_tail, B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._bwd_ws, B._stream())
+        B._check(rc, "ps_gated_ffn_bwd")
         self.stored = -1
-        return self.dX[:N], self.dWg, self.dWu, self.dWd
+        return _first(self.dX, N), self.dWg, self.dWu, self.dWd
 
     def check_status(self):
         """Raise PsppoError if a workspace reports a device-side error."""
@@ -139,52 +164,52 @@ class QKNormRope:
             if table is None or table.dim() != 3:
                 raise ValueError("a table [T][R/2][2] is needed (rope_table)")
             _whole("table", table, (table.shape[0], s.R // 2, 2), torch.float32)
-        self.s, self.table, self.device = s, table, device
-        self.code = B.dtype_code(torch.empty(0, dtype=s.dtype))
-        self.layout = B.PS_ROPE_EVEN if s.interleaved else B.PS_ROPE_HALF
+        self.s, self.table, self.device = s, table if s.R > 0 else None, device
+        L = B.lib()
+        self._fwd, self._bwd = L.ps_qk_norm_rope_fwd, L.ps_qk_norm_rope_bwd
+        code = B.dtype_code(torch.empty(0, dtype=s.dtype))
+        self._head = (s.Hq, s.Hk, s.D, s.R, code, B.PS_ROPE_EVEN if s.interleaved else B.PS_ROPE_HALF)
+        self._table = (table.shape[0], table.data_ptr()) if s.R > 0 else (0, None)
+        self._wq, self._wk = s.Hq * s.D, s.Hk * s.D
         t = dict(dtype=s.dtype, device=device)
-        self.q, self.k = torch.empty(s.rows, s.Hq * s.D, **t), torch.empty(s.rows, s.Hk * s.D, **t)
+        self.q, self.k = torch.empty(s.rows, self._wq, **t), torch.empty(s.rows, self._wk, **t)
         size = B.ps_qk_norm_rope_workspace_size(s.D) if s.train else 256
         self.ws = torch.zeros(max(size, 256), dtype=torch.uint8, device=device)
+        self._ws = (self.ws.data_ptr(), self.ws.numel())
+        self._out = (self.q.data_ptr(), self._wq, self.k.data_ptr(), self._wk)
         if s.train:
-            self.dq, self.dk = torch.empty(s.rows, s.Hq * s.D, **t), torch.empty(s.rows, s.Hk * s.D, **t)
+            self.dq, self.dk = torch.empty(s.rows, self._wq, **t), torch.empty(s.rows, self._wk, **t)
             self.dgq, self.dgk = (torch.empty(s.D, dtype=torch.float32, device=device) for _ in range(2))
+            self._grads = (self.dq.data_ptr(), self._wq, self.dk.data_ptr(), self._wk, self.dgq.data_ptr(),
+                           self.dgk.data_ptr())
 
-    def _inputs(self, q, k, gq, gk, pos) -> int:
-        s, N = self.s, q.shape[0]
-        if N > s.rows:
-            raise ValueError(f"q: {N} rows, built for {s.rows}")
-        _rows("q", q, N, s.Hq * s.D, s.dtype)
-        _rows("k", k, N, s.Hk * s.D, s.dtype)
-        for name, g in (("gq", gq), ("gk", gk)):
-            if g is not None:
-                _whole(name, g, (s.D,), s.dtype)
-        if s.R > 0:
-            _whole("pos", pos, (N,), torch.int32)
-        return N
-
-    def _rope(self, pos, pos_base):
-        return (pos, pos_base, self.table.shape[0], self.table) if self.s.R > 0 else (None, 0, 0, None)
+    def _inputs(self, N, q, k, gq, gk, pos, pos_base):
+        s = self.s
+        t, gain = s.dtype, (s.D,)
+        return (q.data_ptr(), _pitch("q", q, N, self._wq, t), k.data_ptr(), _pitch("k", k, N, self._wk, t),
+                None if gq is None else _whole("gq", gq, gain, t), None if gk is None else _whole("gk", gk, gain, t),
+                s.eps, _whole("pos", pos, (N,), torch.int32) if s.R > 0 else None, pos_base, *self._table)
 
     def forward(self, q, k, gq, gk, pos, pos_base: int = 1, in_place: bool = False):
         """(q, k) normed and rotated; in_place writes over the inputs (serving: no backward follows)."""
-        s, N = self.s, self._inputs(q, k, gq, gk, pos)
-        qo, ko = (q, k) if in_place else (self.q[:N], self.k[:N])
-        B.ps_qk_norm_rope_fwd(N, s.Hq, s.Hk, s.D, s.R, self.code, self.layout, q, k, gq, gk, s.eps,
-                              *self._rope(pos, pos_base), qo, ko, self.ws)
-        return qo, ko
+        N = _row_count("q", q, self.s.rows)
+        inputs = self._inputs(N, q, k, gq, gk, pos, pos_base)
+        rc = self._fwd(N, *self._head, *inputs, *(inputs[:4] if in_place else self._out), *self._ws, B._stream())
+        B._check(rc, "ps_qk_norm_rope_fwd")
+        return (q, k) if in_place else (_first(self.q, N), _first(self.k, N))
 
     def backward(self, dq_out, dk_out, q, k, gq, gk, pos, pos_base: int = 1, dw_accumulate: bool = False):
         """(dq, dk, dgq, dgk) from the gradients of the forward's outputs and its inputs."""
-        s, N = self.s, self._inputs(q, k, gq, gk, pos)
+        s = self.s
+        N = _row_count("q", q, s.rows)
         if not s.train:
             raise RuntimeError("built without a backward (train=False)")
-        _rows("dq_out", dq_out, N, s.Hq * s.D, s.dtype)
-        _rows("dk_out", dk_out, N, s.Hk * s.D, s.dtype)
-        B.ps_qk_norm_rope_bwd(N, s.Hq, s.Hk, s.D, s.R, self.code, self.layout, dq_out, dk_out, q, k, gq, gk, s.eps,
-                              *self._rope(pos, pos_base), self.dq[:N], self.dk[:N], self.dgq, self.dgk,
-                              B.PS_DW_ACCUMULATE if dw_accumulate else 0, self.ws)
-        return self.dq[:N], self.dk[:N], self.dgq, self.dgk
+        rc = self._bwd(N, *self._head, dq_out.data_ptr(), _pitch("dq_out", dq_out, N, self._wq, s.dtype),
+                       dk_out.data_ptr(), _pitch("dk_out", dk_out, N, self._wk, s.dtype),
+                       *self._inputs(N, q, k, gq, gk, pos, pos_base), *self._grads,
+                       B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._ws, B._stream())
+        B._check(rc, "ps_qk_norm_rope_bwd")
+        return _first(self.dq, N), _first(self.dk, N), self.dgq, self.dgk
 
     def check_status(self):
         _status("q/k norm and rotation", self.ws)
@@ -197,17 +222,19 @@ class RowDropout:
 
     def __init__(self, p: float, site: int = 0):
         self.p, self.site = float(p), int(site)
+        self._call = B.lib().ps_dropout_rows
 
     def _run(self, x, row_traj, row_pos, seed, step, res, traj_base, out):
         N, d = x.shape
-        _rows("x", x, None, d, x.dtype)
-        code = B.dtype_code(x)
-        _whole("row_traj", row_traj, (N,), torch.int32)
-        _whole("row_pos", row_pos, (N,), torch.int32)
-        if res is not None:
-            _rows("res", res, N, d, x.dtype)
-        y = torch.empty(N, d, dtype=x.dtype, device=x.device) if out is None else _rows("out", out, N, d, x.dtype)
-        B.ps_dropout_rows(N, d, code, x, res, row_traj, row_pos, traj_base, self.p, seed, step, self.site, y)
+        t = x.dtype
+        pitch = _pitch("x", x, N, d, t)
+        y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
+        rc = self._call(N, d, B.dtype_code(x), x.data_ptr(), pitch, None if res is None else res.data_ptr(),
+                        0 if res is None else _pitch("res", res, N, d, t), _whole("row_traj", row_traj, (N,), torch.int32),
+                        _whole("row_pos", row_pos, (N,), torch.int32), traj_base, self.p, seed & (2**64 - 1),
+                        step & (2**64 - 1), self.site, y.data_ptr(), d if out is None else _pitch("out", out, N, d, t),
+                        B._stream())
+        B._check(rc, "ps_dropout_rows")
         return y
 
     def forward(self, x, row_traj, row_pos, seed: int, step: int, res=None, traj_base: int = 0, out=None):

@@ -120,43 +120,267 @@ struct FfnDaEpi {
     const uint32_t* scale;
   };
   struct State {};
+  // Four lanes load the 64 bytes of a row: unit lane % 4 of the warp's row 8 i + lane / 4 (a lane loading its own row
+  // touched four times the lines an instruction).
   struct Ahead {
     uint4 p[4], q[4];
-    uint32_t scale;
+    uint32_t scale;   // of the lane's own row
   };
   static __device__ __forceinline__ int cols(const Params& p) { return p.F; }
   static __device__ __forceinline__ void begin_unit(const Params&, State&, int, int) {}
   static __device__ __forceinline__ void end_unit(const Params&, State&, int, int) {}
   static __device__ __forceinline__ void load_ahead(const Params& p, int row, int col0, Ahead& a) {
-    const bool in = row < p.M;
-    const int64_t at = static_cast<int64_t>(row) * p.F + col0;
+    const int lane = threadIdx.x & 31, col = col0 + 8 * (lane & 3);
+    const int first = row - lane + (lane >> 2);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const bool here = in && col0 + 8 * i < p.F;   // F is a multiple of 8
-      a.p[i] = here ? *reinterpret_cast<const uint4*>(p.P + at + 8 * i) : make_uint4(0, 0, 0, 0);
-      a.q[i] = here ? *reinterpret_cast<const uint4*>(p.Q + at + 8 * i) : make_uint4(0, 0, 0, 0);
+      const bool here = first + 8 * i < p.M && col < p.F;   // F is a multiple of 8
+      const int64_t at = static_cast<int64_t>(first + 8 * i) * p.F + col;
+      a.p[i] = here ? *reinterpret_cast<const uint4*>(p.P + at) : make_uint4(0, 0, 0, 0);
+      a.q[i] = here ? *reinterpret_cast<const uint4*>(p.Q + at) : make_uint4(0, 0, 0, 0);
     }
-    a.scale = in && col0 < p.F ? p.scale[static_cast<int64_t>(col0 >> 5) * p.M + row] : 0u;
+    a.scale = row < p.M && col0 < p.F ? p.scale[static_cast<int64_t>(col0 >> 5) * p.M + row] : 0u;
+  }
+  // One plane of the slice: through the staging buffer to the lanes that own the rows, which put the products back
+  // where they read.
+  static __device__ __forceinline__ void plane(const uint32_t (&r)[32], const uint4 (&kept)[4], float factor, uint8_t* buf,
+                                               int lane) {
+    uint4* b = reinterpret_cast<uint4*>(buf);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int rr = 8 * i + (lane >> 2);
+      b[rr * 4 + ((lane & 3) ^ ((rr >> 1) & 3))] = kept[i];
+    }
+    __syncwarp();
+    uint4* own = b + lane * 4;
+    const int x = (lane >> 1) & 3;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint4 v = own[q ^ x];
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      uint32_t o[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 f = unpack_f16x2(w[j]);
+        o[j] = pack_bf16x2(__uint_as_float(r[8 * q + 2 * j]) * f.x * factor,
+                           __uint_as_float(r[8 * q + 2 * j + 1]) * f.y * factor);
+      }
+      own[q ^ x] = make_uint4(o[0], o[1], o[2], o[3]);
+    }
   }
   static __device__ __forceinline__ void chunk_own(const Params&, int, int col0, const uint32_t (&r)[32],
-                                                   const uint32_t (&)[1], const Ahead& a, uint8_t* bufs,
-                                                   uint32_t& stored, int lane, int row_base, const CUtensorMap* mapG,
+                                                   const uint32_t (&)[1], const Ahead& a, uint8_t* bufs, uint32_t&,
+                                                   int lane, int row_base, const CUtensorMap* mapG,
                                                    const CUtensorMap* mapU, const CUtensorMap*) {
-    auto out = [&](const uint4 (&kept)[4], float factor, const CUtensorMap* map) {
-      const uint32_t w[16] = {kept[0].x, kept[0].y, kept[0].z, kept[0].w, kept[1].x, kept[1].y, kept[1].z, kept[1].w,
-                              kept[2].x, kept[2].y, kept[2].z, kept[2].w, kept[3].x, kept[3].y, kept[3].z, kept[3].w};
-      uint32_t pk[16];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const float2 v = unpack_f16x2(w[j]);
-        pk[j] = pack_bf16x2(__uint_as_float(r[2 * j]) * v.x * factor, __uint_as_float(r[2 * j + 1]) * v.y * factor);
-      }
-      store_slice16(pk, bufs, stored, lane, map, col0, row_base);
-    };
-    out(a.p, __uint_as_float((a.scale & 255u) << 23), mapG);
-    out(a.q, __uint_as_float((a.scale >> 8 & 255u) << 23), mapU);
+    if (lane == 0) bulk_wait_group_read<0>();
+    __syncwarp();
+    plane(r, a.p, __uint_as_float((a.scale & 255u) << 23), bufs, lane);
+    plane(r, a.q, __uint_as_float((a.scale >> 8 & 255u) << 23), bufs + 32 * 64, lane);
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store_2d(mapG, bufs, col0, row_base);
+      tma_store_2d(mapU, bufs + 32 * 64, col0, row_base);
+      bulk_commit_group();
+    }
   }
 };
+
+// ============================================================================= few rows
+// Up to 128 rows: reading the weights is all that costs (one row at d = 3584, F = 16384: 352 MB), so the weights are the
+// 128-row operand of the MMA and the rows its N side (NT = 16 to 128 columns), and every SM streams weights. A CTA takes
+// 64 columns of F (their 64 gate and 64 up rows are one tile) or 128 outputs of Y; where that gives too few CTAs a
+// cluster shares the K loop, and the partial tiles are added in rank order through distributed shared memory. Two CTAs
+// fit on an SM. The second product is launched while the first runs and loads its first weights before it waits for A.
+// One row of d = 3584, F = 16384 57 us (6.1 TB/s of weights), 128 rows 73; d = 1536, F = 8192 21 and 33 (the general
+// kernels, 128 rows to a tile and F or d / 256 CTAs: 145 and 138, 68 and 66).
+constexpr int kFewThreads = 192;
+constexpr uint32_t kFewWBytes = 128 * kBK * 2;
+template <int NT>
+struct FewCfg {
+  static constexpr uint32_t kXBytes = NT * kBK * 2;
+  static constexpr uint32_t kStage = kFewWBytes + kXBytes;
+  static constexpr int kStages = (112 * 1024 - 1024 - 256) / kStage;
+  static constexpr uint32_t kCols = NT < 32 ? 32 : NT;
+  static_assert(kStages * kStage >= NT * 128 * 4, "the partial tile lies over the ring");
+};
+template <int NT>
+struct FewSmem {
+  uint8_t ring[FewCfg<NT>::kStages][FewCfg<NT>::kStage];   // weights, then rows (both 1024-byte aligned)
+  uint64_t full[FewCfg<NT>::kStages];
+  uint64_t empty[FewCfg<NT>::kStages];
+  uint64_t tfull;
+  uint32_t tmem_base;
+  int abort;
+};
+
+static __device__ __forceinline__ float2 ld_cluster_v2(uint32_t cl_addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(cl_addr) : "memory");
+  return v;
+}
+
+// UP: out[n][f] = s(x_n . Wg_f) (x_n . Wu_f), tmW and tmW2 the two weights in boxes of 64 rows; otherwise out[n][c] =
+// x_n . W_c, tmW in boxes of 128 rows. N rows, C output columns (a multiple of 8).
+template <int NT, bool UP, int ACT>
+__global__ void __launch_bounds__(kFewThreads, 2)
+    ffn_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmW2,
+                   const __grid_constant__ CUtensorMap tmX, int N, int C, int num_kb, uint16_t* out, int64_t ldo,
+                   uint32_t* status, uint64_t timeout_ns) {
+  using Cfg = FewCfg<NT>;
+  constexpr int S = Cfg::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  FewSmem<NT>& sm = *reinterpret_cast<FewSmem<NT>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int nranks = static_cast<int>(cluster_nctarank()), rank = static_cast<int>(cluster_ctarank());
+  const int unit = blockIdx.x / nranks;
+  const int kb0 = static_cast<int>(static_cast<long long>(num_kb) * rank / nranks);
+  const int kb1 = static_cast<int>(static_cast<long long>(num_kb) * (rank + 1) / nranks);
+  const int row0 = unit * (UP ? 64 : 128);
+
+  if (threadIdx.x == 0) {
+    if (UP && blockIdx.x == 0) clear_status(status);   // (a bit is set only after seconds)
+    for (int s = 0; s < S; ++s) {
+      mbar_init(&sm.full[s], 1);
+      mbar_init(&sm.empty[s], 1);
+    }
+    mbar_init(&sm.tfull, 1);
+    sm.abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&sm.tmem_base, Cfg::kCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (UP) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const uint32_t tmem_base = sm.tmem_base;
+  volatile int* abort = &sm.abort;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      auto weights = [&](int kb, int s) {
+        mbar_arrive_expect_tx(&sm.full[s], Cfg::kStage);
+        tma_load_2d(sm.ring[s], &tmW, &sm.full[s], kb * kBK, row0);
+        if (UP) tma_load_2d(sm.ring[s] + kFewWBytes / 2, &tmW2, &sm.full[s], kb * kBK, row0);
+      };
+      auto rows = [&](int kb, int s) { tma_load_2d(sm.ring[s] + kFewWBytes, &tmX, &sm.full[s], kb * kBK, 0); };
+      // the weights come from before the call: a ring of them before the kernel that writes the rows is done
+      const int ahead = min(S, kb1 - kb0);
+      for (int i = 0; i < ahead; ++i) weights(kb0 + i, i);
+      wait_for_previous_kernel();
+      for (int i = 0; i < ahead; ++i) rows(kb0 + i, i);
+      bool ok = true;
+      int kc = ahead;
+      for (int kb = kb0 + ahead; kb < kb1; ++kb, ++kc) {
+        const int s = kc % S;
+        if (!mbar_wait(&sm.empty[s], ((kc / S) & 1u) ^ 1u, timeout_ns, abort)) { ok = false; break; }
+        weights(kb, s);
+        rows(kb, s);
+      }
+      if (!ok) {
+        *abort = 1;
+        raise_status(status, PS_DEV_TIMEOUT);
+      }
+      // the ring is reused below: every load has landed
+      for (int j = kc > S ? kc - S : 0; j < kc; ++j) mbar_wait(&sm.full[j % S], (j / S) & 1u, timeout_ns, nullptr);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr uint32_t idesc = idesc_bf16_f32(128, NT, false, false);
+      int kc = 0;
+      for (int kb = kb0; kb < kb1; ++kb, ++kc) {
+        const int s = kc % S;
+        if (!mbar_wait(&sm.full[s], (kc / S) & 1u, timeout_ns, abort)) {
+          *abort = 1;
+          raise_status(status, PS_DEV_TIMEOUT);
+          break;
+        }
+        tc_fence_after();
+        const uint32_t w = smem_addr(sm.ring[s]);
+#pragma unroll
+        for (int k = 0; k < kBK / 16; ++k)
+          umma_bf16(tmem_base, smem_desc_sw128(w + k * 32, 16, 1024), smem_desc_sw128(w + kFewWBytes + k * 32, 16, 1024),
+                    idesc, (kc | k) != 0 ? 1u : 0u);
+        umma_commit(&sm.empty[s]);
+      }
+      umma_commit(&sm.tfull);   // also after an expired wait: the MMAs issued so far still finish
+    }
+  }
+  __syncwarp();
+  {
+    int got = 0;
+    if (lane == 0) got = mbar_wait(&sm.tfull, 0, timeout_ns, nullptr) ? 1 : 0;
+    got = __shfl_sync(0xffffffffu, got, 0);
+    if (!got && lane == 0) raise_status(status, PS_DEV_TIMEOUT);
+  }
+  tc_fence_after();
+  __syncthreads();   // the loads have landed (warp 0), the MMAs are done: the ring is idle
+
+  // this rank's partial tile, [row n][128 outputs] f32
+  float* part = reinterpret_cast<float*>(sm.ring);
+  if (warp >= 2) {
+    const int r = (warp & 3) * 32 + lane;
+    const uint32_t t_row = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+#pragma unroll 1
+    for (int c = 0; c < NT && c < N; c += 32) {
+      uint32_t v[32];
+      tmem_ld32(t_row + c, v);
+      tmem_ld_wait();
+#pragma unroll
+      for (int j = 0; j < 32; ++j)
+        if (j < NT - c && c + j < N) part[(c + j) * 128 + r] = __uint_as_float(v[j]);
+    }
+  }
+  tc_fence_before();
+  if (nranks > 1) cluster_sync_all();
+  else __syncthreads();
+
+  // rows rank, rank + nranks, ...: the ranks' partials added in rank order
+  const uint32_t base = smem_addr(part);
+  constexpr int kPer = 32;   // threads of a row: two columns of F each, or four of Y
+  for (int i = threadIdx.x; ; i += kFewThreads) {
+    const int n = rank + (i / kPer) * nranks, j = i % kPer;
+    if (n >= N) break;
+    if (UP) {
+      float2 g = make_float2(0.f, 0.f), u = g;
+      for (int k = 0; k < nranks; ++k) {
+        const float2 a = ld_cluster_v2(mapa_shared(base + (n * 128 + 2 * j) * 4, k));
+        const float2 b = ld_cluster_v2(mapa_shared(base + (n * 128 + 64 + 2 * j) * 4, k));
+        g.x += a.x;
+        g.y += a.y;
+        u.x += b.x;
+        u.y += b.y;
+      }
+      float q0, q1, s0, s1;
+      act_and_slope<ACT>(g.x, q0, s0);
+      act_and_slope<ACT>(g.y, q1, s1);
+      if (row0 + 2 * j < C)
+        *reinterpret_cast<uint32_t*>(out + static_cast<int64_t>(n) * ldo + row0 + 2 * j) = pack_bf16x2(q0 * u.x, q1 * u.y);
+    } else {
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < nranks; ++k) {
+        const float4 a = ld_cluster_v4(mapa_shared(base + (n * 128 + 4 * j) * 4, k));
+        y.x += a.x;
+        y.y += a.y;
+        y.z += a.z;
+        y.w += a.w;
+      }
+      if (row0 + 4 * j < C)
+        *reinterpret_cast<uint2*>(out + static_cast<int64_t>(n) * ldo + row0 + 4 * j) =
+            make_uint2(pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
+    }
+  }
+  __syncwarp();
+  if (nranks > 1) cluster_sync_all();   // nobody reads this rank's partial any more
+  else __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, Cfg::kCols);
+  }
+}
 
 // ============================================================================= host side
 struct FfnStore {
@@ -183,10 +407,54 @@ static int band_of_rows(int64_t K, int halves) {
 }
 constexpr int kBandLongK = 4;   // products with a long K loop: column tiles of 4 row blocks side by side
 
+constexpr int kFewRows = 128;
+
+// CTAs that share a unit's K loop: as many as keep all units' CTAs resident at once (two per SM), with at least 8
+// k blocks each.
+static int few_ranks(int64_t units, int num_kb) {
+  const int64_t slots = 2 * static_cast<int64_t>(num_sms_current());
+  int r = 8;
+  while (r > 1 && (units * r > slots || num_kb / r < 8)) r /= 2;
+  return r;
+}
+
+template <int NT, bool UP, int ACT>
+static int launch_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, const void* W, const void* W2, void* out,
+                      int64_t ldo, uint32_t* status, cudaStream_t s) {
+  CUtensorMap tw, tw2, tx;
+  if (!map_kmajor(&tw, W, C, K, K, UP ? 64 : 128) || !map_kmajor(&tw2, W2, C, K, K, UP ? 64 : 128) ||
+      !map_kmajor(&tx, X, N, K, ldx, NT))
+    return PS_ERR_INVALID_ARG;
+  auto kern = ffn_few_kernel<NT, UP, ACT>;
+  constexpr size_t smem = sizeof(FewSmem<NT>) + 1024;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
+    return PS_ERR_CUDA;
+  const int64_t units = (C + (UP ? 63 : 127)) / (UP ? 64 : 128);
+  const int num_kb = static_cast<int>((K + kBK - 1) / kBK);
+  int ranks = few_ranks(units, num_kb);
+  for (;; ranks /= 2) {
+    if (launch_after(kern, dim3(static_cast<unsigned>(units * ranks)), kFewThreads, smem, s, static_cast<unsigned>(ranks),
+                     1, !UP, tw, tw2, tx, static_cast<int>(N), C, num_kb, static_cast<uint16_t*>(out), ldo, status,
+                     kDefaultTimeoutNs) == cudaSuccess)
+      return PS_OK;
+    cudaGetLastError();
+    if (ranks == 1) return PS_ERR_CUDA;   // (else the context's SMs do not hold such a cluster)
+  }
+}
+template <bool UP, int ACT>
+static int ffn_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, const void* W, const void* W2, void* out,
+                   int64_t ldo, uint32_t* status, cudaStream_t s) {
+  if (N <= 16) return launch_few<16, UP, ACT>(N, C, K, X, ldx, W, W2, out, ldo, status, s);
+  if (N <= 32) return launch_few<32, UP, ACT>(N, C, K, X, ldx, W, W2, out, ldo, status, s);
+  if (N <= 64) return launch_few<64, UP, ACT>(N, C, K, X, ldx, W, W2, out, ldo, status, s);
+  return launch_few<128, UP, ACT>(N, C, K, X, ldx, W, W2, out, ldo, status, s);
+}
+
 template <int ACT, bool KEEP>
 static int ffn_up(int64_t N, int d, int F, const void* X, int64_t ldx, const void* Wg, const void* Wu,
                   const FfnStore& f, uint32_t* status, cudaStream_t s) {
   using Epi = FfnUpEpi<ACT, KEEP>;
+  if (!KEEP && N <= kFewRows) return ffn_few<true, ACT>(N, F, d, X, ldx, Wg, Wu, f.A, F, status, s);
   const int halves = tile_halves(N, 2 * static_cast<int64_t>(F), 18);
   TwoMaps m;
   if (!map_kmajor(&m.a, X, N, d, ldx, kBM * halves) || !map_kmajor(&m.b, Wg, F, d, d, kBN / 2) ||
@@ -205,6 +473,7 @@ static int ffn_up(int64_t N, int d, int F, const void* X, int64_t ldx, const voi
 
 static int ffn_down(int64_t N, int d, int F, const void* A, const void* Wd, void* Y, int64_t ldy, uint32_t* status,
                     cudaStream_t s) {
+  if (N <= kFewRows) return ffn_few<false, PS_ACT_SILU>(N, d, F, A, F, Wd, Wd, Y, ldy, status, s);
   const int halves = tile_halves(N, d, 18);
   CUtensorMap ta, tb, tc;
   if (!map_kmajor(&ta, A, N, F, F, kBM * halves) || !map_kmajor(&tb, Wd, d, F, F, kBN) || !map_out_16(&tc, Y, N, d, ldy))

@@ -126,6 +126,15 @@ struct OwnStore<Epi, decltype(static_cast<void>(Epi::kOwnStore))> {
   static constexpr bool value = Epi::kOwnStore;
 };
 
+template <class Epi, bool = OwnStore<Epi>::value>
+struct AheadOf {
+  struct type {};
+};
+template <class Epi>
+struct AheadOf<Epi, true> {
+  using type = typename Epi::Ahead;
+};
+
 // tmC: the output map of epilogues that store through TMA (unused by the others). An epilogue's
 // begin_unit / end_unit see the unit's split index times the column groups (1 with 4 epilogue
 // warps, 2 with 8) plus the thread's column group.
@@ -330,6 +339,8 @@ __device__ __forceinline__ void umma_gemm_body(const CUtensorMap& tmA, const CUt
       for (int nb = n0; nb < n1; ++nb, ++tile) {
         const uint32_t acc = tile % NB;
         const uint32_t aph = (tile / NB) & 1u;
+        [[maybe_unused]] typename AheadOf<Epi>::type next;
+        if constexpr (OwnStore<Epi>::value) Epi::load_ahead(ep, row0, nb * TN + grp * CPG * 32, next);
         // one lane waits; the warp follows it, so tcgen05.ld always runs on a converged warp
         int got = 0;
         if (lane == 0) got = mbar_wait(&sm.tfull[acc], aph, timeout_ns, abort) ? 1 : 0;
@@ -372,8 +383,10 @@ __device__ __forceinline__ void umma_gemm_body(const CUtensorMap& tmA, const CUt
             for (int c = grp * CPG; c < grp * CPG + CPG; ++c) {
               uint32_t r[32], r2[PAIR == kTwoB ? 32 : 1];
               const int col0 = nb * TN + c * 32;
-              typename Epi::Ahead ahead;
-              Epi::load_ahead(ep, row, col0, ahead);
+              const typename Epi::Ahead ahead = next;
+              // what the next slice of this tile needs beside its accumulator
+              if (c + 1 < grp * CPG + CPG) Epi::load_ahead(ep, row, col0 + 32, next);
+              else if (h + 1 < HALVES) Epi::load_ahead(ep, row + kBM, nb * TN + grp * CPG * 32, next);
               tmem_ld32(t_row + c * 32, r);
               if constexpr (PAIR == kTwoB) tmem_ld32(t_row + TN + c * 32, r2);
               tmem_ld_wait();

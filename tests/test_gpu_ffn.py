@@ -64,7 +64,8 @@ def _make(N, d, F, act=0, train=True, dx=torch.bfloat16, dw=torch.bfloat16):
 
 
 SIZES = [(1, 8, 8), (2, 8, 264), (3, 24, 40), (1, 1536, 520), (17, 72, 128), (64, 512, 1024), (127, 64, 72),
-         (128, 128, 128), (129, 392, 1048), (257, 136, 1056), (300, 1032, 248), (571, 392, 1048), (1100, 264, 4104)]
+         (128, 128, 128), (129, 392, 1048), (257, 136, 1056), (300, 1032, 248), (571, 392, 1048), (1100, 264, 4104),
+         (5, 2048, 4104), (20, 72, 8200), (33, 1032, 4104), (100, 1032, 4104), (128, 8, 2048)]
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
