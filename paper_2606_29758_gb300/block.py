@@ -15,6 +15,9 @@ import torch
 from . import _binding as B
 
 
+_CODE = {torch.bfloat16: B.PS_DTYPE_BF16, torch.float32: B.PS_DTYPE_F32}
+
+
 # The checks below run before a pointer is taken; together with the library's own they are most of a small call's host
 # time, so each is one comparison of what a right call has, and the reason is looked for only after it fails.
 def _pitch(name: str, t: torch.Tensor, n: int, cols: int, dtype: torch.dtype) -> int:
@@ -228,8 +231,8 @@ class RowDropout:
         N, d = x.shape
         t = x.dtype
         pitch = _pitch("x", x, N, d, t)
-        y = torch.empty_like(x, memory_format=torch.contiguous_format) if out is None else out
-        rc = self._call(N, d, B.dtype_code(x), x.data_ptr(), pitch, None if res is None else res.data_ptr(),
+        y = torch.empty(N, d, dtype=t, device=x.device) if out is None else out
+        rc = self._call(N, d, _CODE[t] if t in _CODE else B.dtype_code(x), x.data_ptr(), pitch, None if res is None else res.data_ptr(),
                         0 if res is None else _pitch("res", res, N, d, t), _whole("row_traj", row_traj, (N,), torch.int32),
                         _whole("row_pos", row_pos, (N,), torch.int32), traj_base, self.p, seed & (2**64 - 1),
                         step & (2**64 - 1), self.site, y.data_ptr(), d if out is None else _pitch("out", out, N, d, t),

@@ -77,8 +77,9 @@ struct Raw8<float> {
 // HBM-bound (a read and a write of every element; the backward two reads and a write). A head lies on G lanes, 16
 // values each: eight pairs, so a lane rotates by itself and only the mean crosses lanes (log2 G shuffles). A warp takes
 // 32 / G heads of one row at a time, queries first, and keeps its lanes' cosines and sines for the row; the loads of
-// the next heads are under way while it works on these.
-constexpr int kQkThreads = 256;
+// the heads after these (of two steps of bf16, one of f32, across rows) are under way meanwhile: what bounds it is the
+// bytes in flight, about 45 KB an SM, so registers go to loads and resident warps.
+constexpr int kQkThreads = 128;
 constexpr int kQkWarps = kQkThreads / 32;
 
 struct QkArgs {
@@ -99,16 +100,16 @@ struct QkArgs {
   float* part;                  // backward: [blocks][2][D] partial gain gradients, nullptr without
   float *dgq, *dgk;             // their sums, or nullptr
   int accumulate;
-  uint32_t* status;             // status word and the count of finished blocks
+  uint32_t* status;
 };
 
 // cos and sin of the lane's eight pairs at a row's position (1 and 0 where the lane's dims are not rotated).
-static __device__ __forceinline__ void row_turn(const QkArgs& a, int64_t row, int c, bool rotated, float (&cs)[8],
+static __device__ __forceinline__ void row_turn(const QkArgs& a, int pos, int c, bool rotated, float (&cs)[8],
                                                 float (&sn)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) cs[i] = 1.f, sn[i] = 0.f;
   if (a.R == 0) return;
-  const int64_t t = static_cast<int64_t>(__ldg(a.pos + row)) - a.pos_base;
+  const int64_t t = static_cast<int64_t>(pos) - a.pos_base;
   if (t < 0 || t >= a.T) {   // outside the table: NaN in the row's rotated dims
     raise_status(a.status, PS_DEV_BAD_LENGTH);
     if (rotated)
@@ -139,12 +140,22 @@ static __device__ __forceinline__ void turn16(float (&v)[16], const float (&cs)[
 }
 
 static __device__ __forceinline__ float group_sum(float v, int G) {
-  for (int o = G >> 1; o >= 1; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1)
+    if (G > o) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
 
+// A step under way: the raw values of the lane's heads, and its row's position.
+template <class T, bool BWD>
+struct QkStep {
+  Raw8<T> xa, xb;
+  Raw8<T> ya, yb;   // backward
+  int pos;
+};
+
 template <class T, bool EVEN, bool BWD>
-__global__ void __launch_bounds__(kQkThreads) qk_kernel(const QkArgs a) {
+__global__ void __launch_bounds__(kQkThreads, BWD ? 3 : 5) qk_kernel(const QkArgs a) {
   extern __shared__ float qk_smem[];          // gains [2][D]; backward: then a warp's gain gradients [warps][2][D]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (gridDim.x == 1 && threadIdx.x == 0) clear_status(a.status);   // (several blocks: a memset before the launch)
@@ -160,109 +171,166 @@ __global__ void __launch_bounds__(kQkThreads) qk_kernel(const QkArgs a) {
   const int hi = EVEN || !rotated ? 16 * c + 8 : a.R / 2 + 8 * c;
   const int steps_q = (a.Hq + at_once - 1) / at_once, steps = steps_q + (a.Hk + at_once - 1) / at_once;
   const float inv_d = 1.f / static_cast<float>(a.D);
-  float accq[16], acck[16];
+  const float* const gains = qk_smem + (here ? lo : 0);
+  float acc[16], alt[16];   // gain gradients of the side (queries or keys) at work, and of the other
   if (BWD) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) accq[i] = acck[i] = 0.f;
+    for (int i = 0; i < 16; ++i) acc[i] = alt[i] = 0.f;
   }
 
+  // This warp's units (a row's steps, or a part of them), step after step. `left`: heads of the side from the step's
+  // first on; a group whose slot is not below it has none.
   const int64_t units = a.N * a.parts, stride = static_cast<int64_t>(gridDim.x) * kQkWarps;
-  for (int64_t u = static_cast<int64_t>(blockIdx.x) * kQkWarps + warp; u < units; u += stride) {
-    const int64_t row = u / a.parts;
-    const int part = static_cast<int>(u - row * a.parts);
-    const int s0 = steps * part / a.parts, s1 = steps * (part + 1) / a.parts;
-    Raw8<T> xa, xb, ya, yb;
-    // the head of step s that lies on this lane's group; false where there is none
-    auto place = [&](int s, bool& of_q, int& head) {
-      of_q = s < steps_q;
-      head = (of_q ? s : s - steps_q) * at_once + slot;
-      return here && s < s1 && head < (of_q ? a.Hq : a.Hk);
-    };
-    auto fetch = [&](int s) {
-      bool of_q;
-      int head;
-      xa.zero(), xb.zero();
-      if (BWD) ya.zero(), yb.zero();
-      if (!place(s, of_q, head)) return;
-      const T* x = static_cast<const T*>(of_q ? a.q : a.k) + row * (of_q ? a.ldq : a.ldk) + static_cast<int64_t>(head) * a.D;
-      xa.load(x + lo);
-      xb.load(x + hi);
-      if (BWD) {
-        const T* y = static_cast<const T*>(of_q ? a.dqy : a.dky) + row * (of_q ? a.lddqy : a.lddky) +
-                     static_cast<int64_t>(head) * a.D;
-        ya.load(y + lo);
-        yb.load(y + hi);
-      }
-    };
-    fetch(s0);
-    float cs[8], sn[8];
-    row_turn(a, row, c, rotated, cs, sn);
-    for (int s = s0; s < s1; ++s) {
-      float x[16], y[16];
-      xa.get(x);
-      xb.get(x + 8);
-      if (BWD) {
-        ya.get(y);
-        yb.get(y + 8);
-      }
-      bool of_q;
-      int head;
-      const bool mine = place(s, of_q, head);
-      if (s + 1 < s1) fetch(s + 1);
-      float ss = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
-      const float r = rsqrtf(fmaf(group_sum(ss, a.G), inv_d, a.eps));
-      const float* g = qk_smem + (of_q ? 0 : a.D);
-      float gain[16];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        gain[i] = here ? g[lo + i] : 0.f;
-        gain[8 + i] = here ? g[hi + i] : 0.f;
-      }
-      if (!BWD) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) y[i] = x[i] * r * gain[i];
-        turn16<EVEN>(y, cs, sn, 1.f);
+  struct At {
+    int64_t u, row;
+    int s, s1, left;
+    bool keys;
+    const T *x, *y;   // the lane's first element
+    T* out;
+  };
+  auto side = [&](At& t, bool loads) {
+    t.keys = t.s >= steps_q;
+    const int first = (t.keys ? t.s - steps_q : t.s) * at_once;
+    t.left = (t.keys ? a.Hk : a.Hq) - first;
+    const int64_t in_row = static_cast<int64_t>(first + slot) * a.D + lo;
+    if (loads) {
+      t.x = static_cast<const T*>(t.keys ? a.k : a.q) + t.row * (t.keys ? a.ldk : a.ldq) + in_row;
+      if (BWD) t.y = static_cast<const T*>(t.keys ? a.dky : a.dqy) + t.row * (t.keys ? a.lddky : a.lddqy) + in_row;
+    } else {
+      t.out = static_cast<T*>(t.keys ? a.ko : a.qo) + t.row * (t.keys ? a.ldko : a.ldqo) + in_row;
+    }
+  };
+  auto enter = [&](At& t, bool loads) {
+    if (t.u >= units) return;
+    t.row = a.parts == 1 ? t.u : t.u / a.parts;
+    const int part = static_cast<int>(t.u - t.row * a.parts);
+    t.s = steps * part / a.parts;
+    t.s1 = steps * (part + 1) / a.parts;
+    side(t, loads);
+  };
+  const int step_elems = at_once * a.D;
+  auto advance = [&](At& t, bool loads) {
+    if (++t.s >= t.s1) {
+      t.u += stride;
+      enter(t, loads);
+    } else if (t.s == steps_q) {
+      side(t, loads);
+    } else {
+      t.left -= at_once;
+      if (loads) {
+        t.x += step_elems;
+        if (BWD) t.y += step_elems;
       } else {
-        turn16<EVEN>(y, cs, sn, -1.f);
-        float dot = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float t = y[i] * (x[i] * r);
-          if (mine) {
-            if (of_q) accq[i] += t;
-            else acck[i] += t;
-          }
-          y[i] *= gain[i];
-          dot = fmaf(y[i], x[i], dot);
-        }
-        const float m = group_sum(dot, a.G) * inv_d * r * r;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) y[i] = r * (y[i] - x[i] * m);
-      }
-      if (mine) {
-        T* out = static_cast<T*>(of_q ? a.qo : a.ko) + row * (of_q ? a.ldqo : a.ldko) + static_cast<int64_t>(head) * a.D;
-        Raw8<T>::store(out + lo, y);
-        Raw8<T>::store(out + hi, y + 8);
+        t.out += step_elems;
       }
     }
+  };
+  const bool whole = a.D == 16 * a.G;   // no lane of a group without dims
+  const int apart = hi - lo;
+  auto fetch = [&](At& t, QkStep<T, BWD>& f) {
+    if (t.u >= units) return;
+    if (a.R > 0) f.pos = __ldg(a.pos + t.row);
+    if (!(whole && t.left >= at_once)) {
+      f.xa.zero(), f.xb.zero();
+      if (BWD) f.ya.zero(), f.yb.zero();
+    }
+    if ((whole && t.left >= at_once) || (here && slot < t.left)) {
+      f.xa.load(t.x);
+      f.xb.load(t.x + apart);
+      if (BWD) {
+        f.ya.load(t.y);
+        f.yb.load(t.y + apart);
+      }
+    }
+    advance(t, true);
+  };
+  float cs[8], sn[8];
+  int64_t turned = -1;   // the unit whose cosines and sines these are
+  bool keys = false;     // the side that acc belongs to
+  auto work = [&](At& t, QkStep<T, BWD>& f, At& then) {
+    float x[16], y[16];
+    f.xa.get(x);
+    f.xb.get(x + 8);
+    if (BWD) {
+      f.ya.get(y);
+      f.yb.get(y + 8);
+    }
+    if (t.u != turned) row_turn(a, f.pos, c, rotated, cs, sn);
+    turned = t.u;
+    fetch(then, f);
+    if (BWD && t.keys != keys) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float v = acc[i];
+        acc[i] = alt[i];
+        alt[i] = v;
+      }
+      keys = t.keys;
+    }
+    const bool mine = here && slot < t.left;
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
+    const float sum = group_sum(ss, a.G);
+    const float r = mine ? rsqrtf(fmaf(sum, inv_d, a.eps)) : 0.f;   // (no head here: nothing to add to the gains)
+    const float* g = gains + (t.keys ? a.D : 0);
+    float gain[16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 v = reinterpret_cast<const float4*>(i < 2 ? g : g + apart)[i & 1];
+      gain[4 * i] = v.x, gain[4 * i + 1] = v.y, gain[4 * i + 2] = v.z, gain[4 * i + 3] = v.w;
+    }
+    if (!BWD) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] = x[i] * r * gain[i];
+      turn16<EVEN>(y, cs, sn, 1.f);
+    } else {
+      turn16<EVEN>(y, cs, sn, -1.f);
+      // with n = x r: dg += dn n, dx = r (g dn - n mean(g dn n))
+      float dot = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[i] *= r;
+        acc[i] = fmaf(y[i], x[i], acc[i]);
+        y[i] *= gain[i];
+        dot = fmaf(y[i], x[i], dot);
+      }
+      const float m = group_sum(dot, a.G) * inv_d;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] = r * fmaf(-x[i], m, y[i]);
+    }
+    if (mine) {
+      Raw8<T>::store(t.out, y);
+      Raw8<T>::store(t.out + apart, y + 8);
+    }
+    advance(t, false);
+  };
+  At t, n;
+  t.u = n.u = static_cast<int64_t>(blockIdx.x) * kQkWarps + warp;
+  enter(t, false);
+  enter(n, true);
+  constexpr bool kTwo = sizeof(T) == 2;   // two steps ahead
+  QkStep<T, BWD> f0, f1;
+  fetch(n, f0);
+  if (kTwo) fetch(n, f1);
+  while (t.u < units) {
+    work(t, f0, n);
+    if (kTwo && t.u < units) work(t, f1, n);
   }
   if (!BWD || a.part == nullptr) return;
 
-  // gain gradients: over the warp's heads, the block's warps, then (the last block to finish) the blocks, in f64 and
-  // in a fixed order, so that reruns give the same bits
+  // gain gradients: over the warp's heads, then the block's warps; qk_gain_sum_kernel adds the blocks'
   float* mineq = qk_smem + 2 * a.D + warp * 2 * a.D;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     for (int o = 16; o >= a.G; o >>= 1) {
-      accq[i] += __shfl_xor_sync(0xffffffffu, accq[i], o);
-      acck[i] += __shfl_xor_sync(0xffffffffu, acck[i], o);
+      acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], o);
+      alt[i] += __shfl_xor_sync(0xffffffffu, alt[i], o);
     }
     if (here && slot == 0) {
       const int at = i < 8 ? lo + i : hi + i - 8;
-      mineq[at] = accq[i];
-      mineq[a.D + at] = acck[i];
+      mineq[at] = keys ? alt[i] : acc[i];
+      mineq[a.D + at] = keys ? acc[i] : alt[i];
     }
   }
   __syncthreads();
@@ -273,35 +341,28 @@ __global__ void __launch_bounds__(kQkThreads) qk_kernel(const QkArgs a) {
     for (int w = 0; w < kQkWarps; ++w) t += qk_smem[2 * a.D + w * 2 * a.D + i];
     part[i] = t;
   }
-  __threadfence();
-  __syncthreads();
-  __shared__ bool last;
-  if (threadIdx.x == 0) last = atomicAdd(a.status + 1, 1u) == gridDim.x - 1;
-  __syncthreads();
-  if (!last) return;
-  __threadfence();
-  // a warp per 32 columns and share of the blocks: shares in shared memory, added up in order
-  double* sums = reinterpret_cast<double*>(qk_smem);   // [warps][32]
-  for (int col0 = 0; col0 < 2 * a.D; col0 += 32) {
-    const int b0 = static_cast<int>(static_cast<int64_t>(gridDim.x) * warp / kQkWarps);
-    const int b1 = static_cast<int>(static_cast<int64_t>(gridDim.x) * (warp + 1) / kQkWarps);
-    double t = 0.0;
+}
+
+// The blocks' partial gain gradients [blocks][2][D], eight columns a block: a thread adds every 32nd block's, the shares are
+// added in order, all in f64, so that reruns give the same bits. (The last block to finish did it before, alone: 456
+// blocks of 256 columns took it 40 us.)
+__global__ void __launch_bounds__(256) qk_gain_sum_kernel(int D, int blocks, const float* __restrict__ part, float* dgq,
+                                                          float* dgk, int accumulate) {
+  __shared__ double sums[32][8];
+  wait_for_previous_kernel();
+  const int j = threadIdx.x & 7, share = threadIdx.x >> 3, col = blockIdx.x * 8 + j;
+  double t = 0.0;
 #pragma unroll 8
-    for (int b = b0; b < b1; ++b) t += static_cast<double>(__ldcg(a.part + static_cast<int64_t>(b) * 2 * a.D + col0 + lane));
-    __syncthreads();
-    sums[warp * 32 + lane] = t;
-    __syncthreads();
-    if (warp == 0) {
-      double v = 0.0;
-      for (int w = 0; w < kQkWarps; ++w) v += sums[w * 32 + lane];
-      const int col = col0 + lane;
-      float* out = col < a.D ? a.dgq : a.dgk;
-      if (out) {
-        float& o = out[col < a.D ? col : col - a.D];
-        o = static_cast<float>(a.accumulate ? v + o : v);
-      }
-    }
-  }
+  for (int b = share; b < blocks; b += 32) t += static_cast<double>(part[static_cast<int64_t>(b) * 2 * D + col]);
+  sums[share][j] = t;
+  __syncthreads();
+  if (share != 0) return;
+  t = 0.0;
+  for (int k = 0; k < 32; ++k) t += sums[k][j];
+  float* out = col < D ? dgq : dgk;
+  if (!out) return;
+  float& o = out[col < D ? col : col - D];
+  o = static_cast<float>(accumulate ? t + o : t);
 }
 
 // cos and sin of t theta^(-2 i / R), in double and rounded once.
@@ -343,74 +404,145 @@ struct DropArgs {
   float scale;
 };
 
-// Bit j: column 8 b + j of the row is kept.
-static __device__ __forceinline__ uint32_t keep8(const DropArgs& a, uint32_t traj, uint32_t pos, int b) {
-  const uint4 w = philox4x32_10(make_uint4((a.site << 16) + static_cast<uint32_t>(b), pos, traj, a.step), a.k0, a.k1);
-  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+// The four words of a row's block b of eight columns; column 8 b + j is kept where the low (even j) or high half of word
+// j / 2 is at least the cut. Halves are compared in the upper 16 bits of a word: cut is K 2^16, and what lies below the
+// half does not change the comparison.
+static __device__ __forceinline__ uint4 draw8(const DropArgs& a, uint32_t traj, uint32_t pos, int b) {
+  return philox4x32_10(make_uint4((a.site << 16) + static_cast<uint32_t>(b), pos, traj, a.step), a.k0, a.k1);
+}
+static __device__ __forceinline__ bool kept(const uint4& w, int j, uint32_t cut) {
+  const uint32_t v = j < 2 ? w.x : j < 4 ? w.y : j < 6 ? w.z : w.w;
+  return ((j & 1) ? v : v << 16) >= cut;
+}
+
+static __device__ __forceinline__ uint32_t kept8(const DropArgs& a, uint32_t traj, uint32_t pos, int b) {
+  const uint4 w = draw8(a, traj, pos, b);
   uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    m |= ((v[i] & 0xffffu) >= a.cut ? 1u << 2 * i : 0u) | ((v[i] >> 16) >= a.cut ? 2u << 2 * i : 0u);
+  for (int j = 0; j < 8; ++j) m |= kept(w, j, a.cut) ? 1u << j : 0u;
   return m;
 }
 
-// HBM-bound next to about ten integer operations an element. VEC: rows of whole blocks at 16-byte boundaries, a
-// lane's eight columns in 16-byte accesses. Otherwise the lanes of a warp load 32 neighbouring elements at a time and
-// get each one's bit from the lane that drew it.
+// HBM-bound next to about a dozen integer operations an element.
+//   kWhole    rows of whole blocks at 16-byte boundaries: a lane's eight columns in 16-byte accesses, two blocks under way
+//   kShifted  rows that start anywhere, but x, res and y alike: a lane takes the eight columns at a 16-byte boundary, which
+//             lie in two blocks; the mask of the other one comes from its neighbour (from the round before for the first
+//             lane), and only a row's two ends go element by element
+//   kAnyhow   otherwise: the lanes load G neighbouring elements of a row at a time, all of a round before its first is
+//             used, and get each one's bit from the lane that drew it
+enum DropRows { kWhole = 0, kShifted = 1, kAnyhow = 2 };
 constexpr int kDropThreads = 256;
 
-template <class T, bool RES, bool VEC>
-__global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropArgs a) {
+template <class T, bool RES, int ROWS>
+__global__ void __launch_bounds__(kDropThreads, sizeof(T) == 4 || ROWS != kWhole ? 3 : 4) dropout_kernel(const DropArgs a) {
   const int lane = threadIdx.x & 31, c = lane & (a.G - 1), slot = lane / a.G, rows = 32 / a.G;
   const int64_t row_units = (a.N + rows - 1) / rows, units = row_units * a.parts;
   const int64_t stride = static_cast<int64_t>(gridDim.x) * (kDropThreads / 32);
-  const T* xs = static_cast<const T*>(a.x);
-  const T* rs = static_cast<const T*>(a.res);
-  T* ys = static_cast<T*>(a.y);
   for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kDropThreads / 32) + (threadIdx.x >> 5); u < units; u += stride) {
-    const int64_t ru = u / a.parts;
+    const int64_t ru = a.parts == 1 ? u : u / a.parts;
     const int part = static_cast<int>(u - ru * a.parts);
     const int64_t row = ru * rows + slot;
     const bool live = row < a.N;
     const uint32_t traj = live ? static_cast<uint32_t>(__ldg(a.traj + row)) + a.traj_base : 0u;
     const uint32_t pos = live ? static_cast<uint32_t>(__ldg(a.pos + row)) : 0u;
+    const T* xs = static_cast<const T*>(a.x) + row * a.ldx;
+    const T* rs = static_cast<const T*>(a.res) + (RES ? row * a.ldr : 0);
+    T* ys = static_cast<T*>(a.y) + row * a.ldy;
     // this warp's share of the row's blocks, in whole rounds of G
     const int rounds = (a.blocks + a.G - 1) / a.G;
     const int t0 = static_cast<int>(static_cast<int64_t>(rounds) * part / a.parts);
     const int t1 = static_cast<int>(static_cast<int64_t>(rounds) * (part + 1) / a.parts);
-    if (VEC) {
-#pragma unroll 2
-      for (int t = t0; t < t1; ++t) {
-        const int b = t * a.G + c;
-        if (!live || b >= a.blocks) continue;
-        Raw8<T> rx, rr;
-        rx.load(xs + row * a.ldx + 8 * b);
-        if (RES) rr.load(rs + row * a.ldr + 8 * b);
-        const uint32_t m = keep8(a, traj, pos, b);
-        float x[8], r[8], y[8];
-        rx.get(x);
-        if (RES) rr.get(r);
+    if (ROWS == kWhole) {
+      for (int t = t0; t < t1; t += 2) {
+        Raw8<T> rx[2], rr[2];
+        bool in[2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float base = RES ? r[j] : 0.f;
-          y[j] = (m >> j & 1u) ? fmaf(x[j], a.scale, base) : base;
+        for (int h = 0; h < 2; ++h) {
+          const int b = (t + h) * a.G + c;
+          in[h] = live && t + h < t1 && b < a.blocks;
+          rx[h].zero();
+          if (RES) rr[h].zero();
+          if (!in[h]) continue;
+          rx[h].load(xs + 8 * b);
+          if (RES) rr[h].load(rs + 8 * b);
         }
-        Raw8<T>::store(ys + row * a.ldy + 8 * b, y);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int b = (t + h) * a.G + c;
+          const uint4 w = draw8(a, traj, pos, b);
+          float x[8], y[8];
+          rx[h].get(x);
+          if (RES) rr[h].get(y);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float base = RES ? y[j] : 0.f;
+            y[j] = kept(w, j, a.cut) ? fmaf(x[j], a.scale, base) : base;
+          }
+          if (in[h]) Raw8<T>::store(ys + 8 * b, y);
+        }
+      }
+    } else if (ROWS == kShifted) {
+      const int off = static_cast<int>((reinterpret_cast<uintptr_t>(xs) & 15) / sizeof(T));
+      // the mask of the block before this share's first (there is none before column 0)
+      uint32_t carry = t0 > 0 ? kept8(a, traj, pos, t0 * a.G - 1) : 0u;
+      for (int t = t0; t < t1; t += 2) {
+        Raw8<T> rx[2], rr[2];
+        int c0[2];
+        bool all[2], some[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          c0[h] = 8 * ((t + h) * a.G + c) - off;
+          some[h] = live && t + h < t1 && c0[h] < a.d;
+          all[h] = some[h] && c0[h] >= 0 && c0[h] + 8 <= a.d;
+          rx[h].zero();
+          if (RES) rr[h].zero();
+          if (!all[h]) continue;
+          rx[h].load(xs + c0[h]);
+          if (RES) rr[h].load(rs + c0[h]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t m = kept8(a, traj, pos, (t + h) * a.G + c);
+          const uint32_t before = __shfl_sync(0xffffffffu, m, slot * a.G + ((c + a.G - 1) & (a.G - 1)));
+          const uint32_t k = ((c == 0 ? carry : before) | m << 8) >> (8 - off);   // bit j: column c0 + j
+          carry = before;
+          if (all[h]) {
+            float x[8], y[8];
+            rx[h].get(x);
+            if (RES) rr[h].get(y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float base = RES ? y[j] : 0.f;
+              y[j] = (k >> j & 1u) ? fmaf(x[j], a.scale, base) : base;
+            }
+            Raw8<T>::store(ys + c0[h], y);
+          } else if (some[h]) {
+            for (int j = 0; j < 8; ++j) {
+              const int col = c0[h] + j;
+              if (col < 0 || col >= a.d) continue;
+              const float base = RES ? Elem<T>::get(rs[col]) : 0.f;
+              ys[col] = Elem<T>::put((k >> j & 1u) ? fmaf(Elem<T>::get(xs[col]), a.scale, base) : base);
+            }
+          }
+        }
       }
     } else {
       for (int t = t0; t < t1; ++t) {
         const int b0 = t * a.G;
-        const uint32_t m = b0 + c < a.blocks ? keep8(a, traj, pos, b0 + c) : 0u;
-        // the round's 8 G columns of this lane's row, G at a time
+        float x[8], y[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int in_round = j * a.G + c;
+          const int col = b0 * 8 + j * a.G + c;
+          const bool in = live && col < a.d;
+          x[j] = in ? Elem<T>::get(xs[col]) : 0.f;
+          y[j] = RES && in ? Elem<T>::get(rs[col]) : 0.f;
+        }
+        const uint32_t m = kept8(a, traj, pos, b0 + c);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int in_round = j * a.G + c, col = b0 * 8 + in_round;
           const uint32_t mm = __shfl_sync(0xffffffffu, m, slot * a.G + (in_round >> 3));
-          const int col = b0 * 8 + in_round;
-          if (!live || col >= a.d) continue;
-          const float base = RES ? Elem<T>::get(rs[row * a.ldr + col]) : 0.f;
-          const float x = Elem<T>::get(xs[row * a.ldx + col]);
-          ys[row * a.ldy + col] = Elem<T>::put((mm >> (in_round & 7) & 1u) ? fmaf(x, a.scale, base) : base);
+          if (live && col < a.d) ys[col] = Elem<T>::put((mm >> (in_round & 7) & 1u) ? fmaf(x[j], a.scale, y[j]) : y[j]);
         }
       }
     }
@@ -431,7 +563,7 @@ static int parts_for(int64_t rows, int64_t want, int steps) {
   const int64_t p = want / rows;
   return static_cast<int>(p < steps ? p : steps);
 }
-constexpr int64_t kQkMaxBlocks = 608;   // four per SM; the backward's workspace holds this many partial sums
+constexpr int64_t kQkMaxBlocks = 760;   // five per SM; the backward's workspace holds a partial sum of each
 
 // A row of heads: its pitch, base and the rows' last element stay within what the kernel addresses.
 static bool rows_ok(const void* p, int64_t ld, int64_t cols, int dtype) {
@@ -449,17 +581,23 @@ static int launch_qk(QkArgs a, int dtype, int layout, cudaStream_t s) {
   const int at_once = 32 / a.G;
   const int steps = (a.Hq + at_once - 1) / at_once + (a.Hk + at_once - 1) / at_once;
   const int sms = num_sms_current();
-  a.parts = parts_for(a.N, static_cast<int64_t>(sms) * kQkWarps, steps);
+  a.parts = parts_for(a.N, static_cast<int64_t>(sms) * 2 * kQkWarps, steps);
   const int64_t want = (a.N * a.parts + kQkWarps - 1) / kQkWarps;
-  const unsigned grid = static_cast<unsigned>(want < kQkMaxBlocks ? want : kQkMaxBlocks);
-  const size_t gains = 2 * sizeof(float) * a.D, least = sizeof(double) * kQkWarps * 32;
-  const size_t all = BWD ? gains * (1 + kQkWarps) : gains;
-  const size_t smem = all > least ? all : least;
+  // resident blocks (see the launch bounds) take their units in turn
+  int64_t most = static_cast<int64_t>(sms) * (BWD ? 3 : 5);
+  if (most > kQkMaxBlocks) most = kQkMaxBlocks;
+  const unsigned grid = static_cast<unsigned>(want < most ? want : most);
+  const size_t gains = 2 * sizeof(float) * a.D, smem = BWD ? gains * (1 + kQkWarps) : gains;
   // a block sets its bit early, so one block of several cannot clear the status
   if (grid > 1 && cudaMemsetAsync(a.status, 0, kWsHeader, s) != cudaSuccess) return PS_ERR_CUDA;
   auto go = [&](auto kern) {
     kern<<<grid, kQkThreads, smem, s>>>(a);
-    return cudaGetLastError() == cudaSuccess ? PS_OK : refused(PS_ERR_CUDA, a.status, s);
+    if (cudaGetLastError() != cudaSuccess) return refused(PS_ERR_CUDA, a.status, s);
+    if (!a.part) return static_cast<int>(PS_OK);
+    return launch_after(qk_gain_sum_kernel, dim3(static_cast<unsigned>(2 * a.D / 8)), 256, 0, s, 1, 1, true, a.D,
+                        static_cast<int>(grid), a.part, a.dgq, a.dgk, a.accumulate) == cudaSuccess
+               ? static_cast<int>(PS_OK)
+               : static_cast<int>(PS_ERR_CUDA);
   };
   if (dtype == PS_DTYPE_BF16)
     return layout == PS_ROPE_EVEN ? go(qk_kernel<Bf16, true, BWD>) : go(qk_kernel<Bf16, false, BWD>);
@@ -570,28 +708,38 @@ int ps_dropout_rows(int64_t N, int d, int dtype, const void* x, int64_t ldx, con
   a.x = x, a.res = res, a.y = y, a.ldx = ldx, a.ldr = ldr, a.ldy = ldy, a.traj = row_traj, a.pos = row_pos;
   a.traj_base = static_cast<uint32_t>(traj_base), a.step = static_cast<uint32_t>(step);
   a.site = static_cast<uint32_t>(site), a.k0 = static_cast<uint32_t>(seed), a.k1 = static_cast<uint32_t>(seed >> 32);
-  a.cut = static_cast<uint32_t>(cut);
+  a.cut = static_cast<uint32_t>(cut) << 16;
   a.scale = static_cast<float>(65536.0 / (65536.0 - cut));
+  // rows whose starts lie alike to 16 bytes can be read and written 16 bytes at a time
+  auto start = [&](const void* v, int64_t ld, int64_t row) {
+    return (reinterpret_cast<uintptr_t>(v) + static_cast<uint64_t>(row) * static_cast<uint64_t>(ld) * e) % 16;
+  };
+  auto alike = [&](const void* v, int64_t ld) {   // the first two rows decide all
+    return start(v, ld, 0) == start(x, ldx, 0) && (N == 1 || start(v, ld, 1) == start(x, ldx, 1));
+  };
+  int kind = alike(y, ldy) && (!res || alike(res, ldr)) ? kShifted : kAnyhow;
+  if (kind == kShifted && d % 8 == 0 && start(x, ldx, 0) == 0 && (N == 1 || start(x, ldx, 1) == 0)) kind = kWhole;
+  if (kind == kShifted) a.blocks = (d + 16 / e - 1 + 7) / 8;   // at the largest shift
   a.G = lanes_for(a.blocks);
   const int rows = 32 / a.G, sms = num_sms_current();
   const int64_t row_units = (N + rows - 1) / rows;
   a.parts = parts_for(row_units, static_cast<int64_t>(sms) * 32, (a.blocks + a.G - 1) / a.G);
   const int64_t want = (row_units * a.parts + kDropThreads / 32 - 1) / (kDropThreads / 32);
-  const int64_t most = static_cast<int64_t>(sms) * 8;
+  const int64_t most = static_cast<int64_t>(sms) * 4;
   const unsigned grid = static_cast<unsigned>(want < most ? want : most);
-  const bool vec = d % 8 == 0 && rows_ok(x, ldx, d, dtype) && rows_ok(y, ldy, d, dtype) &&
-                   (!res || rows_ok(res, ldr, d, dtype));
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   auto go = [&](auto kern) {
     kern<<<grid, kDropThreads, 0, s>>>(a);
     return cudaGetLastError() == cudaSuccess ? PS_OK : PS_ERR_CUDA;
   };
   if (dtype == PS_DTYPE_BF16) {
-    if (vec) return res ? go(dropout_kernel<Bf16, true, true>) : go(dropout_kernel<Bf16, false, true>);
-    return res ? go(dropout_kernel<Bf16, true, false>) : go(dropout_kernel<Bf16, false, false>);
+    if (kind == kWhole) return res ? go(dropout_kernel<Bf16, true, kWhole>) : go(dropout_kernel<Bf16, false, kWhole>);
+    if (kind == kShifted) return res ? go(dropout_kernel<Bf16, true, kShifted>) : go(dropout_kernel<Bf16, false, kShifted>);
+    return res ? go(dropout_kernel<Bf16, true, kAnyhow>) : go(dropout_kernel<Bf16, false, kAnyhow>);
   }
-  if (vec) return res ? go(dropout_kernel<float, true, true>) : go(dropout_kernel<float, false, true>);
-  return res ? go(dropout_kernel<float, true, false>) : go(dropout_kernel<float, false, false>);
+  if (kind == kWhole) return res ? go(dropout_kernel<float, true, kWhole>) : go(dropout_kernel<float, false, kWhole>);
+  if (kind == kShifted) return res ? go(dropout_kernel<float, true, kShifted>) : go(dropout_kernel<float, false, kShifted>);
+  return res ? go(dropout_kernel<float, true, kAnyhow>) : go(dropout_kernel<float, false, kAnyhow>);
 }
 
 }  // extern "C"
