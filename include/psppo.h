@@ -473,11 +473,11 @@ int ps_lmhead_ppo_fwd_noalloc(int64_t N, int d, int V, int dtype, const void* Hp
  * ------------------------------------------------------------------------- */
 enum { PS_ACT_SILU = 0, PS_ACT_GELU = 1 };
 size_t ps_gated_ffn_store_size(int64_t N, int F);
-size_t ps_gated_ffn_fwd_workspace_size(int64_t N, int F, int with_store);
+size_t ps_gated_ffn_fwd_workspace_size(int64_t N, int d, int F, int with_store);
 int ps_gated_ffn_fwd(int64_t N, int d, int F, int dtype, int act, const void* X, int64_t ldx,
                      const void* Wg, const void* Wu, const void* Wd, void* Y, int64_t ldy,
                      void* store, size_t store_bytes, void* ws, size_t ws_bytes, ps_stream_t stream);
-size_t ps_gated_ffn_bwd_workspace_size(void);
+size_t ps_gated_ffn_bwd_workspace_size(int64_t N, int d, int F);
 int ps_gated_ffn_bwd(int64_t N, int d, int F, int dtype, const void* dY, int64_t lddy,
                      const void* X, int64_t ldx, const void* Wg, const void* Wu, const void* Wd,
                      void* store, size_t store_bytes, void* dX, int64_t lddx, int dx_dtype,

@@ -116,10 +116,10 @@ _SIGS = {
     "ps_lmhead_ppo_fwd_noalloc": (_i32, [_i64, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _f64, _f64,
                                          _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
     "ps_gated_ffn_store_size": (_sz, [_i64, _i32]),
-    "ps_gated_ffn_fwd_workspace_size": (_sz, [_i64, _i32, _i32]),
+    "ps_gated_ffn_fwd_workspace_size": (_sz, [_i64, _i32, _i32, _i32]),
     "ps_gated_ffn_fwd": (_i32, [_i64, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _sz, _vp, _sz,
                                 _vp]),
-    "ps_gated_ffn_bwd_workspace_size": (_sz, []),
+    "ps_gated_ffn_bwd_workspace_size": (_sz, [_i64, _i32, _i32]),
     "ps_gated_ffn_bwd": (_i32, [_i64, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _sz, _vp, _i64, _i32,
                                 _vp, _vp, _vp, _i32, _i32, _vp, _sz, _vp]),
     "ps_rope_table": (_i32, [_i32, _i32, _f64, _vp, _vp]),
@@ -393,8 +393,8 @@ def ps_gated_ffn_store_size(N: int, F: int) -> int:
     return lib().ps_gated_ffn_store_size(N, F)
 
 
-def ps_gated_ffn_fwd_workspace_size(N: int, F: int, with_store: bool) -> int:
-    return lib().ps_gated_ffn_fwd_workspace_size(N, F, int(with_store))
+def ps_gated_ffn_fwd_workspace_size(N: int, d: int, F: int, with_store: bool) -> int:
+    return lib().ps_gated_ffn_fwd_workspace_size(N, d, F, int(with_store))
 
 
 def ps_gated_ffn_fwd(N, d, F, dtype, act, X, Wg, Wu, Wd, Y, store, ws, stream=None):
@@ -405,8 +405,8 @@ def ps_gated_ffn_fwd(N, d, F, dtype, act, X, Wg, Wu, Wd, Y, store, ws, stream=No
     _check(rc, "ps_gated_ffn_fwd")
 
 
-def ps_gated_ffn_bwd_workspace_size() -> int:
-    return lib().ps_gated_ffn_bwd_workspace_size()
+def ps_gated_ffn_bwd_workspace_size(N: int, d: int, F: int) -> int:
+    return lib().ps_gated_ffn_bwd_workspace_size(N, d, F)
 
 
 def ps_gated_ffn_bwd(N, d, F, dtype, dY, X, Wg, Wu, Wd, store, dX, dx_dtype, dWg, dWu, dWd, dw_dtype, flags, ws,

@@ -83,13 +83,13 @@ class GatedFFN:
         bf16 = dict(dtype=torch.bfloat16, device=device)
         u8 = dict(dtype=torch.uint8, device=device)   # zeroed: a status word never written reads clear
         self.Y = torch.empty(s.rows, s.d, **bf16)
-        self.ws_fwd = torch.zeros(B.ps_gated_ffn_fwd_workspace_size(s.rows, s.F, s.train), **u8)
+        self.ws_fwd = torch.zeros(B.ps_gated_ffn_fwd_workspace_size(s.rows, s.d, s.F, s.train), **u8)
         self._fwd_tail = (None, 0, self.ws_fwd.data_ptr(), self.ws_fwd.numel())
         self.store = self.ws_bwd = None
         self.stored = -1              # rows of the last forward, until its backward has used the store
         if s.train:
             self.store = torch.empty(B.ps_gated_ffn_store_size(s.rows, s.F), **u8)
-            self.ws_bwd = torch.zeros(B.ps_gated_ffn_bwd_workspace_size(), **u8)
+            self.ws_bwd = torch.zeros(B.ps_gated_ffn_bwd_workspace_size(s.rows, s.d, s.F), **u8)
             self.dX = torch.empty(s.rows, s.d, dtype=s.dx_dtype, device=device)
             self.dWg, self.dWu = (torch.empty(s.F, s.d, dtype=s.dw_dtype, device=device) for _ in range(2))
             self.dWd = torch.empty(s.d, s.F, dtype=s.dw_dtype, device=device)

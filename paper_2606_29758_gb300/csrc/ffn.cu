@@ -18,6 +18,7 @@
 
 #include "internal.h"
 #include "ps_nvtx.h"
+#include "umma_group.cuh"
 #include "umma_host.cuh"
 
 namespace psk {
@@ -388,8 +389,9 @@ struct FfnStore {
   uint32_t* scale;       // [ceil(F / 32)][N]: the biased exponents of P (bits 0-7) and Q (8-15)
   size_t bytes;
 };
+static size_t plane_bytes(int64_t N, int F) { return (static_cast<size_t>(N) * F * 2 + 255) / 256 * 256; }
 static FfnStore ffn_store(void* base, int64_t N, int F) {
-  const size_t plane = (static_cast<size_t>(N) * F * 2 + 255) / 256 * 256;
+  const size_t plane = plane_bytes(N, F);
   uint8_t* b = static_cast<uint8_t*>(base);
   FfnStore f;
   f.A = reinterpret_cast<uint16_t*>(b);
@@ -460,7 +462,6 @@ static int ffn_up(int64_t N, int d, int F, const void* X, int64_t ldx, const voi
   if (!map_kmajor(&m.a, X, N, d, ldx, kBM * halves) || !map_kmajor(&m.b, Wg, F, d, d, kBN / 2) ||
       !map_kmajor(&m.b2, Wu, F, d, d, kBN / 2) || !map_out_16(&m.c, f.A, N, F, F))
     return PS_ERR_INVALID_ARG;
-  m.a2 = m.a;
   m.c2 = m.c3 = m.c;
   if (KEEP && (!map_out_16(&m.c2, f.P, N, F, F, CU_TENSOR_MAP_DATA_TYPE_FLOAT16) ||
                !map_out_16(&m.c3, f.Q, N, F, F, CU_TENSOR_MAP_DATA_TYPE_FLOAT16)))
@@ -471,19 +472,6 @@ static int ffn_up(int64_t N, int d, int F, const void* X, int64_t ldx, const voi
                      : launch_gemm_two<false, false, Epi, 2, kTwoB>(m, N, F, d, band, ep, status, s, true);
 }
 
-static int ffn_down(int64_t N, int d, int F, const void* A, const void* Wd, void* Y, int64_t ldy, uint32_t* status,
-                    cudaStream_t s) {
-  if (N <= kFewRows) return ffn_few<false, PS_ACT_SILU>(N, d, F, A, F, Wd, Wd, Y, ldy, status, s);
-  const int halves = tile_halves(N, d, 18);
-  CUtensorMap ta, tb, tc;
-  if (!map_kmajor(&ta, A, N, F, F, kBM * halves) || !map_kmajor(&tb, Wd, d, F, F, kBN) || !map_out_16(&tc, Y, N, d, ldy))
-    return PS_ERR_INVALID_ARG;
-  const StoreBf16Epi::Params ep{d};
-  return halves == 1
-             ? launch_gemm_single<false, false, StoreBf16Epi, 1>(ta, tb, tc, N, d, F, 0, 2 * kBandLongK, ep, status, s)
-             : launch_gemm_single<false, false, StoreBf16Epi, 2>(ta, tb, tc, N, d, F, 0, kBandLongK, ep, status, s);
-}
-
 // dA = dY Wd and, from the kept P and Q, dG and dU over them.
 static int ffn_da(int64_t N, int d, int F, const void* dY, int64_t lddy, const void* Wd, const FfnStore& f,
                   uint32_t* status, cudaStream_t s) {
@@ -492,7 +480,6 @@ static int ffn_da(int64_t N, int d, int F, const void* dY, int64_t lddy, const v
   if (!map_kmajor(&m.a, dY, N, d, lddy, kBM * halves) || !map_mnmajor(&m.b, Wd, d, F, F) ||
       !map_out_16(&m.c, f.P, N, F, F) || !map_out_16(&m.c2, f.Q, N, F, F))
     return PS_ERR_INVALID_ARG;
-  m.a2 = m.a;
   m.b2 = m.b;
   m.c3 = m.c;
   const FfnDaEpi::Params ep{static_cast<int>(N), F, f.P, f.Q, f.scale};
@@ -501,64 +488,274 @@ static int ffn_da(int64_t N, int d, int F, const void* dY, int64_t lddy, const v
                      : launch_gemm_two<false, true, FfnDaEpi, 2, kNoPair>(m, N, F, d, band, ep, status, s, true);
 }
 
-template <class Epi>
-static typename Epi::Params store_params(int N, int accumulate);
-template <>
-StoreF32Epi::Params store_params<StoreF32Epi>(int N, int accumulate) {
-  return {N, accumulate};
+// ----------------------------------------------------------------------------- products in one launch
+// The products of a group as the caller states them, and how they are cut (the same on every device: what the workspace
+// holds depends on it).
+struct Product {
+  int64_t M, N, K;              // outputs and the K loop (of each operand set)
+  bool two_sets;                // product 0 only
+  bool a_mn, b_mn;
+  const void *A, *A2, *B, *B2;
+  int64_t lda, ldb;
+  void* out;
+  int64_t ldo;
+  int kind;                     // kOutBf16, kOutF32 or kOutF32Add
+};
+struct GroupPlan {
+  int halves;
+  int splits[kGroupMost];
+  size_t part_off[kGroupMost], bytes;   // the partial tiles' places
+};
+constexpr int kPlanSms = 152;
+constexpr int kLeastKb = 12;   // k blocks a share has at least: below that its partial tile costs more than it saves
+
+static int64_t tiles_of(const Product& p, int halves) {
+  return (p.M + kBM * halves - 1) / (kBM * halves) * ((p.N + kBN - 1) / kBN);
 }
-template <>
-StoreBf16Epi::Params store_params<StoreBf16Epi>(int N, int) {
-  return {N};
+static int kb_of(const Product& p) {
+  const int64_t kb = (p.K + kBK - 1) / kBK;
+  return static_cast<int>(p.two_sets ? 2 * kb : kb);
 }
-template <class Epi>
-static bool map_out(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t pitch) {
-  return std::is_same<Epi, StoreF32Epi>::value ? map_out_f32(m, base, rows, cols, pitch)
-                                               : map_out_16(m, base, rows, cols, pitch);
+// What a unit costs, in hundredths of a wide tile's k block (0.55 us): its k blocks, or the writing of its outputs where
+// that takes longer (43 GB/s an SM), and its start and end.
+static double unit_cost(const Product& p, int halves, int splits) {
+  const double kb = static_cast<double>(kb_of(p)) / splits * (halves == 2 ? 100 : 66);
+  const double out = kBM * halves * kBN * (splits > 1 || p.kind != kOutBf16 ? 4 : 2) * 4.2e-3;
+  return (kb > out ? kb : out) + (halves == 2 ? 200 : 120);
 }
 
-// dX (+)= dG Wg + dU Wu
-template <class Epi>
-static int ffn_dx(int64_t N, int d, int F, const FfnStore& f, const void* Wg, const void* Wu, void* dX, int64_t lddx,
-                  int accumulate, uint32_t* status, cudaStream_t s) {
-  const int halves = tile_halves(N, d, 18);
-  TwoMaps m;
-  if (!map_kmajor(&m.a, f.P, N, F, F, kBM * halves) || !map_kmajor(&m.a2, f.Q, N, F, F, kBM * halves) ||
-      !map_mnmajor(&m.b, Wg, F, d, d) || !map_mnmajor(&m.b2, Wu, F, d, d) || !map_out<Epi>(&m.c, dX, N, d, lddx))
-    return PS_ERR_INVALID_ARG;
-  m.c2 = m.c3 = m.c;
-  const auto ep = store_params<Epi>(d, accumulate);
-  return halves == 1 ? launch_gemm_two<false, true, Epi, 1, kSumK>(m, N, d, F, 2 * kBandLongK, ep, status, s, false)
-                     : launch_gemm_two<false, true, Epi, 2, kSumK>(m, N, d, F, kBandLongK, ep, status, s, false);
+// CTAs with the same load, side by side.
+struct LoadSeg {
+  int cta0, cta1;
+  double load;
+};
+struct Loads {
+  LoadSeg seg[kGroupSegs];
+  int n;
+};
+// n units of one cost dealt to the CTAs so that the highest load is lowest: what fits under the level that they would fill
+// if they could be cut anywhere, then one more each for those that it leaves lowest. Splits one segment at most. Returns
+// the highest load; out: what each segment takes.
+static_assert(kGroupSegs > kGroupMost + 1, "a segment more with each product");
+static double deal(Loads& L, int64_t n, double cost, GroupSeg* out, int* out_n) {
+  int64_t take[kGroupSegs];
+  bool more[kGroupSegs];
+  double level = 0;
+  for (int i = 0; i < L.n; ++i) more[i] = true;
+  for (bool again = true; again;) {   // the level, without the segments that are above it already
+    double sum = static_cast<double>(n) * cost, ctas = 0;
+    for (int i = 0; i < L.n; ++i)
+      if (more[i]) {
+        sum += L.seg[i].load * (L.seg[i].cta1 - L.seg[i].cta0);
+        ctas += L.seg[i].cta1 - L.seg[i].cta0;
+      }
+    level = sum / ctas;
+    again = false;
+    for (int i = 0; i < L.n; ++i)
+      if (more[i] && L.seg[i].load > level) {
+        more[i] = false;
+        again = true;
+      }
+  }
+  int64_t left = n;
+  for (int i = 0; i < L.n; ++i) {
+    const int len = L.seg[i].cta1 - L.seg[i].cta0;
+    take[i] = more[i] ? static_cast<int64_t>((level - L.seg[i].load) / cost) : 0;
+    if (take[i] * len > left) take[i] = left / len;   // (rounding)
+    left -= take[i] * len;
+  }
+  while (left > 0) {
+    int w = 0;
+    for (int i = 1; i < L.n; ++i)
+      if (L.seg[i].load + take[i] * cost < L.seg[w].load + take[w] * cost) w = i;
+    const int len = L.seg[w].cta1 - L.seg[w].cta0;
+    if (left < len) {
+      for (int i = L.n; i > w + 1; --i) {
+        L.seg[i] = L.seg[i - 1];
+        take[i] = take[i - 1];
+      }
+      L.seg[w + 1] = L.seg[w];
+      L.seg[w].cta1 = L.seg[w + 1].cta0 = L.seg[w].cta0 + static_cast<int>(left);
+      take[w + 1] = take[w];
+      ++L.n;
+    }
+    ++take[w];
+    left -= L.seg[w].cta1 - L.seg[w].cta0;
+  }
+  double most = 0;
+  int64_t unit = 0;
+  *out_n = 0;
+  for (int i = 0; i < L.n; ++i) {
+    const int len = L.seg[i].cta1 - L.seg[i].cta0;
+    if (take[i] > 0) {
+      out[(*out_n)++] = {L.seg[i].cta0, L.seg[i].cta1, static_cast<int>(take[i]), static_cast<int>(unit)};
+      unit += take[i] * len;
+      L.seg[i].load += take[i] * cost;
+    }
+    if (L.seg[i].load > most) most = L.seg[i].load;
+  }
+  return most;
 }
 
-// dWg (+)= dG^T X and dWu (+)= dU^T X, one below the other
-template <class Epi>
-static int ffn_dw_up(int64_t N, int d, int F, const FfnStore& f, const void* X, int64_t ldx, void* dWg, void* dWu,
-                     int accumulate, uint32_t* status, cudaStream_t s) {
-  TwoMaps m;
-  if (!map_mnmajor(&m.a, f.P, N, F, F) || !map_mnmajor(&m.a2, f.Q, N, F, F) || !map_mnmajor(&m.b, X, N, d, ldx) ||
-      !map_out<Epi>(&m.c, dWg, F, d, d) || !map_out<Epi>(&m.c2, dWu, F, d, d))
-    return PS_ERR_INVALID_ARG;
-  m.b2 = m.b;
-  m.c3 = m.c;
-  const auto ep = store_params<Epi>(d, accumulate);
-  const int halves = tile_halves(2 * static_cast<int64_t>(F), d, 17);
-  return halves == 1 ? launch_gemm_two<true, true, Epi, 1, kTwoM>(m, F, d, N, 2 * kBandLongK, ep, status, s, false)
-                     : launch_gemm_two<true, true, Epi, 2, kTwoM>(m, F, d, N, kBandLongK, ep, status, s, false);
+// The tile's height and each product's shares: a product whose tiles are fewer than the SMs is split into shares of what an
+// SM has to do anyway, or of kLeastKb; the height is the one whose dealt units end first.
+static GroupPlan plan_group(const Product* p, int count) {
+  GroupPlan best;
+  double best_cost = 0;
+  for (int halves = 2; halves >= 1; --halves) {
+    GroupPlan g;
+    g.halves = halves;
+    double work = 0, cost = 0;
+    for (int t = 0; t < count; ++t) work += static_cast<double>(tiles_of(p[t], halves)) * unit_cost(p[t], halves, 1);
+    const double fair = work / kPlanSms / (halves == 2 ? 100 : 66);   // k blocks
+    Loads L;
+    L.n = 1;
+    L.seg[0] = {0, kPlanSms, 0.0};
+    for (int t = 0; t < count; ++t) {
+      const int kb = kb_of(p[t]);
+      const int64_t tiles = tiles_of(p[t], halves);
+      const double share = fair > kLeastKb ? fair : kLeastKb;
+      int s = static_cast<int>(kb / share + 0.5);
+      if (tiles >= kPlanSms) s = 1;
+      if (s * tiles > 2 * kPlanSms) s = static_cast<int>(2 * kPlanSms / tiles);
+      g.splits[t] = s < 2 ? 1 : s;
+      GroupSeg seg[kGroupSegs];
+      int n;
+      const double end = deal(L, tiles * g.splits[t], unit_cost(p[t], halves, g.splits[t]), seg, &n);
+      if (end > cost) cost = end;
+    }
+    for (int t = 0; t < count; ++t)
+      if (g.splits[t] > 1) cost += 500 + 1.45e-4 * g.splits[t] * p[t].M * p[t].N;   // the shares' way through L2
+    if (best_cost == 0 || cost < best_cost) {
+      best = g;
+      best_cost = cost;
+    }
+  }
+  best.bytes = 0;
+  for (int t = 0; t < count; ++t) {
+    best.part_off[t] = best.bytes;
+    if (best.splits[t] == 1) continue;
+    const size_t rows = (p[t].M + kBM * best.halves - 1) / (kBM * best.halves) * (kBM * best.halves);
+    best.bytes += (best.splits[t] * rows * p[t].N * 4 + 255) / 256 * 256;
+  }
+  return best;
 }
 
-// dWd (+)= dY^T A
-template <class Epi>
-static int ffn_dw_down(int64_t N, int d, int F, const void* dY, int64_t lddy, const FfnStore& f, void* dWd,
-                       int accumulate, uint32_t* status, cudaStream_t s) {
-  CUtensorMap ta, tb, tc;
-  if (!map_mnmajor(&ta, dY, N, d, lddy) || !map_mnmajor(&tb, f.A, N, F, F) || !map_out<Epi>(&tc, dWd, d, F, F))
-    return PS_ERR_INVALID_ARG;
-  const auto ep = store_params<Epi>(F, accumulate);
-  const int halves = tile_halves(d, F, 17);
-  return halves == 1 ? launch_gemm_single<true, true, Epi, 1>(ta, tb, tc, d, F, N, 0, 2 * kBandLongK, ep, status, s)
-                     : launch_gemm_single<true, true, Epi, 2>(ta, tb, tc, d, F, N, 0, kBandLongK, ep, status, s);
+// Bytes that hold the partial tiles of these products or of any some of them, and of as many with fewer rows: a share has
+// at least kLeastKb k blocks, and there are at most two tiles of at most 256 x 256 per SM.
+static size_t part_bytes(const Product* p, int count) {
+  size_t sum = 0;
+  for (int t = 0; t < count; ++t) {
+    const size_t shares = static_cast<size_t>(kb_of(p[t])) / kLeastKb + 1;
+    if (shares < 2) continue;
+    const size_t all = shares * ((p[t].M + 2 * kBM - 1) / (2 * kBM) * (2 * kBM)) * p[t].N * 4;
+    const size_t most = static_cast<size_t>(2 * kPlanSms) * 2 * kBM * kBN * 4;
+    sum += ((all < most ? all : most) + 255) / 256 * 256;
+  }
+  return sum;
+}
+
+template <int HALVES>
+static int launch_group(const GroupArgs& g, uint32_t* status, cudaStream_t s, bool clear) {
+  auto kern = umma_group_kernel<HALVES>;
+  constexpr size_t smem = sizeof(GroupSmem<HALVES>) + 1024;
+  static_assert(smem <= 232448, "shared memory of one CTA");
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
+    return PS_ERR_CUDA;
+  int ctas = 1;
+  for (int t = 0; t < g.count; ++t)
+    for (int i = 0; i < g.segs[t]; ++i) ctas = g.seg[t][i].cta1 > ctas ? g.seg[t][i].cta1 : ctas;
+  return launch_after(kern, dim3(static_cast<unsigned>(ctas)), kGroupThreads, smem, s, 1, 1,
+                      !clear, g, status, kDefaultTimeoutNs) == cudaSuccess
+             ? PS_OK
+             : PS_ERR_CUDA;
+}
+
+// The products p[0 .. count), cut as plan_group says, partial tiles at `part`.
+static int run_group(const Product* p, int count, void* part, uint32_t* status, cudaStream_t s) {
+  const GroupPlan plan = plan_group(p, count);
+  GroupArgs g;
+  SumArgs sums;
+  sums.count = 0;
+  g.count = count;
+  g.clear = 0;
+  Loads loads;
+  loads.n = 1;
+  loads.seg[0] = {0, num_sms_current(), 0.0};
+  const int rows = kBM * plan.halves;
+  for (int t = 0; t < count; ++t) {
+    const Product& q = p[t];
+    GroupProduct& o = g.p[t];
+    o.m_blocks = static_cast<int>((q.M + rows - 1) / rows);
+    o.n_blocks = static_cast<int>((q.N + kBN - 1) / kBN);
+    o.splits = plan.splits[t];
+    o.num_kb = kb_of(q);
+    o.first_kb = q.two_sets ? o.num_kb / 2 : o.num_kb;
+    o.band_m = kBandLongK * (3 - plan.halves);
+    o.a_mn = q.a_mn;
+    o.b_mn = q.b_mn;
+    o.cols = static_cast<int>(q.N);
+    o.part_rows = o.m_blocks * rows;
+    o.out = o.splits > 1 ? kOutPartial : q.kind;
+    deal(loads, static_cast<int64_t>(o.m_blocks) * o.n_blocks * o.splits, unit_cost(q, plan.halves, o.splits), g.seg[t],
+         &g.segs[t]);
+    auto map_a = [&](CUtensorMap* m, const void* at) {
+      return q.a_mn ? map_mnmajor(m, at, q.K, q.M, q.lda) : map_kmajor(m, at, q.M, q.K, q.lda, rows);
+    };
+    auto map_b = [&](CUtensorMap* m, const void* at) {
+      return q.b_mn ? map_mnmajor(m, at, q.K, q.N, q.ldb) : map_kmajor(m, at, q.N, q.K, q.ldb, kBN);
+    };
+    if (!map_a(&g.a[t], q.A) || !map_b(&g.b[t], q.B)) return PS_ERR_INVALID_ARG;
+    if (q.two_sets && (!map_a(&g.a2, q.A2) || !map_b(&g.b2, q.B2))) return PS_ERR_INVALID_ARG;
+    bool ok;
+    if (o.splits > 1) {
+      float* planes = reinterpret_cast<float*>(static_cast<uint8_t*>(part) + plan.part_off[t]);
+      ok = map_out_f32(&g.c[t], planes, static_cast<int64_t>(o.splits) * o.part_rows, q.N, q.N);
+      SumItem& it = sums.item[sums.count];
+      it = {planes, static_cast<int64_t>(o.part_rows) * q.N, o.splits, static_cast<int>(q.M), static_cast<int>(q.N / 4),
+            q.out, q.ldo, q.kind};
+      sums.end[sums.count] = q.M * (q.N / 4) + (sums.count > 0 ? sums.end[sums.count - 1] : 0);
+      ++sums.count;
+    } else {
+      ok = q.kind == kOutBf16 ? map_out_16(&g.c[t], q.out, q.M, q.N, q.ldo) : map_out_f32(&g.c[t], q.out, q.M, q.N, q.ldo);
+    }
+    if (!ok) return PS_ERR_INVALID_ARG;
+  }
+  const int rc = plan.halves == 2 ? launch_group<2>(g, status, s, false) : launch_group<1>(g, status, s, false);
+  if (rc != PS_OK || sums.count == 0) return rc;
+  const int64_t blocks = (sums.end[sums.count - 1] + 255) / 256, most = 8 * static_cast<int64_t>(num_sms_current());
+  return launch_after(sum_partials_kernel, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), 256, 0, s, 1, 1, true,
+                      sums) == cudaSuccess
+             ? PS_OK
+             : PS_ERR_CUDA;
+}
+
+static Product down_product(int64_t N, int d, int F, const void* A, const void* Wd, void* Y, int64_t ldy) {
+  return {N, d, F, false, false, false, A, nullptr, Wd, nullptr, F, F, Y, ldy, kOutBf16};
+}
+static int ffn_down(int64_t N, int d, int F, const void* A, const void* Wd, void* Y, int64_t ldy, void* part,
+                    uint32_t* status, cudaStream_t s) {
+  if (N <= kFewRows) return ffn_few<false, PS_ACT_SILU>(N, d, F, A, F, Wd, Wd, Y, ldy, status, s);
+  const Product p = down_product(N, d, F, A, Wd, Y, ldy);
+  return run_group(&p, 1, part, status, s);
+}
+static size_t down_part_bytes(int64_t N, int d, int F) {
+  const Product p = down_product(N, d, F, nullptr, nullptr, nullptr, d);
+  return N <= kFewRows ? 0 : part_bytes(&p, 1);
+}
+
+// dX = dG Wg + dU Wu, dWg = dG^T X, dWu = dU^T X and dWd = dY^T A, the longest K loop first; those asked for.
+static int grad_products(Product* p, int64_t N, int d, int F, const FfnStore& f, const void* dY, int64_t lddy,
+                         const void* X, int64_t ldx, const void* Wg, const void* Wu, void* dX, int64_t lddx, int dx_kind,
+                         void* dWg, void* dWu, void* dWd, int dw_kind) {
+  int n = 0;
+  if (dX) p[n++] = {N, d, F, true, false, true, f.P, f.Q, Wg, Wu, F, d, dX, lddx, dx_kind};
+  if (dWg) {
+    p[n++] = {F, d, N, false, true, true, f.P, nullptr, X, nullptr, F, ldx, dWg, d, dw_kind};
+    p[n++] = {F, d, N, false, true, true, f.Q, nullptr, X, nullptr, F, ldx, dWu, d, dw_kind};
+  }
+  if (dWd) p[n++] = {d, F, N, false, true, true, dY, nullptr, f.A, nullptr, lddy, F, dWd, F, dw_kind};
+  return n;
 }
 
 static bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -584,9 +781,9 @@ size_t ps_gated_ffn_store_size(int64_t N, int F) {
   return ffn_store(nullptr, N, F).bytes;
 }
 
-size_t ps_gated_ffn_fwd_workspace_size(int64_t N, int F, int with_store) {
-  if (N < 0 || F < 8 || F % 8) return 0;
-  return kWsHeader + (with_store ? 0 : static_cast<size_t>(N) * F * 2);
+size_t ps_gated_ffn_fwd_workspace_size(int64_t N, int d, int F, int with_store) {
+  if (!sizes_ok(N, d, F)) return 0;
+  return kWsHeader + (with_store ? 0 : plane_bytes(N, F)) + down_part_bytes(N, d, F);
 }
 
 int ps_gated_ffn_fwd(int64_t N, int d, int F, int dtype, int act, const void* X, int64_t ldx, const void* Wg,
@@ -602,12 +799,16 @@ int ps_gated_ffn_fwd(int64_t N, int d, int F, int dtype, int act, const void* X,
     return al16(store) ? PS_ERR_WORKSPACE : PS_ERR_INVALID_ARG;
   if (!sizes_fit(N, d, F) || !device_is_sm103()) return PS_ERR_UNSUPPORTED;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  int rc = check_ws(ws, ws_bytes, ps_gated_ffn_fwd_workspace_size(N, F, store != nullptr));
+  int rc = check_ws(ws, ws_bytes, ps_gated_ffn_fwd_workspace_size(N, d, F, store != nullptr));
   if (rc != PS_OK) return rc;
   if (N == 0) return refused(PS_OK, ws, s);
   uint32_t* status = static_cast<uint32_t*>(ws);
   FfnStore f = ffn_store(store, N, F);
-  if (!store) f.A = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(ws) + kWsHeader);
+  uint8_t* scratch = static_cast<uint8_t*>(ws) + kWsHeader;
+  if (!store) {
+    f.A = reinterpret_cast<uint16_t*>(scratch);
+    scratch += plane_bytes(N, F);
+  }
   if (act == PS_ACT_SILU)
     rc = store ? ffn_up<PS_ACT_SILU, true>(N, d, F, X, ldx, Wg, Wu, f, status, s)
                : ffn_up<PS_ACT_SILU, false>(N, d, F, X, ldx, Wg, Wu, f, status, s);
@@ -615,10 +816,17 @@ int ps_gated_ffn_fwd(int64_t N, int d, int F, int dtype, int act, const void* X,
     rc = store ? ffn_up<PS_ACT_GELU, true>(N, d, F, X, ldx, Wg, Wu, f, status, s)
                : ffn_up<PS_ACT_GELU, false>(N, d, F, X, ldx, Wg, Wu, f, status, s);
   if (rc != PS_OK) return refused(rc, ws, s);
-  return ffn_down(N, d, F, f.A, Wd, Y, ldy, status, s);
+  return ffn_down(N, d, F, f.A, Wd, Y, ldy, scratch, status, s);
 }
 
-size_t ps_gated_ffn_bwd_workspace_size(void) { return kWsHeader; }
+size_t ps_gated_ffn_bwd_workspace_size(int64_t N, int d, int F) {
+  if (!sizes_ok(N, d, F)) return 0;
+  Product p[kGroupMost];
+  void* some = reinterpret_cast<void*>(16);   // (not read)
+  const int n = grad_products(p, N, d, F, ffn_store(nullptr, N, F), nullptr, d, nullptr, d, nullptr, nullptr, some, d,
+                              kOutF32, some, some, some, kOutF32);
+  return kWsHeader + part_bytes(p, n);
+}
 
 int ps_gated_ffn_bwd(int64_t N, int d, int F, int dtype, const void* dY, int64_t lddy, const void* X, int64_t ldx,
                      const void* Wg, const void* Wu, const void* Wd, void* store, size_t store_bytes, void* dX,
@@ -642,7 +850,7 @@ int ps_gated_ffn_bwd(int64_t N, int d, int F, int dtype, const void* dY, int64_t
   if (N > 0 && store_bytes < ffn_store(nullptr, N, F).bytes) return PS_ERR_WORKSPACE;
   if (!sizes_fit(N, d, F) || !device_is_sm103()) return PS_ERR_UNSUPPORTED;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  int rc = check_ws(ws, ws_bytes, kWsHeader);
+  int rc = check_ws(ws, ws_bytes, N == 0 ? kWsHeader : ps_gated_ffn_bwd_workspace_size(N, d, F));
   if (rc != PS_OK) return rc;
   uint32_t* status = static_cast<uint32_t*>(ws);
   const int dw_acc = (flags & PS_DW_ACCUMULATE) ? 1 : 0, dx_acc = (flags & PS_DH_ACCUMULATE) ? 1 : 0;
@@ -656,22 +864,11 @@ int ps_gated_ffn_bwd(int64_t N, int d, int F, int dtype, const void* dY, int64_t
   const FfnStore f = ffn_store(store, N, F);
   rc = ffn_da(N, d, F, dY, lddy, Wd, f, status, s);
   if (rc != PS_OK) return refused(rc, ws, s);
-  if (dX) {
-    rc = dx_dtype == PS_DTYPE_F32 ? ffn_dx<StoreF32Epi>(N, d, F, f, Wg, Wu, dX, lddx, dx_acc, status, s)
-                                  : ffn_dx<StoreBf16Epi>(N, d, F, f, Wg, Wu, dX, lddx, 0, status, s);
-    if (rc != PS_OK) return rc;
-  }
-  if (dWg) {
-    rc = dw_dtype == PS_DTYPE_F32 ? ffn_dw_up<StoreF32Epi>(N, d, F, f, X, ldx, dWg, dWu, dw_acc, status, s)
-                                  : ffn_dw_up<StoreBf16Epi>(N, d, F, f, X, ldx, dWg, dWu, 0, status, s);
-    if (rc != PS_OK) return rc;
-  }
-  if (dWd) {
-    rc = dw_dtype == PS_DTYPE_F32 ? ffn_dw_down<StoreF32Epi>(N, d, F, dY, lddy, f, dWd, dw_acc, status, s)
-                                  : ffn_dw_down<StoreBf16Epi>(N, d, F, dY, lddy, f, dWd, 0, status, s);
-    if (rc != PS_OK) return rc;
-  }
-  return PS_OK;
+  auto kind = [](int dtype, int acc) { return dtype == PS_DTYPE_BF16 ? kOutBf16 : acc ? kOutF32Add : kOutF32; };
+  Product p[kGroupMost];
+  const int n = grad_products(p, N, d, F, f, dY, lddy, X, ldx, Wg, Wu, dX, lddx, kind(dx_dtype, dx_acc), dWg, dWu, dWd,
+                              kind(dw_dtype, dw_acc));
+  return n == 0 ? PS_OK : run_group(p, n, static_cast<uint8_t*>(ws) + kWsHeader, status, s);
 }
 
 }  // extern "C"

@@ -535,7 +535,6 @@ static int launch_gemm_pair(const CUtensorMap& ta, const CUtensorMap& tb, int64_
   sc.band_m = band_m > 0 ? band_m : 1;
   sc.num_units = sc.m_blocks * sc.splits;
   sc.num_kb = static_cast<int>((K + kBK - 1) / kBK);
-  sc.first = 0;
   if (sc.num_units == 0) return PS_OK;
   if (sc.num_kb == 0) return PS_ERR_INVALID_ARG;
   auto kern = umma_gemm_pair_kernel<A_MN, B_MN, Epi>;

@@ -41,7 +41,6 @@ struct Sched {
   int num_units;  // m_blocks * splits
   int num_kb;     // ceil(K / 64)
   int clear;      // this launch opens a library call: it zeroes the status words
-  int first;      // k blocks (Pair::kSumK) or m blocks (Pair::kTwoM) of the first of two operand sets
 
   __device__ __forceinline__ void unit(int u, int& m_blk, int& split, int& n0, int& n1) const {
     const int per_band = band_m * splits;
@@ -106,13 +105,9 @@ constexpr size_t gemm_smem_bytes() {   // + alignment slack
   return sizeof(GemmSmemT<HALVES, EpiWarps<Epi>::value, Epi::kStageBytes>) + 1024;
 }
 
-// Products with two operand sets in one launch:
-//   kTwoB  D1 = A B1^T and D2 = A B2^T side by side: a tile is 128 columns of each (columns 0..127 and 128..255 of
-//          the accumulator), and the epilogue gets the same 32-column slice of both (a gate and what it gates)
-//   kSumK  D = A1 B1^T + A2 B2^T: the K loop runs over the first set's k blocks, then over the second's
-//   kTwoM  D1 = A1 B^T and D2 = A2 B^T below each other, each with an output of its own: m blocks from
-//          Sched::first on belong to the second
-enum Pair { kNoPair = 0, kTwoB = 1, kSumK = 2, kTwoM = 3 };
+// kTwoB: D1 = A B1^T and D2 = A B2^T side by side: a tile is 128 columns of each (columns 0..127 and 128..255 of the
+// accumulator), and the epilogue gets the same 32-column slice of both (a gate and what it gates).
+enum Pair { kNoPair = 0, kTwoB = 1 };
 
 // An epilogue with kOwnStore stages and stores its slices itself: chunk_own() gets the slice (with kTwoB those of
 // both products), what load_ahead() loaded beside the accumulator, the warp's staging buffer and its count of
@@ -140,8 +135,8 @@ struct AheadOf<Epi, true> {
 // warps, 2 with 8) plus the thread's column group.
 template <bool A_MN, bool B_MN, class Epi, int HALVES, int PAIR>
 __device__ __forceinline__ void umma_gemm_body(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC,
-                                               const CUtensorMap& tmA2, const CUtensorMap& tmB2,
-                                               const CUtensorMap& tmC2, const CUtensorMap& tmC3, const Sched& sched,
+                                               const CUtensorMap& tmB2, const CUtensorMap& tmC2,
+                                               const CUtensorMap& tmC3, const Sched& sched,
                                                const typename Epi::Params& ep, uint32_t* status, uint64_t timeout_ns) {
   static_assert(PAIR != kTwoB || (!B_MN && OwnStore<Epi>::value), "two B operands: K-major, epilogue of its own");
   constexpr int TN = PAIR == kTwoB ? kBN / 2 : kBN;   // output columns per tile
@@ -201,25 +196,21 @@ __device__ __forceinline__ void umma_gemm_body(const CUtensorMap& tmA, const CUt
             const uint32_t ph = (kc / S) & 1u;
             if (!mbar_wait(&sm.empty[s], ph ^ 1u, timeout_ns, abort)) { ok = false; break; }
             mbar_arrive_expect_tx(&sm.full[s], Cfg::kABytes + kTileBBytes);
-            const bool second = (PAIR == kSumK && kb >= sched.first) || (PAIR == kTwoM && m_blk >= sched.first);
-            const CUtensorMap* const mapA = second ? &tmA2 : &tmA;
-            const CUtensorMap* const mapB = PAIR == kSumK && second ? &tmB2 : &tmB;
-            const int m0 = (PAIR == kTwoM && second ? m_blk - sched.first : m_blk) * Cfg::kRows, nn0 = nb * TN;
-            const int k0 = (PAIR == kSumK && second ? kb - sched.first : kb) * kBK;
+            const int m0 = m_blk * Cfg::kRows, nn0 = nb * TN, k0 = kb * kBK;
             if (A_MN) {
               for (int i = 0; i < Cfg::kRows / 64; ++i)
-                tma_load_2d(sm.a[s] + i * (kBK * 128), mapA, &sm.full[s], m0 + i * 64, k0);
+                tma_load_2d(sm.a[s] + i * (kBK * 128), &tmA, &sm.full[s], m0 + i * 64, k0);
             } else {
-              tma_load_2d(sm.a[s], mapA, &sm.full[s], k0, m0);   // box of kRows rows
+              tma_load_2d(sm.a[s], &tmA, &sm.full[s], k0, m0);   // box of kRows rows
             }
             if (PAIR == kTwoB) {   // boxes of 128 rows
               tma_load_2d(sm.b[s], &tmB, &sm.full[s], k0, nn0);
               tma_load_2d(sm.b[s] + kTileBBytes / 2, &tmB2, &sm.full[s], k0, nn0);
             } else if (B_MN) {
               for (int i = 0; i < kBN / 64; ++i)
-                tma_load_2d(sm.b[s] + i * (kBK * 128), mapB, &sm.full[s], nn0 + i * 64, k0);
+                tma_load_2d(sm.b[s] + i * (kBK * 128), &tmB, &sm.full[s], nn0 + i * 64, k0);
             } else {
-              tma_load_2d(sm.b[s], mapB, &sm.full[s], k0, nn0);
+              tma_load_2d(sm.b[s], &tmB, &sm.full[s], k0, nn0);
             }
           }
         }
@@ -330,9 +321,6 @@ __device__ __forceinline__ void umma_gemm_body(const CUtensorMap& tmA, const CUt
     for (int u = blockIdx.x; ok && u < sched.num_units; u += gridDim.x) {
       int m_blk, split, n0, n1;
       sched.unit(u, m_blk, split, n0, n1);
-      const bool second = PAIR == kTwoM && m_blk >= sched.first;
-      const CUtensorMap* const mapC = second ? &tmC2 : &tmC;
-      if (second) m_blk -= sched.first;
       const int row0 = m_blk * Cfg::kRows + row_in_tile;
 #pragma unroll
       for (int h = 0; h < HALVES; ++h) Epi::begin_unit(ep, st[h], row0 + h * kBM, split * G + grp);
@@ -373,7 +361,7 @@ __device__ __forceinline__ void umma_gemm_body(const CUtensorMap& tmA, const CUt
                 fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) {
-                  Epi::store(ep, mapC, buf, col0, m_blk * Cfg::kRows + h * kBM + quad * 32);
+                  Epi::store(ep, &tmC, buf, col0, m_blk * Cfg::kRows + h * kBM + quad * 32);
                   bulk_commit_group();
                 }
               }
@@ -421,7 +409,7 @@ __device__ __forceinline__ void umma_gemm_body(const CUtensorMap& tmA, const CUt
                   fence_proxy_async_smem();
                   __syncwarp();
                   if (lane == 0) {
-                    Epi::store(ep, mapC, buf, col0, m_blk * Cfg::kRows + h * kBM + quad * 32);
+                    Epi::store(ep, &tmC, buf, col0, m_blk * Cfg::kRows + h * kBM + quad * 32);
                     bulk_commit_group();
                   }
                 }
@@ -458,18 +446,17 @@ __global__ void __launch_bounds__(64 + 32 * EpiWarps<Epi>::value, 1)
     umma_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                      const __grid_constant__ CUtensorMap tmC, const Sched sched, const typename Epi::Params ep,
                      uint32_t* status, uint64_t timeout_ns) {
-  umma_gemm_body<A_MN, B_MN, Epi, HALVES, kNoPair>(tmA, tmB, tmC, tmA, tmB, tmC, tmC, sched, ep, status, timeout_ns);
+  umma_gemm_body<A_MN, B_MN, Epi, HALVES, kNoPair>(tmA, tmB, tmC, tmB, tmC, tmC, sched, ep, status, timeout_ns);
 }
 
-// The same with a second operand set (Pair), or an epilogue that writes up to three outputs.
+// The same with two B operands (Pair), or an epilogue that writes up to three outputs.
 template <bool A_MN, bool B_MN, class Epi, int HALVES, int PAIR>
 __global__ void __launch_bounds__(64 + 32 * EpiWarps<Epi>::value, 1)
     umma_gemm_two_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                         const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmA2,
-                         const __grid_constant__ CUtensorMap tmB2, const __grid_constant__ CUtensorMap tmC2,
-                         const __grid_constant__ CUtensorMap tmC3, const Sched sched, const typename Epi::Params ep,
-                         uint32_t* status, uint64_t timeout_ns) {
-  umma_gemm_body<A_MN, B_MN, Epi, HALVES, PAIR>(tmA, tmB, tmC, tmA2, tmB2, tmC2, tmC3, sched, ep, status, timeout_ns);
+                         const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmB2,
+                         const __grid_constant__ CUtensorMap tmC2, const __grid_constant__ CUtensorMap tmC3,
+                         const Sched sched, const typename Epi::Params ep, uint32_t* status, uint64_t timeout_ns) {
+  umma_gemm_body<A_MN, B_MN, Epi, HALVES, PAIR>(tmA, tmB, tmC, tmB2, tmC2, tmC3, sched, ep, status, timeout_ns);
 }
 
 // =============================================================================================

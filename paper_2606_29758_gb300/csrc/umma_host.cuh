@@ -39,32 +39,6 @@ struct StoreF32Epi {
   static __device__ __forceinline__ void end_unit(const Params&, State&, int, int) {}
 };
 
-// The accumulator rounded once to bf16, through TMA from 64-byte-swizzled staging.
-struct StoreBf16Epi {
-  static constexpr int kEpiWarps = 8;
-  static constexpr bool kTmaStore = true, kReadAhead = true;
-  static constexpr int kStageBytes = 32 * 64;
-  struct Params {
-    int N;
-  };
-  struct State {};
-  static __device__ __forceinline__ int cols(const Params& p) { return p.N; }
-  static __device__ __forceinline__ void begin_unit(const Params&, State&, int, int) {}
-  static __device__ __forceinline__ void chunk_to_smem(const Params&, State&, int, int, const uint32_t (&r)[32],
-                                                       uint8_t* buf, int lane) {
-    uint4* dst = reinterpret_cast<uint4*>(buf + lane * 64);
-    const int x = (lane >> 1) & 3;
-    auto two = [&](int j) { return pack_bf16x2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])); };
-#pragma unroll
-    for (int q = 0; q < 4; ++q) dst[q ^ x] = make_uint4(two(8 * q), two(8 * q + 2), two(8 * q + 4), two(8 * q + 6));
-  }
-  static __device__ __forceinline__ void store(const Params&, const CUtensorMap* map, const uint8_t* buf, int col,
-                                               int row) {
-    tma_store_2d(map, buf, col, row);
-  }
-  static __device__ __forceinline__ void end_unit(const Params&, State&, int, int) {}
-};
-
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -132,7 +106,6 @@ static int launch_gemm_single(const CUtensorMap& ta, const CUtensorMap& tb, cons
   sc.band_m = band_m > 0 ? band_m : 1;
   sc.num_units = sc.m_blocks * sc.splits;
   sc.num_kb = static_cast<int>((K + kBK - 1) / kBK);
-  sc.first = 0;
   if (sc.num_units == 0) return PS_OK;
   if (sc.num_kb == 0) return PS_ERR_INVALID_ARG;
   auto kern = umma_gemm_kernel<A_MN, B_MN, Epi, HALVES>;
@@ -148,27 +121,24 @@ static int launch_gemm_single(const CUtensorMap& ta, const CUtensorMap& tb, cons
              : PS_ERR_CUDA;
 }
 
-// The maps of a product with two operand sets (Pair) or several outputs; the unused ones repeat another.
+// The maps of a product with two B operands or several outputs; the unused ones repeat another.
 struct TwoMaps {
-  CUtensorMap a, b, c, a2, b2, c2, c3;
+  CUtensorMap a, b, c, b2, c2, c3;
 };
 
-// M x N outputs of each product (kTwoM: the two lie below each other; kTwoB: side by side), K of each (kSumK: added up).
+// M x N outputs of each product.
 template <bool A_MN, bool B_MN, class Epi, int HALVES, int PAIR>
 static int launch_gemm_two(const TwoMaps& m, int64_t M, int64_t N, int64_t K, int band_m,
                            const typename Epi::Params& ep, uint32_t* status, cudaStream_t s, bool clear) {
   Sched sc;
   sc.clear = clear ? 1 : 0;
-  const int mb = static_cast<int>((M + kBM * HALVES - 1) / (kBM * HALVES));
-  const int kb = static_cast<int>((K + kBK - 1) / kBK);
   constexpr int tn = PAIR == kTwoB ? kBN / 2 : kBN;
-  sc.m_blocks = PAIR == kTwoM ? 2 * mb : mb;
+  sc.m_blocks = static_cast<int>((M + kBM * HALVES - 1) / (kBM * HALVES));
   sc.n_blocks = static_cast<int>((N + tn - 1) / tn);
   sc.splits = sc.n_blocks;
   sc.band_m = band_m > 0 ? band_m : 1;
   sc.num_units = sc.m_blocks * sc.splits;
-  sc.num_kb = PAIR == kSumK ? 2 * kb : kb;
-  sc.first = PAIR == kSumK ? kb : mb;
+  sc.num_kb = static_cast<int>((K + kBK - 1) / kBK);
   if (sc.num_units == 0) return PS_OK;
   if (sc.num_kb == 0) return PS_ERR_INVALID_ARG;
   auto kern = umma_gemm_two_kernel<A_MN, B_MN, Epi, HALVES, PAIR>;
@@ -178,7 +148,7 @@ static int launch_gemm_two(const TwoMaps& m, int64_t M, int64_t N, int64_t K, in
     return PS_ERR_CUDA;
   const int grid = sc.num_units < num_sms_current() ? sc.num_units : num_sms_current();
   return launch_after(kern, dim3(static_cast<unsigned>(grid)), 64 + 32 * EpiWarps<Epi>::value, smem, s, 1, 1, !clear,
-                      m.a, m.b, m.c, m.a2, m.b2, m.c2, m.c3, sc, ep, status, kDefaultTimeoutNs) == cudaSuccess
+                      m.a, m.b, m.c, m.b2, m.c2, m.c3, sc, ep, status, kDefaultTimeoutNs) == cudaSuccess
              ? PS_OK
              : PS_ERR_CUDA;
 }
