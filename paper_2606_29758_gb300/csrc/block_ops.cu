@@ -71,16 +71,115 @@ struct Raw8<float> {
   }
 };
 
+// Two f32 in one register pair: an instruction for both.
+struct F2 {
+  unsigned long long v;
+};
+static __device__ __forceinline__ F2 pair2(float x, float y) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
+  return r;
+}
+static __device__ __forceinline__ void split2(F2 a, float& x, float& y) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a.v));
+}
+static __device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+static __device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+
+// The 16 values of a lane as eight pairs to be turned together: a[j] holds the first members of pairs 2 j and 2 j + 1, b[j]
+// the second ones. Half: the pairs are (lo[i], hi[i]) of the lane's two runs of eight; even: (v[2 i], v[2 i + 1]).
+template <bool EVEN>
+static __device__ __forceinline__ void to_pairs(const Raw8<Bf16>& lo, const Raw8<Bf16>& hi, F2 (&a)[4], F2 (&b)[4]) {
+  const uint32_t l[4] = {lo.v.x, lo.v.y, lo.v.z, lo.v.w}, h[4] = {hi.v.x, hi.v.y, hi.v.z, hi.v.w};
+  auto low = [](uint32_t w) { return __uint_as_float(w << 16); };
+  auto high = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (EVEN) {
+      const uint32_t w0 = j < 2 ? l[2 * j] : h[2 * j - 4], w1 = j < 2 ? l[2 * j + 1] : h[2 * j - 3];
+      a[j] = pair2(low(w0), low(w1));
+      b[j] = pair2(high(w0), high(w1));
+    } else {
+      a[j] = pair2(low(l[j]), high(l[j]));
+      b[j] = pair2(low(h[j]), high(h[j]));
+    }
+  }
+}
+template <bool EVEN>
+static __device__ __forceinline__ void to_pairs(const Raw8<float>& lo, const Raw8<float>& hi, F2 (&a)[4], F2 (&b)[4]) {
+  const float l[8] = {lo.a.x, lo.a.y, lo.a.z, lo.a.w, lo.b.x, lo.b.y, lo.b.z, lo.b.w};
+  const float h[8] = {hi.a.x, hi.a.y, hi.a.z, hi.a.w, hi.b.x, hi.b.y, hi.b.z, hi.b.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (EVEN) {
+      const float* v = j < 2 ? l + 4 * j : h + 4 * j - 8;
+      a[j] = pair2(v[0], v[2]);
+      b[j] = pair2(v[1], v[3]);
+    } else {
+      a[j] = pair2(l[2 * j], l[2 * j + 1]);
+      b[j] = pair2(h[2 * j], h[2 * j + 1]);
+    }
+  }
+}
+template <bool EVEN, class T>
+static __device__ __forceinline__ void store_pairs(T* lo, T* hi, const F2 (&a)[4], const F2 (&b)[4]) {
+  float u[8], v[8], l[8], h[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    split2(a[j], u[2 * j], u[2 * j + 1]);
+    split2(b[j], v[2 * j], v[2 * j + 1]);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    l[i] = EVEN ? (i & 1 ? v[i / 2] : u[i / 2]) : u[i];
+    h[i] = EVEN ? (i & 1 ? v[4 + i / 2] : u[4 + i / 2]) : v[i];
+  }
+  Raw8<T>::store(lo, l);
+  Raw8<T>::store(hi, h);
+}
+
 // ================================================================== q/k norms and rotation
 //   n = x r g, r = (mean x^2 + eps)^(-1/2) over a head's D values; y = rotation(position) of n's first R dims.
 //   backward: dn = rotation^T dy, dg = sum dn x r, dx = r (g dn - x r^2 mean(g dn x)).
 // HBM-bound (a read and a write of every element; the backward two reads and a write). A head lies on G lanes, 16
 // values each: eight pairs, so a lane rotates by itself and only the mean crosses lanes (log2 G shuffles). A warp takes
-// 32 / G heads of one row at a time, queries first, and keeps its lanes' cosines and sines for the row; the loads of
-// the heads after these (of two steps of bf16, one of f32, across rows) are under way meanwhile: what bounds it is the
-// bytes in flight, about 45 KB an SM, so registers go to loads and resident warps.
+// 32 / G heads of one row at a time, queries first, and keeps its lanes' cosines and sines for the row and their gains for
+// the side; the arithmetic is on pairs of f32 (two to an instruction: with one the issue slots were what ran out).
+// What HBM then wants is bytes in flight. RING: the heads come through a ring in shared memory of the warp's own, filled by
+// bulk copies some steps ahead (one lane issues them), the next row's part of the table likewise. Otherwise a lane loads its
+// part of the next step into registers, which is enough for f32 (twice the bytes) and better for few steps a row or
+// few rows. Measured, us forward / backward, ring against registers: bf16, 106k rows of 28 + 4 heads of 128 282 / 473, 341 /
+// 507 (6.2 and 5.5 TB/s); 20k of 40 + 8 of 256 185 / 247, 195 / 280; 4000 of 28 + 4 18.6 / 35.1, 16.6 / 33.0; 100k of 6 + 2
+// of 96 (3 steps a row) 149 / 247, 143 / 224; f32, 50k of 28 + 4 280 / 419, 257 / 379 (6.4 and 6.5 TB/s).
 constexpr int kQkThreads = 128;
 constexpr int kQkWarps = kQkThreads / 32;
+template <class T, bool BWD, bool RING>
+struct QkCfg {
+  static constexpr int kArrays = BWD ? 2 : 1;                      // x, and dy
+  static constexpr int kStages = 4;
+  static constexpr int kSlot = 512 * sizeof(T);                    // a step's heads: at most 32 lanes of 16 values
+  // a warp's shared memory: its ring, in the end its gain gradients [2][D]
+  static constexpr int kWarp = RING ? kStages * kArrays * kSlot : BWD ? 2 * 512 * 4 : 0;
+  static constexpr int kBlocks = BWD ? 3 : RING ? 5 : 4;           // per SM
+};
+static_assert(QkCfg<uint16_t, true, true>::kWarp >= 2 * 512 * 4, "a warp's gain gradients lie over its ring");
+constexpr int kQkRingSteps = 4, kQkRingUnits = 4;   // the ring: from so many steps a row and rows a warp on
+
+// Bulk copy global -> shared (16-byte aligned, whole 16 bytes), counted on `bar`.
+static __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                   smem_addr(dst)),
+               "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_addr(bar))
+               : "memory");
+}
 
 struct QkArgs {
   int64_t N;
@@ -103,42 +202,6 @@ struct QkArgs {
   uint32_t* status;
 };
 
-// cos and sin of the lane's eight pairs at a row's position (1 and 0 where the lane's dims are not rotated).
-static __device__ __forceinline__ void row_turn(const QkArgs& a, int pos, int c, bool rotated, float (&cs)[8],
-                                                float (&sn)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) cs[i] = 1.f, sn[i] = 0.f;
-  if (a.R == 0) return;
-  const int64_t t = static_cast<int64_t>(pos) - a.pos_base;
-  if (t < 0 || t >= a.T) {   // outside the table: NaN in the row's rotated dims
-    raise_status(a.status, PS_DEV_BAD_LENGTH);
-    if (rotated)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) cs[i] = sn[i] = __int_as_float(0x7fffffff);
-    return;
-  }
-  if (!rotated) return;
-  const float4* at = reinterpret_cast<const float4*>(a.table + t * (a.R / 2) + 8 * c);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float4 v = __ldg(at + i);
-    cs[2 * i] = v.x, sn[2 * i] = v.y, cs[2 * i + 1] = v.z, sn[2 * i + 1] = v.w;
-  }
-}
-
-// The lane's 16 values as eight pairs (half: (v[i], v[8 + i]); even: (v[2 i], v[2 i + 1])), turned by (cs, sign sn).
-template <bool EVEN>
-static __device__ __forceinline__ void turn16(float (&v)[16], const float (&cs)[8], const float (&sn)[8], float sign) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float& x = v[EVEN ? 2 * i : i];
-    float& y = v[EVEN ? 2 * i + 1 : 8 + i];
-    const float s = sign * sn[i], x0 = x, y0 = y;
-    x = x0 * cs[i] - y0 * s;
-    y = x0 * s + y0 * cs[i];
-  }
-}
-
 static __device__ __forceinline__ float group_sum(float v, int G) {
 #pragma unroll
   for (int o = 16; o >= 1; o >>= 1)
@@ -146,191 +209,295 @@ static __device__ __forceinline__ float group_sum(float v, int G) {
   return v;
 }
 
-// A step under way: the raw values of the lane's heads, and its row's position.
-template <class T, bool BWD>
-struct QkStep {
-  Raw8<T> xa, xb;
-  Raw8<T> ya, yb;   // backward
-  int pos;
-};
-
-template <class T, bool EVEN, bool BWD>
-__global__ void __launch_bounds__(kQkThreads, BWD ? 3 : 5) qk_kernel(const QkArgs a) {
-  extern __shared__ float qk_smem[];          // gains [2][D]; backward: then a warp's gain gradients [warps][2][D]
+template <class T, bool EVEN, bool BWD, bool RING>
+__global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk_kernel(const QkArgs a) {
+  using Ring = QkCfg<T, BWD, RING>;
+  constexpr int ST = Ring::kStages;
+  extern __shared__ __align__(128) uint8_t qk_smem[];   // the warps' parts, two table rows each (RING), gains [2][D]
+  __shared__ uint64_t full[kQkWarps][ST], tfull[kQkWarps][2];
+  __shared__ float4 other[BWD ? kQkWarps : 1][4][32];   // gain gradients of the side that is not at work
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint8_t* const ring = qk_smem + warp * Ring::kWarp;
+  const uint32_t tab_bytes = RING ? static_cast<uint32_t>(a.R) * 4 : 0;
+  uint8_t* const tab = qk_smem + kQkWarps * Ring::kWarp + warp * 2 * tab_bytes;
+  float* const all_gains = reinterpret_cast<float*>(qk_smem + kQkWarps * Ring::kWarp + kQkWarps * 2 * tab_bytes);
   if (gridDim.x == 1 && threadIdx.x == 0) clear_status(a.status);   // (several blocks: a memset before the launch)
+  if (lane == 0) {
+    for (int s = 0; s < ST; ++s) mbar_init(&full[warp][s], 1);
+    for (int s = 0; s < 2; ++s) mbar_init(&tfull[warp][s], 1);
+    fence_mbar_init();
+  }
   for (int i = threadIdx.x; i < 2 * a.D; i += kQkThreads) {
     const void* g = i < a.D ? a.gq : a.gk;
-    qk_smem[i] = g ? Elem<T>::get(static_cast<const T*>(g)[i < a.D ? i : i - a.D]) : 1.f;
+    all_gains[i] = g ? Elem<T>::get(static_cast<const T*>(g)[i < a.D ? i : i - a.D]) : 1.f;
   }
+  if (BWD)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) other[warp][i][lane] = make_float4(0.f, 0.f, 0.f, 0.f);
   __syncthreads();
 
   const int c = lane & (a.G - 1), slot = lane / a.G, at_once = 32 / a.G;
   const bool here = 16 * c < a.D, rotated = 16 * c < a.R;
   const int lo = EVEN || !rotated ? 16 * c : 8 * c;
   const int hi = EVEN || !rotated ? 16 * c + 8 : a.R / 2 + 8 * c;
+  const int apart = hi - lo, in_step = slot * a.D + lo;
   const int steps_q = (a.Hq + at_once - 1) / at_once, steps = steps_q + (a.Hk + at_once - 1) / at_once;
-  const float inv_d = 1.f / static_cast<float>(a.D);
-  const float* const gains = qk_smem + (here ? lo : 0);
-  float acc[16], alt[16];   // gain gradients of the side (queries or keys) at work, and of the other
-  if (BWD) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = alt[i] = 0.f;
-  }
-
-  // This warp's units (a row's steps, or a part of them), step after step. `left`: heads of the side from the step's
-  // first on; a group whose slot is not below it has none.
-  const int64_t units = a.N * a.parts, stride = static_cast<int64_t>(gridDim.x) * kQkWarps;
-  struct At {
-    int64_t u, row;
-    int s, s1, left;
-    bool keys;
-    const T *x, *y;   // the lane's first element
-    T* out;
-  };
-  auto side = [&](At& t, bool loads) {
-    t.keys = t.s >= steps_q;
-    const int first = (t.keys ? t.s - steps_q : t.s) * at_once;
-    t.left = (t.keys ? a.Hk : a.Hq) - first;
-    const int64_t in_row = static_cast<int64_t>(first + slot) * a.D + lo;
-    if (loads) {
-      t.x = static_cast<const T*>(t.keys ? a.k : a.q) + t.row * (t.keys ? a.ldk : a.ldq) + in_row;
-      if (BWD) t.y = static_cast<const T*>(t.keys ? a.dky : a.dqy) + t.row * (t.keys ? a.lddky : a.lddqy) + in_row;
-    } else {
-      t.out = static_cast<T*>(t.keys ? a.ko : a.qo) + t.row * (t.keys ? a.ldko : a.ldqo) + in_row;
-    }
-  };
-  auto enter = [&](At& t, bool loads) {
-    if (t.u >= units) return;
-    t.row = a.parts == 1 ? t.u : t.u / a.parts;
-    const int part = static_cast<int>(t.u - t.row * a.parts);
-    t.s = steps * part / a.parts;
-    t.s1 = steps * (part + 1) / a.parts;
-    side(t, loads);
-  };
   const int step_elems = at_once * a.D;
-  auto advance = [&](At& t, bool loads) {
-    if (++t.s >= t.s1) {
-      t.u += stride;
-      enter(t, loads);
-    } else if (t.s == steps_q) {
-      side(t, loads);
+  const float inv_d = 1.f / static_cast<float>(a.D);
+  const bool whole = a.D == 16 * a.G;     // no lane of a group without dims
+
+  // This warp's units (a row's steps, or a part of them): runs of steps of one side (queries or keys) of a row. `left`:
+  // heads of the side from the step's first on; a group whose slot is not below it has none.
+  const int64_t units = a.N * a.parts, stride = static_cast<int64_t>(gridDim.x) * kQkWarps;
+  auto row_of = [&](int64_t u) { return a.parts == 1 ? u : u / a.parts; };
+  struct Run {
+    int64_t u;
+    int s, s1;        // steps of the unit still to come: [s, s1) after this run
+    int steps, left;
+    bool keys;
+    const T *x, *y;   // where the copies come from
+    T* out;           // where this lane's results go
+  };
+  auto open = [&](Run& r, bool loads) {   // the run that begins at step r.s of unit r.u
+    if (r.s >= r.s1) {
+      r.u += stride;
+      if (r.u >= units) return;
+      const int part = static_cast<int>(r.u - row_of(r.u) * a.parts);
+      r.s = steps * part / a.parts;
+      r.s1 = steps * (part + 1) / a.parts;
+    }
+    const int64_t row = row_of(r.u);
+    r.keys = r.s >= steps_q;
+    const int end = r.keys ? r.s1 : min(r.s1, steps_q), first = (r.keys ? r.s - steps_q : r.s) * at_once;
+    r.steps = end - r.s;
+    r.s = end;
+    r.left = (r.keys ? a.Hk : a.Hq) - first;
+    const int64_t in_row = static_cast<int64_t>(first) * a.D;
+    if (loads) {
+      r.x = static_cast<const T*>(r.keys ? a.k : a.q) + row * (r.keys ? a.ldk : a.ldq) + in_row;
+      if (BWD) r.y = static_cast<const T*>(r.keys ? a.dky : a.dqy) + row * (r.keys ? a.lddky : a.lddqy) + in_row;
     } else {
-      t.left -= at_once;
-      if (loads) {
-        t.x += step_elems;
-        if (BWD) t.y += step_elems;
-      } else {
-        t.out += step_elems;
-      }
+      r.out = static_cast<T*>(r.keys ? a.ko : a.qo) + row * (r.keys ? a.ldko : a.ldqo) + in_row + in_step;
     }
   };
-  const bool whole = a.D == 16 * a.G;   // no lane of a group without dims
-  const int apart = hi - lo;
-  auto fetch = [&](At& t, QkStep<T, BWD>& f) {
-    if (t.u >= units) return;
-    if (a.R > 0) f.pos = __ldg(a.pos + t.row);
-    if (!(whole && t.left >= at_once)) {
-      f.xa.zero(), f.xb.zero();
-      if (BWD) f.ya.zero(), f.yb.zero();
-    }
-    if ((whole && t.left >= at_once) || (here && slot < t.left)) {
-      f.xa.load(t.x);
-      f.xb.load(t.x + apart);
-      if (BWD) {
-        f.ya.load(t.y);
-        f.yb.load(t.y + apart);
-      }
-    }
-    advance(t, true);
+  auto begin = [&](Run& r, bool loads) {
+    r.u = static_cast<int64_t>(blockIdx.x) * kQkWarps + warp - stride;
+    r.s = r.s1 = 0;
+    open(r, loads);
   };
-  float cs[8], sn[8];
-  int64_t turned = -1;   // the unit whose cosines and sines these are
-  bool keys = false;     // the side that acc belongs to
-  auto work = [&](At& t, QkStep<T, BWD>& f, At& then) {
-    float x[16], y[16];
-    f.xa.get(x);
-    f.xb.get(x + 8);
-    if (BWD) {
-      f.ya.get(y);
-      f.yb.get(y + 8);
-    }
-    if (t.u != turned) row_turn(a, f.pos, c, rotated, cs, sn);
-    turned = t.u;
-    fetch(then, f);
-    if (BWD && t.keys != keys) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float v = acc[i];
-        acc[i] = alt[i];
-        alt[i] = v;
+  Raw8<T> va, vb, wa, wb;   // (without the ring) the next step's heads
+  // the copies of the next step's heads into stage st, or its loads
+  auto issue = [&](Run& r, int st) {
+    if (r.u >= units) return;
+    if (!RING) {
+      if (!(whole && r.left >= at_once)) {
+        va.zero(), vb.zero();
+        if (BWD) wa.zero(), wb.zero();
       }
-      keys = t.keys;
+      if ((whole && r.left >= at_once) || (here && slot < r.left)) {
+        va.load(r.x + in_step);
+        vb.load(r.x + in_step + apart);
+        if (BWD) {
+          wa.load(r.y + in_step);
+          wb.load(r.y + in_step + apart);
+        }
+      }
+    } else if (lane == 0) {
+      const uint32_t bytes = static_cast<uint32_t>(min(r.left * a.D, step_elems)) * static_cast<uint32_t>(sizeof(T));
+      uint8_t* to = ring + st * Ring::kArrays * Ring::kSlot;
+      mbar_arrive_expect_tx(&full[warp][st], bytes * Ring::kArrays);
+      bulk_load(to, r.x, bytes, &full[warp][st]);
+      if (BWD) bulk_load(to + Ring::kSlot, r.y, bytes, &full[warp][st]);
     }
-    const bool mine = here && slot < t.left;
-    float ss = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) ss = fmaf(x[i], x[i], ss);
-    const float sum = group_sum(ss, a.G);
-    const float r = mine ? rsqrtf(fmaf(sum, inv_d, a.eps)) : 0.f;   // (no head here: nothing to add to the gains)
-    const float* g = gains + (t.keys ? a.D : 0);
-    float gain[16];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 v = reinterpret_cast<const float4*>(i < 2 ? g : g + apart)[i & 1];
-      gain[4 * i] = v.x, gain[4 * i + 1] = v.y, gain[4 * i + 2] = v.z, gain[4 * i + 3] = v.w;
-    }
-    if (!BWD) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) y[i] = x[i] * r * gain[i];
-      turn16<EVEN>(y, cs, sn, 1.f);
+    if (--r.steps == 0) {
+      open(r, true);
     } else {
-      turn16<EVEN>(y, cs, sn, -1.f);
-      // with n = x r: dg += dn n, dx = r (g dn - n mean(g dn n))
-      float dot = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        x[i] *= r;
-        acc[i] = fmaf(y[i], x[i], acc[i]);
-        y[i] *= gain[i];
-        dot = fmaf(y[i], x[i], dot);
-      }
-      const float m = group_sum(dot, a.G) * inv_d;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) y[i] = r * fmaf(-x[i], m, y[i]);
+      r.x += step_elems;
+      if (BWD) r.y += step_elems;
+      r.left -= at_once;
     }
-    if (mine) {
-      Raw8<T>::store(t.out, y);
-      Raw8<T>::store(t.out + apart, y + 8);
-    }
-    advance(t, false);
   };
-  At t, n;
-  t.u = n.u = static_cast<int64_t>(blockIdx.x) * kQkWarps + warp;
-  enter(t, false);
-  enter(n, true);
-  constexpr bool kTwo = sizeof(T) == 2;   // two steps ahead
-  QkStep<T, BWD> f0, f1;
-  fetch(n, f0);
-  if (kTwo) fetch(n, f1);
+  // the table's row of unit u's position into table slot `to`; the position is known a unit earlier
+  auto position = [&](int64_t u) { return a.R > 0 && u < units ? __ldg(a.pos + row_of(u)) : 0; };
+  auto in_table = [&](int pos) {
+    const int64_t t = static_cast<int64_t>(pos) - a.pos_base;
+    return t >= 0 && t < a.T;
+  };
+  auto issue_table = [&](int64_t u, int pos, int to) {
+    if (!RING || a.R == 0 || u >= units || lane != 0) return;
+    const int64_t t = in_table(pos) ? static_cast<int64_t>(pos) - a.pos_base : 0;
+    mbar_arrive_expect_tx(&tfull[warp][to], tab_bytes);
+    bulk_load(tab + to * tab_bytes, a.table + t * (a.R / 2), tab_bytes, &tfull[warp][to]);
+  };
+
+  Run t, n;
+  begin(t, false);
+  begin(n, true);
+  int pos = position(t.u), pos_next = position(t.u + stride);
+#pragma unroll
+  for (int s = 0; s < (RING ? ST : 1); ++s) issue(n, s);
+  issue_table(t.u, pos, 0);
+  const F2 zero2 = pair2(0.f, 0.f), one2 = pair2(1.f, 1.f), minus2 = pair2(-1.f, -1.f);
+  F2 cs[4], sn[4], ga[4], gb[4];          // the row's cosines and sines; the side's gains
+  F2 acca[4], accb[4];                    // backward: the side's gain gradients
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    cs[j] = one2;
+    sn[j] = zero2;
+    if (BWD) acca[j] = accb[j] = zero2;
+  }
+  auto load_gains = [&](bool keys) {
+    const float* g = all_gains + (keys ? a.D : 0) + (here ? lo : 0);
+    Raw8<float> l, h;
+    l.load(g);
+    h.load(g + apart);
+    to_pairs<EVEN>(l, h, ga, gb);
+  };
+  bool keys = false;                      // the side that gains and gradients are of
+  load_gains(false);
+  int64_t turned = -1;                    // the unit that cs and sn are of
+  bool ok = true;
+  uint32_t rows = 0, phase = 0;           // units so far; the ring's phase
+  int st = 0;
   while (t.u < units) {
-    work(t, f0, n);
-    if (kTwo && t.u < units) work(t, f1, n);
+    if (t.u != turned && a.R > 0) {
+      const int to = rows & 1;
+      if (RING && !mbar_wait(&tfull[warp][to], (rows >> 1) & 1u, kDefaultTimeoutNs, nullptr)) { ok = false; break; }
+      const bool good = in_table(pos);
+      if (!good) raise_status(a.status, PS_DEV_BAD_LENGTH);
+      if (rotated) {
+        const int64_t row = good ? static_cast<int64_t>(pos) - a.pos_base : 0;
+        const float4* at = RING ? reinterpret_cast<const float4*>(tab + to * tab_bytes + c * 64)
+                                : reinterpret_cast<const float4*>(a.table + row * (a.R / 2) + 8 * c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float4 v = RING ? at[i] : __ldg(at + i);
+          if (!good) v.x = v.y = v.z = v.w = __int_as_float(0x7fffffff);   // outside the table: NaN
+          cs[i] = pair2(v.x, v.z);
+          sn[i] = pair2(v.y, v.w);
+        }
+      }
+      // (the other slot was read a unit ago)
+      issue_table(t.u + stride, pos_next, to ^ 1);
+      pos = pos_next;
+      pos_next = position(t.u + 2 * stride);
+      ++rows;
+    }
+    turned = t.u;
+    if (t.keys != keys) {
+      keys = t.keys;
+      load_gains(keys);
+      if (BWD)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float4 v = other[warp][j][lane];
+          float4 w;
+          split2(acca[j], w.x, w.y);
+          split2(accb[j], w.z, w.w);
+          other[warp][j][lane] = w;
+          acca[j] = pair2(v.x, v.y);
+          accb[j] = pair2(v.z, v.w);
+        }
+    }
+    for (; t.steps > 0; --t.steps, t.left -= at_once, t.out += step_elems) {
+      if (RING && !mbar_wait(&full[warp][st], phase, kDefaultTimeoutNs, nullptr)) { ok = false; break; }
+      const bool mine = here && slot < t.left;
+      F2 xa[4], xb[4], ya[4], yb[4];
+      if (RING) {
+        const T* from = reinterpret_cast<const T*>(ring + st * Ring::kArrays * Ring::kSlot) + (mine ? in_step : 0);
+        const int far = mine ? apart : 0;
+        va.load(from);
+        vb.load(from + far);
+        if (BWD) {
+          wa.load(from + 512);
+          wb.load(from + 512 + far);
+        }
+        if (!(whole && t.left >= at_once) && !mine) {   // (what lies there belongs to another head)
+          va.zero(), vb.zero();
+          if (BWD) wa.zero(), wb.zero();
+        }
+      }
+      to_pairs<EVEN>(va, vb, xa, xb);
+      if (BWD) to_pairs<EVEN>(wa, wb, ya, yb);
+      if (RING) __syncwarp();   // the stage has been read
+      issue(n, st);
+      if (RING && ++st == ST) {
+        st = 0;
+        phase ^= 1u;
+      }
+      F2 sq = zero2;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sq = fma2(xb[j], xb[j], fma2(xa[j], xa[j], sq));
+      float s0, s1;
+      split2(sq, s0, s1);
+      const float sum = group_sum(s0 + s1, a.G);
+      const float r = mine ? rsqrtf(fmaf(sum, inv_d, a.eps)) : 0.f;   // (no head here: nothing to add to the gains)
+      const F2 r2 = pair2(r, r);
+      if (!BWD) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const F2 na = mul2(mul2(xa[j], r2), ga[j]), nb = mul2(mul2(xb[j], r2), gb[j]);
+          ya[j] = fma2(minus2, mul2(nb, sn[j]), mul2(na, cs[j]));
+          yb[j] = fma2(na, sn[j], mul2(nb, cs[j]));
+        }
+      } else {
+        // with n = x r: dg += dn n, dx = r (g dn - n mean(g dn n))
+        F2 dot = zero2;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const F2 da = fma2(yb[j], sn[j], mul2(ya[j], cs[j])), db = fma2(minus2, mul2(ya[j], sn[j]), mul2(yb[j], cs[j]));
+          xa[j] = mul2(xa[j], r2);
+          xb[j] = mul2(xb[j], r2);
+          acca[j] = fma2(da, xa[j], acca[j]);
+          accb[j] = fma2(db, xb[j], accb[j]);
+          ya[j] = mul2(da, ga[j]);
+          yb[j] = mul2(db, gb[j]);
+          dot = fma2(yb[j], xb[j], fma2(ya[j], xa[j], dot));
+        }
+        split2(dot, s0, s1);
+        const float m = -group_sum(s0 + s1, a.G) * inv_d;
+        const F2 m2 = pair2(m, m);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          ya[j] = mul2(r2, fma2(xa[j], m2, ya[j]));
+          yb[j] = mul2(r2, fma2(xb[j], m2, yb[j]));
+        }
+      }
+      if (mine) store_pairs<EVEN>(t.out, t.out + apart, ya, yb);
+    }
+    if (!ok) break;
+    open(t, false);
+  }
+  if (!ok) {
+    // a copy did not land: let those under way land (bounded), then leave
+    raise_status(a.status, PS_DEV_TIMEOUT);
+    for (int j = 0; j < ST; ++j) mbar_wait(&full[warp][(st + j) % ST], st + j < ST ? phase : phase ^ 1u, kDefaultTimeoutNs, nullptr);
+    for (uint32_t j = rows; j < rows + 2; ++j) mbar_wait(&tfull[warp][j & 1], (j >> 1) & 1u, kDefaultTimeoutNs, nullptr);
   }
   if (!BWD || a.part == nullptr) return;
+  __syncwarp();
 
   // gain gradients: over the warp's heads, then the block's warps; qk_gain_sum_kernel adds the blocks'
-  float* mineq = qk_smem + 2 * a.D + warp * 2 * a.D;
+  float* mineq = reinterpret_cast<float*>(ring);   // (every copy into it has been waited for)
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    for (int o = 16; o >= a.G; o >>= 1) {
-      acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], o);
-      alt[i] += __shfl_xor_sync(0xffffffffu, alt[i], o);
-    }
-    if (here && slot == 0) {
-      const int at = i < 8 ? lo + i : hi + i - 8;
-      mineq[at] = keys ? alt[i] : acc[i];
-      mineq[a.D + at] = keys ? acc[i] : alt[i];
+  for (int j = 0; j < 4; ++j) {
+    float v[4], w[4];   // this side's a and b of two pairs, the other side's
+    split2(acca[j], v[0], v[1]);
+    split2(accb[j], v[2], v[3]);
+    const float4 o = other[warp][j][lane];
+    w[0] = o.x, w[1] = o.y, w[2] = o.z, w[3] = o.w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      for (int d = 16; d >= a.G; d >>= 1) {
+        v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
+        w[i] += __shfl_xor_sync(0xffffffffu, w[i], d);
+      }
+      if (here && slot == 0) {
+        const int p = 2 * j + (i & 1);   // the pair
+        const int at = EVEN ? lo + 2 * p + (i >> 1) : (i < 2 ? lo : hi) + p;
+        mineq[at] = keys ? w[i] : v[i];
+        mineq[a.D + at] = keys ? v[i] : w[i];
+      }
     }
   }
   __syncthreads();
@@ -338,7 +505,7 @@ __global__ void __launch_bounds__(kQkThreads, BWD ? 3 : 5) qk_kernel(const QkArg
   for (int i = threadIdx.x; i < 2 * a.D; i += kQkThreads) {
     float t = 0.f;
 #pragma unroll
-    for (int w = 0; w < kQkWarps; ++w) t += qk_smem[2 * a.D + w * 2 * a.D + i];
+    for (int w = 0; w < kQkWarps; ++w) t += reinterpret_cast<const float*>(qk_smem + w * Ring::kWarp)[i];
     part[i] = t;
   }
 }
@@ -575,33 +742,39 @@ static bool qk_sizes_ok(int64_t N, int Hq, int Hk, int D, int R, int dtype, int 
   return (dtype == PS_DTYPE_BF16 || dtype == PS_DTYPE_F32) && (layout == PS_ROPE_HALF || layout == PS_ROPE_EVEN);
 }
 
+template <class T, bool BWD, bool RING>
+static int launch_qk(const QkArgs& a, int layout, cudaStream_t s) {
+  using Cfg = QkCfg<T, BWD, RING>;
+  // resident blocks take their units in turn
+  const int64_t want = (a.N * a.parts + kQkWarps - 1) / kQkWarps;
+  int64_t most = static_cast<int64_t>(num_sms_current()) * Cfg::kBlocks;
+  if (most > kQkMaxBlocks) most = kQkMaxBlocks;
+  const unsigned grid = static_cast<unsigned>(want < most ? want : most);
+  const size_t smem = kQkWarps * (Cfg::kWarp + (RING ? 2 * 4 * static_cast<size_t>(a.R) : 0)) + 2 * sizeof(float) * a.D;
+  auto kern = layout == PS_ROPE_EVEN ? qk_kernel<T, true, BWD, RING> : qk_kernel<T, false, BWD, RING>;
+  if (smem > 32 * 1024 &&
+      cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
+    return refused(PS_ERR_CUDA, a.status, s);
+  // a block sets its bit early, so one block of several cannot clear the status
+  if (grid > 1 && cudaMemsetAsync(a.status, 0, kWsHeader, s) != cudaSuccess) return PS_ERR_CUDA;
+  kern<<<grid, kQkThreads, smem, s>>>(a);
+  if (cudaGetLastError() != cudaSuccess) return refused(PS_ERR_CUDA, a.status, s);
+  if (!a.part) return PS_OK;
+  return launch_after(qk_gain_sum_kernel, dim3(static_cast<unsigned>(2 * a.D / 8)), 256, 0, s, 1, 1, true, a.D,
+                      static_cast<int>(grid), a.part, a.dgq, a.dgk, a.accumulate) == cudaSuccess
+             ? PS_OK
+             : PS_ERR_CUDA;
+}
 template <bool BWD>
-static int launch_qk(QkArgs a, int dtype, int layout, cudaStream_t s) {
+static int run_qk(QkArgs a, int dtype, int layout, cudaStream_t s) {
   a.G = lanes_for(a.D / 16);
   const int at_once = 32 / a.G;
   const int steps = (a.Hq + at_once - 1) / at_once + (a.Hk + at_once - 1) / at_once;
-  const int sms = num_sms_current();
-  a.parts = parts_for(a.N, static_cast<int64_t>(sms) * 2 * kQkWarps, steps);
-  const int64_t want = (a.N * a.parts + kQkWarps - 1) / kQkWarps;
-  // resident blocks (see the launch bounds) take their units in turn
-  int64_t most = static_cast<int64_t>(sms) * (BWD ? 3 : 5);
-  if (most > kQkMaxBlocks) most = kQkMaxBlocks;
-  const unsigned grid = static_cast<unsigned>(want < most ? want : most);
-  const size_t gains = 2 * sizeof(float) * a.D, smem = BWD ? gains * (1 + kQkWarps) : gains;
-  // a block sets its bit early, so one block of several cannot clear the status
-  if (grid > 1 && cudaMemsetAsync(a.status, 0, kWsHeader, s) != cudaSuccess) return PS_ERR_CUDA;
-  auto go = [&](auto kern) {
-    kern<<<grid, kQkThreads, smem, s>>>(a);
-    if (cudaGetLastError() != cudaSuccess) return refused(PS_ERR_CUDA, a.status, s);
-    if (!a.part) return static_cast<int>(PS_OK);
-    return launch_after(qk_gain_sum_kernel, dim3(static_cast<unsigned>(2 * a.D / 8)), 256, 0, s, 1, 1, true, a.D,
-                        static_cast<int>(grid), a.part, a.dgq, a.dgk, a.accumulate) == cudaSuccess
-               ? static_cast<int>(PS_OK)
-               : static_cast<int>(PS_ERR_CUDA);
-  };
-  if (dtype == PS_DTYPE_BF16)
-    return layout == PS_ROPE_EVEN ? go(qk_kernel<Bf16, true, BWD>) : go(qk_kernel<Bf16, false, BWD>);
-  return layout == PS_ROPE_EVEN ? go(qk_kernel<float, true, BWD>) : go(qk_kernel<float, false, BWD>);
+  const int64_t sms = num_sms_current();
+  a.parts = parts_for(a.N, sms * 2 * kQkWarps, steps);
+  if (dtype == PS_DTYPE_F32) return launch_qk<float, BWD, false>(a, layout, s);
+  const bool ring = steps >= kQkRingSteps && a.N >= sms * QkCfg<Bf16, BWD, true>::kBlocks * kQkWarps * kQkRingUnits;
+  return ring ? launch_qk<Bf16, BWD, true>(a, layout, s) : launch_qk<Bf16, BWD, false>(a, layout, s);
 }
 
 }  // namespace psk
@@ -647,7 +820,7 @@ int ps_qk_norm_rope_fwd(int64_t N, int Hq, int Hk, int D, int R, int dtype, int 
   a.pos = pos, a.pos_base = pos_base, a.T = T, a.table = reinterpret_cast<const float2*>(table);
   a.qo = q_out, a.ko = k_out, a.ldqo = ldqo, a.ldko = ldko;
   a.status = static_cast<uint32_t*>(ws);
-  return launch_qk<false>(a, dtype, layout, s);
+  return run_qk<false>(a, dtype, layout, s);
 }
 
 int ps_qk_norm_rope_bwd(int64_t N, int Hq, int Hk, int D, int R, int dtype, int layout, const void* dq_out,
@@ -686,7 +859,7 @@ int ps_qk_norm_rope_bwd(int64_t N, int Hq, int Hk, int D, int R, int dtype, int 
   a.part = gains ? reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kWsHeader) : nullptr;
   a.dgq = dgq, a.dgk = dgk, a.accumulate = (flags & PS_DW_ACCUMULATE) ? 1 : 0;
   a.status = static_cast<uint32_t*>(ws);
-  return launch_qk<true>(a, dtype, layout, s);
+  return run_qk<true>(a, dtype, layout, s);
 }
 
 int ps_dropout_rows(int64_t N, int d, int dtype, const void* x, int64_t ldx, const void* res, int64_t ldr,

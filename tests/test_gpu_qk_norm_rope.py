@@ -91,6 +91,33 @@ def test_forward_and_backward(N, Hq, Hk, D, R, inter, dtype):
         assert not dgb.any()
 
 
+# Rows enough for several a warp, whose heads then come through shared memory (bf16); a lane adds up at most 8 rows of them.
+LARGE = [(12500, 13, 3, 128, 64), (12300, 11, 2, 80, 80), (12200, 4, 4, 256, 256)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N,Hq,Hk,D,R", LARGE)
+def test_many_rows(N, Hq, Hk, D, R, dtype):
+    q, k, gq, gk, dq, dk, pos = _data(N, Hq, Hk, D, dtype, seed=N)
+    m = _make(N, Hq, Hk, D, R, dtype, Hk == 2)
+    pos[777] = T + 5                               # outside the table
+    qo, ko = m.forward(q, k, gq, gk, pos)
+    rc, bits = _B().ps_workspace_status(m.ws)
+    assert bits == _B().PS_DEV_BAD_LENGTH and torch.isnan(qo.view(N, Hq, D)[777, :, :R]).all()
+    pos[777] = T
+    qo, ko = (t.clone() for t in m.forward(q, k, gq, gk, pos))
+    first = [t.clone() for t in m.backward(dq, dk, q, k, gq, gk, pos)]
+    angles = ob.rope_angles(pos.cpu().numpy() - 1, R, THETA)
+    terms = 8 * max(Hq, Hk)
+    _check_part(q, gq, dq, qo, first[0], first[2], angles, 1e-6, Hk == 2, dtype, terms)
+    _check_part(k, gk, dk, ko, first[1], first[3], angles, 1e-6, Hk == 2, dtype, terms)
+    for a, b in zip(m.backward(dq, dk, q, k, gq, gk, pos), first):
+        assert torch.equal(a, b)                   # reruns
+    m.forward(q, k, gq, gk, pos, in_place=True)
+    assert torch.equal(q, qo) and torch.equal(k, ko)
+    m.check_status()
+
+
 def test_the_table():
     from paper_2606_29758_gb300 import rope_table
     t = rope_table(3000, 96, 1e4).cpu().numpy()
