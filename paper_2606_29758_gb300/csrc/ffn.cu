@@ -24,11 +24,12 @@
 namespace psk {
 
 // ============================================================================= epilogues
-// A slice of 32 rows x 32 2-byte values (this lane's row: pk) through one of the warp's two staging buffers.
+// A slice of 32 rows x 32 2-byte values (this lane's row: pk) through one of the warp's BUFS staging buffers in turn.
+template <int BUFS>
 static __device__ __forceinline__ void store_slice16(const uint32_t (&pk)[16], uint8_t* bufs, uint32_t& stored, int lane,
                                                      const CUtensorMap* map, int col0, int row_base) {
-  uint8_t* buf = bufs + (stored++ & 1u) * (32 * 64);
-  if (lane == 0) bulk_wait_group_read<1>();   // the store before the last one has read this buffer
+  uint8_t* buf = bufs + (stored++ % BUFS) * (32 * 64);
+  if (lane == 0) bulk_wait_group_read<BUFS - 1>();   // the store that last used this buffer has read it
   __syncwarp();
   uint4* dst = reinterpret_cast<uint4*>(buf + lane * 64);
   const int x = (lane >> 1) & 3;
@@ -63,11 +64,11 @@ static __device__ __forceinline__ void act_and_slope(float g, float& q, float& s
 }
 
 // Gate and up slices -> A, and for a backward P, Q and their exponents.
-template <int ACT, bool KEEP>
+template <int ACT, bool KEEP, int BUFS>
 struct FfnUpEpi {
   static constexpr int kEpiWarps = 8;
   static constexpr bool kTmaStore = true, kReadAhead = false, kOwnStore = true;
-  static constexpr int kStageBytes = 2 * 32 * 64;
+  static constexpr int kStageBytes = BUFS * 32 * 64;
   struct Params {
     int M, F;
     uint32_t* scale;   // [ceil(F / 32)][M]
@@ -89,7 +90,7 @@ struct FfnUpEpi {
 #pragma unroll
     for (int j = 0; j < 16; ++j)
       pk[j] = pack_bf16x2(q[2 * j] * __uint_as_float(ru[2 * j]), q[2 * j + 1] * __uint_as_float(ru[2 * j + 1]));
-    store_slice16(pk, bufs, stored, lane, mapA, col0, row_base);
+    store_slice16<BUFS>(pk, bufs, stored, lane, mapA, col0, row_base);
     if (!KEEP) return;
     float mp = 0.f, mq = 0.f;
 #pragma unroll
@@ -102,10 +103,10 @@ struct FfnUpEpi {
     const float ip = __uint_as_float((254u - ep) << 23), iq = __uint_as_float((254u - eq) << 23);
 #pragma unroll
     for (int j = 0; j < 16; ++j) pk[j] = pack_f16x2(s[2 * j] * ip, s[2 * j + 1] * ip);
-    store_slice16(pk, bufs, stored, lane, mapP, col0, row_base);
+    store_slice16<BUFS>(pk, bufs, stored, lane, mapP, col0, row_base);
 #pragma unroll
     for (int j = 0; j < 16; ++j) pk[j] = pack_f16x2(q[2 * j] * iq, q[2 * j + 1] * iq);
-    store_slice16(pk, bufs, stored, lane, mapQ, col0, row_base);
+    store_slice16<BUFS>(pk, bufs, stored, lane, mapQ, col0, row_base);
     if (row < p.M) p.scale[static_cast<int64_t>(col0 >> 5) * p.M + row] = ep | eq << 8;
   }
 };
@@ -114,7 +115,7 @@ struct FfnUpEpi {
 struct FfnDaEpi {
   static constexpr int kEpiWarps = 8;
   static constexpr bool kTmaStore = true, kReadAhead = false, kOwnStore = true;
-  static constexpr int kStageBytes = 2 * 32 * 64;
+  static constexpr int kStageBytes = 2 * 2 * 32 * 64;   // two planes, twice
   struct Params {
     int M, F;
     const uint16_t *P, *Q;   // [M][F]
@@ -170,10 +171,11 @@ struct FfnDaEpi {
     }
   }
   static __device__ __forceinline__ void chunk_own(const Params&, int, int col0, const uint32_t (&r)[32],
-                                                   const uint32_t (&)[1], const Ahead& a, uint8_t* bufs, uint32_t&,
-                                                   int lane, int row_base, const CUtensorMap* mapG,
+                                                   const uint32_t (&)[1], const Ahead& a, uint8_t* bufs,
+                                                   uint32_t& stored, int lane, int row_base, const CUtensorMap* mapG,
                                                    const CUtensorMap* mapU, const CUtensorMap*) {
-    if (lane == 0) bulk_wait_group_read<0>();
+    bufs += (stored++ & 1u) * (2 * 32 * 64);
+    if (lane == 0) bulk_wait_group_read<1>();   // the stores that last used these two have read them
     __syncwarp();
     plane(r, a.p, __uint_as_float((a.scale & 255u) << 23), bufs, lane);
     plane(r, a.q, __uint_as_float((a.scale >> 8 & 255u) << 23), bufs + 32 * 64, lane);
@@ -221,13 +223,19 @@ static __device__ __forceinline__ float2 ld_cluster_v2(uint32_t cl_addr) {
   return v;
 }
 
+// What the first product keeps for a backward (KEEP), [N][C] and the exponents of each row and 32 columns.
+struct FewKept {
+  uint16_t *P, *Q;
+  uint32_t* scale;
+};
+
 // UP: out[n][f] = s(x_n . Wg_f) (x_n . Wu_f), tmW and tmW2 the two weights in boxes of 64 rows; otherwise out[n][c] =
 // x_n . W_c, tmW in boxes of 128 rows. N rows, C output columns (a multiple of 8).
-template <int NT, bool UP, int ACT>
+template <int NT, bool UP, int ACT, bool KEEP>
 __global__ void __launch_bounds__(kFewThreads, 2)
     ffn_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmW2,
                    const __grid_constant__ CUtensorMap tmX, int N, int C, int num_kb, uint16_t* out, int64_t ldo,
-                   uint32_t* status, uint64_t timeout_ns) {
+                   const FewKept kept, uint32_t* status, uint64_t timeout_ns) {
   using Cfg = FewCfg<NT>;
   constexpr int S = Cfg::kStages;
   extern __shared__ uint8_t smem_raw[];
@@ -358,8 +366,26 @@ __global__ void __launch_bounds__(kFewThreads, 2)
       float q0, q1, s0, s1;
       act_and_slope<ACT>(g.x, q0, s0);
       act_and_slope<ACT>(g.y, q1, s1);
-      if (row0 + 2 * j < C)
-        *reinterpret_cast<uint32_t*>(out + static_cast<int64_t>(n) * ldo + row0 + 2 * j) = pack_bf16x2(q0 * u.x, q1 * u.y);
+      const int64_t at = static_cast<int64_t>(n) * ldo + row0 + 2 * j;
+      const bool in = row0 + 2 * j < C;
+      if (in) *reinterpret_cast<uint32_t*>(out + at) = pack_bf16x2(q0 * u.x, q1 * u.y);
+      if (KEEP) {   // a warp has the row's 64 columns, so half of it a slice of 32 (columns past C hold zeros)
+        s0 *= u.x;
+        s1 *= u.y;
+        float mp = fmaxf(fabsf(s0), fabsf(s1)), mq = fmaxf(fabsf(q0), fabsf(q1));
+#pragma unroll
+        for (int o = 8; o >= 1; o >>= 1) {
+          mp = fmaxf(mp, __shfl_xor_sync(0xffffffffu, mp, o));
+          mq = fmaxf(mq, __shfl_xor_sync(0xffffffffu, mq, o));
+        }
+        const uint32_t ep = slice_exponent(mp), eq = slice_exponent(mq);
+        const float ip = __uint_as_float((254u - ep) << 23), iq = __uint_as_float((254u - eq) << 23);
+        if (in) {
+          *reinterpret_cast<uint32_t*>(kept.P + at) = pack_f16x2(s0 * ip, s1 * ip);
+          *reinterpret_cast<uint32_t*>(kept.Q + at) = pack_f16x2(q0 * iq, q1 * iq);
+          if ((j & 15) == 0) kept.scale[static_cast<int64_t>((row0 + 2 * j) >> 5) * N + n] = ep | eq << 8;
+        }
+      }
     } else {
       float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int k = 0; k < nranks; ++k) {
@@ -402,9 +428,9 @@ static FfnStore ffn_store(void* base, int64_t N, int F) {
   return f;
 }
 
-// Row blocks walked together: the X (or dY) rows of a band stay in a quarter of L2 while the weights stream by.
-static int band_of_rows(int64_t K, int halves) {
-  const int b = static_cast<int>(30e6 / (2.0 * K * kBM * halves));
+// Blocks of 256 rows walked together: the X (or dY) rows of a band stay in a quarter of L2 while the weights stream by.
+static int band_of_rows(int64_t K) {
+  const int b = static_cast<int>(30e6 / (2.0 * K * 2 * kBM));
   return b < 1 ? 1 : b;
 }
 constexpr int kBandLongK = 4;   // products with a long K loop: column tiles of 4 row blocks side by side
@@ -420,14 +446,14 @@ static int few_ranks(int64_t units, int num_kb) {
   return r;
 }
 
-template <int NT, bool UP, int ACT>
+template <int NT, bool UP, int ACT, bool KEEP>
 static int launch_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, const void* W, const void* W2, void* out,
-                      int64_t ldo, uint32_t* status, cudaStream_t s) {
+                      int64_t ldo, const FewKept& kept, uint32_t* status, cudaStream_t s) {
   CUtensorMap tw, tw2, tx;
   if (!map_kmajor(&tw, W, C, K, K, UP ? 64 : 128) || !map_kmajor(&tw2, W2, C, K, K, UP ? 64 : 128) ||
       !map_kmajor(&tx, X, N, K, ldx, NT))
     return PS_ERR_INVALID_ARG;
-  auto kern = ffn_few_kernel<NT, UP, ACT>;
+  auto kern = ffn_few_kernel<NT, UP, ACT, KEEP>;
   constexpr size_t smem = sizeof(FewSmem<NT>) + 1024;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
     return PS_ERR_CUDA;
@@ -436,56 +462,65 @@ static int launch_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, c
   int ranks = few_ranks(units, num_kb);
   for (;; ranks /= 2) {
     if (launch_after(kern, dim3(static_cast<unsigned>(units * ranks)), kFewThreads, smem, s, static_cast<unsigned>(ranks),
-                     1, !UP, tw, tw2, tx, static_cast<int>(N), C, num_kb, static_cast<uint16_t*>(out), ldo, status,
-                     kDefaultTimeoutNs) == cudaSuccess)
+                     1, !UP, tw, tw2, tx, static_cast<int>(N), C, num_kb, static_cast<uint16_t*>(out), ldo, kept,
+                     status, kDefaultTimeoutNs) == cudaSuccess)
       return PS_OK;
     cudaGetLastError();
     if (ranks == 1) return PS_ERR_CUDA;   // (else the context's SMs do not hold such a cluster)
   }
 }
-template <bool UP, int ACT>
+template <bool UP, int ACT, bool KEEP>
 static int ffn_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, const void* W, const void* W2, void* out,
-                   int64_t ldo, uint32_t* status, cudaStream_t s) {
-  if (N <= 16) return launch_few<16, UP, ACT>(N, C, K, X, ldx, W, W2, out, ldo, status, s);
-  if (N <= 32) return launch_few<32, UP, ACT>(N, C, K, X, ldx, W, W2, out, ldo, status, s);
-  if (N <= 64) return launch_few<64, UP, ACT>(N, C, K, X, ldx, W, W2, out, ldo, status, s);
-  return launch_few<128, UP, ACT>(N, C, K, X, ldx, W, W2, out, ldo, status, s);
+                   int64_t ldo, const FewKept& kept, uint32_t* status, cudaStream_t s) {
+  if (N <= 16) return launch_few<16, UP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
+  if (N <= 32) return launch_few<32, UP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
+  if (N <= 64) return launch_few<64, UP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
+  return launch_few<128, UP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
 }
 
 template <int ACT, bool KEEP>
 static int ffn_up(int64_t N, int d, int F, const void* X, int64_t ldx, const void* Wg, const void* Wu,
                   const FfnStore& f, uint32_t* status, cudaStream_t s) {
-  using Epi = FfnUpEpi<ACT, KEEP>;
-  if (!KEEP && N <= kFewRows) return ffn_few<true, ACT>(N, F, d, X, ldx, Wg, Wu, f.A, F, status, s);
-  const int halves = tile_halves(N, 2 * static_cast<int64_t>(F), 18);
+  using Epi = FfnUpEpi<ACT, KEEP, 2>;
+  using PairEpi = FfnUpEpi<ACT, KEEP, 4>;
+  if (N <= kFewRows) return ffn_few<true, ACT, KEEP>(N, F, d, X, ldx, Wg, Wu, f.A, F, {f.P, f.Q, f.scale}, status, s);
   TwoMaps m;
-  if (!map_kmajor(&m.a, X, N, d, ldx, kBM * halves) || !map_kmajor(&m.b, Wg, F, d, d, kBN / 2) ||
-      !map_kmajor(&m.b2, Wu, F, d, d, kBN / 2) || !map_out_16(&m.c, f.A, N, F, F))
-    return PS_ERR_INVALID_ARG;
-  m.c2 = m.c3 = m.c;
-  if (KEEP && (!map_out_16(&m.c2, f.P, N, F, F, CU_TENSOR_MAP_DATA_TYPE_FLOAT16) ||
-               !map_out_16(&m.c3, f.Q, N, F, F, CU_TENSOR_MAP_DATA_TYPE_FLOAT16)))
-    return PS_ERR_INVALID_ARG;
-  const typename Epi::Params ep{static_cast<int>(N), F, f.scale};
-  const int band = band_of_rows(d, halves);
-  return halves == 1 ? launch_gemm_two<false, false, Epi, 1, kTwoB>(m, N, F, d, band, ep, status, s, true)
-                     : launch_gemm_two<false, false, Epi, 2, kTwoB>(m, N, F, d, band, ep, status, s, true);
+  auto maps = [&](int rows) {
+    if (!map_kmajor(&m.a, X, N, d, ldx, rows) || !map_kmajor(&m.b, Wg, F, d, d, kBN / 2) ||
+        !map_kmajor(&m.b2, Wu, F, d, d, kBN / 2) || !map_out_16(&m.c, f.A, N, F, F))
+      return false;
+    m.c2 = m.c3 = m.c;
+    return !KEEP || (map_out_16(&m.c2, f.P, N, F, F, CU_TENSOR_MAP_DATA_TYPE_FLOAT16) &&
+                     map_out_16(&m.c3, f.Q, N, F, F, CU_TENSOR_MAP_DATA_TYPE_FLOAT16));
+  };
+  // On CTA pairs the epilogue runs beside the next tile's main loop, and a round over the SMs is half a wide tile. Alone
+  // (a store to write, 5 KB a row and 1000 columns) they are the faster throughout; without one a wide tile per SM is 5%
+  // faster where the rounds do not decide. Measured, us wide / pairs, kept: 6030 rows, d = 1536, F = 8192 207 / 193; 2000, 2000,
+  // 8000 105 / 88; 1200, 3584, 16384 192 / 177; 7835, 3584, 16384 1011 / 1006; not kept: 173 / 173, 94 / 80, 178 / 169, 912 / 965.
+  const int64_t tiles = (N + 255) / 256 * ((F + kBN / 2 - 1) / (kBN / 2)), sms = num_sms_current();
+  const int64_t wide_rounds = (tiles + sms - 1) / sms, pair_rounds = (2 * tiles + sms - 1) / sms;
+  if (!KEEP && wide_rounds * 2000 <= pair_rounds * 1055) {
+    if (!maps(2 * kBM)) return PS_ERR_INVALID_ARG;
+    using Epi = FfnUpEpi<ACT, false, 2>;
+    return launch_gemm_two<false, false, Epi, 2, kTwoB>(m, N, F, d, band_of_rows(d), {static_cast<int>(N), F, f.scale},
+                                                        status, s, true);
+  }
+  if (!maps(kBM)) return PS_ERR_INVALID_ARG;
+  return launch_pair_own<false, FfnUpEpi<ACT, KEEP, 4>, kTwoB>(m, N, F, d, band_of_rows(d),
+                                                               {static_cast<int>(N), F, f.scale}, status, s, true);
 }
 
 // dA = dY Wd and, from the kept P and Q, dG and dU over them.
 static int ffn_da(int64_t N, int d, int F, const void* dY, int64_t lddy, const void* Wd, const FfnStore& f,
                   uint32_t* status, cudaStream_t s) {
-  const int halves = tile_halves(N, F, 18);
   TwoMaps m;
-  if (!map_kmajor(&m.a, dY, N, d, lddy, kBM * halves) || !map_mnmajor(&m.b, Wd, d, F, F) ||
-      !map_out_16(&m.c, f.P, N, F, F) || !map_out_16(&m.c2, f.Q, N, F, F))
+  if (!map_kmajor(&m.a, dY, N, d, lddy, kBM) || !map_mnmajor(&m.b, Wd, d, F, F) || !map_out_16(&m.c, f.P, N, F, F) ||
+      !map_out_16(&m.c2, f.Q, N, F, F))
     return PS_ERR_INVALID_ARG;
   m.b2 = m.b;
   m.c3 = m.c;
-  const FfnDaEpi::Params ep{static_cast<int>(N), F, f.P, f.Q, f.scale};
-  const int band = band_of_rows(d, halves);
-  return halves == 1 ? launch_gemm_two<false, true, FfnDaEpi, 1, kNoPair>(m, N, F, d, band, ep, status, s, true)
-                     : launch_gemm_two<false, true, FfnDaEpi, 2, kNoPair>(m, N, F, d, band, ep, status, s, true);
+  return launch_pair_own<true, FfnDaEpi, kNoPair>(m, N, F, d, band_of_rows(d),
+                                                  {static_cast<int>(N), F, f.P, f.Q, f.scale}, status, s, true);
 }
 
 // ----------------------------------------------------------------------------- products in one launch
@@ -735,7 +770,7 @@ static Product down_product(int64_t N, int d, int F, const void* A, const void* 
 }
 static int ffn_down(int64_t N, int d, int F, const void* A, const void* Wd, void* Y, int64_t ldy, void* part,
                     uint32_t* status, cudaStream_t s) {
-  if (N <= kFewRows) return ffn_few<false, PS_ACT_SILU>(N, d, F, A, F, Wd, Wd, Y, ldy, status, s);
+  if (N <= kFewRows) return ffn_few<false, PS_ACT_SILU, false>(N, d, F, A, F, Wd, Wd, Y, ldy, {}, status, s);
   const Product p = down_product(N, d, F, A, Wd, Y, ldy);
   return run_group(&p, 1, part, status, s);
 }

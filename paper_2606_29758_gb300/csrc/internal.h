@@ -74,6 +74,9 @@ struct SplitK {
 };
 SplitK choose_splitk(int64_t M, int64_t N, int num_kb, bool narrow_too, int sms, const int (&at_once)[3]);
 
+// Clusters of 2 << i CTAs, one CTA per SM, that run at once in the current context; 0 where none fits.
+int clusters_at_once(int i);
+
 // Plain tensor-core GEMM (test hook): C[M][N] (+)= sum_k A(m,k) B(k,n), f32 out. variant: 0 one
 // CTA per 128 x 256 tile, 1 a CTA pair per 256 x 256 tile, 2 one CTA per 256 x 256 tile.
 int gemm_bf16(int M, int N, int K, int a_mn, int b_mn, const void* A, int64_t lda, const void* B, int64_t ldb,

@@ -549,7 +549,7 @@ static int launch_gemm_pair(const CUtensorMap& ta, const CUtensorMap& tb, int64_
 // Clusters of 2 << i CTAs of the split-K kernel that run at once in the current context (one CTA per SM; a cluster
 // stays inside a GPC, so 152 SMs hold 76 pairs but 36 clusters of four and 16 of eight), 0 where none fits. Asked once
 // per context, which has its own set of SMs; a slot holds (context id, answer + 1) in one word.
-static int splitk_clusters_at_once(int i) {
+int clusters_at_once(int i) {
   constexpr int kSlots = 64;
   static std::atomic<uint64_t> known[kSlots][3];
   static const auto ctx_id = reinterpret_cast<CUresult (*)(CUcontext, unsigned long long*)>(driver_fn("cuCtxGetId"));
@@ -619,7 +619,7 @@ SplitK choose_splitk(int64_t M, int64_t N, int num_kb, bool narrow_too, int sms,
 static SplitK choose_splitk_here(int64_t M, int64_t N, int num_kb, bool narrow_too) {
   const int sms = num_sms_current();
   int at_once[3];
-  for (int i = 0; i < 3; ++i) at_once[i] = splitk_clusters_at_once(i);
+  for (int i = 0; i < 3; ++i) at_once[i] = clusters_at_once(i);
   return choose_splitk(M, N, num_kb, narrow_too, sms, at_once);
 }
 

@@ -671,6 +671,197 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
   }
 }
 
+// The CTA pair for epilogues with a store of their own (OwnStore; A K-major): a pair's accumulator takes half of each CTA's
+// TMEM, so there are two and the whole epilogue of one tile runs beside the next tile's main loop, with the operand
+// bytes per FLOP of a wide tile. With kTwoB the even CTA's half of the B tile is B1's 128 rows and the odd one's B2's.
+constexpr int kStagesPairOwn = 5;   // (8 KB of store staging per epilogue warp beside them)
+template <class Epi>
+struct PairOwnSmem {
+  uint8_t a[kStagesPairOwn][kTileABytes];
+  uint8_t b[kStagesPairOwn][kHalfBBytes];
+  uint8_t stage[8][Epi::kStageBytes];
+  uint64_t full[kStagesPairOwn];
+  uint64_t empty[kStagesPairOwn];
+  uint64_t tfull[2];
+  uint64_t tempty[2];
+  uint64_t drain;
+  uint32_t tmem_base;
+  int abort;
+};
+
+template <bool B_MN, class Epi, int PAIR>
+__global__ void __launch_bounds__(320, 1)
+    umma_pair_own_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                         const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmB2,
+                         const __grid_constant__ CUtensorMap tmC2, const __grid_constant__ CUtensorMap tmC3,
+                         const Sched sched, const typename Epi::Params ep, uint32_t* status, uint64_t timeout_ns) {
+  static_assert(OwnStore<Epi>::value && Epi::kEpiWarps == 8, "an epilogue that stores its slices");
+  constexpr int TN = PAIR == kTwoB ? kBN / 2 : kBN;
+  constexpr int CPG = TN / 32 / 2;   // 32-column chunks per column group
+  extern __shared__ uint8_t smem_raw[];
+  PairOwnSmem<Epi>& sm =
+      *reinterpret_cast<PairOwnSmem<Epi>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = static_cast<int>(cluster_ctarank());
+  const bool leader = rank == 0;
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    if (sched.clear && blockIdx.x == 0) clear_status(status);   // (a bit is set only after seconds)
+    for (int s = 0; s < kStagesPairOwn; ++s) {
+      mbar_init(&sm.full[s], 2);
+      mbar_init(&sm.empty[s], 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(&sm.tfull[a], 1);
+      mbar_init(&sm.tempty[a], 16);   // the epilogue warps of both CTAs
+    }
+    mbar_init(&sm.drain, 1);
+    sm.abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0 && lane == 0) {
+    tma_prefetch_desc(&tmA);
+    tma_prefetch_desc(&tmB);
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(&sm.tmem_base, kTmemCols);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  cluster_sync_all();   // barriers of both CTAs initialised before any remote arrival
+  tc_fence_after();
+  wait_for_previous_kernel();
+  const uint32_t tmem_base = sm.tmem_base;
+  volatile int* abort = &sm.abort;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ TMA producer (both CTAs)
+    if (lane == 0) {
+      uint32_t kc = 0;
+      bool ok = true;
+      for (int u = pair; ok && u < sched.num_units; u += npairs) {
+        int m_blk, split, nb, n1;
+        sched.unit(u, m_blk, split, nb, n1);
+        const int m0 = m_blk * 256 + rank * 128;
+        const int n0 = PAIR == kTwoB ? nb * TN : nb * kBN + rank * 128;
+        const CUtensorMap* const mapB = PAIR == kTwoB && rank == 1 ? &tmB2 : &tmB;
+        for (int kb = 0; kb < sched.num_kb; ++kb, ++kc) {
+          const int s = kc % kStagesPairOwn;
+          if (!mbar_wait(&sm.empty[s], ((kc / kStagesPairOwn) & 1u) ^ 1u, timeout_ns, abort)) { ok = false; break; }
+          const uint32_t lfull = mapa_shared(smem_addr(&sm.full[s]), 0);
+          mbar_arrive_expect_tx_cluster(lfull, kTileABytes + kHalfBBytes);
+          const int k0 = kb * kBK;
+          tma_load_2d_pair(sm.a[s], &tmA, lfull, k0, m0);
+          if (B_MN) {
+            for (int i = 0; i < 2; ++i) tma_load_2d_pair(sm.b[s] + i * (kBK * 128), mapB, lfull, n0 + i * 64, k0);
+          } else {
+            tma_load_2d_pair(sm.b[s], mapB, lfull, k0, n0);
+          }
+        }
+      }
+      if (!ok) {
+        *abort = 1;
+        raise_status(status, PS_DEV_TIMEOUT);
+        // (as in the kernel above)
+        if (leader) {
+          const uint32_t first = kc > kStagesPairOwn ? kc - kStagesPairOwn : 0;
+          for (uint32_t j = first; j < kc; ++j)
+            mbar_wait(&sm.full[j % kStagesPairOwn], (j / kStagesPairOwn) & 1u, timeout_ns, nullptr);
+        } else {
+          const uint64_t t0 = globaltimer_ns();
+          while (globaltimer_ns() - t0 < 2000000ull) {
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer (leader only)
+    if (lane == 0 && leader) {
+      constexpr uint32_t idesc = idesc_bf16_f32(256, kBN, false, B_MN);
+      constexpr uint32_t b_lbo = B_MN ? kBK * 128 : 16, b_step = B_MN ? 2048 : 32;
+      uint32_t kc = 0, tile = 0;
+      bool ok = true;
+      for (int u = pair; ok && u < sched.num_units; u += npairs, ++tile) {
+        const uint32_t acc = tile & 1u, aph = (tile >> 1) & 1u;
+        if (!mbar_wait(&sm.tempty[acc], aph ^ 1u, timeout_ns, abort)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + acc * kBN;
+        for (int kb = 0; kb < sched.num_kb; ++kb, ++kc) {
+          const int s = kc % kStagesPairOwn;
+          if (!mbar_wait(&sm.full[s], (kc / kStagesPairOwn) & 1u, timeout_ns, abort)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t a_base = smem_addr(sm.a[s]), b_base = smem_addr(sm.b[s]);
+#pragma unroll
+          for (int k = 0; k < kBK / 16; ++k)
+            umma_bf16_pair(d_tmem, smem_desc_sw128(a_base + k * 32, 16, 1024),
+                           smem_desc_sw128(b_base + k * b_step, b_lbo, 1024), idesc, (kb | k) != 0 ? 1u : 0u);
+          umma_commit_pair_multicast(&sm.empty[s], 0x3);
+        }
+        if (ok) umma_commit_pair_multicast(&sm.tfull[acc], 0x3);
+      }
+      if (!ok) {
+        *abort = 1;
+        raise_status(status, PS_DEV_TIMEOUT);
+        umma_commit_pair_multicast(&sm.drain, 0x1);
+        mbar_wait(&sm.drain, 0, timeout_ns, nullptr);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ epilogue (both CTAs)
+    const int quad = warp & 3, ew = warp - 2, grp = ew >> 2;
+    const uint32_t ltempty0 = mapa_shared(smem_addr(&sm.tempty[0]), 0);
+    const uint32_t ltempty1 = mapa_shared(smem_addr(&sm.tempty[1]), 0);
+    uint32_t tile = 0, stored = 0;
+    bool ok = true;
+    for (int u = pair; u < sched.num_units; u += npairs, ++tile) {
+      int m_blk, split, nb, n1;
+      sched.unit(u, m_blk, split, nb, n1);
+      const int row_base = m_blk * 256 + rank * 128 + quad * 32, row = row_base + lane;
+      const int first = nb * TN + grp * CPG * 32;
+      const uint32_t acc = tile & 1u, aph = (tile >> 1) & 1u;
+      typename Epi::Ahead next;
+      Epi::load_ahead(ep, row, first, next);
+      int got = 0;
+      if (lane == 0) got = mbar_wait(&sm.tfull[acc], aph, timeout_ns, abort) ? 1 : 0;
+      got = __shfl_sync(0xffffffffu, got, 0);
+      if (!got) { ok = false; break; }
+      tc_fence_after();
+      const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16) + acc * kBN + grp * CPG * 32;
+#pragma unroll 1
+      for (int c = 0; c < CPG; ++c) {
+        uint32_t r[32], r2[PAIR == kTwoB ? 32 : 1];
+        const int col0 = first + c * 32;
+        const typename Epi::Ahead ahead = next;
+        if (c + 1 < CPG) Epi::load_ahead(ep, row, col0 + 32, next);
+        tmem_ld32(t_row + c * 32, r);
+        if constexpr (PAIR == kTwoB) tmem_ld32(t_row + TN + c * 32, r2);
+        tmem_ld_wait();
+        if (c == CPG - 1) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(acc ? ltempty1 : ltempty0);
+        }
+        if (col0 < Epi::cols(ep))
+          Epi::chunk_own(ep, row, col0, r, r2, ahead, sm.stage[ew], stored, lane, row_base, &tmC, &tmC2, &tmC3);
+      }
+    }
+    if (!ok) {
+      *abort = 1;
+      raise_status(status, PS_DEV_TIMEOUT);
+    }
+    if (lane == 0) bulk_wait_group_all();
+  }
+
+  tc_fence_before();
+  __syncwarp();
+  cluster_sync_all();   // no remote arrival or multicast commit can target an exited CTA
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem_base, kTmemCols);
+  }
+}
+
 // =============================================================================================
 // Split-K variant: a cluster of S = 2, 4 or 8 CTAs computes one 128 x 256 (HALVES = 1) or 256 x 256
 // output tile, rank r accumulating its share of the k-blocks in its own TMEM. The partial tiles meet

@@ -153,6 +153,34 @@ static int launch_gemm_two(const TwoMaps& m, int64_t M, int64_t N, int64_t K, in
              : PS_ERR_CUDA;
 }
 
+// The same on CTA pairs (A K-major, one 256 x TN tile a pair): the A map's boxes are of 128 rows, B's of 128 as well.
+template <bool B_MN, class Epi, int PAIR>
+static int launch_pair_own(const TwoMaps& m, int64_t M, int64_t N, int64_t K, int band_m, const typename Epi::Params& ep,
+                           uint32_t* status, cudaStream_t s, bool clear) {
+  const int pairs = clusters_at_once(0);
+  if (pairs < 1) return PS_ERR_CUDA;
+  Sched sc;
+  sc.clear = clear ? 1 : 0;
+  constexpr int tn = PAIR == kTwoB ? kBN / 2 : kBN;
+  sc.m_blocks = static_cast<int>((M + 255) / 256);
+  sc.n_blocks = static_cast<int>((N + tn - 1) / tn);
+  sc.splits = sc.n_blocks;
+  sc.band_m = band_m > 0 ? band_m : 1;
+  sc.num_units = sc.m_blocks * sc.splits;
+  sc.num_kb = static_cast<int>((K + kBK - 1) / kBK);
+  auto kern = umma_pair_own_kernel<B_MN, Epi, PAIR>;
+  constexpr size_t smem = sizeof(PairOwnSmem<Epi>) + 1024;
+  static_assert(smem <= 232448, "shared memory of one CTA");
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
+    return PS_ERR_CUDA;
+  const int n = sc.num_units < pairs ? sc.num_units : pairs;
+  if (launch_after(kern, dim3(static_cast<unsigned>(2 * n)), 320, smem, s, 2, 1, !clear, m.a, m.b, m.c, m.b2, m.c2, m.c3, sc,
+                   ep, status, kDefaultTimeoutNs) == cudaSuccess)
+    return PS_OK;
+  cudaGetLastError();
+  return PS_ERR_CUDA;
+}
+
 // Tile height in 128-row halves (see GemmCfg) of a GEMM whose units are M x N tiles. The wide tile moves a third
 // fewer operand bytes per FLOP (about 0.8 vs 0.95 pJ per FLOP at the power cap) and takes 1.8-1.95 times as long as
 // a 128 x 256 one, so it is the faster of the two unless the narrow one needs clearly fewer than twice its rounds
