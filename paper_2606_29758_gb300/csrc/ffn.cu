@@ -436,6 +436,7 @@ static int band_of_rows(int64_t K) {
 constexpr int kBandLongK = 4;   // products with a long K loop: column tiles of 4 row blocks side by side
 
 constexpr int kFewRows = 128;
+constexpr int kPlanSms = 152;   // the SMs that sizes and rules go by
 
 // CTAs that share a unit's K loop: as many as keep all units' CTAs resident at once (two per SM), with at least 8
 // k blocks each.
@@ -478,12 +479,21 @@ static int ffn_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, cons
   return launch_few<128, UP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
 }
 
+// Whether gate and up of these rows go by the kernel for few rows: always up to 64; from there to 128 unless the general
+// kernel's CTA pairs come in one round that is enough to stream the weights, or the weights are small. Measured at 128 rows,
+// us few / pairs (both products, nothing kept): d = 3584, F = 16384 71 / 77; 2048, 3000 23 / 28; 1536, 8192 32 / 30; 3000, 9000
+// 55 / 50; 768, 2048 17.9 / 17.6 (kept: 21 / 19).
+static bool few_up(int64_t N, int d, int F) {
+  const int tiles = (F + 127) / 128;
+  return N <= 64 || (N <= kFewRows && (tiles > kPlanSms / 2 || (tiles < kPlanSms / 3 && d >= 1024)));
+}
+
 template <int ACT, bool KEEP>
 static int ffn_up(int64_t N, int d, int F, const void* X, int64_t ldx, const void* Wg, const void* Wu,
                   const FfnStore& f, uint32_t* status, cudaStream_t s) {
   using Epi = FfnUpEpi<ACT, KEEP, 2>;
   using PairEpi = FfnUpEpi<ACT, KEEP, 4>;
-  if (N <= kFewRows) return ffn_few<true, ACT, KEEP>(N, F, d, X, ldx, Wg, Wu, f.A, F, {f.P, f.Q, f.scale}, status, s);
+  if (few_up(N, d, F)) return ffn_few<true, ACT, KEEP>(N, F, d, X, ldx, Wg, Wu, f.A, F, {f.P, f.Q, f.scale}, status, s);
   TwoMaps m;
   auto maps = [&](int rows) {
     if (!map_kmajor(&m.a, X, N, d, ldx, rows) || !map_kmajor(&m.b, Wg, F, d, d, kBN / 2) ||
@@ -541,7 +551,6 @@ struct GroupPlan {
   int splits[kGroupMost];
   size_t part_off[kGroupMost], bytes;   // the partial tiles' places
 };
-constexpr int kPlanSms = 152;
 constexpr int kLeastKb = 12;   // k blocks a share has at least: below that its partial tile costs more than it saves
 
 static int64_t tiles_of(const Product& p, int halves) {
