@@ -68,6 +68,7 @@ template <int ACT, bool KEEP, int BUFS>
 struct FfnUpEpi {
   static constexpr int kEpiWarps = 8;
   static constexpr bool kTmaStore = true, kReadAhead = false, kOwnStore = true;
+  static constexpr int kLoadSets = 0;
   static constexpr int kStageBytes = BUFS * 32 * 64;
   struct Params {
     int M, F;
@@ -111,50 +112,31 @@ struct FfnUpEpi {
   }
 };
 
-// A dA slice with the kept P and Q of the same place -> dG and dU over them.
+// A dA slice with the kept P and Q of the same place -> dG and dU over them, in place in the staging buffer too. P and Q
+// by TMA: 571 rows at d = 392, F = 1048 13.0 us, 8000 rows at d = 392, F = 2000 33, 6030 at d = 1536, F = 8192 133; into registers
+// a slice ahead 16.5, 46 and 121 (with a long K loop the 64-byte rows of the slices are in the operands' way).
 struct FfnDaEpi {
   static constexpr int kEpiWarps = 8;
   static constexpr bool kTmaStore = true, kReadAhead = false, kOwnStore = true;
-  static constexpr int kStageBytes = 2 * 2 * 32 * 64;   // two planes, twice
+  static constexpr int kLoadSets = 2;
+  static constexpr int kStageBytes = kLoadSets * 2 * 32 * 64;
   struct Params {
     int M, F;
-    const uint16_t *P, *Q;   // [M][F]
     const uint32_t* scale;
   };
   struct State {};
-  // Four lanes load the 64 bytes of a row: unit lane % 4 of the warp's row 8 i + lane / 4 (a lane loading its own row
-  // touched four times the lines an instruction).
   struct Ahead {
-    uint4 p[4], q[4];
-    uint32_t scale;   // of the lane's own row
+    uint32_t scale[4];   // of the lane's row, for the tile's slices
   };
   static __device__ __forceinline__ int cols(const Params& p) { return p.F; }
-  static __device__ __forceinline__ void begin_unit(const Params&, State&, int, int) {}
-  static __device__ __forceinline__ void end_unit(const Params&, State&, int, int) {}
-  static __device__ __forceinline__ void load_ahead(const Params& p, int row, int col0, Ahead& a) {
-    const int lane = threadIdx.x & 31, col = col0 + 8 * (lane & 3);
-    const int first = row - lane + (lane >> 2);
+  static __device__ __forceinline__ void load_ahead(const Params& p, int row, int first, Ahead& a) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool here = first + 8 * i < p.M && col < p.F;   // F is a multiple of 8
-      const int64_t at = static_cast<int64_t>(first + 8 * i) * p.F + col;
-      a.p[i] = here ? *reinterpret_cast<const uint4*>(p.P + at) : make_uint4(0, 0, 0, 0);
-      a.q[i] = here ? *reinterpret_cast<const uint4*>(p.Q + at) : make_uint4(0, 0, 0, 0);
-    }
-    a.scale = row < p.M && col0 < p.F ? p.scale[static_cast<int64_t>(col0 >> 5) * p.M + row] : 0u;
+    for (int c = 0; c < 4; ++c)
+      a.scale[c] = row < p.M && first + 32 * c < p.F ? p.scale[static_cast<int64_t>((first >> 5) + c) * p.M + row] : 0u;
   }
-  // One plane of the slice: through the staging buffer to the lanes that own the rows, which put the products back
-  // where they read.
-  static __device__ __forceinline__ void plane(const uint32_t (&r)[32], const uint4 (&kept)[4], float factor, uint8_t* buf,
-                                               int lane) {
-    uint4* b = reinterpret_cast<uint4*>(buf);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int rr = 8 * i + (lane >> 2);
-      b[rr * 4 + ((lane & 3) ^ ((rr >> 1) & 3))] = kept[i];
-    }
-    __syncwarp();
-    uint4* own = b + lane * 4;
+  // One plane of the slice, the lane's own row.
+  static __device__ __forceinline__ void plane(const uint32_t (&r)[32], float factor, uint8_t* buf, int lane) {
+    uint4* own = reinterpret_cast<uint4*>(buf) + lane * 4;
     const int x = (lane >> 1) & 3;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -172,13 +154,13 @@ struct FfnDaEpi {
   }
   static __device__ __forceinline__ void chunk_own(const Params&, int, int col0, const uint32_t (&r)[32],
                                                    const uint32_t (&)[1], const Ahead& a, uint8_t* bufs,
-                                                   uint32_t& stored, int lane, int row_base, const CUtensorMap* mapG,
+                                                   uint32_t& set, int lane, int row_base, const CUtensorMap* mapG,
                                                    const CUtensorMap* mapU, const CUtensorMap*) {
-    bufs += (stored++ & 1u) * (2 * 32 * 64);
-    if (lane == 0) bulk_wait_group_read<1>();   // the stores that last used these two have read them
-    __syncwarp();
-    plane(r, a.p, __uint_as_float((a.scale & 255u) << 23), bufs, lane);
-    plane(r, a.q, __uint_as_float((a.scale >> 8 & 255u) << 23), bufs + 32 * 64, lane);
+    bufs += set * (2 * 32 * 64);
+    const int c = (col0 >> 5) & 3;   // (a column group's slices begin at a multiple of 128)
+    const uint32_t scale = c == 0 ? a.scale[0] : c == 1 ? a.scale[1] : c == 2 ? a.scale[2] : a.scale[3];
+    plane(r, __uint_as_float((scale & 255u) << 23), bufs, lane);
+    plane(r, __uint_as_float((scale >> 8 & 255u) << 23), bufs + 32 * 64, lane);
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) {
@@ -530,7 +512,7 @@ static int ffn_da(int64_t N, int d, int F, const void* dY, int64_t lddy, const v
   m.b2 = m.b;
   m.c3 = m.c;
   return launch_pair_own<true, FfnDaEpi, kNoPair>(m, N, F, d, band_of_rows(d),
-                                                  {static_cast<int>(N), F, f.P, f.Q, f.scale}, status, s, true);
+                                                  {static_cast<int>(N), F, f.scale}, status, s, true);
 }
 
 // ----------------------------------------------------------------------------- products in one launch

@@ -110,8 +110,8 @@ constexpr size_t gemm_smem_bytes() {   // + alignment slack
 enum Pair { kNoPair = 0, kTwoB = 1 };
 
 // An epilogue with kOwnStore stages and stores its slices itself: chunk_own() gets the slice (with kTwoB those of
-// both products), what load_ahead() loaded beside the accumulator, the warp's staging buffer and its count of
-// stores, the row of its lane 0 and the output maps.
+// both products), what load_ahead() loaded for the tile (CTA pairs), the warp's staging buffers and its count of
+// stores (or the set that holds what was loaded), the row of its lane 0 and the output maps.
 template <class Epi, class = void>
 struct OwnStore {
   static constexpr bool value = false;
@@ -119,15 +119,6 @@ struct OwnStore {
 template <class Epi>
 struct OwnStore<Epi, decltype(static_cast<void>(Epi::kOwnStore))> {
   static constexpr bool value = Epi::kOwnStore;
-};
-
-template <class Epi, bool = OwnStore<Epi>::value>
-struct AheadOf {
-  struct type {};
-};
-template <class Epi>
-struct AheadOf<Epi, true> {
-  using type = typename Epi::Ahead;
 };
 
 // tmC: the output map of epilogues that store through TMA (unused by the others). An epilogue's
@@ -327,8 +318,6 @@ __device__ __forceinline__ void umma_gemm_body(const CUtensorMap& tmA, const CUt
       for (int nb = n0; nb < n1; ++nb, ++tile) {
         const uint32_t acc = tile % NB;
         const uint32_t aph = (tile / NB) & 1u;
-        [[maybe_unused]] typename AheadOf<Epi>::type next;
-        if constexpr (OwnStore<Epi>::value) Epi::load_ahead(ep, row0, nb * TN + grp * CPG * 32, next);
         // one lane waits; the warp follows it, so tcgen05.ld always runs on a converged warp
         int got = 0;
         if (lane == 0) got = mbar_wait(&sm.tfull[acc], aph, timeout_ns, abort) ? 1 : 0;
@@ -371,10 +360,6 @@ __device__ __forceinline__ void umma_gemm_body(const CUtensorMap& tmA, const CUt
             for (int c = grp * CPG; c < grp * CPG + CPG; ++c) {
               uint32_t r[32], r2[PAIR == kTwoB ? 32 : 1];
               const int col0 = nb * TN + c * 32;
-              const typename Epi::Ahead ahead = next;
-              // what the next slice of this tile needs beside its accumulator
-              if (c + 1 < grp * CPG + CPG) Epi::load_ahead(ep, row, col0 + 32, next);
-              else if (h + 1 < HALVES) Epi::load_ahead(ep, row + kBM, nb * TN + grp * CPG * 32, next);
               tmem_ld32(t_row + c * 32, r);
               if constexpr (PAIR == kTwoB) tmem_ld32(t_row + TN + c * 32, r2);
               tmem_ld_wait();
@@ -383,7 +368,7 @@ __device__ __forceinline__ void umma_gemm_body(const CUtensorMap& tmA, const CUt
                 mbar_arrive(&sm.tempty[HALVES == 2 ? h : acc]);
               }
               if (col0 < Epi::cols(ep))
-                Epi::chunk_own(ep, row, col0, r, r2, ahead, sm.stage[ew], stored, lane,
+                Epi::chunk_own(ep, row, col0, r, r2, {}, sm.stage[ew], stored, lane,
                                m_blk * Cfg::kRows + h * kBM + quad * 32, &tmC, &tmC2, &tmC3);
             }
           } else {
@@ -674,14 +659,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
 // The CTA pair for epilogues with a store of their own (OwnStore; A K-major): a pair's accumulator takes half of each CTA's
 // TMEM, so there are two and the whole epilogue of one tile runs beside the next tile's main loop, with the operand
 // bytes per FLOP of a wide tile. With kTwoB the even CTA's half of the B tile is B1's 128 rows and the odd one's B2's.
-constexpr int kStagesPairOwn = 5;   // (8 KB of store staging per epilogue warp beside them)
+// An epilogue with kLoadSets > 0 reads two planes of what it overwrites: their slices come by TMA (the output maps) into
+// the staging buffers, kLoadSets pairs of slices in turn, are worked on in place and stored from there; the next slice's
+// loads are under way beside one. (Loaded into registers a slice ahead they were waited for by the
+// proxy fence of every slice before its store: 2.2 us a slice on an idle chip.)
 template <class Epi>
 struct PairOwnSmem {
-  uint8_t a[kStagesPairOwn][kTileABytes];
-  uint8_t b[kStagesPairOwn][kHalfBBytes];
+  static constexpr int kStages = 5;   // (8 KB of staging per epilogue warp beside them)
+  uint8_t a[kStages][kTileABytes];
+  uint8_t b[kStages][kHalfBBytes];
   uint8_t stage[8][Epi::kStageBytes];
-  uint64_t full[kStagesPairOwn];
-  uint64_t empty[kStagesPairOwn];
+  uint64_t full[kStages];
+  uint64_t empty[kStages];
+  uint64_t loaded[8][Epi::kLoadSets > 0 ? Epi::kLoadSets : 1];
   uint64_t tfull[2];
   uint64_t tempty[2];
   uint64_t drain;
@@ -698,6 +688,7 @@ __global__ void __launch_bounds__(320, 1)
   static_assert(OwnStore<Epi>::value && Epi::kEpiWarps == 8, "an epilogue that stores its slices");
   constexpr int TN = PAIR == kTwoB ? kBN / 2 : kBN;
   constexpr int CPG = TN / 32 / 2;   // 32-column chunks per column group
+  constexpr int kStagesPairOwn = PairOwnSmem<Epi>::kStages, SETS = Epi::kLoadSets;
   extern __shared__ uint8_t smem_raw[];
   PairOwnSmem<Epi>& sm =
       *reinterpret_cast<PairOwnSmem<Epi>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -716,6 +707,8 @@ __global__ void __launch_bounds__(320, 1)
       mbar_init(&sm.tfull[a], 1);
       mbar_init(&sm.tempty[a], 16);   // the epilogue warps of both CTAs
     }
+    for (int w = 0; w < 8; ++w)
+      for (int i = 0; i < SETS; ++i) mbar_init(&sm.loaded[w][i], 1);
     mbar_init(&sm.drain, 1);
     sm.abort = 0;
     fence_mbar_init();
@@ -814,14 +807,44 @@ __global__ void __launch_bounds__(320, 1)
     const uint32_t ltempty1 = mapa_shared(smem_addr(&sm.tempty[1]), 0);
     uint32_t tile = 0, stored = 0;
     bool ok = true;
+    // the slices to load, in the order in which they are worked on
+    [[maybe_unused]] int lu = pair - npairs, lc = CPG, lrow = 0, lcol = 0;
+    [[maybe_unused]] uint32_t loads = 0, used = 0;
+    auto load_next = [&]() {
+      if constexpr (SETS > 0) {
+        ++lc;
+        lcol += 32;
+        while (lc >= CPG || lcol >= Epi::cols(ep)) {   // the next tile's first
+          lu += npairs;
+          if (lu >= sched.num_units) {
+            lu = sched.num_units;
+            return;
+          }
+          int m_blk, split, nb, n1;
+          sched.unit(lu, m_blk, split, nb, n1);
+          lc = 0;
+          lrow = m_blk * 256 + rank * 128 + quad * 32;
+          lcol = nb * TN + grp * CPG * 32;
+        }
+        if (lane == 0) {
+          const uint32_t set = loads % SETS;
+          uint8_t* to = sm.stage[ew] + set * (2 * 32 * 64);
+          mbar_arrive_expect_tx(&sm.loaded[ew][set], 2 * 32 * 64);
+          tma_load_2d(to, &tmC, &sm.loaded[ew][set], lcol, lrow);
+          tma_load_2d(to + 32 * 64, &tmC2, &sm.loaded[ew][set], lcol, lrow);
+        }
+        ++loads;
+      }
+    };
+    for (int i = 0; i + 1 < SETS; ++i) load_next();
     for (int u = pair; u < sched.num_units; u += npairs, ++tile) {
       int m_blk, split, nb, n1;
       sched.unit(u, m_blk, split, nb, n1);
       const int row_base = m_blk * 256 + rank * 128 + quad * 32, row = row_base + lane;
       const int first = nb * TN + grp * CPG * 32;
       const uint32_t acc = tile & 1u, aph = (tile >> 1) & 1u;
-      typename Epi::Ahead next;
-      Epi::load_ahead(ep, row, first, next);
+      typename Epi::Ahead ahead;
+      Epi::load_ahead(ep, row, first, ahead);
       int got = 0;
       if (lane == 0) got = mbar_wait(&sm.tfull[acc], aph, timeout_ns, abort) ? 1 : 0;
       got = __shfl_sync(0xffffffffu, got, 0);
@@ -832,8 +855,6 @@ __global__ void __launch_bounds__(320, 1)
       for (int c = 0; c < CPG; ++c) {
         uint32_t r[32], r2[PAIR == kTwoB ? 32 : 1];
         const int col0 = first + c * 32;
-        const typename Epi::Ahead ahead = next;
-        if (c + 1 < CPG) Epi::load_ahead(ep, row, col0 + 32, next);
         tmem_ld32(t_row + c * 32, r);
         if constexpr (PAIR == kTwoB) tmem_ld32(t_row + TN + c * 32, r2);
         tmem_ld_wait();
@@ -842,10 +863,25 @@ __global__ void __launch_bounds__(320, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(acc ? ltempty1 : ltempty0);
         }
-        if (col0 < Epi::cols(ep))
-          Epi::chunk_own(ep, row, col0, r, r2, ahead, sm.stage[ew], stored, lane, row_base, &tmC, &tmC2, &tmC3);
+        if (col0 >= Epi::cols(ep)) continue;
+        if constexpr (SETS > 0) {
+          const uint32_t set = used % SETS;
+          got = mbar_wait(&sm.loaded[ew][set], (used / SETS) & 1u, timeout_ns, abort) ? 1 : 0;
+          if (!__all_sync(0xffffffffu, got)) { ok = false; break; }
+          ++used;
+          // the slice before this one has been stored from the set that the next load takes
+          if (lane == 0) bulk_wait_group_read<0>();
+          __syncwarp();
+          load_next();
+          stored = set;
+        }
+        Epi::chunk_own(ep, row, col0, r, r2, ahead, sm.stage[ew], stored, lane, row_base, &tmC, &tmC2, &tmC3);
       }
+      if (!ok) break;
     }
+    if (SETS > 0)   // (after an expired wait: the loads under way land before the CTA can exit)
+      for (; used < loads; ++used)
+        mbar_wait(&sm.loaded[ew][used % (SETS > 0 ? SETS : 1)], (used / (SETS > 0 ? SETS : 1)) & 1u, timeout_ns, nullptr);
     if (!ok) {
       *abort = 1;
       raise_status(status, PS_DEV_TIMEOUT);
