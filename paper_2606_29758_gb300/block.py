@@ -15,6 +15,10 @@ import torch
 from . import _binding as B
 
 
+# the current stream's raw handle; the tensors that a call was given are on the device already, so torch is set up
+_raw_stream, _device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+_stream = (lambda: _raw_stream(_device())) if _raw_stream and _device else B._stream
+
 _CODE = {torch.bfloat16: B.PS_DTYPE_BF16, torch.float32: B.PS_DTYPE_F32}
 
 
@@ -111,7 +115,7 @@ class GatedFFN:
         N, *inputs = self._inputs(X, Wg, Wu, Wd)
         Y = _first(self.Y, N) if out is None else out
         rc = self._fwd(N, s.d, s.F, B.PS_DTYPE_BF16, s.act, *inputs, Y.data_ptr(),
-                       s.d if out is None else _pitch("out", out, N, s.d, torch.bfloat16), *self._fwd_tail, B._stream())
+                       s.d if out is None else _pitch("out", out, N, s.d, torch.bfloat16), *self._fwd_tail, _stream())
         B._check(rc, "ps_gated_ffn_fwd")
         self.stored = N if s.train else -1
         return Y
@@ -124,7 +128,7 @@ class GatedFFN:
         if self.stored != N:
             raise RuntimeError("backward needs a forward of the same rows before it (train=True, one backward each)")
         rc = self._bwd(N, s.d, s.F, B.PS_DTYPE_BF16, dY.data_ptr(), _pitch("dY", dY, N, s.d, torch.bfloat16), *inputs,
-                       *self._bwd_tail, B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._bwd_ws, B._stream())
+                       *self._bwd_tail, B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._bwd_ws, _stream())
         B._check(rc, "ps_gated_ffn_bwd")
         self.stored = -1
         return _first(self.dX, N), self.dWg, self.dWu, self.dWd
@@ -197,7 +201,7 @@ class QKNormRope:
         """(q, k) normed and rotated; in_place writes over the inputs (serving: no backward follows)."""
         N = _row_count("q", q, self.s.rows)
         inputs = self._inputs(N, q, k, gq, gk, pos, pos_base)
-        rc = self._fwd(N, *self._head, *inputs, *(inputs[:4] if in_place else self._out), *self._ws, B._stream())
+        rc = self._fwd(N, *self._head, *inputs, *(inputs[:4] if in_place else self._out), *self._ws, _stream())
         B._check(rc, "ps_qk_norm_rope_fwd")
         return (q, k) if in_place else (_first(self.q, N), _first(self.k, N))
 
@@ -210,7 +214,7 @@ class QKNormRope:
         rc = self._bwd(N, *self._head, dq_out.data_ptr(), _pitch("dq_out", dq_out, N, self._wq, s.dtype),
                        dk_out.data_ptr(), _pitch("dk_out", dk_out, N, self._wk, s.dtype),
                        *self._inputs(N, q, k, gq, gk, pos, pos_base), *self._grads,
-                       B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._ws, B._stream())
+                       B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._ws, _stream())
         B._check(rc, "ps_qk_norm_rope_bwd")
         return _first(self.dq, N), _first(self.dk, N), self.dgq, self.dgk
 
@@ -236,7 +240,7 @@ class RowDropout:
                         0 if res is None else _pitch("res", res, N, d, t), _whole("row_traj", row_traj, (N,), torch.int32),
                         _whole("row_pos", row_pos, (N,), torch.int32), traj_base, self.p, seed & (2**64 - 1),
                         step & (2**64 - 1), self.site, y.data_ptr(), d if out is None else _pitch("out", out, N, d, t),
-                        B._stream())
+                        _stream())
         B._check(rc, "ps_dropout_rows")
         return y
 

@@ -50,6 +50,8 @@ static __device__ __forceinline__ uint32_t slice_exponent(float largest) {
   return min(max(e, 15u), 254u) - 14u;
 }
 
+static __device__ __forceinline__ float finite_size(float x) { return fabsf(x) <= 3.4028235e38f ? fabsf(x) : 0.f; }
+
 template <int ACT>
 static __device__ __forceinline__ void act_and_slope(float g, float& q, float& slope) {
   if (ACT == PS_ACT_SILU) {
@@ -99,6 +101,14 @@ struct FfnUpEpi {
       s[j] *= __uint_as_float(ru[j]);
       mp = fmaxf(mp, fabsf(s[j]));
       mq = fmaxf(mq, fabsf(q[j]));
+    }
+    if (fmaxf(mp, mq) > 3.4028235e38f) {   // beside an infinity the finite values keep their own scale
+      mp = mq = 0.f;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        mp = fmaxf(mp, finite_size(s[j]));
+        mq = fmaxf(mq, finite_size(q[j]));
+      }
     }
     const uint32_t ep = slice_exponent(mp), eq = slice_exponent(mq);
     const float ip = __uint_as_float((254u - ep) << 23), iq = __uint_as_float((254u - eq) << 23);
@@ -354,7 +364,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
       if (KEEP) {   // a warp has the row's 64 columns, so half of it a slice of 32 (columns past C hold zeros)
         s0 *= u.x;
         s1 *= u.y;
-        float mp = fmaxf(fabsf(s0), fabsf(s1)), mq = fmaxf(fabsf(q0), fabsf(q1));
+        float mp = fmaxf(finite_size(s0), finite_size(s1)), mq = fmaxf(finite_size(q0), finite_size(q1));
 #pragma unroll
         for (int o = 8; o >= 1; o >>= 1) {
           mp = fmaxf(mp, __shfl_xor_sync(0xffffffffu, mp, o));

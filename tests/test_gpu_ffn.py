@@ -153,6 +153,34 @@ def test_nonfinite_rows_stay_in_their_rows():
     _close(dX[ok], _wanted(X[ok], Wg, Wu, Wd, dY[ok], "silu")[1], "dx")
 
 
+@pytest.mark.parametrize("N", [60, 150])
+def test_an_infinite_up_leaves_its_neighbours(N):
+    """One up overflows (row n, column f): the other columns of its slice keep that row's share of their gradients."""
+    d, F, n, f, j = 64, 104, 33, 5, 7
+    X, Wg, Wu, Wd, dY = _data(N, d, F, seed=11)
+    Wg[:, j] = 0.0
+    Wu[:, j] = 0.0
+    Wu[f, j] = 1e20
+    X[:, j] = 0.0
+    X[n, j] = 1e30
+    m = _make(N, d, F)
+    y = m.forward(X, Wg, Wu, Wd)
+    dX, dWg, dWu, dWd = m.backward(dY, X, Wg, Wu, Wd)
+    rows, cols, dims = (torch.arange(k) != i for k, i in ((N, n), (F, f), (d, j)))
+    Xs, Wus = X.clone(), Wu.clone()
+    Wus[f, j] = 0.0                                # (finite; differs in column f alone)
+    want = _wanted(Xs, Wg, Wus, Wd, dY, "silu")
+    part = lambda w, a, b: (w[0][a][:, b], w[1][a][:, b], w[2])  # noqa: E731
+    every = lambda k: torch.ones(k, dtype=torch.bool)  # noqa: E731
+    assert not torch.isfinite(y[n]).any() and not torch.isfinite(dX[n]).all()
+    _close(y[rows], part(want[0], rows.numpy(), every(d).numpy()), "y")
+    # (dim j of dX has the weight that the finite copy lacks)
+    _close(dX[rows][:, dims], part(want[1], rows.numpy(), dims.numpy()), "dx")
+    _close(dWg[cols][:, dims], part(want[2], cols.numpy(), dims.numpy()), "dwg")
+    _close(dWu[:, dims], part(want[3], every(F).numpy(), dims.numpy()), "dwu")
+    _close(dWd[:, cols], part(want[4], every(d).numpy(), cols.numpy()), "dwd")
+
+
 def test_pitches_reruns_and_accumulation():
     N, d, F = 200, 136, 264
     X, Wg, Wu, Wd, dY = _data(N, d, F, seed=6)
