@@ -182,9 +182,9 @@ struct FfnDaEpi {
 };
 
 // ============================================================================= few rows
-// Up to 128 rows: reading the weights is all that costs (one row at d = 3584, F = 16384: 352 MB), so the weights are the
+// Up to 128 rows (dA: 64): reading the weights is all that costs (one row at d = 3584, F = 16384: 352 MB), so the weights are the
 // 128-row operand of the MMA and the rows its N side (NT = 16 to 128 columns), and every SM streams weights. A CTA takes
-// 64 columns of F (their 64 gate and 64 up rows are one tile) or 128 outputs of Y; where that gives too few CTAs a
+// 64 columns of F (their 64 gate and 64 up rows are one tile), or 128 outputs of Y or dA; where that gives too few CTAs a
 // cluster shares the K loop, and the partial tiles are added in rank order through distributed shared memory. Two CTAs
 // fit on an SM. The second product is launched while the first runs and loads its first weights before it waits for A.
 // One row of d = 3584, F = 16384 57 us (6.1 TB/s of weights), 128 rows 73; d = 1536, F = 8192 21 and 33 (the general
@@ -215,21 +215,25 @@ static __device__ __forceinline__ float2 ld_cluster_v2(uint32_t cl_addr) {
   return v;
 }
 
-// What the first product keeps for a backward (KEEP), [N][C] and the exponents of each row and 32 columns.
+// What the first product keeps for a backward (KEEP), [N][C] and the exponents of each row and 32 columns; what dA turns
+// into dG and dU.
 struct FewKept {
   uint16_t *P, *Q;
   uint32_t* scale;
 };
 
-// UP: out[n][f] = s(x_n . Wg_f) (x_n . Wu_f), tmW and tmW2 the two weights in boxes of 64 rows; otherwise out[n][c] =
-// x_n . W_c, tmW in boxes of 128 rows. N rows, C output columns (a multiple of 8).
-template <int NT, bool UP, int ACT, bool KEEP>
+// kFewUp: out[n][f] = s(x_n . Wg_f) (x_n . Wu_f), tmW and tmW2 the two weights in boxes of 64 rows; kFewDown: out[n][c] =
+// x_n . W_c, tmW in boxes of 128 rows; kFewDa: dA[n][f] = sum_c x_n,c W_c,f (W as it lies, MN-major, in boxes of 64 x 64) and
+// dG, dU over the kept P, Q. N rows, C output columns (a multiple of 8).
+enum FewOp { kFewUp, kFewDown, kFewDa };
+template <int NT, int OP, int ACT, bool KEEP>
 __global__ void __launch_bounds__(kFewThreads, 2)
     ffn_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmW2,
                    const __grid_constant__ CUtensorMap tmX, int N, int C, int num_kb, uint16_t* out, int64_t ldo,
                    const FewKept kept, uint32_t* status, uint64_t timeout_ns) {
   using Cfg = FewCfg<NT>;
   constexpr int S = Cfg::kStages;
+  constexpr bool UP = OP == kFewUp, DA = OP == kFewDa;
   extern __shared__ uint8_t smem_raw[];
   FewSmem<NT>& sm = *reinterpret_cast<FewSmem<NT>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -240,7 +244,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
   const int row0 = unit * (UP ? 64 : 128);
 
   if (threadIdx.x == 0) {
-    if (UP && blockIdx.x == 0) clear_status(status);   // (a bit is set only after seconds)
+    if ((UP || DA) && blockIdx.x == 0) clear_status(status);   // (a bit is set only after seconds)
     for (int s = 0; s < S; ++s) {
       mbar_init(&sm.full[s], 1);
       mbar_init(&sm.empty[s], 1);
@@ -256,7 +260,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (UP) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (UP || DA) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tmem_base = sm.tmem_base;
   volatile int* abort = &sm.abort;
 
@@ -264,6 +268,11 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     if (lane == 0) {
       auto weights = [&](int kb, int s) {
         mbar_arrive_expect_tx(&sm.full[s], Cfg::kStage);
+        if (DA) {
+          tma_load_2d(sm.ring[s], &tmW, &sm.full[s], row0, kb * kBK);
+          tma_load_2d(sm.ring[s] + kFewWBytes / 2, &tmW, &sm.full[s], row0 + 64, kb * kBK);
+          return;
+        }
         tma_load_2d(sm.ring[s], &tmW, &sm.full[s], kb * kBK, row0);
         if (UP) tma_load_2d(sm.ring[s] + kFewWBytes / 2, &tmW2, &sm.full[s], kb * kBK, row0);
       };
@@ -290,7 +299,8 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     }
   } else if (warp == 1) {
     if (lane == 0) {
-      constexpr uint32_t idesc = idesc_bf16_f32(128, NT, false, false);
+      constexpr uint32_t idesc = idesc_bf16_f32(128, NT, DA, false);
+      constexpr uint32_t w_lbo = DA ? kBK * 128 : 16, w_step = DA ? 2048 : 32;
       int kc = 0;
       for (int kb = kb0; kb < kb1; ++kb, ++kc) {
         const int s = kc % S;
@@ -303,7 +313,8 @@ __global__ void __launch_bounds__(kFewThreads, 2)
         const uint32_t w = smem_addr(sm.ring[s]);
 #pragma unroll
         for (int k = 0; k < kBK / 16; ++k)
-          umma_bf16(tmem_base, smem_desc_sw128(w + k * 32, 16, 1024), smem_desc_sw128(w + kFewWBytes + k * 32, 16, 1024),
+          umma_bf16(tmem_base, smem_desc_sw128(w + k * w_step, w_lbo, 1024),
+                    smem_desc_sw128(w + kFewWBytes + k * 32, 16, 1024),
                     idesc, (kc | k) != 0 ? 1u : 0u);
         umma_commit(&sm.empty[s]);
       }
@@ -379,6 +390,15 @@ __global__ void __launch_bounds__(kFewThreads, 2)
         }
       }
     } else {
+      const bool in = row0 + 4 * j < C;
+      const int64_t at = static_cast<int64_t>(n) * ldo + row0 + 4 * j;
+      uint2 p, q;
+      uint32_t scale = 0;
+      if (DA && in) {   // (under way beside the partials)
+        p = *reinterpret_cast<const uint2*>(kept.P + at);
+        q = *reinterpret_cast<const uint2*>(kept.Q + at);
+        scale = kept.scale[static_cast<int64_t>((row0 + 4 * j) >> 5) * N + n];
+      }
       float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int k = 0; k < nranks; ++k) {
         const float4 a = ld_cluster_v4(mapa_shared(base + (n * 128 + 4 * j) * 4, k));
@@ -387,9 +407,19 @@ __global__ void __launch_bounds__(kFewThreads, 2)
         y.z += a.z;
         y.w += a.w;
       }
-      if (row0 + 4 * j < C)
-        *reinterpret_cast<uint2*>(out + static_cast<int64_t>(n) * ldo + row0 + 4 * j) =
-            make_uint2(pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
+      if (!in) continue;
+      if (DA) {
+        auto over = [&](uint16_t* plane, uint2 v, uint32_t exponent) {
+          const float factor = __uint_as_float(exponent << 23);
+          const float2 a = unpack_f16x2(v.x), b = unpack_f16x2(v.y);
+          *reinterpret_cast<uint2*>(plane + at) = make_uint2(pack_bf16x2(y.x * a.x * factor, y.y * a.y * factor),
+                                                             pack_bf16x2(y.z * b.x * factor, y.w * b.y * factor));
+        };
+        over(kept.P, p, scale & 255u);
+        over(kept.Q, q, scale >> 8 & 255u);
+      } else {
+        *reinterpret_cast<uint2*>(out + at) = make_uint2(pack_bf16x2(y.x, y.y), pack_bf16x2(y.z, y.w));
+      }
     }
   }
   __syncwarp();
@@ -425,7 +455,7 @@ static int band_of_rows(int64_t K) {
   const int b = static_cast<int>(30e6 / (2.0 * K * 2 * kBM));
   return b < 1 ? 1 : b;
 }
-constexpr int kBandLongK = 4;   // products with a long K loop: column tiles of 4 row blocks side by side
+constexpr int kBandRows = 1024;   // products with a long K loop: column tiles of these rows side by side
 
 constexpr int kFewRows = 128;
 constexpr int kPlanSms = 152;   // the SMs that sizes and rules go by
@@ -439,14 +469,16 @@ static int few_ranks(int64_t units, int num_kb) {
   return r;
 }
 
-template <int NT, bool UP, int ACT, bool KEEP>
+template <int NT, int OP, int ACT, bool KEEP>
 static int launch_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, const void* W, const void* W2, void* out,
                       int64_t ldo, const FewKept& kept, uint32_t* status, cudaStream_t s) {
+  constexpr bool UP = OP == kFewUp;
   CUtensorMap tw, tw2, tx;
-  if (!map_kmajor(&tw, W, C, K, K, UP ? 64 : 128) || !map_kmajor(&tw2, W2, C, K, K, UP ? 64 : 128) ||
-      !map_kmajor(&tx, X, N, K, ldx, NT))
-    return PS_ERR_INVALID_ARG;
-  auto kern = ffn_few_kernel<NT, UP, ACT, KEEP>;
+  auto map_w = [&](CUtensorMap* m, const void* w) {
+    return OP == kFewDa ? map_mnmajor(m, w, K, C, C) : map_kmajor(m, w, C, K, K, UP ? 64 : 128);
+  };
+  if (!map_w(&tw, W) || !map_w(&tw2, W2) || !map_kmajor(&tx, X, N, K, ldx, NT)) return PS_ERR_INVALID_ARG;
+  auto kern = ffn_few_kernel<NT, OP, ACT, KEEP>;
   constexpr size_t smem = sizeof(FewSmem<NT>) + 1024;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
     return PS_ERR_CUDA;
@@ -455,20 +487,20 @@ static int launch_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, c
   int ranks = few_ranks(units, num_kb);
   for (;; ranks /= 2) {
     if (launch_after(kern, dim3(static_cast<unsigned>(units * ranks)), kFewThreads, smem, s, static_cast<unsigned>(ranks),
-                     1, !UP, tw, tw2, tx, static_cast<int>(N), C, num_kb, static_cast<uint16_t*>(out), ldo, kept,
+                     1, OP == kFewDown, tw, tw2, tx, static_cast<int>(N), C, num_kb, static_cast<uint16_t*>(out), ldo, kept,
                      status, kDefaultTimeoutNs) == cudaSuccess)
       return PS_OK;
     cudaGetLastError();
     if (ranks == 1) return PS_ERR_CUDA;   // (else the context's SMs do not hold such a cluster)
   }
 }
-template <bool UP, int ACT, bool KEEP>
+template <int OP, int ACT, bool KEEP>
 static int ffn_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, const void* W, const void* W2, void* out,
                    int64_t ldo, const FewKept& kept, uint32_t* status, cudaStream_t s) {
-  if (N <= 16) return launch_few<16, UP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
-  if (N <= 32) return launch_few<32, UP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
-  if (N <= 64) return launch_few<64, UP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
-  return launch_few<128, UP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
+  if (N <= 16) return launch_few<16, OP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
+  if (N <= 32) return launch_few<32, OP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
+  if (OP == kFewDa || N <= 64) return launch_few<64, OP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
+  if constexpr (OP != kFewDa) return launch_few<128, OP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
 }
 
 // Whether gate and up of these rows go by the kernel for few rows: always up to 64; from there to 128 unless the general
@@ -485,7 +517,7 @@ static int ffn_up(int64_t N, int d, int F, const void* X, int64_t ldx, const voi
                   const FfnStore& f, uint32_t* status, cudaStream_t s) {
   using Epi = FfnUpEpi<ACT, KEEP, 2>;
   using PairEpi = FfnUpEpi<ACT, KEEP, 4>;
-  if (few_up(N, d, F)) return ffn_few<true, ACT, KEEP>(N, F, d, X, ldx, Wg, Wu, f.A, F, {f.P, f.Q, f.scale}, status, s);
+  if (few_up(N, d, F)) return ffn_few<kFewUp, ACT, KEEP>(N, F, d, X, ldx, Wg, Wu, f.A, F, {f.P, f.Q, f.scale}, status, s);
   TwoMaps m;
   auto maps = [&](int rows) {
     if (!map_kmajor(&m.a, X, N, d, ldx, rows) || !map_kmajor(&m.b, Wg, F, d, d, kBN / 2) ||
@@ -512,9 +544,14 @@ static int ffn_up(int64_t N, int d, int F, const void* X, int64_t ldx, const voi
                                                                {static_cast<int>(N), F, f.scale}, status, s, true);
 }
 
-// dA = dY Wd and, from the kept P and Q, dG and dU over them.
+// dA = dY Wd and, from the kept P and Q, dG and dU over them. Few rows / CTA pairs, us: 1 row, d = 3584, F = 16384 21.6 / 40; 20,
+// 1600, 6400 9.0 / 15.5; 64, 3000, 12000 19 / 23; 64, 1000, 3000 11.7 / 13.1; 100, 3000, 12000 26 / 23; 100, 600, 2000 18 / 11; 128,
+// 1536, 8192 15.2 / 15.7 (each row is a turn of the join's loads).
+constexpr int kFewDaRows = 64;   // (of the 16, 32 and 64 row kernels)
 static int ffn_da(int64_t N, int d, int F, const void* dY, int64_t lddy, const void* Wd, const FfnStore& f,
                   uint32_t* status, cudaStream_t s) {
+  if (N <= kFewDaRows)
+    return ffn_few<kFewDa, PS_ACT_SILU, false>(N, F, d, dY, lddy, Wd, Wd, nullptr, F, {f.P, f.Q, f.scale}, status, s);
   TwoMaps m;
   if (!map_kmajor(&m.a, dY, N, d, lddy, kBM) || !map_mnmajor(&m.b, Wd, d, F, F) || !map_out_16(&m.c, f.P, N, F, F) ||
       !map_out_16(&m.c2, f.Q, N, F, F))
@@ -538,29 +575,35 @@ struct Product {
   int64_t ldo;
   int kind;                     // kOutBf16, kOutF32 or kOutF32Add
 };
+struct GroupTile {
+  int halves, ctas;   // of the kernel
+  int rows() const { return kBM * halves * ctas; }
+  int workers() const { return kPlanSms / ctas; }
+};
 struct GroupPlan {
-  int halves;
+  GroupTile tile;
   int splits[kGroupMost];
   size_t part_off[kGroupMost], bytes;   // the partial tiles' places
 };
 constexpr int kLeastKb = 12;   // k blocks a share has at least: below that its partial tile costs more than it saves
 
-static int64_t tiles_of(const Product& p, int halves) {
-  return (p.M + kBM * halves - 1) / (kBM * halves) * ((p.N + kBN - 1) / kBN);
-}
+static int64_t tiles_of(const Product& p, int rows) { return (p.M + rows - 1) / rows * ((p.N + kBN - 1) / kBN); }
 static int kb_of(const Product& p) {
   const int64_t kb = (p.K + kBK - 1) / kBK;
   return static_cast<int>(p.two_sets ? 2 * kb : kb);
 }
-// What a unit costs, in hundredths of a wide tile's k block (0.55 us): its k blocks, or the writing of its outputs where
-// that takes longer (43 GB/s an SM), and its start and end.
-static double unit_cost(const Product& p, int halves, int splits) {
-  const double kb = static_cast<double>(kb_of(p)) / splits * (halves == 2 ? 100 : 66);
-  const double out = kBM * halves * kBN * (splits > 1 || p.kind != kOutBf16 ? 4 : 2) * 4.2e-3;
-  return (kb > out ? kb : out) + (halves == 2 ? 200 : 120);
+// What a unit costs, in hundredths of a 256 x 256 k block's MMAs on one SM (0.55 us): its k blocks at the rate that the tile
+// sustains (or at the rate at which an SM gets its share of the weights from HBM, 43 GB/s, where few row blocks read them),
+// its outputs at 43 GB/s, and its start and end. Loads and outputs share an SM's port to L2, so they add up.
+static double unit_cost(const Product& p, GroupTile t, int splits) {
+  double kb_cost = t.halves == 2 ? 100 : t.ctas == 2 ? 62 : 68;
+  const double hbm = kTileBBytes / t.ctas * (t.ctas == 2 && p.M <= kBM ? 5.5e-3 : 4.2e-3) / static_cast<double>((p.M + t.rows() - 1) / t.rows());
+  if (!p.a_mn && hbm > kb_cost) kb_cost = hbm;
+  const double out = kBM * t.halves * kBN * (splits > 1 || p.kind != kOutBf16 ? 4 : 2) * 4.2e-3;
+  return kb_cost * kb_of(p) / splits + out + (t.halves == 2 ? 200 : 120);
 }
 
-// CTAs with the same load, side by side.
+// CTAs (or pairs) with the same load, side by side.
 struct LoadSeg {
   int cta0, cta1;
   double load;
@@ -633,31 +676,32 @@ static double deal(Loads& L, int64_t n, double cost, GroupSeg* out, int* out_n) 
   return most;
 }
 
-// The tile's height and each product's shares: a product whose tiles are fewer than the SMs is split into shares of what an
-// SM has to do anyway, or of kLeastKb; the height is the one whose dealt units end first.
+// The tile and each product's shares: a product whose tiles are fewer than the workers (CTAs or pairs) is split into shares of
+// what one has to do anyway, or of kLeastKb; the tile is the one whose dealt units end first.
 static GroupPlan plan_group(const Product* p, int count) {
   GroupPlan best;
   double best_cost = 0;
-  for (int halves = 2; halves >= 1; --halves) {
+  for (const GroupTile tile : {GroupTile{2, 2}, GroupTile{1, 2}, GroupTile{1, 1}}) {
     GroupPlan g;
-    g.halves = halves;
+    g.tile = tile;
+    const int workers = tile.workers();
     double work = 0, cost = 0;
-    for (int t = 0; t < count; ++t) work += static_cast<double>(tiles_of(p[t], halves)) * unit_cost(p[t], halves, 1);
-    const double fair = work / kPlanSms / (halves == 2 ? 100 : 66);   // k blocks
+    for (int t = 0; t < count; ++t) work += static_cast<double>(tiles_of(p[t], tile.rows())) * unit_cost(p[t], tile, 1);
+    const double fair = work / workers * (count > 1 ? 0.66 : 1.0);
     Loads L;
     L.n = 1;
-    L.seg[0] = {0, kPlanSms, 0.0};
+    L.seg[0] = {0, workers, 0.0};
     for (int t = 0; t < count; ++t) {
       const int kb = kb_of(p[t]);
-      const int64_t tiles = tiles_of(p[t], halves);
-      const double share = fair > kLeastKb ? fair : kLeastKb;
+      const int64_t tiles = tiles_of(p[t], tile.rows());
+      const double fair_kb = fair / unit_cost(p[t], tile, 1) * kb, share = fair_kb > kLeastKb ? fair_kb : kLeastKb;
       int s = static_cast<int>(kb / share + 0.5);
-      if (tiles >= kPlanSms) s = 1;
-      if (s * tiles > 2 * kPlanSms) s = static_cast<int>(2 * kPlanSms / tiles);
+      if (tiles >= workers) s = 1;
+      if (s * tiles > 2 * workers) s = static_cast<int>(2 * workers / tiles);
       g.splits[t] = s < 2 ? 1 : s;
       GroupSeg seg[kGroupSegs];
       int n;
-      const double end = deal(L, tiles * g.splits[t], unit_cost(p[t], halves, g.splits[t]), seg, &n);
+      const double end = deal(L, tiles * g.splits[t], unit_cost(p[t], tile, g.splits[t]), seg, &n);
       if (end > cost) cost = end;
     }
     for (int t = 0; t < count; ++t)
@@ -671,40 +715,41 @@ static GroupPlan plan_group(const Product* p, int count) {
   for (int t = 0; t < count; ++t) {
     best.part_off[t] = best.bytes;
     if (best.splits[t] == 1) continue;
-    const size_t rows = (p[t].M + kBM * best.halves - 1) / (kBM * best.halves) * (kBM * best.halves);
+    const size_t unit = best.tile.rows(), rows = (p[t].M + unit - 1) / unit * unit;
     best.bytes += (best.splits[t] * rows * p[t].N * 4 + 255) / 256 * 256;
   }
   return best;
 }
 
 // Bytes that hold the partial tiles of these products or of any some of them, and of as many with fewer rows: a share has
-// at least kLeastKb k blocks, and there are at most two tiles of at most 256 x 256 per SM.
+// at least kLeastKb k blocks, and there are at most two tiles of at most 256 x 256 per SM (or 512 x 256 per pair).
 static size_t part_bytes(const Product* p, int count) {
   size_t sum = 0;
   for (int t = 0; t < count; ++t) {
     const size_t shares = static_cast<size_t>(kb_of(p[t])) / kLeastKb + 1;
     if (shares < 2) continue;
-    const size_t all = shares * ((p[t].M + 2 * kBM - 1) / (2 * kBM) * (2 * kBM)) * p[t].N * 4;
+    const size_t all = shares * ((p[t].M + 4 * kBM - 1) / (4 * kBM) * (4 * kBM)) * p[t].N * 4;
     const size_t most = static_cast<size_t>(2 * kPlanSms) * 2 * kBM * kBN * 4;
     sum += ((all < most ? all : most) + 255) / 256 * 256;
   }
   return sum;
 }
 
-template <int HALVES>
-static int launch_group(const GroupArgs& g, uint32_t* status, cudaStream_t s, bool clear) {
-  auto kern = umma_group_kernel<HALVES>;
-  constexpr size_t smem = sizeof(GroupSmem<HALVES>) + 1024;
+template <int HALVES, int CTAS>
+static int launch_group(const GroupArgs& g, uint32_t* status, cudaStream_t s) {
+  auto kern = umma_group_kernel<HALVES, CTAS>;
+  constexpr size_t smem = sizeof(GroupSmem<HALVES, CTAS>) + 1024;
   static_assert(smem <= 232448, "shared memory of one CTA");
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
     return PS_ERR_CUDA;
-  int ctas = 1;
+  int workers = 1;
   for (int t = 0; t < g.count; ++t)
-    for (int i = 0; i < g.segs[t]; ++i) ctas = g.seg[t][i].cta1 > ctas ? g.seg[t][i].cta1 : ctas;
-  return launch_after(kern, dim3(static_cast<unsigned>(ctas)), kGroupThreads, smem, s, 1, 1,
-                      !clear, g, status, kDefaultTimeoutNs) == cudaSuccess
-             ? PS_OK
-             : PS_ERR_CUDA;
+    for (int i = 0; i < g.segs[t]; ++i) workers = g.seg[t][i].cta1 > workers ? g.seg[t][i].cta1 : workers;
+  if (launch_after(kern, dim3(static_cast<unsigned>(workers * CTAS)), kGroupThreads, smem, s, CTAS, 1, true, g, status,
+                   kDefaultTimeoutNs) == cudaSuccess)
+    return PS_OK;
+  cudaGetLastError();
+  return PS_ERR_CUDA;
 }
 
 // The products p[0 .. count), cut as plan_group says, partial tiles at `part`.
@@ -714,11 +759,11 @@ static int run_group(const Product* p, int count, void* part, uint32_t* status, 
   SumArgs sums;
   sums.count = 0;
   g.count = count;
-  g.clear = 0;
   Loads loads;
   loads.n = 1;
-  loads.seg[0] = {0, num_sms_current(), 0.0};
-  const int rows = kBM * plan.halves;
+  const int rows = plan.tile.rows(), workers = plan.tile.ctas == 2 ? clusters_at_once(0) : num_sms_current();
+  if (workers < 1) return PS_ERR_CUDA;
+  loads.seg[0] = {0, workers, 0.0};
   for (int t = 0; t < count; ++t) {
     const Product& q = p[t];
     GroupProduct& o = g.p[t];
@@ -727,19 +772,19 @@ static int run_group(const Product* p, int count, void* part, uint32_t* status, 
     o.splits = plan.splits[t];
     o.num_kb = kb_of(q);
     o.first_kb = q.two_sets ? o.num_kb / 2 : o.num_kb;
-    o.band_m = kBandLongK * (3 - plan.halves);
+    o.band_m = kBandRows / rows;
     o.a_mn = q.a_mn;
     o.b_mn = q.b_mn;
     o.cols = static_cast<int>(q.N);
     o.part_rows = o.m_blocks * rows;
     o.out = o.splits > 1 ? kOutPartial : q.kind;
-    deal(loads, static_cast<int64_t>(o.m_blocks) * o.n_blocks * o.splits, unit_cost(q, plan.halves, o.splits), g.seg[t],
+    deal(loads, static_cast<int64_t>(o.m_blocks) * o.n_blocks * o.splits, unit_cost(q, plan.tile, o.splits), g.seg[t],
          &g.segs[t]);
     auto map_a = [&](CUtensorMap* m, const void* at) {
-      return q.a_mn ? map_mnmajor(m, at, q.K, q.M, q.lda) : map_kmajor(m, at, q.M, q.K, q.lda, rows);
+      return q.a_mn ? map_mnmajor(m, at, q.K, q.M, q.lda) : map_kmajor(m, at, q.M, q.K, q.lda, kBM * plan.tile.halves);
     };
     auto map_b = [&](CUtensorMap* m, const void* at) {
-      return q.b_mn ? map_mnmajor(m, at, q.K, q.N, q.ldb) : map_kmajor(m, at, q.N, q.K, q.ldb, kBN);
+      return q.b_mn ? map_mnmajor(m, at, q.K, q.N, q.ldb) : map_kmajor(m, at, q.N, q.K, q.ldb, kBN / plan.tile.ctas);
     };
     if (!map_a(&g.a[t], q.A) || !map_b(&g.b[t], q.B)) return PS_ERR_INVALID_ARG;
     if (q.two_sets && (!map_a(&g.a2, q.A2) || !map_b(&g.b2, q.B2))) return PS_ERR_INVALID_ARG;
@@ -753,11 +798,13 @@ static int run_group(const Product* p, int count, void* part, uint32_t* status, 
       sums.end[sums.count] = q.M * (q.N / 4) + (sums.count > 0 ? sums.end[sums.count - 1] : 0);
       ++sums.count;
     } else {
-      ok = q.kind == kOutBf16 ? map_out_16(&g.c[t], q.out, q.M, q.N, q.ldo) : map_out_f32(&g.c[t], q.out, q.M, q.N, q.ldo);
+      ok = q.kind == kOutBf16 ? map_out_bf16(&g.c[t], q.out, q.M, q.N, q.ldo) : map_out_f32(&g.c[t], q.out, q.M, q.N, q.ldo);
     }
     if (!ok) return PS_ERR_INVALID_ARG;
   }
-  const int rc = plan.halves == 2 ? launch_group<2>(g, status, s, false) : launch_group<1>(g, status, s, false);
+  const int rc = plan.tile.ctas == 1     ? launch_group<1, 1>(g, status, s)
+                 : plan.tile.halves == 1 ? launch_group<1, 2>(g, status, s)
+                                         : launch_group<2, 2>(g, status, s);
   if (rc != PS_OK || sums.count == 0) return rc;
   const int64_t blocks = (sums.end[sums.count - 1] + 255) / 256, most = 8 * static_cast<int64_t>(num_sms_current());
   return launch_after(sum_partials_kernel, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), 256, 0, s, 1, 1, true,
@@ -771,7 +818,7 @@ static Product down_product(int64_t N, int d, int F, const void* A, const void* 
 }
 static int ffn_down(int64_t N, int d, int F, const void* A, const void* Wd, void* Y, int64_t ldy, void* part,
                     uint32_t* status, cudaStream_t s) {
-  if (N <= kFewRows) return ffn_few<false, PS_ACT_SILU, false>(N, d, F, A, F, Wd, Wd, Y, ldy, {}, status, s);
+  if (N <= kFewRows) return ffn_few<kFewDown, PS_ACT_SILU, false>(N, d, F, A, F, Wd, Wd, Y, ldy, {}, status, s);
   const Product p = down_product(N, d, F, A, Wd, Y, ldy);
   return run_group(&p, 1, part, status, s);
 }

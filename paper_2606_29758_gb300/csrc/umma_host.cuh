@@ -90,6 +90,10 @@ static bool map_out_16(CUtensorMap* m, const void* base, int64_t rows, int64_t c
                        CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16) {
   return make_map(m, base, cols, rows, pitch_elems * 2, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B, type);
 }
+// Output map of bf16 [rows][cols]: boxes of 32 rows x 64 columns from 128-byte-swizzled staging.
+static bool map_out_bf16(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t pitch_elems) {
+  return make_map(m, base, cols, rows, pitch_elems * 2, 64, 32);
+}
 static bool map_mnmajor(CUtensorMap* m, const void* base, int64_t K, int64_t MN, int64_t pitch_elems) {
   return make_map(m, base, MN, K, pitch_elems * 2, 64, kBK);
 }
