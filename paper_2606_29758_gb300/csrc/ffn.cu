@@ -244,7 +244,6 @@ __global__ void __launch_bounds__(kFewThreads, 2)
   const int row0 = unit * (UP ? 64 : 128);
 
   if (threadIdx.x == 0) {
-    if ((UP || DA) && blockIdx.x == 0) clear_status(status);   // (a bit is set only after seconds)
     for (int s = 0; s < S; ++s) {
       mbar_init(&sm.full[s], 1);
       mbar_init(&sm.empty[s], 1);
@@ -260,7 +259,11 @@ __global__ void __launch_bounds__(kFewThreads, 2)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (UP || DA) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (UP || DA) {   // a call's first kernel: what the calls before it wrote is there from here on
+    wait_for_previous_kernel();
+    let_next_kernel_in();
+    if (blockIdx.x == 0 && threadIdx.x == 0) clear_status(status);   // (a bit is set only after seconds)
+  }
   const uint32_t tmem_base = sm.tmem_base;
   volatile int* abort = &sm.abort;
 
@@ -277,10 +280,13 @@ __global__ void __launch_bounds__(kFewThreads, 2)
         if (UP) tma_load_2d(sm.ring[s] + kFewWBytes / 2, &tmW2, &sm.full[s], kb * kBK, row0);
       };
       auto rows = [&](int kb, int s) { tma_load_2d(sm.ring[s] + kFewWBytes, &tmX, &sm.full[s], kb * kBK, 0); };
-      // the weights come from before the call: a ring of them before the kernel that writes the rows is done
+      // the weights come from before the call: in its second kernel a ring of them before the rows' kernel is done
       const int ahead = min(S, kb1 - kb0);
       for (int i = 0; i < ahead; ++i) weights(kb0 + i, i);
-      wait_for_previous_kernel();
+      if (!UP && !DA) {
+        wait_for_previous_kernel();
+        let_next_kernel_in();
+      }
       for (int i = 0; i < ahead; ++i) rows(kb0 + i, i);
       bool ok = true;
       int kc = ahead;
@@ -487,7 +493,7 @@ static int launch_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, c
   int ranks = few_ranks(units, num_kb);
   for (;; ranks /= 2) {
     if (launch_after(kern, dim3(static_cast<unsigned>(units * ranks)), kFewThreads, smem, s, static_cast<unsigned>(ranks),
-                     1, OP == kFewDown, tw, tw2, tx, static_cast<int>(N), C, num_kb, static_cast<uint16_t*>(out), ldo, kept,
+                     1, true, tw, tw2, tx, static_cast<int>(N), C, num_kb, static_cast<uint16_t*>(out), ldo, kept,
                      status, kDefaultTimeoutNs) == cudaSuccess)
       return PS_OK;
     cudaGetLastError();

@@ -698,7 +698,6 @@ __global__ void __launch_bounds__(320, 1)
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
 
   if (threadIdx.x == 0) {
-    if (sched.clear && blockIdx.x == 0) clear_status(status);   // (a bit is set only after seconds)
     for (int s = 0; s < kStagesPairOwn; ++s) {
       mbar_init(&sm.full[s], 2);
       mbar_init(&sm.empty[s], 1);
@@ -725,6 +724,8 @@ __global__ void __launch_bounds__(320, 1)
   cluster_sync_all();   // barriers of both CTAs initialised before any remote arrival
   tc_fence_after();
   wait_for_previous_kernel();
+  let_next_kernel_in();
+  if (sched.clear && blockIdx.x == 0 && threadIdx.x == 0) clear_status(status);   // (a bit is set only after seconds)
   const uint32_t tmem_base = sm.tmem_base;
   volatile int* abort = &sm.abort;
 

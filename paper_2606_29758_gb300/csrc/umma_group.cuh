@@ -158,6 +158,7 @@ __global__ void __launch_bounds__(kGroupThreads, 1)
   else __syncthreads();
   tc_fence_after();
   wait_for_previous_kernel();
+  let_next_kernel_in();
   const uint32_t tmem_base = sm.tmem_base;
   volatile int* abort = &sm.abort;
 
@@ -427,6 +428,7 @@ struct SumArgs {
 };
 static __global__ void __launch_bounds__(256) sum_partials_kernel(const __grid_constant__ SumArgs a) {
   wait_for_previous_kernel();
+  let_next_kernel_in();
   const int64_t all = a.end[a.count - 1];
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * 256) {
     int t = 0;

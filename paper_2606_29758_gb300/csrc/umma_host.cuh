@@ -178,7 +178,7 @@ static int launch_pair_own(const TwoMaps& m, int64_t M, int64_t N, int64_t K, in
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
     return PS_ERR_CUDA;
   const int n = sc.num_units < pairs ? sc.num_units : pairs;
-  if (launch_after(kern, dim3(static_cast<unsigned>(2 * n)), 320, smem, s, 2, 1, !clear, m.a, m.b, m.c, m.b2, m.c2, m.c3, sc,
+  if (launch_after(kern, dim3(static_cast<unsigned>(2 * n)), 320, smem, s, 2, 1, true, m.a, m.b, m.c, m.b2, m.c2, m.c3, sc,
                    ep, status, kDefaultTimeoutNs) == cudaSuccess)
     return PS_OK;
   cudaGetLastError();
