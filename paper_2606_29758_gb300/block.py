@@ -235,7 +235,7 @@ class RowDropout:
         N, d = x.shape
         t = x.dtype
         pitch = _pitch("x", x, N, d, t)
-        y = torch.empty(N, d, dtype=t, device=x.device) if out is None else out
+        y = torch.empty_like(x) if out is None else out
         rc = self._call(N, d, _CODE[t] if t in _CODE else B.dtype_code(x), x.data_ptr(), pitch, None if res is None else res.data_ptr(),
                         0 if res is None else _pitch("res", res, N, d, t), _whole("row_traj", row_traj, (N,), torch.int32),
                         _whole("row_pos", row_pos, (N,), torch.int32), traj_base, self.p, seed & (2**64 - 1),

@@ -171,6 +171,9 @@ struct QkCfg {
   static constexpr int kBlocks = BWD ? 3 : RING ? 5 : 4;           // per SM
 };
 static_assert(QkCfg<uint16_t, true, true>::kWarp >= 2 * 512 * 4, "a warp's gain gradients lie over its ring");
+// The status is cleared by a memset before the launch, as any block may set it early; of fewer rows the first block looks at
+// every position and sets the word alone (a token's call takes one launch, 6.3 -> 4 us on the device).
+constexpr int kQkCheckRows = 2048;
 constexpr int kQkRingSteps = 4, kQkRingUnits = 4;   // the ring: from so many steps a row and rows a warp on
 
 // Bulk copy global -> shared (16-byte aligned, whole 16 bytes), counted on `bar`.
@@ -221,7 +224,6 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
   const uint32_t tab_bytes = RING ? static_cast<uint32_t>(a.R) * 4 : 0;
   uint8_t* const tab = qk_smem + kQkWarps * Ring::kWarp + warp * 2 * tab_bytes;
   float* const all_gains = reinterpret_cast<float*>(qk_smem + kQkWarps * Ring::kWarp + kQkWarps * 2 * tab_bytes);
-  if (gridDim.x == 1 && threadIdx.x == 0) clear_status(a.status);   // (several blocks: a memset before the launch)
   if (lane == 0) {
     for (int s = 0; s < ST; ++s) mbar_init(&full[warp][s], 1);
     for (int s = 0; s < 2; ++s) mbar_init(&tfull[warp][s], 1);
@@ -359,12 +361,22 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
   bool ok = true;
   uint32_t rows = 0, phase = 0;           // units so far; the ring's phase
   int st = 0;
+  if (a.N <= kQkCheckRows && blockIdx.x == 0) {   // (the loads above are under way)
+    int bad = 0;
+    if (a.R > 0)
+      for (int i = threadIdx.x; i < a.N; i += kQkThreads) bad |= !in_table(__ldg(a.pos + i));
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) {
+      clear_status(a.status);
+      if (bad) raise_status(a.status, PS_DEV_BAD_LENGTH);
+    }
+  }
   while (t.u < units) {
     if (t.u != turned && a.R > 0) {
       const int to = rows & 1;
       if (RING && !mbar_wait(&tfull[warp][to], (rows >> 1) & 1u, kDefaultTimeoutNs, nullptr)) { ok = false; break; }
       const bool good = in_table(pos);
-      if (!good) raise_status(a.status, PS_DEV_BAD_LENGTH);
+      if (!good && a.N > kQkCheckRows) raise_status(a.status, PS_DEV_BAD_LENGTH);
       if (rotated) {
         const int64_t row = good ? static_cast<int64_t>(pos) - a.pos_base : 0;
         const float4* at = RING ? reinterpret_cast<const float4*>(tab + to * tab_bytes + c * 64)
@@ -756,8 +768,7 @@ static int launch_qk(const QkArgs& a, int layout, cudaStream_t s) {
   if (smem > 32 * 1024 &&
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
     return refused(PS_ERR_CUDA, a.status, s);
-  // a block sets its bit early, so one block of several cannot clear the status
-  if (grid > 1 && cudaMemsetAsync(a.status, 0, kWsHeader, s) != cudaSuccess) return PS_ERR_CUDA;
+  if (a.N > kQkCheckRows && cudaMemsetAsync(a.status, 0, kWsHeader, s) != cudaSuccess) return PS_ERR_CUDA;
   kern<<<grid, kQkThreads, smem, s>>>(a);
   if (cudaGetLastError() != cudaSuccess) return refused(PS_ERR_CUDA, a.status, s);
   if (!a.part) return PS_OK;
