@@ -90,6 +90,20 @@ def test_forward_and_backward(N, d, F, act):
         m.check_status()
 
 
+@pytest.mark.parametrize("N,d,F", [(2, 4104, 72), (63, 1032, 136), (65, 520, 264), (512, 512, 256), (513, 520, 1032),
+                                   (1025, 264, 520), (700, 1544, 2056), (16, 8, 16), (64, 8, 264), (10, 600, 2000)])
+def test_more_rows_and_columns_around_the_tiles(N, d, F):
+    """Tiles of 512 rows on CTA pairs, long and short K loops beside each other, few rows of dA."""
+    X, Wg, Wu, Wd, dY = _data(N, d, F, seed=N + d + F)
+    want, *grads = _wanted(X, Wg, Wu, Wd, dY, "silu")
+    for dt in (torch.bfloat16, torch.float32):
+        m = _make(N, d, F, dx=dt, dw=dt)
+        _close(m.forward(X, Wg, Wu, Wd), want, "y")
+        for g, w, name in zip(m.backward(dY, X, Wg, Wu, Wd), grads, ("dx", "dwg", "dwu", "dwd")):
+            _close(g, w, name)
+        m.check_status()
+
+
 def test_backward_is_the_difference_of_the_forward():
     """The loss sum(Y dY) along random directions, in float64, against the library's f32 gradients. The gradient's 2-norm
     error is WHOLE of its norm, so along a unit direction it is at most that."""

@@ -182,6 +182,26 @@ def test_position_outside_the_table():
     m.check_status()                               # a call clears what the last one reported
 
 
+@pytest.mark.parametrize("N", [1, 2047, 2048, 2049, 6000])
+def test_the_last_row_outside_the_table(N):
+    """Whoever looks at the positions: one block, or every one at its own rows."""
+    B = _B()
+    q, k, gq, gk, dq, dk, pos = _data(N, 4, 1, 64, torch.bfloat16, seed=N)
+    m = _make(N, 4, 1, 64, 64, torch.bfloat16, False)
+    for call in (lambda: m.forward(q, k, gq, gk, pos), lambda: m.backward(dq, dk, q, k, gq, gk, pos)):
+        call()
+        m.check_status()
+        last = int(pos[-1])
+        for wrong in (0, T + 1, -2 ** 31, 2 ** 31 - 1):
+            pos[-1] = wrong
+            out = call()[0]
+            assert B.ps_workspace_status(m.ws) == (B.PS_ERR_DEVICE_DATA, B.PS_DEV_BAD_LENGTH)
+            assert torch.isnan(out[-1]).all() and torch.isfinite(out[:-1]).all()
+        pos[-1] = last
+        assert torch.isfinite(call()[0]).all()
+        m.check_status()
+
+
 def test_nan_stays_in_its_head_and_streams():
     N, Hq, Hk, D = 40, 4, 2, 128
     q, k, gq, gk, dq, dk, pos = _data(N, Hq, Hk, D, torch.bfloat16, seed=4)
