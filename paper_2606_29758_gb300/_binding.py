@@ -149,6 +149,24 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
+_calls = None
+
+
+def calls():
+    """The module of the block operators' small calls (csrc/small_calls.cpp), bound to the library."""
+    global _calls
+    if _calls is None:
+        L = lib()
+        try:
+            from . import _calls as module
+        except ImportError as e:
+            raise ImportError("_calls.so is not built or not for this torch; run __graft_entry__.build()") from e
+        module.bind(*(ctypes.cast(f, _vp).value for f in (L.ps_dropout_rows, L.ps_qk_norm_rope_fwd, L.ps_qk_norm_rope_bwd,
+                                                          L.ps_gated_ffn_fwd, L.ps_gated_ffn_bwd)))
+        _calls = module
+    return _calls
+
+
 def status_string(status: int) -> str:
     return lib().ps_status_string(int(status)).decode()
 

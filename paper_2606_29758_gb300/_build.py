@@ -1,8 +1,10 @@
-"""Build libpsppo.so in place (nvcc, sm_103a only).
+"""Build libpsppo.so (nvcc, sm_103a only) and _calls.so (the host compiler) in place.
 
 Each translation unit compiles in parallel; the objects link into
 paper_2606_29758_gb300/libpsppo.so with the CUDA runtime linked statically, so the
-library needs only the driver at run time. No cmake, no torch extension machinery.
+library needs only the driver at run time. _calls.so is a Python module over torch's
+headers that makes the block operators' small calls; nothing in libpsppo.so depends on it.
+No cmake, no torch extension machinery.
 """
 from __future__ import annotations
 
@@ -10,6 +12,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -18,6 +21,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libpsppo.so")
+CALLS = os.path.join(PKG, "_calls.so")
 SOURCES = ["psppo_api.cu", "lmhead_bf16.cu", "lmhead_f32.cu", "fwd_static_scratch.cu", "design.cu", "ffn.cu", "block_ops.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
@@ -43,10 +47,26 @@ def _compile(src: str, verbose_ptxas: bool) -> str:
     return obj
 
 
+def _build_calls() -> None:
+    import torch
+    base = os.path.dirname(torch.__file__)
+    dirs = [INCLUDE, os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"),
+            sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(nvcc())), "include")]
+    tmp = CALLS + f".tmp{os.getpid()}"
+    cmd = [shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-I{d}" for d in dirs),
+           os.path.join(CSRC, "small_calls.cpp"), "-o", tmp, "-L" + os.path.join(base, "lib"),
+           "-ltorch_python", "-ltorch_cuda", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed for small_calls.cpp:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, CALLS)
+
+
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALLS):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + \
         [os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE)] + [os.path.abspath(__file__)]
     return any(os.path.getmtime(p) > t for p in deps)
@@ -56,8 +76,10 @@ def build(force: bool = False, verbose_ptxas: bool = False) -> str:
     if not force and not _stale():
         return LIB
     os.makedirs(BUILD, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        calls = ex.submit(_build_calls)
         objs = list(ex.map(lambda s: _compile(s, verbose_ptxas), SOURCES))
+        calls.result()
     tmp = LIB + f".tmp{os.getpid()}"
     r = subprocess.run([nvcc(), *ARCH, "-shared", "-o", tmp, *objs], capture_output=True, text=True)
     if r.returncode != 0:

@@ -103,20 +103,32 @@ class GatedFFN:
                                      self.dWu.data_ptr(), self.dWd.data_ptr(), B.dtype_code(self.dWd))
             self._bwd_ws = (self.ws_bwd.data_ptr(), self.ws_bwd.numel())
         self._w1, self._w2 = (s.F, s.d), (s.d, s.F)
+        calls = B.calls()
+        self._fast_fwd, self._fast_bwd = calls.ffn_fwd, calls.ffn_bwd
+        at = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
+        size = lambda t: 0 if t is None else t.numel()  # noqa: E731
+        grads = (self.dX, self.dWg, self.dWu, self.dWd) if s.train else [None] * 4
+        self._plan = calls.ffn_plan(s.rows, s.d, s.F, s.act, *(self._bwd_tail[4], self._bwd_tail[8]) if s.train else (0, 0),
+                                    *map(at, (self.Y, self.store, self.ws_fwd, self.ws_bwd, *grads)),
+                                    *map(size, (self.store, self.ws_fwd, self.ws_bwd)))
 
     def _inputs(self, X, Wg, Wu, Wd):
-        N, t = _row_count("X", X, self.s.rows), torch.bfloat16
-        return (N, X.data_ptr(), _pitch("X", X, N, self.s.d, t), _whole("Wg", Wg, self._w1, t),
+        N, t = X.shape[0], torch.bfloat16
+        return (X.data_ptr(), _pitch("X", X, N, self.s.d, t), _whole("Wg", Wg, self._w1, t),
                 _whole("Wu", Wu, self._w1, t), _whole("Wd", Wd, self._w2, t))
 
     def forward(self, X, Wg, Wu, Wd, out=None):
         """Y [N][d] (in `out` if given)."""
         s = self.s
-        N, *inputs = self._inputs(X, Wg, Wu, Wd)
+        rc = self._fast_fwd(self._plan, X, Wg, Wu, Wd, out)
+        N = _row_count("X", X, s.rows)
         Y = _first(self.Y, N) if out is None else out
-        rc = self._fwd(N, s.d, s.F, B.PS_DTYPE_BF16, s.act, *inputs, Y.data_ptr(),
-                       s.d if out is None else _pitch("out", out, N, s.d, torch.bfloat16), *self._fwd_tail, _stream())
-        B._check(rc, "ps_gated_ffn_fwd")
+        if rc is None:
+            inputs = self._inputs(X, Wg, Wu, Wd)
+            rc = self._fwd(N, s.d, s.F, B.PS_DTYPE_BF16, s.act, *inputs, Y.data_ptr(),
+                           s.d if out is None else _pitch("out", out, N, s.d, torch.bfloat16), *self._fwd_tail, _stream())
+        if rc:
+            B._check(rc, "ps_gated_ffn_fwd")
         self.stored = N if s.train else -1
         return Y
 
@@ -124,12 +136,17 @@ class GatedFFN:
         """(dX, dWg, dWu, dWd) of the last forward, which must have been given the same X and weights: one
         backward per forward (it turns the store into dG and dU in place)."""
         s = self.s
-        N, *inputs = self._inputs(X, Wg, Wu, Wd)
+        N = _row_count("X", X, s.rows)
         if self.stored != N:
+            self._inputs(X, Wg, Wu, Wd)
             raise RuntimeError("backward needs a forward of the same rows before it (train=True, one backward each)")
-        rc = self._bwd(N, s.d, s.F, B.PS_DTYPE_BF16, dY.data_ptr(), _pitch("dY", dY, N, s.d, torch.bfloat16), *inputs,
-                       *self._bwd_tail, B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._bwd_ws, _stream())
-        B._check(rc, "ps_gated_ffn_bwd")
+        rc = self._fast_bwd(self._plan, dY, X, Wg, Wu, Wd, dw_accumulate)
+        if rc is None:
+            inputs = self._inputs(X, Wg, Wu, Wd)
+            rc = self._bwd(N, s.d, s.F, B.PS_DTYPE_BF16, dY.data_ptr(), _pitch("dY", dY, N, s.d, torch.bfloat16), *inputs,
+                           *self._bwd_tail, B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._bwd_ws, _stream())
+        if rc:
+            B._check(rc, "ps_gated_ffn_bwd")
         self.stored = -1
         return _first(self.dX, N), self.dWg, self.dWu, self.dWd
 
@@ -189,6 +206,11 @@ class QKNormRope:
             self.dgq, self.dgk = (torch.empty(s.D, dtype=torch.float32, device=device) for _ in range(2))
             self._grads = (self.dq.data_ptr(), self._wq, self.dk.data_ptr(), self._wk, self.dgq.data_ptr(),
                            self.dgk.data_ptr())
+        calls = B.calls()
+        self._fast_fwd, self._fast_bwd = calls.qk_fwd, calls.qk_bwd
+        grads = [t.data_ptr() for t in (self.dq, self.dk, self.dgq, self.dgk)] if s.train else [0] * 4
+        self._plan = calls.qk_plan(s.rows, *self._head, self._table[0], s.eps, self._table[1] or 0, self.q.data_ptr(),
+                                   self.k.data_ptr(), *self._ws, *grads)
 
     def _inputs(self, N, q, k, gq, gk, pos, pos_base):
         s = self.s
@@ -199,23 +221,29 @@ class QKNormRope:
 
     def forward(self, q, k, gq, gk, pos, pos_base: int = 1, in_place: bool = False):
         """(q, k) normed and rotated; in_place writes over the inputs (serving: no backward follows)."""
+        rc = self._fast_fwd(self._plan, q, k, gq, gk, pos, pos_base, in_place)
         N = _row_count("q", q, self.s.rows)
-        inputs = self._inputs(N, q, k, gq, gk, pos, pos_base)
-        rc = self._fwd(N, *self._head, *inputs, *(inputs[:4] if in_place else self._out), *self._ws, _stream())
-        B._check(rc, "ps_qk_norm_rope_fwd")
+        if rc is None:
+            inputs = self._inputs(N, q, k, gq, gk, pos, pos_base)
+            rc = self._fwd(N, *self._head, *inputs, *(inputs[:4] if in_place else self._out), *self._ws, _stream())
+        if rc:
+            B._check(rc, "ps_qk_norm_rope_fwd")
         return (q, k) if in_place else (_first(self.q, N), _first(self.k, N))
 
     def backward(self, dq_out, dk_out, q, k, gq, gk, pos, pos_base: int = 1, dw_accumulate: bool = False):
         """(dq, dk, dgq, dgk) from the gradients of the forward's outputs and its inputs."""
         s = self.s
+        rc = self._fast_bwd(self._plan, dq_out, dk_out, q, k, gq, gk, pos, pos_base, dw_accumulate)
         N = _row_count("q", q, s.rows)
-        if not s.train:
-            raise RuntimeError("built without a backward (train=False)")
-        rc = self._bwd(N, *self._head, dq_out.data_ptr(), _pitch("dq_out", dq_out, N, self._wq, s.dtype),
-                       dk_out.data_ptr(), _pitch("dk_out", dk_out, N, self._wk, s.dtype),
-                       *self._inputs(N, q, k, gq, gk, pos, pos_base), *self._grads,
-                       B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._ws, _stream())
-        B._check(rc, "ps_qk_norm_rope_bwd")
+        if rc is None:
+            if not s.train:
+                raise RuntimeError("built without a backward (train=False)")
+            rc = self._bwd(N, *self._head, dq_out.data_ptr(), _pitch("dq_out", dq_out, N, self._wq, s.dtype),
+                           dk_out.data_ptr(), _pitch("dk_out", dk_out, N, self._wk, s.dtype),
+                           *self._inputs(N, q, k, gq, gk, pos, pos_base), *self._grads,
+                           B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._ws, _stream())
+        if rc:
+            B._check(rc, "ps_qk_norm_rope_bwd")
         return _first(self.dq, N), _first(self.dk, N), self.dgq, self.dgk
 
     def check_status(self):
@@ -229,9 +257,14 @@ class RowDropout:
 
     def __init__(self, p: float, site: int = 0):
         self.p, self.site = float(p), int(site)
-        self._call = B.lib().ps_dropout_rows
+        self._call, self._fast = B.lib().ps_dropout_rows, B.calls().dropout_rows
 
     def _run(self, x, row_traj, row_pos, seed, step, res, traj_base, out):
+        y = self._fast(x, row_traj, row_pos, seed, step, res, traj_base, out, self.p, self.site)
+        if y is not None:
+            if type(y) is int:
+                B._check(y, "ps_dropout_rows")
+            return y
         N, d = x.shape
         t = x.dtype
         pitch = _pitch("x", x, N, d, t)
