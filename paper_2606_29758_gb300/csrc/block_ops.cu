@@ -442,10 +442,11 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
       for (int j = 0; j < 4; ++j) sq = fma2(xb[j], xb[j], fma2(xa[j], xa[j], sq));
       float s0, s1;
       split2(sq, s0, s1);
-      const float sum = group_sum(s0 + s1, a.G);
-      const float r = mine ? rsqrtf(fmaf(sum, inv_d, a.eps)) : 0.f;   // (no head here: nothing to add to the gains)
-      const F2 r2 = pair2(r, r);
+      float sum = s0 + s1;
       if (!BWD) {
+        sum = group_sum(sum, a.G);
+        const float r = mine ? rsqrtf(fmaf(sum, inv_d, a.eps)) : 0.f;
+        const F2 r2 = pair2(r, r);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const F2 na = mul2(mul2(xa[j], r2), ga[j]), nb = mul2(mul2(xb[j], r2), gb[j]);
@@ -453,21 +454,59 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
           yb[j] = fma2(na, sn[j], mul2(nb, cs[j]));
         }
       } else {
-        // with n = x r: dg += dn n, dx = r (g dn - n mean(g dn n))
-        F2 dot = zero2;
+        // With n = x r: dg += dn n, dx = r (g dn - n mean(g dn n)). bf16: the two sums over the head go side by side, the
+        // second over x instead of n (106k rows of 28 + 4 heads of 128 463 us, one after the other 476); f32, whose loads
+        // ahead take the registers that this needs, would be slower by 6%.
+        constexpr bool kBoth = sizeof(T) == 2;
+        auto inverse = [&]() { return mine ? rsqrtf(fmaf(sum, inv_d, a.eps)) : 0.f; };   // (no head here: gains get nothing)
+        float r = 0.f;
+        if (!kBoth) {
+          sum = group_sum(sum, a.G);
+          r = inverse();
+        }
+        F2 r2 = pair2(r, r), dot = zero2;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const F2 da = fma2(yb[j], sn[j], mul2(ya[j], cs[j])), db = fma2(minus2, mul2(ya[j], sn[j]), mul2(yb[j], cs[j]));
-          xa[j] = mul2(xa[j], r2);
-          xb[j] = mul2(xb[j], r2);
-          acca[j] = fma2(da, xa[j], acca[j]);
-          accb[j] = fma2(db, xb[j], accb[j]);
-          ya[j] = mul2(da, ga[j]);
-          yb[j] = mul2(db, gb[j]);
-          dot = fma2(yb[j], xb[j], fma2(ya[j], xa[j], dot));
+          if (kBoth) {
+            ya[j] = da;
+            yb[j] = db;
+            dot = fma2(mul2(db, gb[j]), xb[j], fma2(mul2(da, ga[j]), xa[j], dot));
+          } else {
+            xa[j] = mul2(xa[j], r2);
+            xb[j] = mul2(xb[j], r2);
+            acca[j] = fma2(da, xa[j], acca[j]);
+            accb[j] = fma2(db, xb[j], accb[j]);
+            ya[j] = mul2(da, ga[j]);
+            yb[j] = mul2(db, gb[j]);
+            dot = fma2(yb[j], xb[j], fma2(ya[j], xa[j], dot));
+          }
         }
         split2(dot, s0, s1);
-        const float m = -group_sum(s0 + s1, a.G) * inv_d;
+        float m = s0 + s1;
+        if (kBoth) {
+#pragma unroll
+          for (int o = 16; o >= 1; o >>= 1)
+            if (a.G > o) {
+              sum += __shfl_xor_sync(0xffffffffu, sum, o);
+              m += __shfl_xor_sync(0xffffffffu, m, o);
+            }
+          r = inverse();
+          r2 = pair2(r, r);
+          m *= r;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            xa[j] = mul2(xa[j], r2);
+            xb[j] = mul2(xb[j], r2);
+            acca[j] = fma2(ya[j], xa[j], acca[j]);
+            accb[j] = fma2(yb[j], xb[j], accb[j]);
+            ya[j] = mul2(ya[j], ga[j]);
+            yb[j] = mul2(yb[j], gb[j]);
+          }
+        } else {
+          m = group_sum(m, a.G);
+        }
+        m *= -inv_d;
         const F2 m2 = pair2(m, m);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
