@@ -243,20 +243,23 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
   const int lo = EVEN || !rotated ? 16 * c : 8 * c;
   const int hi = EVEN || !rotated ? 16 * c + 8 : a.R / 2 + 8 * c;
   const int apart = hi - lo, in_step = slot * a.D + lo;
-  const int steps_q = (a.Hq + at_once - 1) / at_once, steps = steps_q + (a.Hk + at_once - 1) / at_once;
+  // the ring's steps are of queries or of keys; otherwise keys follow queries within a step
+  const int heads = a.Hq + a.Hk, steps_q = (a.Hq + at_once - 1) / at_once;
+  const int steps = RING ? steps_q + (a.Hk + at_once - 1) / at_once : (heads + at_once - 1) / at_once;
   const int step_elems = at_once * a.D;
   const float inv_d = 1.f / static_cast<float>(a.D);
   const bool whole = a.D == 16 * a.G;     // no lane of a group without dims
 
-  // This warp's units (a row's steps, or a part of them): runs of steps of one side (queries or keys) of a row. `left`:
-  // heads of the side from the step's first on; a group whose slot is not below it has none.
+  // This warp's units (a row's steps, or a part of them). With the ring: runs of steps of one side (queries or keys) of a
+  // row; `left`: heads of the side from the step's first on (a group whose slot is not below it has none).
   const int64_t units = a.N * a.parts, stride = static_cast<int64_t>(gridDim.x) * kQkWarps;
   auto row_of = [&](int64_t u) { return a.parts == 1 ? u : u / a.parts; };
   struct Run {
     int64_t u;
-    int s, s1;        // steps of the unit still to come: [s, s1) after this run
+    int s, s1;        // steps of the unit still to come: [s, s1) (RING: after this run)
     int steps, left;
     bool keys;
+    int64_t row;      // (without the ring)
     const T *x, *y;   // where the copies come from
     T* out;           // where this lane's results go
   };
@@ -267,6 +270,10 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
       const int part = static_cast<int>(r.u - row_of(r.u) * a.parts);
       r.s = steps * part / a.parts;
       r.s1 = steps * (part + 1) / a.parts;
+      if (!RING) {
+        r.row = row_of(r.u);
+        return;
+      }
     }
     const int64_t row = row_of(r.u);
     r.keys = r.s >= steps_q;
@@ -292,19 +299,28 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
   auto issue = [&](Run& r, int st) {
     if (r.u >= units) return;
     if (!RING) {
-      if (!(whole && r.left >= at_once)) {
+      const bool all = whole && (r.s + 1) * at_once <= heads;
+      const int h = r.s * at_once + slot;
+      if (!all) {
         va.zero(), vb.zero();
         if (BWD) wa.zero(), wb.zero();
       }
-      if ((whole && r.left >= at_once) || (here && slot < r.left)) {
-        va.load(r.x + in_step);
-        vb.load(r.x + in_step + apart);
+      if (all || (here && h < heads)) {
+        const bool k = h >= a.Hq;
+        const int64_t in_row = static_cast<int64_t>(k ? h - a.Hq : h) * a.D + lo;
+        const T* x = static_cast<const T*>(k ? a.k : a.q) + r.row * (k ? a.ldk : a.ldq) + in_row;
+        va.load(x);
+        vb.load(x + apart);
         if (BWD) {
-          wa.load(r.y + in_step);
-          wb.load(r.y + in_step + apart);
+          const T* y = static_cast<const T*>(k ? a.dky : a.dqy) + r.row * (k ? a.lddky : a.lddqy) + in_row;
+          wa.load(y);
+          wb.load(y + apart);
         }
       }
-    } else if (lane == 0) {
+      if (++r.s >= r.s1) open(r, true);
+      return;
+    }
+    if (lane == 0) {
       const uint32_t bytes = static_cast<uint32_t>(min(r.left * a.D, step_elems)) * static_cast<uint32_t>(sizeof(T));
       uint8_t* to = ring + st * Ring::kArrays * Ring::kSlot;
       mbar_arrive_expect_tx(&full[warp][st], bytes * Ring::kArrays);
@@ -355,8 +371,23 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
     h.load(g + apart);
     to_pairs<EVEN>(l, h, ga, gb);
   };
-  bool keys = false;                      // the side that gains and gradients are of
+  bool keys = false;                      // the side that gains and gradients are of (without the ring: this lane's)
   load_gains(false);
+  auto turn_to = [&](bool side) {
+    keys = side;
+    load_gains(side);
+    if (BWD)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 v = other[warp][j][lane];
+        float4 w;
+        split2(acca[j], w.x, w.y);
+        split2(accb[j], w.z, w.w);
+        other[warp][j][lane] = w;
+        acca[j] = pair2(v.x, v.y);
+        accb[j] = pair2(v.z, v.w);
+      }
+  };
   int64_t turned = -1;                    // the unit that cs and sn are of
   bool ok = true;
   uint32_t rows = 0, phase = 0;           // units so far; the ring's phase
@@ -396,24 +427,15 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
       ++rows;
     }
     turned = t.u;
-    if (t.keys != keys) {
-      keys = t.keys;
-      load_gains(keys);
-      if (BWD)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float4 v = other[warp][j][lane];
-          float4 w;
-          split2(acca[j], w.x, w.y);
-          split2(accb[j], w.z, w.w);
-          other[warp][j][lane] = w;
-          acca[j] = pair2(v.x, v.y);
-          accb[j] = pair2(v.z, v.w);
-        }
-    }
-    for (; t.steps > 0; --t.steps, t.left -= at_once, t.out += step_elems) {
+    if (RING && t.keys != keys) turn_to(t.keys);
+    for (int still = RING ? t.steps : t.s1 - t.s; still > 0; --still) {
       if (RING && !mbar_wait(&full[warp][st], phase, kDefaultTimeoutNs, nullptr)) { ok = false; break; }
-      const bool mine = here && slot < t.left;
+      const int head = RING ? 0 : t.s * at_once + slot;
+      const bool mine = here && (RING ? slot < t.left : head < heads);
+      if (!RING) {   // (a group without a head stays on a side that the row has)
+        const bool side = min(head, heads - 1) >= a.Hq;
+        if (side != keys) turn_to(side);
+      }
       F2 xa[4], xb[4], ya[4], yb[4];
       if (RING) {
         const T* from = reinterpret_cast<const T*>(ring + st * Ring::kArrays * Ring::kSlot) + (mine ? in_step : 0);
@@ -514,7 +536,19 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
           yb[j] = mul2(r2, fma2(xb[j], m2, yb[j]));
         }
       }
-      if (mine) store_pairs<EVEN>(t.out, t.out + apart, ya, yb);
+      T* out;
+      if (RING)
+        out = t.out;
+      else
+        out = static_cast<T*>(keys ? a.ko : a.qo) + t.row * (keys ? a.ldko : a.ldqo) +
+              static_cast<int64_t>(keys ? head - a.Hq : head) * a.D + lo;
+      if (mine) store_pairs<EVEN>(out, out + apart, ya, yb);
+      if (RING) {
+        t.left -= at_once;
+        t.out += step_elems;
+      } else {
+        ++t.s;
+      }
     }
     if (!ok) break;
     open(t, false);
@@ -526,6 +560,7 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
     for (uint32_t j = rows; j < rows + 2; ++j) mbar_wait(&tfull[warp][j & 1], (j >> 1) & 1u, kDefaultTimeoutNs, nullptr);
   }
   if (!BWD || a.part == nullptr) return;
+  if (!RING && keys) turn_to(false);
   __syncwarp();
 
   // gain gradients: over the warp's heads, then the block's warps; qk_gain_sum_kernel adds the blocks'
@@ -822,12 +857,15 @@ template <bool BWD>
 static int run_qk(QkArgs a, int dtype, int layout, cudaStream_t s) {
   a.G = lanes_for(a.D / 16);
   const int at_once = 32 / a.G;
-  const int steps = (a.Hq + at_once - 1) / at_once + (a.Hk + at_once - 1) / at_once;
-  const int64_t sms = num_sms_current();
-  a.parts = parts_for(a.N, sms * 2 * kQkWarps, steps);
-  if (dtype == PS_DTYPE_F32) return launch_qk<float, BWD, false>(a, layout, s);
-  const bool ring = steps >= kQkRingSteps && a.N >= sms * QkCfg<Bf16, BWD, true>::kBlocks * kQkWarps * kQkRingUnits;
-  return ring ? launch_qk<Bf16, BWD, true>(a, layout, s) : launch_qk<Bf16, BWD, false>(a, layout, s);
+  const int ring_steps = (a.Hq + at_once - 1) / at_once + (a.Hk + at_once - 1) / at_once;
+  const int64_t sms = num_sms_current(), want = sms * 2 * kQkWarps;
+  if (dtype == PS_DTYPE_BF16 && ring_steps >= kQkRingSteps &&
+      a.N >= sms * QkCfg<Bf16, BWD, true>::kBlocks * kQkWarps * kQkRingUnits) {
+    a.parts = parts_for(a.N, want, ring_steps);
+    return launch_qk<Bf16, BWD, true>(a, layout, s);
+  }
+  a.parts = parts_for(a.N, want, (a.Hq + a.Hk + at_once - 1) / at_once);
+  return dtype == PS_DTYPE_F32 ? launch_qk<float, BWD, false>(a, layout, s) : launch_qk<Bf16, BWD, false>(a, layout, s);
 }
 
 }  // namespace psk
