@@ -267,9 +267,13 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
     if (r.s >= r.s1) {
       r.u += stride;
       if (r.u >= units) return;
-      const int part = static_cast<int>(r.u - row_of(r.u) * a.parts);
-      r.s = steps * part / a.parts;
-      r.s1 = steps * (part + 1) / a.parts;
+      r.s = 0;
+      r.s1 = steps;
+      if (a.parts > 1) {   // (the divisions are a quarter of what a short row takes)
+        const int part = static_cast<int>(r.u - row_of(r.u) * a.parts);
+        r.s = steps * part / a.parts;
+        r.s1 = steps * (part + 1) / a.parts;
+      }
       if (!RING) {
         r.row = row_of(r.u);
         return;
