@@ -149,39 +149,39 @@ static __device__ __forceinline__ void store_pairs(T* lo, T* hi, const F2 (&a)[4
 // ================================================================== q/k norms and rotation
 //   n = x r g, r = (mean x^2 + eps)^(-1/2) over a head's D values; y = rotation(position) of n's first R dims.
 //   backward: dn = rotation^T dy, dg = sum dn x r, dx = r (g dn - x r^2 mean(g dn x)).
-// HBM-bound (a read and a write of every element; the backward two reads and a write). A head lies on G lanes, 16
-// values each: eight pairs, so a lane rotates by itself and only the mean crosses lanes (log2 G shuffles). A warp takes
-// 32 / G heads of one row at a time, queries first, and keeps its lanes' cosines and sines for the row and their gains for
-// the side; the arithmetic is on pairs of f32 (two to an instruction: with one the issue slots were what ran out).
-// What HBM then wants is bytes in flight. RING: the heads come through a ring in shared memory of the warp's own, filled by
-// bulk copies some steps ahead (one lane issues them), the next row's part of the table likewise. Otherwise a lane loads its
-// part of the next step into registers, which is enough for f32 (twice the bytes) and better for few steps a row or
-// few rows. Measured, us forward / backward, ring against registers: bf16, 106k rows of 28 + 4 heads of 128 282 / 473, 341 /
-// 507 (6.2 and 5.5 TB/s); 20k of 40 + 8 of 256 185 / 247, 195 / 280; 4000 of 28 + 4 18.6 / 35.1, 16.6 / 33.0; 100k of 6 + 2
-// of 96 (3 steps a row) 149 / 247, 143 / 224; f32, 50k of 28 + 4 280 / 419, 257 / 379 (6.4 and 6.5 TB/s).
+// HBM-bound (a read and a write of every element; the backward two reads and a write); short rows by the issue slots. A head
+// lies on G lanes, 16 values each: eight pairs, so a lane rotates by itself and only the mean crosses lanes (log2 G
+// shuffles). A warp takes 32 / G heads of one row at a time, keys after queries, and keeps its lanes' cosines and sines for
+// the row and their gains for the side; the arithmetic is on pairs of f32 (two to an instruction). The heads come through a
+// ring in shared memory of the warp's own, filled by its lanes' copies some steps ahead. us forward / backward, before from
+// bulk copies (bf16, from 4 steps a row on) or registers a step ahead: bf16, 106k rows of 28 + 4 heads of 128 270 / 421 (6.4 and
+// 6.2 TB/s; 282 / 452); 20k of 40 + 8 of 256 160 / 232 (182 / 237); 100k of 6 + 2 of 96 91 / 143 (100 / 153), of 64 57 / 86 (68 /
+// 103); 4000 of 28 + 4 18 / 31; f32, 50k of 28 + 4 253 / 366 (259 / 380), 100k of 6 + 2 of 64 78 / 124 (93 / 146).
 constexpr int kQkThreads = 128;
 constexpr int kQkWarps = kQkThreads / 32;
-template <class T, bool BWD, bool RING>
+template <class T, bool BWD>
 struct QkCfg {
   static constexpr int kArrays = BWD ? 2 : 1;                      // x, and dy
-  static constexpr int kStages = 4;
+  static constexpr int kStages = sizeof(T) == 2 ? 4 : BWD ? 2 : 3;
   static constexpr int kSlot = 512 * sizeof(T);                    // a step's heads: at most 32 lanes of 16 values
-  // a warp's shared memory: its ring, in the end its gain gradients [2][D]
-  static constexpr int kWarp = RING ? kStages * kArrays * kSlot : BWD ? 2 * 512 * 4 : 0;
-  static constexpr int kBlocks = BWD ? 3 : RING ? 5 : 4;           // per SM
+  static constexpr int kWarp = kStages * kArrays * kSlot;          // a warp's ring, in the end its gain gradients [2][D]
+  static constexpr int kBlocks = BWD ? 3 : 4;                      // per SM
+  // Of long rows fewer at once, which HBM prefers. 3 / 2, us: f32, 50k rows of 28 + 4 heads of 128 285 / 253 (backward 418 / 366), of
+  // 16 + 16 of 64 (8 KB) 144 / 138, of 12 + 2 of 128 (7 KB) 115 / 135; 4 / 3: bf16, 20k of 40 + 8 of 256 178 / 160, 106k of 28 + 4 of
+  // 128 (8 KB) 270 / 300.
+  static int blocks_of(int64_t row_bytes) {
+    if (sizeof(T) == 4 && row_bytes >= 8 * 1024) return 2;
+    return !BWD && sizeof(T) == 2 && row_bytes >= 16 * 1024 ? 3 : kBlocks;
+  }
 };
-static_assert(QkCfg<uint16_t, true, true>::kWarp >= 2 * 512 * 4, "a warp's gain gradients lie over its ring");
+static_assert(QkCfg<uint16_t, true>::kWarp >= 2 * 512 * 4, "a warp's gain gradients lie over its ring");
 // The status is cleared by a memset before the launch, as any block may set it early; of fewer rows the first block looks at
 // every position and sets the word alone (a token's call takes one launch, 6.3 -> 4 us on the device).
 constexpr int kQkCheckRows = 2048;
-constexpr int kQkRingSteps = 4, kQkRingUnits = 4;   // the ring: from so many steps a row and rows a warp on
 
-// Bulk copy global -> shared (16-byte aligned, whole 16 bytes), counted on `bar`.
-static __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                   smem_addr(dst)),
-               "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_addr(bar))
-               : "memory");
+// 16 bytes global -> shared.
+static __device__ __forceinline__ void lane_copy(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
 struct QkArgs {
@@ -212,23 +212,15 @@ static __device__ __forceinline__ float group_sum(float v, int G) {
   return v;
 }
 
-template <class T, bool EVEN, bool BWD, bool RING>
-__global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk_kernel(const QkArgs a) {
-  using Ring = QkCfg<T, BWD, RING>;
-  constexpr int ST = Ring::kStages;
-  extern __shared__ __align__(128) uint8_t qk_smem[];   // the warps' parts, two table rows each (RING), gains [2][D]
-  __shared__ uint64_t full[kQkWarps][ST], tfull[kQkWarps][2];
+template <class T, bool EVEN, bool BWD>
+__global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD>::kBlocks)) qk_kernel(const QkArgs a) {
+  using Cfg = QkCfg<T, BWD>;
+  constexpr int ST = Cfg::kStages;
+  extern __shared__ __align__(128) uint8_t qk_smem[];   // the warps' rings, gains [2][D]
   __shared__ float4 other[BWD ? kQkWarps : 1][4][32];   // gain gradients of the side that is not at work
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint8_t* const ring = qk_smem + warp * Ring::kWarp;
-  const uint32_t tab_bytes = RING ? static_cast<uint32_t>(a.R) * 4 : 0;
-  uint8_t* const tab = qk_smem + kQkWarps * Ring::kWarp + warp * 2 * tab_bytes;
-  float* const all_gains = reinterpret_cast<float*>(qk_smem + kQkWarps * Ring::kWarp + kQkWarps * 2 * tab_bytes);
-  if (lane == 0) {
-    for (int s = 0; s < ST; ++s) mbar_init(&full[warp][s], 1);
-    for (int s = 0; s < 2; ++s) mbar_init(&tfull[warp][s], 1);
-    fence_mbar_init();
-  }
+  uint8_t* const ring = qk_smem + warp * Cfg::kWarp;
+  float* const all_gains = reinterpret_cast<float*>(qk_smem + kQkWarps * Cfg::kWarp);
   for (int i = threadIdx.x; i < 2 * a.D; i += kQkThreads) {
     const void* g = i < a.D ? a.gq : a.gk;
     all_gains[i] = g ? Elem<T>::get(static_cast<const T*>(g)[i < a.D ? i : i - a.D]) : 1.f;
@@ -243,122 +235,78 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
   const int lo = EVEN || !rotated ? 16 * c : 8 * c;
   const int hi = EVEN || !rotated ? 16 * c + 8 : a.R / 2 + 8 * c;
   const int apart = hi - lo, in_step = slot * a.D + lo;
-  // the ring's steps are of queries or of keys; otherwise keys follow queries within a step
-  const int heads = a.Hq + a.Hk, steps_q = (a.Hq + at_once - 1) / at_once;
-  const int steps = RING ? steps_q + (a.Hk + at_once - 1) / at_once : (heads + at_once - 1) / at_once;
-  const int step_elems = at_once * a.D;
+  const int heads = a.Hq + a.Hk, steps = (heads + at_once - 1) / at_once;   // keys follow queries within a step
   const float inv_d = 1.f / static_cast<float>(a.D);
-  const bool whole = a.D == 16 * a.G;     // no lane of a group without dims
 
-  // This warp's units (a row's steps, or a part of them). With the ring: runs of steps of one side (queries or keys) of a
-  // row; `left`: heads of the side from the step's first on (a group whose slot is not below it has none).
+  // This warp's units: a row's steps, or a part of them.
   const int64_t units = a.N * a.parts, stride = static_cast<int64_t>(gridDim.x) * kQkWarps;
   auto row_of = [&](int64_t u) { return a.parts == 1 ? u : u / a.parts; };
   struct Run {
-    int64_t u;
-    int s, s1;        // steps of the unit still to come: [s, s1) (RING: after this run)
-    int steps, left;
-    bool keys;
-    int64_t row;      // (without the ring)
-    const T *x, *y;   // where the copies come from
-    T* out;           // where this lane's results go
+    int64_t u, row;
+    int s, s1;        // steps of the unit still to come
   };
-  auto open = [&](Run& r, bool loads) {   // the run that begins at step r.s of unit r.u
-    if (r.s >= r.s1) {
-      r.u += stride;
-      if (r.u >= units) return;
-      r.s = 0;
-      r.s1 = steps;
-      if (a.parts > 1) {   // (the divisions are a quarter of what a short row takes)
-        const int part = static_cast<int>(r.u - row_of(r.u) * a.parts);
-        r.s = steps * part / a.parts;
-        r.s1 = steps * (part + 1) / a.parts;
-      }
-      if (!RING) {
-        r.row = row_of(r.u);
-        return;
-      }
-    }
-    const int64_t row = row_of(r.u);
-    r.keys = r.s >= steps_q;
-    const int end = r.keys ? r.s1 : min(r.s1, steps_q), first = (r.keys ? r.s - steps_q : r.s) * at_once;
-    r.steps = end - r.s;
-    r.s = end;
-    r.left = (r.keys ? a.Hk : a.Hq) - first;
-    const int64_t in_row = static_cast<int64_t>(first) * a.D;
-    if (loads) {
-      r.x = static_cast<const T*>(r.keys ? a.k : a.q) + row * (r.keys ? a.ldk : a.ldq) + in_row;
-      if (BWD) r.y = static_cast<const T*>(r.keys ? a.dky : a.dqy) + row * (r.keys ? a.lddky : a.lddqy) + in_row;
-    } else {
-      r.out = static_cast<T*>(r.keys ? a.ko : a.qo) + row * (r.keys ? a.ldko : a.ldqo) + in_row + in_step;
-    }
-  };
-  auto begin = [&](Run& r, bool loads) {
-    r.u = static_cast<int64_t>(blockIdx.x) * kQkWarps + warp - stride;
-    r.s = r.s1 = 0;
-    open(r, loads);
-  };
-  Raw8<T> va, vb, wa, wb;   // (without the ring) the next step's heads
-  // the copies of the next step's heads into stage st, or its loads
-  auto issue = [&](Run& r, int st) {
+  auto open = [&](Run& r) {   // the next unit
+    r.u += stride;
     if (r.u >= units) return;
-    if (!RING) {
-      const bool all = whole && (r.s + 1) * at_once <= heads;
-      const int h = r.s * at_once + slot;
-      if (!all) {
-        va.zero(), vb.zero();
-        if (BWD) wa.zero(), wb.zero();
-      }
-      if (all || (here && h < heads)) {
-        const bool k = h >= a.Hq;
-        const int64_t in_row = static_cast<int64_t>(k ? h - a.Hq : h) * a.D + lo;
-        const T* x = static_cast<const T*>(k ? a.k : a.q) + r.row * (k ? a.ldk : a.ldq) + in_row;
-        va.load(x);
-        vb.load(x + apart);
-        if (BWD) {
-          const T* y = static_cast<const T*>(k ? a.dky : a.dqy) + r.row * (k ? a.lddky : a.lddqy) + in_row;
-          wa.load(y);
-          wb.load(y + apart);
-        }
-      }
-      if (++r.s >= r.s1) open(r, true);
-      return;
-    }
-    if (lane == 0) {
-      const uint32_t bytes = static_cast<uint32_t>(min(r.left * a.D, step_elems)) * static_cast<uint32_t>(sizeof(T));
-      uint8_t* to = ring + st * Ring::kArrays * Ring::kSlot;
-      mbar_arrive_expect_tx(&full[warp][st], bytes * Ring::kArrays);
-      bulk_load(to, r.x, bytes, &full[warp][st]);
-      if (BWD) bulk_load(to + Ring::kSlot, r.y, bytes, &full[warp][st]);
-    }
-    if (--r.steps == 0) {
-      open(r, true);
-    } else {
-      r.x += step_elems;
-      if (BWD) r.y += step_elems;
-      r.left -= at_once;
+    r.row = row_of(r.u);
+    r.s = 0;
+    r.s1 = steps;
+    if (a.parts > 1) {   // (the divisions are a quarter of what a short row takes)
+      const int part = static_cast<int>(r.u - r.row * a.parts);
+      r.s = steps * part / a.parts;
+      r.s1 = steps * (part + 1) / a.parts;
     }
   };
-  // the table's row of unit u's position into table slot `to`; the position is known a unit earlier
+  // The copies of the next step's heads into stage st: P pieces of 16 bytes a lane, counted through the row's heads (queries,
+  // then keys). A group of copies for each step, be it empty.
+  constexpr int P = Cfg::kSlot / 512, E = 16 / sizeof(T);
+  const int step_elems = at_once * a.D, row_elems = heads * a.D, first_k = a.Hq * a.D;
+  const T *xq, *xk, *yq, *yk;   // the row's queries, and its keys less the queries' elements, at this lane's first piece
+  auto sources = [&](const Run& r) {
+    auto at = [&](const void* base, int64_t ld, int before) {
+      return static_cast<const T*>(base) + (r.row * ld + lane * E - before);
+    };
+    xq = at(a.q, a.ldq, 0);
+    xk = at(a.k, a.ldk, first_k);
+    if (BWD) {
+      yq = at(a.dqy, a.lddqy, 0);
+      yk = at(a.dky, a.lddky, first_k);
+    }
+  };
+  auto issue = [&](Run& r, int st) {
+    if (r.u < units) {
+      const uint32_t to = smem_addr(ring) + st * Cfg::kArrays * Cfg::kSlot + lane * 16;
+      const int e0 = r.s * step_elems, end = min(e0 + step_elems, row_elems) - lane * E;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const int e = e0 + i * 32 * E;
+        if (e >= end) continue;
+        const bool k = e + lane * E >= first_k;
+        lane_copy(to + i * 512, (k ? xk : xq) + e);
+        if (BWD) lane_copy(to + Cfg::kSlot + i * 512, (k ? yk : yq) + e);
+      }
+      if (++r.s >= r.s1) {
+        open(r);
+        if (r.u < units) sources(r);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // the table's row of unit u's position; the position is known a unit earlier
   auto position = [&](int64_t u) { return a.R > 0 && u < units ? __ldg(a.pos + row_of(u)) : 0; };
   auto in_table = [&](int pos) {
     const int64_t t = static_cast<int64_t>(pos) - a.pos_base;
     return t >= 0 && t < a.T;
   };
-  auto issue_table = [&](int64_t u, int pos, int to) {
-    if (!RING || a.R == 0 || u >= units || lane != 0) return;
-    const int64_t t = in_table(pos) ? static_cast<int64_t>(pos) - a.pos_base : 0;
-    mbar_arrive_expect_tx(&tfull[warp][to], tab_bytes);
-    bulk_load(tab + to * tab_bytes, a.table + t * (a.R / 2), tab_bytes, &tfull[warp][to]);
-  };
 
   Run t, n;
-  begin(t, false);
-  begin(n, true);
+  t.u = static_cast<int64_t>(blockIdx.x) * kQkWarps + warp - stride;
+  open(t);
+  n = t;
+  if (n.u < units) sources(n);
   int pos = position(t.u), pos_next = position(t.u + stride);
 #pragma unroll
-  for (int s = 0; s < (RING ? ST : 1); ++s) issue(n, s);
-  issue_table(t.u, pos, 0);
+  for (int s = 0; s < ST; ++s) issue(n, s);
   const F2 zero2 = pair2(0.f, 0.f), one2 = pair2(1.f, 1.f), minus2 = pair2(-1.f, -1.f);
   F2 cs[4], sn[4], ga[4], gb[4];          // the row's cosines and sines; the side's gains
   F2 acca[4], accb[4];                    // backward: the side's gain gradients
@@ -375,7 +323,7 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
     h.load(g + apart);
     to_pairs<EVEN>(l, h, ga, gb);
   };
-  bool keys = false;                      // the side that gains and gradients are of (without the ring: this lane's)
+  bool keys = false;                      // the side that this lane's gains and gradients are of
   load_gains(false);
   auto turn_to = [&](bool side) {
     keys = side;
@@ -392,9 +340,6 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
         accb[j] = pair2(v.z, v.w);
       }
   };
-  int64_t turned = -1;                    // the unit that cs and sn are of
-  bool ok = true;
-  uint32_t rows = 0, phase = 0;           // units so far; the ring's phase
   int st = 0;
   if (a.N <= kQkCheckRows && blockIdx.x == 0) {   // (the loads above are under way)
     int bad = 0;
@@ -406,63 +351,49 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
       if (bad) raise_status(a.status, PS_DEV_BAD_LENGTH);
     }
   }
-  while (t.u < units) {
-    if (t.u != turned && a.R > 0) {
-      const int to = rows & 1;
-      if (RING && !mbar_wait(&tfull[warp][to], (rows >> 1) & 1u, kDefaultTimeoutNs, nullptr)) { ok = false; break; }
+  for (; t.u < units; open(t)) {
+    if (a.R > 0) {
       const bool good = in_table(pos);
       if (!good && a.N > kQkCheckRows) raise_status(a.status, PS_DEV_BAD_LENGTH);
       if (rotated) {
         const int64_t row = good ? static_cast<int64_t>(pos) - a.pos_base : 0;
-        const float4* at = RING ? reinterpret_cast<const float4*>(tab + to * tab_bytes + c * 64)
-                                : reinterpret_cast<const float4*>(a.table + row * (a.R / 2) + 8 * c);
+        const float4* at = reinterpret_cast<const float4*>(a.table + row * (a.R / 2) + 8 * c);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float4 v = RING ? at[i] : __ldg(at + i);
+          float4 v = __ldg(at + i);
           if (!good) v.x = v.y = v.z = v.w = __int_as_float(0x7fffffff);   // outside the table: NaN
           cs[i] = pair2(v.x, v.z);
           sn[i] = pair2(v.y, v.w);
         }
       }
-      // (the other slot was read a unit ago)
-      issue_table(t.u + stride, pos_next, to ^ 1);
       pos = pos_next;
       pos_next = position(t.u + 2 * stride);
-      ++rows;
     }
-    turned = t.u;
-    if (RING && t.keys != keys) turn_to(t.keys);
-    for (int still = RING ? t.steps : t.s1 - t.s; still > 0; --still) {
-      if (RING && !mbar_wait(&full[warp][st], phase, kDefaultTimeoutNs, nullptr)) { ok = false; break; }
-      const int head = RING ? 0 : t.s * at_once + slot;
-      const bool mine = here && (RING ? slot < t.left : head < heads);
-      if (!RING) {   // (a group without a head stays on a side that the row has)
-        const bool side = min(head, heads - 1) >= a.Hq;
-        if (side != keys) turn_to(side);
-      }
+    for (; t.s < t.s1; ++t.s) {
+      const int head = t.s * at_once + slot;
+      const bool mine = here && head < heads, side = min(head, heads - 1) >= a.Hq;   // (without a head: a side that the row has)
+      if (side != keys) turn_to(side);
+      asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
+      __syncwarp();   // every lane's copies of the step
       F2 xa[4], xb[4], ya[4], yb[4];
-      if (RING) {
-        const T* from = reinterpret_cast<const T*>(ring + st * Ring::kArrays * Ring::kSlot) + (mine ? in_step : 0);
-        const int far = mine ? apart : 0;
+      Raw8<T> va, vb, wa, wb;
+      if (mine) {
+        const T* from = reinterpret_cast<const T*>(ring + st * Cfg::kArrays * Cfg::kSlot) + in_step;
         va.load(from);
-        vb.load(from + far);
+        vb.load(from + apart);
         if (BWD) {
           wa.load(from + 512);
-          wb.load(from + 512 + far);
+          wb.load(from + 512 + apart);
         }
-        if (!(whole && t.left >= at_once) && !mine) {   // (what lies there belongs to another head)
-          va.zero(), vb.zero();
-          if (BWD) wa.zero(), wb.zero();
-        }
+      } else {
+        va.zero(), vb.zero();
+        if (BWD) wa.zero(), wb.zero();
       }
       to_pairs<EVEN>(va, vb, xa, xb);
       if (BWD) to_pairs<EVEN>(wa, wb, ya, yb);
-      if (RING) __syncwarp();   // the stage has been read
+      __syncwarp();   // the stage has been read
       issue(n, st);
-      if (RING && ++st == ST) {
-        st = 0;
-        phase ^= 1u;
-      }
+      st = st + 1 == ST ? 0 : st + 1;
       F2 sq = zero2;
 #pragma unroll
       for (int j = 0; j < 4; ++j) sq = fma2(xb[j], xb[j], fma2(xa[j], xa[j], sq));
@@ -540,31 +471,15 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
           yb[j] = mul2(r2, fma2(xb[j], m2, yb[j]));
         }
       }
-      T* out;
-      if (RING)
-        out = t.out;
-      else
-        out = static_cast<T*>(keys ? a.ko : a.qo) + t.row * (keys ? a.ldko : a.ldqo) +
-              static_cast<int64_t>(keys ? head - a.Hq : head) * a.D + lo;
-      if (mine) store_pairs<EVEN>(out, out + apart, ya, yb);
-      if (RING) {
-        t.left -= at_once;
-        t.out += step_elems;
-      } else {
-        ++t.s;
+      if (mine) {
+        T* out = static_cast<T*>(keys ? a.ko : a.qo) + t.row * (keys ? a.ldko : a.ldqo) +
+                 static_cast<int64_t>(keys ? head - a.Hq : head) * a.D + lo;
+        store_pairs<EVEN>(out, out + apart, ya, yb);
       }
     }
-    if (!ok) break;
-    open(t, false);
-  }
-  if (!ok) {
-    // a copy did not land: let those under way land (bounded), then leave
-    raise_status(a.status, PS_DEV_TIMEOUT);
-    for (int j = 0; j < ST; ++j) mbar_wait(&full[warp][(st + j) % ST], st + j < ST ? phase : phase ^ 1u, kDefaultTimeoutNs, nullptr);
-    for (uint32_t j = rows; j < rows + 2; ++j) mbar_wait(&tfull[warp][j & 1], (j >> 1) & 1u, kDefaultTimeoutNs, nullptr);
   }
   if (!BWD || a.part == nullptr) return;
-  if (!RING && keys) turn_to(false);
+  if (keys) turn_to(false);
   __syncwarp();
 
   // gain gradients: over the warp's heads, then the block's warps; qk_gain_sum_kernel adds the blocks'
@@ -595,7 +510,7 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD, RING>::kBlocks)) qk
   for (int i = threadIdx.x; i < 2 * a.D; i += kQkThreads) {
     float t = 0.f;
 #pragma unroll
-    for (int w = 0; w < kQkWarps; ++w) t += reinterpret_cast<const float*>(qk_smem + w * Ring::kWarp)[i];
+    for (int w = 0; w < kQkWarps; ++w) t += reinterpret_cast<const float*>(qk_smem + w * Cfg::kWarp)[i];
     part[i] = t;
   }
 }
@@ -823,7 +738,7 @@ static int parts_for(int64_t rows, int64_t want, int steps) {
   const int64_t p = want / rows;
   return static_cast<int>(p < steps ? p : steps);
 }
-constexpr int64_t kQkMaxBlocks = 760;   // five per SM; the backward's workspace holds a partial sum of each
+constexpr int64_t kQkMaxBlocks = 760;   // at most; the backward's workspace holds a partial sum of each
 
 // A row of heads: its pitch, base and the rows' last element stay within what the kernel addresses.
 static bool rows_ok(const void* p, int64_t ld, int64_t cols, int dtype) {
@@ -835,16 +750,17 @@ static bool qk_sizes_ok(int64_t N, int Hq, int Hk, int D, int R, int dtype, int 
   return (dtype == PS_DTYPE_BF16 || dtype == PS_DTYPE_F32) && (layout == PS_ROPE_HALF || layout == PS_ROPE_EVEN);
 }
 
-template <class T, bool BWD, bool RING>
+template <class T, bool BWD>
 static int launch_qk(const QkArgs& a, int layout, cudaStream_t s) {
-  using Cfg = QkCfg<T, BWD, RING>;
+  using Cfg = QkCfg<T, BWD>;
   // resident blocks take their units in turn
   const int64_t want = (a.N * a.parts + kQkWarps - 1) / kQkWarps;
-  int64_t most = static_cast<int64_t>(num_sms_current()) * Cfg::kBlocks;
+  int64_t most = static_cast<int64_t>(num_sms_current()) *
+                 Cfg::blocks_of(static_cast<int64_t>(a.Hq + a.Hk) * a.D * static_cast<int64_t>(sizeof(T)));
   if (most > kQkMaxBlocks) most = kQkMaxBlocks;
   const unsigned grid = static_cast<unsigned>(want < most ? want : most);
-  const size_t smem = kQkWarps * (Cfg::kWarp + (RING ? 2 * 4 * static_cast<size_t>(a.R) : 0)) + 2 * sizeof(float) * a.D;
-  auto kern = layout == PS_ROPE_EVEN ? qk_kernel<T, true, BWD, RING> : qk_kernel<T, false, BWD, RING>;
+  const size_t smem = kQkWarps * Cfg::kWarp + 2 * sizeof(float) * a.D;
+  auto kern = layout == PS_ROPE_EVEN ? qk_kernel<T, true, BWD> : qk_kernel<T, false, BWD>;
   if (smem > 32 * 1024 &&
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
     return refused(PS_ERR_CUDA, a.status, s);
@@ -861,15 +777,8 @@ template <bool BWD>
 static int run_qk(QkArgs a, int dtype, int layout, cudaStream_t s) {
   a.G = lanes_for(a.D / 16);
   const int at_once = 32 / a.G;
-  const int ring_steps = (a.Hq + at_once - 1) / at_once + (a.Hk + at_once - 1) / at_once;
-  const int64_t sms = num_sms_current(), want = sms * 2 * kQkWarps;
-  if (dtype == PS_DTYPE_BF16 && ring_steps >= kQkRingSteps &&
-      a.N >= sms * QkCfg<Bf16, BWD, true>::kBlocks * kQkWarps * kQkRingUnits) {
-    a.parts = parts_for(a.N, want, ring_steps);
-    return launch_qk<Bf16, BWD, true>(a, layout, s);
-  }
-  a.parts = parts_for(a.N, want, (a.Hq + a.Hk + at_once - 1) / at_once);
-  return dtype == PS_DTYPE_F32 ? launch_qk<float, BWD, false>(a, layout, s) : launch_qk<Bf16, BWD, false>(a, layout, s);
+  a.parts = parts_for(a.N, static_cast<int64_t>(num_sms_current()) * 2 * kQkWarps, (a.Hq + a.Hk + at_once - 1) / at_once);
+  return dtype == PS_DTYPE_F32 ? launch_qk<float, BWD>(a, layout, s) : launch_qk<Bf16, BWD>(a, layout, s);
 }
 
 }  // namespace psk
