@@ -456,12 +456,14 @@ int ps_lmhead_ppo_fwd_noalloc(int64_t N, int d, int V, int dtype, const void* Hp
  *   dWu = dU^T X, dWd = dY^T A.
  * X, Y, dY [N][d] bf16, Wg, Wu [F][d] and Wd [d][F] bf16, contiguous (the halves of one
  * [2F][d] buffer will do); f32 accumulation. A, dG and dU are rounded to bf16 between the
- * products. PS_DTYPE_F32 returns PS_ERR_UNSUPPORTED.
+ * products; up to 64 rows with F <= 2048 they are kept in two bf16 parts, the second what the first
+ * one's rounding left. PS_DTYPE_F32 returns PS_ERR_UNSUPPORTED.
  * store: NULL (no backward follows; A lies in the workspace), or ps_gated_ffn_store_size(N, F)
  *   bytes, 16-byte aligned, that the forward fills and the backward of the same N, F, X and
  *   weights consumes: A [N][F] bf16, then, each from the next 256-byte boundary, P = U s'(G)
  *   and Q = s(G) [N][F] f16, relative to a power of two per row and 32 columns, and their
- *   exponents [ceil(F/32)][N] (6.1 bytes per row and column of F). The backward overwrites P
+ *   exponents [ceil(F/32)][N] (6.1 bytes per row and column of F; with two parts each of the three
+ *   planes has 2 N rows). The backward overwrites P
  *   and Q with dG and dU (bf16): one backward per forward; calling it twice on one store is
  *   an error the library cannot see. Too small: PS_ERR_WORKSPACE.
  * Backward outputs: dX [N][d], dWg, dWu [F][d], dWd [d][F], in dx_dtype and dw_dtype (bf16:

@@ -8,7 +8,8 @@
 // writes A; then A Wd^T. For a backward the first product also keeps P = U s'(G) and Q = s(G) (the store), and the
 // backward's first product, dA, turns them into dG = dA P and dU = dA Q in its epilogue, in place. So a training
 // step executes the 18 N d F FLOPs of its six products and no recomputation, and no f32 N x F value reaches memory.
-// A, dG and dU are rounded to bf16, the operand type of the products that read them; P and Q are kept in f16 relative to
+// A, dG and dU are rounded to bf16, the operand type of the products that read them (few rows of narrow blocks: in two parts,
+// see kept_parts); P and Q are kept in f16 relative to
 // a power of two per row and 32 columns (2^-11 of the value down to 2^-28 of the slice's largest, 2^-39 of the largest
 // below that), which in bf16 would have been a third rounding of 2^-8 under dX and dW.
 #include <cuda_runtime.h>
@@ -220,7 +221,18 @@ static __device__ __forceinline__ float2 ld_cluster_v2(uint32_t cl_addr) {
 struct FewKept {
   uint16_t *P, *Q;
   uint32_t* scale;
+  int parts;   // of A, dG and dU: 1, or 2 (see kept_parts)
 };
+// Two values in bf16, and with two parts what their rounding leaves, `apart` elements further on.
+static __device__ __forceinline__ void store_parts(uint16_t* to, int64_t apart, int parts, float x, float y) {
+  const uint32_t v = pack_bf16x2(x, y);
+  *reinterpret_cast<uint32_t*>(to) = v;
+  if (parts == 2) {
+    const float hx = __uint_as_float(v << 16), hy = __uint_as_float(v & 0xffff0000u);
+    *reinterpret_cast<uint32_t*>(to + apart) =
+        pack_bf16x2(fabsf(hx) <= 3.4028235e38f ? x - hx : 0.f, fabsf(hy) <= 3.4028235e38f ? y - hy : 0.f);
+  }
+}
 
 // kFewUp: out[n][f] = s(x_n . Wg_f) (x_n . Wu_f), tmW and tmW2 the two weights in boxes of 64 rows; kFewDown: out[n][c] =
 // x_n . W_c, tmW in boxes of 128 rows; kFewDa: dA[n][f] = sum_c x_n,c W_c,f (W as it lies, MN-major, in boxes of 64 x 64) and
@@ -242,6 +254,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
   const int kb0 = static_cast<int>(static_cast<long long>(num_kb) * rank / nranks);
   const int kb1 = static_cast<int>(static_cast<long long>(num_kb) * (rank + 1) / nranks);
   const int row0 = unit * (UP ? 64 : 128);
+  const int operand_rows = N * (OP == kFewDown ? kept.parts : 1);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
@@ -343,13 +356,13 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     const int r = (warp & 3) * 32 + lane;
     const uint32_t t_row = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16);
 #pragma unroll 1
-    for (int c = 0; c < NT && c < N; c += 32) {
+    for (int c = 0; c < NT && c < operand_rows; c += 32) {
       uint32_t v[32];
       tmem_ld32(t_row + c, v);
       tmem_ld_wait();
 #pragma unroll
       for (int j = 0; j < 32; ++j)
-        if (j < NT - c && c + j < N) part[(c + j) * 128 + r] = __uint_as_float(v[j]);
+        if (j < NT - c && c + j < operand_rows) part[(c + j) * 128 + r] = __uint_as_float(v[j]);
     }
   }
   tc_fence_before();
@@ -377,7 +390,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
       act_and_slope<ACT>(g.y, q1, s1);
       const int64_t at = static_cast<int64_t>(n) * ldo + row0 + 2 * j;
       const bool in = row0 + 2 * j < C;
-      if (in) *reinterpret_cast<uint32_t*>(out + at) = pack_bf16x2(q0 * u.x, q1 * u.y);
+      if (in) store_parts(out + at, static_cast<int64_t>(N) * ldo, kept.parts, q0 * u.x, q1 * u.y);
       if (KEEP) {   // a warp has the row's 64 columns, so half of it a slice of 32 (columns past C hold zeros)
         s0 *= u.x;
         s1 *= u.y;
@@ -412,14 +425,22 @@ __global__ void __launch_bounds__(kFewThreads, 2)
         y.y += a.y;
         y.z += a.z;
         y.w += a.w;
+        if (OP == kFewDown && kept.parts == 2) {
+          const float4 b = ld_cluster_v4(mapa_shared(base + ((N + n) * 128 + 4 * j) * 4, k));
+          y.x += b.x;
+          y.y += b.y;
+          y.z += b.z;
+          y.w += b.w;
+        }
       }
       if (!in) continue;
       if (DA) {
         auto over = [&](uint16_t* plane, uint2 v, uint32_t exponent) {
           const float factor = __uint_as_float(exponent << 23);
           const float2 a = unpack_f16x2(v.x), b = unpack_f16x2(v.y);
-          *reinterpret_cast<uint2*>(plane + at) = make_uint2(pack_bf16x2(y.x * a.x * factor, y.y * a.y * factor),
-                                                             pack_bf16x2(y.z * b.x * factor, y.w * b.y * factor));
+          const int64_t apart = static_cast<int64_t>(N) * ldo;
+          store_parts(plane + at, apart, kept.parts, y.x * a.x * factor, y.y * a.y * factor);
+          store_parts(plane + at + 2, apart, kept.parts, y.z * b.x * factor, y.w * b.y * factor);
         };
         over(kept.P, p, scale & 255u);
         over(kept.Q, q, scale >> 8 & 255u);
@@ -444,8 +465,15 @@ struct FfnStore {
   size_t bytes;
 };
 static size_t plane_bytes(int64_t N, int F) { return (static_cast<size_t>(N) * F * 2 + 255) / 256 * 256; }
+// Few rows of a narrow block have A, dG and dU in two parts, each of N rows: the bf16 values, and in bf16 what their rounding
+// left, which the products that read them add up. Over few values the errors do not average out: with one part an
+// output was up to 1.8 times as far off as its own rounding alone leaves it (d = 100, F = 300; 1.55 at 300, 1000; from d = 1000, F =
+// 3000 on 1.41, the two roundings' mean). One part / two, forward and backward, us: 8 rows, d = 304, F = 1000 24.7 / 25.3; 16, 600, 2000
+// 30.4 / 31.5; 64, 304, 1000 34 / 37; beyond, where it would give nothing: 32, 1000, 4000 37.8 / 41.8; 1, 3584, 16384 206 / 237.
+constexpr int kPartsRows = 64, kPartsF = 2048;
+static int kept_parts(int64_t N, int F) { return N <= kPartsRows && F <= kPartsF ? 2 : 1; }
 static FfnStore ffn_store(void* base, int64_t N, int F) {
-  const size_t plane = plane_bytes(N, F);
+  const size_t plane = plane_bytes(N * kept_parts(N, F), F);
   uint8_t* b = static_cast<uint8_t*>(base);
   FfnStore f;
   f.A = reinterpret_cast<uint16_t*>(b);
@@ -454,6 +482,15 @@ static FfnStore ffn_store(void* base, int64_t N, int F) {
   f.scale = reinterpret_cast<uint32_t*>(b + 3 * plane);
   f.bytes = 3 * plane + (static_cast<size_t>(N) * ((F + 31) / 32) * 4 + 255) / 256 * 256;
   return f;
+}
+
+// Rows of a plane, and the store's bytes, that hold a call of N rows or of any fewer.
+static int64_t kept_rows_up_to(int64_t N, int F) {
+  const int64_t two = N < kPartsRows ? N : kPartsRows, rows = two * kept_parts(two, F);
+  return N > rows ? N : rows;
+}
+static size_t store_bytes_up_to(int64_t N, int F) {
+  return 3 * plane_bytes(kept_rows_up_to(N, F), F) + (static_cast<size_t>(N) * ((F + 31) / 32) * 4 + 255) / 256 * 256;
 }
 
 // Blocks of 256 rows walked together: the X (or dY) rows of a band stay in a quarter of L2 while the weights stream by.
@@ -483,12 +520,15 @@ static int launch_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, c
   auto map_w = [&](CUtensorMap* m, const void* w) {
     return OP == kFewDa ? map_mnmajor(m, w, K, C, C) : map_kmajor(m, w, C, K, K, UP ? 64 : 128);
   };
-  if (!map_w(&tw, W) || !map_w(&tw2, W2) || !map_kmajor(&tx, X, N, K, ldx, NT)) return PS_ERR_INVALID_ARG;
+  if (!map_w(&tw, W) || !map_w(&tw2, W2) ||
+      !map_kmajor(&tx, X, OP == kFewDown ? N * kept.parts : N, K, ldx, NT))
+    return PS_ERR_INVALID_ARG;
   auto kern = ffn_few_kernel<NT, OP, ACT, KEEP>;
   constexpr size_t smem = sizeof(FewSmem<NT>) + 1024;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
     return PS_ERR_CUDA;
   const int64_t units = (C + (UP ? 63 : 127)) / (UP ? 64 : 128);
+  static_assert(kPartsRows * 2 <= kFewRows, "both parts are the operand's rows");
   const int num_kb = static_cast<int>((K + kBK - 1) / kBK);
   int ranks = few_ranks(units, num_kb);
   for (;; ranks /= 2) {
@@ -503,9 +543,10 @@ static int launch_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, c
 template <int OP, int ACT, bool KEEP>
 static int ffn_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, const void* W, const void* W2, void* out,
                    int64_t ldo, const FewKept& kept, uint32_t* status, cudaStream_t s) {
-  if (N <= 16) return launch_few<16, OP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
-  if (N <= 32) return launch_few<32, OP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
-  if (OP == kFewDa || N <= 64) return launch_few<64, OP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
+  const int64_t rows = OP == kFewDown ? N * kept.parts : N;
+  if (rows <= 16) return launch_few<16, OP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
+  if (rows <= 32) return launch_few<32, OP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
+  if (OP == kFewDa || rows <= 64) return launch_few<64, OP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
   if constexpr (OP != kFewDa) return launch_few<128, OP, ACT, KEEP>(N, C, K, X, ldx, W, W2, out, ldo, kept, status, s);
 }
 
@@ -523,7 +564,7 @@ static int ffn_up(int64_t N, int d, int F, const void* X, int64_t ldx, const voi
                   const FfnStore& f, uint32_t* status, cudaStream_t s) {
   using Epi = FfnUpEpi<ACT, KEEP, 2>;
   using PairEpi = FfnUpEpi<ACT, KEEP, 4>;
-  if (few_up(N, d, F)) return ffn_few<kFewUp, ACT, KEEP>(N, F, d, X, ldx, Wg, Wu, f.A, F, {f.P, f.Q, f.scale}, status, s);
+  if (few_up(N, d, F)) return ffn_few<kFewUp, ACT, KEEP>(N, F, d, X, ldx, Wg, Wu, f.A, F, {f.P, f.Q, f.scale, kept_parts(N, F)}, status, s);
   TwoMaps m;
   auto maps = [&](int rows) {
     if (!map_kmajor(&m.a, X, N, d, ldx, rows) || !map_kmajor(&m.b, Wg, F, d, d, kBN / 2) ||
@@ -557,7 +598,7 @@ constexpr int kFewDaRows = 64;   // (of the 16, 32 and 64 row kernels)
 static int ffn_da(int64_t N, int d, int F, const void* dY, int64_t lddy, const void* Wd, const FfnStore& f,
                   uint32_t* status, cudaStream_t s) {
   if (N <= kFewDaRows)
-    return ffn_few<kFewDa, PS_ACT_SILU, false>(N, F, d, dY, lddy, Wd, Wd, nullptr, F, {f.P, f.Q, f.scale}, status, s);
+    return ffn_few<kFewDa, PS_ACT_SILU, false>(N, F, d, dY, lddy, Wd, Wd, nullptr, F, {f.P, f.Q, f.scale, kept_parts(N, F)}, status, s);
   TwoMaps m;
   if (!map_kmajor(&m.a, dY, N, d, lddy, kBM) || !map_mnmajor(&m.b, Wd, d, F, F) || !map_out_16(&m.c, f.P, N, F, F) ||
       !map_out_16(&m.c2, f.Q, N, F, F))
@@ -573,13 +614,14 @@ static int ffn_da(int64_t N, int d, int F, const void* dY, int64_t lddy, const v
 // holds depends on it).
 struct Product {
   int64_t M, N, K;              // outputs and the K loop (of each operand set)
-  bool two_sets;                // product 0 only
+  bool two_sets;
   bool a_mn, b_mn;
   const void *A, *A2, *B, *B2;
   int64_t lda, ldb;
   void* out;
   int64_t ldo;
   int kind;                     // kOutBf16, kOutF32 or kOutF32Add
+  bool fold = false;            // the second half of the M rows is added to the first
 };
 struct GroupTile {
   int halves, ctas;   // of the kernel
@@ -598,6 +640,7 @@ static int kb_of(const Product& p) {
   const int64_t kb = (p.K + kBK - 1) / kBK;
   return static_cast<int>(p.two_sets ? 2 * kb : kb);
 }
+static bool partial(const Product& p, int splits) { return splits > 1 || p.fold; }
 // What a unit costs, in hundredths of a 256 x 256 k block's MMAs on one SM (0.55 us): its k blocks at the rate that the tile
 // sustains (or at the rate at which an SM gets its share of the weights from HBM, 43 GB/s, where few row blocks read them),
 // its outputs at 43 GB/s, and its start and end. Loads and outputs share an SM's port to L2, so they add up.
@@ -605,7 +648,7 @@ static double unit_cost(const Product& p, GroupTile t, int splits) {
   double kb_cost = t.halves == 2 ? 100 : t.ctas == 2 ? 62 : 68;
   const double hbm = kTileBBytes / t.ctas * (t.ctas == 2 && p.M <= kBM ? 5.5e-3 : 4.2e-3) / static_cast<double>((p.M + t.rows() - 1) / t.rows());
   if (!p.a_mn && hbm > kb_cost) kb_cost = hbm;
-  const double out = kBM * t.halves * kBN * (splits > 1 || p.kind != kOutBf16 ? 4 : 2) * 4.2e-3;
+  const double out = kBM * t.halves * kBN * (partial(p, splits) || p.kind != kOutBf16 ? 4 : 2) * 4.2e-3;
   return kb_cost * kb_of(p) / splits + out + (t.halves == 2 ? 200 : 120);
 }
 
@@ -720,7 +763,7 @@ static GroupPlan plan_group(const Product* p, int count) {
   best.bytes = 0;
   for (int t = 0; t < count; ++t) {
     best.part_off[t] = best.bytes;
-    if (best.splits[t] == 1) continue;
+    if (!partial(p[t], best.splits[t])) continue;
     const size_t unit = best.tile.rows(), rows = (p[t].M + unit - 1) / unit * unit;
     best.bytes += (best.splits[t] * rows * p[t].N * 4 + 255) / 256 * 256;
   }
@@ -733,7 +776,7 @@ static size_t part_bytes(const Product* p, int count) {
   size_t sum = 0;
   for (int t = 0; t < count; ++t) {
     const size_t shares = static_cast<size_t>(kb_of(p[t])) / kLeastKb + 1;
-    if (shares < 2) continue;
+    if (shares < 2 && !p[t].fold) continue;
     const size_t all = shares * ((p[t].M + 4 * kBM - 1) / (4 * kBM) * (4 * kBM)) * p[t].N * 4;
     const size_t most = static_cast<size_t>(2 * kPlanSms) * 2 * kBM * kBN * 4;
     sum += ((all < most ? all : most) + 255) / 256 * 256;
@@ -783,7 +826,7 @@ static int run_group(const Product* p, int count, void* part, uint32_t* status, 
     o.b_mn = q.b_mn;
     o.cols = static_cast<int>(q.N);
     o.part_rows = o.m_blocks * rows;
-    o.out = o.splits > 1 ? kOutPartial : q.kind;
+    o.out = partial(q, o.splits) ? kOutPartial : q.kind;
     deal(loads, static_cast<int64_t>(o.m_blocks) * o.n_blocks * o.splits, unit_cost(q, plan.tile, o.splits), g.seg[t],
          &g.segs[t]);
     auto map_a = [&](CUtensorMap* m, const void* at) {
@@ -793,15 +836,16 @@ static int run_group(const Product* p, int count, void* part, uint32_t* status, 
       return q.b_mn ? map_mnmajor(m, at, q.K, q.N, q.ldb) : map_kmajor(m, at, q.N, q.K, q.ldb, kBN / plan.tile.ctas);
     };
     if (!map_a(&g.a[t], q.A) || !map_b(&g.b[t], q.B)) return PS_ERR_INVALID_ARG;
-    if (q.two_sets && (!map_a(&g.a2, q.A2) || !map_b(&g.b2, q.B2))) return PS_ERR_INVALID_ARG;
+    if (q.two_sets && (!map_a(&g.a2[t], q.A2) || !map_b(&g.b2[t], q.B2))) return PS_ERR_INVALID_ARG;
     bool ok;
-    if (o.splits > 1) {
+    if (partial(q, o.splits)) {
       float* planes = reinterpret_cast<float*>(static_cast<uint8_t*>(part) + plan.part_off[t]);
       ok = map_out_f32(&g.c[t], planes, static_cast<int64_t>(o.splits) * o.part_rows, q.N, q.N);
       SumItem& it = sums.item[sums.count];
-      it = {planes, static_cast<int64_t>(o.part_rows) * q.N, o.splits, static_cast<int>(q.M), static_cast<int>(q.N / 4),
-            q.out, q.ldo, q.kind};
-      sums.end[sums.count] = q.M * (q.N / 4) + (sums.count > 0 ? sums.end[sums.count - 1] : 0);
+      const int64_t rows_out = q.fold ? q.M / 2 : q.M;
+      it = {planes, static_cast<int64_t>(o.part_rows) * q.N, o.splits, static_cast<int>(rows_out), static_cast<int>(q.N / 4),
+            q.fold ? static_cast<int>(rows_out) : 0, q.out, q.ldo, q.kind};
+      sums.end[sums.count] = rows_out * (q.N / 4) + (sums.count > 0 ? sums.end[sums.count - 1] : 0);
       ++sums.count;
     } else {
       ok = q.kind == kOutBf16 ? map_out_bf16(&g.c[t], q.out, q.M, q.N, q.ldo) : map_out_f32(&g.c[t], q.out, q.M, q.N, q.ldo);
@@ -824,7 +868,7 @@ static Product down_product(int64_t N, int d, int F, const void* A, const void* 
 }
 static int ffn_down(int64_t N, int d, int F, const void* A, const void* Wd, void* Y, int64_t ldy, void* part,
                     uint32_t* status, cudaStream_t s) {
-  if (N <= kFewRows) return ffn_few<kFewDown, PS_ACT_SILU, false>(N, d, F, A, F, Wd, Wd, Y, ldy, {}, status, s);
+  if (N <= kFewRows) return ffn_few<kFewDown, PS_ACT_SILU, false>(N, d, F, A, F, Wd, Wd, Y, ldy, {nullptr, nullptr, nullptr, kept_parts(N, F)}, status, s);
   const Product p = down_product(N, d, F, A, Wd, Y, ldy);
   return run_group(&p, 1, part, status, s);
 }
@@ -837,13 +881,16 @@ static size_t down_part_bytes(int64_t N, int d, int F) {
 static int grad_products(Product* p, int64_t N, int d, int F, const FfnStore& f, const void* dY, int64_t lddy,
                          const void* X, int64_t ldx, const void* Wg, const void* Wu, void* dX, int64_t lddx, int dx_kind,
                          void* dWg, void* dWu, void* dWd, int dw_kind) {
+  // the second parts of A, dG and dU: further rows of dX, a second operand set of the others
+  const bool two = kept_parts(N, F) == 2;
+  auto rest = [&](uint16_t* plane) { return two ? plane + N * F : nullptr; };
   int n = 0;
-  if (dX) p[n++] = {N, d, F, true, false, true, f.P, f.Q, Wg, Wu, F, d, dX, lddx, dx_kind};
+  if (dX) p[n++] = {two ? 2 * N : N, d, F, true, false, true, f.P, f.Q, Wg, Wu, F, d, dX, lddx, dx_kind, two};
   if (dWg) {
-    p[n++] = {F, d, N, false, true, true, f.P, nullptr, X, nullptr, F, ldx, dWg, d, dw_kind};
-    p[n++] = {F, d, N, false, true, true, f.Q, nullptr, X, nullptr, F, ldx, dWu, d, dw_kind};
+    p[n++] = {F, d, N, two, true, true, f.P, rest(f.P), X, X, F, ldx, dWg, d, dw_kind};
+    p[n++] = {F, d, N, two, true, true, f.Q, rest(f.Q), X, X, F, ldx, dWu, d, dw_kind};
   }
-  if (dWd) p[n++] = {d, F, N, false, true, true, dY, nullptr, f.A, nullptr, lddy, F, dWd, F, dw_kind};
+  if (dWd) p[n++] = {d, F, N, two, true, true, dY, dY, f.A, rest(f.A), lddy, F, dWd, F, dw_kind};
   return n;
 }
 
@@ -867,12 +914,12 @@ extern "C" {
 
 size_t ps_gated_ffn_store_size(int64_t N, int F) {
   if (N < 0 || F < 8 || F % 8) return 0;
-  return ffn_store(nullptr, N, F).bytes;
+  return store_bytes_up_to(N, F);
 }
 
 size_t ps_gated_ffn_fwd_workspace_size(int64_t N, int d, int F, int with_store) {
   if (!sizes_ok(N, d, F)) return 0;
-  return kWsHeader + (with_store ? 0 : plane_bytes(N, F)) + down_part_bytes(N, d, F);
+  return kWsHeader + (with_store ? 0 : plane_bytes(kept_rows_up_to(N, F), F)) + down_part_bytes(N, d, F);
 }
 
 int ps_gated_ffn_fwd(int64_t N, int d, int F, int dtype, int act, const void* X, int64_t ldx, const void* Wg,
@@ -896,7 +943,7 @@ int ps_gated_ffn_fwd(int64_t N, int d, int F, int dtype, int act, const void* X,
   uint8_t* scratch = static_cast<uint8_t*>(ws) + kWsHeader;
   if (!store) {
     f.A = reinterpret_cast<uint16_t*>(scratch);
-    scratch += plane_bytes(N, F);
+    scratch += plane_bytes(N * kept_parts(N, F), F);
   }
   if (act == PS_ACT_SILU)
     rc = store ? ffn_up<PS_ACT_SILU, true>(N, d, F, X, ldx, Wg, Wu, f, status, s)
@@ -910,11 +957,15 @@ int ps_gated_ffn_fwd(int64_t N, int d, int F, int dtype, int act, const void* X,
 
 size_t ps_gated_ffn_bwd_workspace_size(int64_t N, int d, int F) {
   if (!sizes_ok(N, d, F)) return 0;
-  Product p[kGroupMost];
-  void* some = reinterpret_cast<void*>(16);   // (not read)
-  const int n = grad_products(p, N, d, F, ffn_store(nullptr, N, F), nullptr, d, nullptr, d, nullptr, nullptr, some, d,
-                              kOutF32, some, some, some, kOutF32);
-  return kWsHeader + part_bytes(p, n);
+  auto parts = [&](int64_t rows) {
+    Product p[kGroupMost];
+    void* some = reinterpret_cast<void*>(16);   // (not read)
+    const int n = grad_products(p, rows, d, F, ffn_store(nullptr, rows, F), nullptr, d, nullptr, d, nullptr, nullptr, some, d,
+                                kOutF32, some, some, some, kOutF32);
+    return part_bytes(p, n);
+  };
+  const size_t all = parts(N), few = parts(N < kPartsRows ? N : kPartsRows);   // (any fewer rows too)
+  return kWsHeader + (all > few ? all : few);
 }
 
 int ps_gated_ffn_bwd(int64_t N, int d, int F, int dtype, const void* dY, int64_t lddy, const void* X, int64_t ldx,

@@ -1,6 +1,6 @@
 // Several tensor-core products in one persistent launch, their K loops split where there are few tiles (sm_103a).
 //
-//   D_t[M_t, N_t] = sum_k A_t[m, k] B_t[n, k],  t = 0 .. count - 1;  product 0 may add up two operand sets over its K loop
+//   D_t[M_t, N_t] = sum_k A_t[m, k] B_t[n, k],  t = 0 .. count - 1;  a product may add up two operand sets over its K loop
 //
 // The kernel of umma_gemm.cuh (tiles, ring, roles, bounded waits), with a unit that is (product, tile, share of the k
 // blocks): what a product's layouts are, where its operands lie and how its accumulator is stored is read per unit. So
@@ -30,14 +30,14 @@ constexpr int kGroupSegs = 12;
 
 struct GroupProduct {
   int m_blocks, n_blocks, splits, num_kb;
-  int first_kb;    // k blocks of the first operand set (product 0; else num_kb)
+  int first_kb;    // k blocks of the first operand set (num_kb without a second)
   int band_m;
   int a_mn, b_mn;  // MN-major operands
   int out, cols;
   int part_rows;   // rows from one share's partial to the next
 };
 struct GroupArgs {
-  CUtensorMap a[kGroupMost], b[kGroupMost], c[kGroupMost], a2, b2;
+  CUtensorMap a[kGroupMost], b[kGroupMost], c[kGroupMost], a2[kGroupMost], b2[kGroupMost];
   GroupProduct p[kGroupMost];
   GroupSeg seg[kGroupMost][kGroupSegs];
   int segs[kGroupMost];
@@ -183,8 +183,8 @@ __global__ void __launch_bounds__(kGroupThreads, 1)
             else tma_load_2d(to, map, &sm.full[s], c0, c1);
           };
           const bool second = kb >= first;
-          const CUtensorMap* const ma = second ? &g.a2 : &g.a[w.t];
-          const CUtensorMap* const mb = second ? &g.b2 : &g.b[w.t];
+          const CUtensorMap* const ma = second ? &g.a2[w.t] : &g.a[w.t];
+          const CUtensorMap* const mb = second ? &g.b2[w.t] : &g.b[w.t];
           const int k0 = (second ? kb - first : kb) * kBK;
           if (a_mn) {
             for (int i = 0; i < 2 * HALVES; ++i) load(sm.a[s] + i * (kBK * 128), ma, m0 + i * 64, k0);
@@ -417,6 +417,7 @@ struct SumItem {
   const float* part;     // [splits][part_rows][cols] f32
   int64_t plane;         // part_rows * cols
   int splits, rows, quads;   // quads of columns a row
+  int fold;              // rows whose outputs come in two parts: the second so many rows further down (0: in one)
   void* out;
   int64_t ld;
   int kind;              // kOutBf16, kOutF32 or kOutF32Add
@@ -445,6 +446,13 @@ static __global__ void __launch_bounds__(256) sum_partials_kernel(const __grid_c
       s.y += v.y;
       s.z += v.z;
       s.w += v.w;
+      if (it.fold > 0) {
+        const float4 u = __ldcg(reinterpret_cast<const float4*>(p + static_cast<int64_t>(it.fold) * it.quads * 4));
+        s.x += u.x;
+        s.y += u.y;
+        s.z += u.z;
+        s.w += u.w;
+      }
     }
     const int64_t at = static_cast<int64_t>(row) * it.ld + col;
     if (it.kind == kOutBf16) {

@@ -26,14 +26,15 @@ def test_ffn(L):
         assert _ffn(L, **bad) == INV, bad
     assert _ffn(L, dt=1) == UNSUP                         # f32
     need = L.ps_gated_ffn_store_size(4, 64)
-    assert need == 3 * 512 + 256 and L.ps_gated_ffn_store_size(-1, 64) == 0 and L.ps_gated_ffn_store_size(4, 60) == 0
+    assert need == 3 * 1024 + 256 and L.ps_gated_ffn_store_size(-1, 64) == 0 and L.ps_gated_ffn_store_size(4, 60) == 0
     assert _ffn(L, store=P, sb=need - 1) == WS
-    assert L.ps_gated_ffn_fwd_workspace_size(4, 64, 64, 0) == 256 + 512
+    assert L.ps_gated_ffn_fwd_workspace_size(4, 64, 64, 0) == 256 + 1024
     assert L.ps_gated_ffn_fwd_workspace_size(4, 64, 64, 1) == 256
     # a workspace for N rows holds any fewer
     for d, F in ((64, 64), (136, 4104), (1536, 8192), (3584, 16384)):
-        for size in (lambda n: L.ps_gated_ffn_fwd_workspace_size(n, d, F, 1), lambda n: L.ps_gated_ffn_bwd_workspace_size(n, d, F)):
-            sizes = [size(n) for n in (0, 1, 127, 129, 400, 1000, 5000, 100000)]
+        for size in (lambda n: L.ps_gated_ffn_fwd_workspace_size(n, d, F, 1), lambda n: L.ps_gated_ffn_bwd_workspace_size(n, d, F),
+                     lambda n: L.ps_gated_ffn_fwd_workspace_size(n, d, F, 0), lambda n: 256 + L.ps_gated_ffn_store_size(n, F)):
+            sizes = [size(n) for n in (0, 1, 63, 64, 65, 100, 127, 128, 129, 400, 1000, 5000, 100000)]
             assert sizes == sorted(sizes) and sizes[0] >= 256
 
     def bwd(N=4, dt=0, dX=P, lddx=64, dxt=0, dWg=P, dWu=P, dwt=0, flags=0, sb=1 << 20, dY=P):

@@ -104,6 +104,23 @@ def test_more_rows_and_columns_around_the_tiles(N, d, F):
         m.check_status()
 
 
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("N,d,F", [(1, 96, 256), (2, 104, 304), (5, 8, 1048), (16, 136, 72), (33, 256, 512), (64, 128, 1048)])
+def test_few_rows_lose_nothing_between_the_products(N, d, F, act):
+    """Up to 64 rows of a narrow block A, dG and dU are two bf16 parts: 2^-17 of a value. What is left in f32 gradients is the kept P and Q, in
+    f16: 2^-12 to 2^-11 of a value at most, 2.8e-4 in 2-norm where all are at their worst, and f32's own 2^-17 of long sums:
+    under 4e-4, where one bf16 rounding gives 1.1e-3 to 2.3e-3. y keeps its own rounding alone, 2.3e-3 at most."""
+    X, Wg, Wu, Wd, dY = _data(N, d, F, seed=3 * N + d + F)
+    want, *grads = _wanted(X, Wg, Wu, Wd, dY, act)
+    code = _B().PS_ACT_GELU if act == "gelu" else _B().PS_ACT_SILU
+    m = _make(100, d, F, code, dx=torch.float32, dw=torch.float32)     # (buffers for more rows)
+    off = lambda got, w: np.linalg.norm(_f64(got)[0] - w[0]) / np.linalg.norm(w[0])  # noqa: E731
+    assert off(m.forward(X, Wg, Wu, Wd), want) <= 2.4e-3
+    for g, w, name in zip(m.backward(dY, X, Wg, Wu, Wd), grads, ("dx", "dwg", "dwu", "dwd")):
+        assert off(g, w) <= 4e-4, (name, off(g, w))
+    m.check_status()
+
+
 def test_backward_is_the_difference_of_the_forward():
     """The loss sum(Y dY) along random directions, in float64, against the library's f32 gradients. The gradient's 2-norm
     error is WHOLE of its norm, so along a unit direction it is at most that."""
