@@ -22,8 +22,8 @@ _stream = (lambda: _raw_stream(_device())) if _raw_stream and _device else B._st
 _CODE = {torch.bfloat16: B.PS_DTYPE_BF16, torch.float32: B.PS_DTYPE_F32}
 
 
-# The checks below run before a pointer is taken; together with the library's own they are most of a small call's host
-# time, so each is one comparison of what a right call has, and the reason is looked for only after it fails.
+# The checks of a call's ordinary way, before a pointer is taken: one comparison of what a right call has, and the reason after
+# it fails. (Calls in order go by B.calls(), which compares the same on the tensors themselves.)
 def _pitch(name: str, t: torch.Tensor, n: int, cols: int, dtype: torch.dtype) -> int:
     """The row pitch of a tensor of n rows of cols elements that lie side by side."""
     st = t.stride()
@@ -127,9 +127,9 @@ class GatedFFN:
             inputs = self._inputs(X, Wg, Wu, Wd)
             rc = self._fwd(N, s.d, s.F, B.PS_DTYPE_BF16, s.act, *inputs, Y.data_ptr(),
                            s.d if out is None else _pitch("out", out, N, s.d, torch.bfloat16), *self._fwd_tail, _stream())
+        self.stored = N if s.train and rc == B.PS_OK else -1
         if rc:
             B._check(rc, "ps_gated_ffn_fwd")
-        self.stored = N if s.train else -1
         return Y
 
     def backward(self, dY, X, Wg, Wu, Wd, dw_accumulate: bool = False):
@@ -145,9 +145,9 @@ class GatedFFN:
             inputs = self._inputs(X, Wg, Wu, Wd)
             rc = self._bwd(N, s.d, s.F, B.PS_DTYPE_BF16, dY.data_ptr(), _pitch("dY", dY, N, s.d, torch.bfloat16), *inputs,
                            *self._bwd_tail, B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._bwd_ws, _stream())
+        self.stored = -1
         if rc:
             B._check(rc, "ps_gated_ffn_bwd")
-        self.stored = -1
         return _first(self.dX, N), self.dWg, self.dWu, self.dWd
 
     def check_status(self):
@@ -269,8 +269,8 @@ class RowDropout:
         t = x.dtype
         pitch = _pitch("x", x, N, d, t)
         y = torch.empty_like(x) if out is None else out
-        rc = self._call(N, d, _CODE[t] if t in _CODE else B.dtype_code(x), x.data_ptr(), pitch, None if res is None else res.data_ptr(),
-                        0 if res is None else _pitch("res", res, N, d, t), _whole("row_traj", row_traj, (N,), torch.int32),
+        rc = self._call(N, d, _CODE[t] if t in _CODE else B.dtype_code(x), x.data_ptr(), pitch,
+                        None if res is None else res.data_ptr(), 0 if res is None else _pitch("res", res, N, d, t), _whole("row_traj", row_traj, (N,), torch.int32),
                         _whole("row_pos", row_pos, (N,), torch.int32), traj_base, self.p, seed & (2**64 - 1),
                         step & (2**64 - 1), self.site, y.data_ptr(), d if out is None else _pitch("out", out, N, d, t),
                         _stream())

@@ -166,9 +166,9 @@ struct QkCfg {
   static constexpr int kSlot = 512 * sizeof(T);                    // a step's heads: at most 32 lanes of 16 values
   static constexpr int kWarp = kStages * kArrays * kSlot;          // a warp's ring, in the end its gain gradients [2][D]
   static constexpr int kBlocks = BWD ? 3 : 4;                      // per SM
-  // Of long rows fewer at once, which HBM prefers. 3 / 2, us: f32, 50k rows of 28 + 4 heads of 128 285 / 253 (backward 418 / 366), of
-  // 16 + 16 of 64 (8 KB) 144 / 138, of 12 + 2 of 128 (7 KB) 115 / 135; 4 / 3: bf16, 20k of 40 + 8 of 256 178 / 160, 106k of 28 + 4 of
-  // 128 (8 KB) 270 / 300.
+  // Of long rows fewer at once, which HBM prefers. 3 / 2, us: f32, 50k rows of 28 + 4 heads of 128 285 / 253 (backward
+  // 418 / 366), of 16 + 16 of 64 (8 KB) 144 / 138, of 12 + 2 of 128 (7 KB) 115 / 135; 4 / 3: bf16, 20k of 40 + 8 of 256
+  // 178 / 160, 106k of 28 + 4 of 128 (8 KB) 270 / 300.
   static int blocks_of(int64_t row_bytes) {
     if (sizeof(T) == 4 && row_bytes >= 8 * 1024) return 2;
     return !BWD && sizeof(T) == 2 && row_bytes >= 16 * 1024 ? 3 : kBlocks;

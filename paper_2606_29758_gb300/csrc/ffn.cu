@@ -8,10 +8,10 @@
 // writes A; then A Wd^T. For a backward the first product also keeps P = U s'(G) and Q = s(G) (the store), and the
 // backward's first product, dA, turns them into dG = dA P and dU = dA Q in its epilogue, in place. So a training
 // step executes the 18 N d F FLOPs of its six products and no recomputation, and no f32 N x F value reaches memory.
-// A, dG and dU are rounded to bf16, the operand type of the products that read them (few rows of narrow blocks: in two parts,
-// see kept_parts); P and Q are kept in f16 relative to
-// a power of two per row and 32 columns (2^-11 of the value down to 2^-28 of the slice's largest, 2^-39 of the largest
-// below that), which in bf16 would have been a third rounding of 2^-8 under dX and dW.
+// A, dG and dU are rounded to bf16, the operand type of the products that read them (few rows of narrow blocks: in two
+// parts, see kept_parts); P and Q are kept in f16 relative to a power of two per row and 32 columns (2^-11 of the value
+// down to 2^-28 of the slice's largest, 2^-39 of the largest below that), which in bf16 would have been a third rounding
+// of 2^-8 under dX and dW.
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -465,11 +465,12 @@ struct FfnStore {
   size_t bytes;
 };
 static size_t plane_bytes(int64_t N, int F) { return (static_cast<size_t>(N) * F * 2 + 255) / 256 * 256; }
-// Few rows of a narrow block have A, dG and dU in two parts, each of N rows: the bf16 values, and in bf16 what their rounding
-// left, which the products that read them add up. Over few values the errors do not average out: with one part an
-// output was up to 1.8 times as far off as its own rounding alone leaves it (d = 100, F = 300; 1.55 at 300, 1000; from d = 1000, F =
-// 3000 on 1.41, the two roundings' mean). One part / two, forward and backward, us: 8 rows, d = 304, F = 1000 24.7 / 25.3; 16, 600, 2000
-// 30.4 / 31.5; 64, 304, 1000 34 / 37; beyond, where it would give nothing: 32, 1000, 4000 37.8 / 41.8; 1, 3584, 16384 206 / 237.
+// Few rows of a narrow block have A, dG and dU in two parts, each of N rows: the bf16 values, and in bf16 what their
+// rounding left, which the products that read them add up. Over few values the errors do not average out: with one part
+// an output was up to 1.8 times as far off as its own rounding alone leaves it (d = 100, F = 300; 1.55 at 300, 1000; from
+// d = 1000, F = 3000 on 1.41, the two roundings' mean). One part / two, forward and backward, us: 8 rows, d = 304,
+// F = 1000 24.7 / 25.5; 16, 600, 2000 30.4 / 31.7; 64, 304, 1000 34 / 37; beyond, where it would give little: 32, 1000,
+// 4000 37.8 / 41.8; 1, 3584, 16384 206 / 237.
 constexpr int kPartsRows = 64, kPartsF = 2048;
 static int kept_parts(int64_t N, int F) { return N <= kPartsRows && F <= kPartsF ? 2 : 1; }
 static FfnStore ffn_store(void* base, int64_t N, int F) {
@@ -564,7 +565,8 @@ static int ffn_up(int64_t N, int d, int F, const void* X, int64_t ldx, const voi
                   const FfnStore& f, uint32_t* status, cudaStream_t s) {
   using Epi = FfnUpEpi<ACT, KEEP, 2>;
   using PairEpi = FfnUpEpi<ACT, KEEP, 4>;
-  if (few_up(N, d, F)) return ffn_few<kFewUp, ACT, KEEP>(N, F, d, X, ldx, Wg, Wu, f.A, F, {f.P, f.Q, f.scale, kept_parts(N, F)}, status, s);
+  const FewKept kept = {f.P, f.Q, f.scale, kept_parts(N, F)};
+  if (few_up(N, d, F)) return ffn_few<kFewUp, ACT, KEEP>(N, F, d, X, ldx, Wg, Wu, f.A, F, kept, status, s);
   TwoMaps m;
   auto maps = [&](int rows) {
     if (!map_kmajor(&m.a, X, N, d, ldx, rows) || !map_kmajor(&m.b, Wg, F, d, d, kBN / 2) ||
@@ -592,13 +594,13 @@ static int ffn_up(int64_t N, int d, int F, const void* X, int64_t ldx, const voi
 }
 
 // dA = dY Wd and, from the kept P and Q, dG and dU over them. Few rows / CTA pairs, us: 1 row, d = 3584, F = 16384 21.6 / 40; 20,
-// 1600, 6400 9.0 / 15.5; 64, 3000, 12000 19 / 23; 64, 1000, 3000 11.7 / 13.1; 100, 3000, 12000 26 / 23; 100, 600, 2000 18 / 11; 128,
-// 1536, 8192 15.2 / 15.7 (each row is a turn of the join's loads).
+// 1600, 6400 9.0 / 15.5; 64, 3000, 12000 19 / 23; 64, 1000, 3000 11.7 / 13.1; 100, 3000, 12000 26 / 23; 100, 600, 2000
+// 18 / 11; 128, 1536, 8192 15.2 / 15.7 (each row is a turn of the join's loads).
 constexpr int kFewDaRows = 64;   // (of the 16, 32 and 64 row kernels)
 static int ffn_da(int64_t N, int d, int F, const void* dY, int64_t lddy, const void* Wd, const FfnStore& f,
                   uint32_t* status, cudaStream_t s) {
-  if (N <= kFewDaRows)
-    return ffn_few<kFewDa, PS_ACT_SILU, false>(N, F, d, dY, lddy, Wd, Wd, nullptr, F, {f.P, f.Q, f.scale, kept_parts(N, F)}, status, s);
+  const FewKept kept = {f.P, f.Q, f.scale, kept_parts(N, F)};
+  if (N <= kFewDaRows) return ffn_few<kFewDa, PS_ACT_SILU, false>(N, F, d, dY, lddy, Wd, Wd, nullptr, F, kept, status, s);
   TwoMaps m;
   if (!map_kmajor(&m.a, dY, N, d, lddy, kBM) || !map_mnmajor(&m.b, Wd, d, F, F) || !map_out_16(&m.c, f.P, N, F, F) ||
       !map_out_16(&m.c2, f.Q, N, F, F))
@@ -646,7 +648,8 @@ static bool partial(const Product& p, int splits) { return splits > 1 || p.fold;
 // its outputs at 43 GB/s, and its start and end. Loads and outputs share an SM's port to L2, so they add up.
 static double unit_cost(const Product& p, GroupTile t, int splits) {
   double kb_cost = t.halves == 2 ? 100 : t.ctas == 2 ? 62 : 68;
-  const double hbm = kTileBBytes / t.ctas * (t.ctas == 2 && p.M <= kBM ? 5.5e-3 : 4.2e-3) / static_cast<double>((p.M + t.rows() - 1) / t.rows());
+  const double row_blocks = static_cast<double>((p.M + t.rows() - 1) / t.rows());
+  const double hbm = kTileBBytes / t.ctas * (t.ctas == 2 && p.M <= kBM ? 5.5e-3 : 4.2e-3) / row_blocks;
   if (!p.a_mn && hbm > kb_cost) kb_cost = hbm;
   const double out = kBM * t.halves * kBN * (partial(p, splits) || p.kind != kOutBf16 ? 4 : 2) * 4.2e-3;
   return kb_cost * kb_of(p) / splits + out + (t.halves == 2 ? 200 : 120);
@@ -868,7 +871,8 @@ static Product down_product(int64_t N, int d, int F, const void* A, const void* 
 }
 static int ffn_down(int64_t N, int d, int F, const void* A, const void* Wd, void* Y, int64_t ldy, void* part,
                     uint32_t* status, cudaStream_t s) {
-  if (N <= kFewRows) return ffn_few<kFewDown, PS_ACT_SILU, false>(N, d, F, A, F, Wd, Wd, Y, ldy, {nullptr, nullptr, nullptr, kept_parts(N, F)}, status, s);
+  const FewKept kept = {nullptr, nullptr, nullptr, kept_parts(N, F)};
+  if (N <= kFewRows) return ffn_few<kFewDown, PS_ACT_SILU, false>(N, d, F, A, F, Wd, Wd, Y, ldy, kept, status, s);
   const Product p = down_product(N, d, F, A, Wd, Y, ldy);
   return run_group(&p, 1, part, status, s);
 }

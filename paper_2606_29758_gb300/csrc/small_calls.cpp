@@ -81,8 +81,8 @@ PyObject* dropout_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int64_t step, base, site;
     if (d > INT32_MAX || !rows(a[0], N, d, type, rx) || !whole(a[1], N, at::kInt, &traj) || !whole(a[2], N, at::kInt, &pos) ||
         (a[5] != Py_None && !rows(a[5], N, d, type, rr)) || (a[7] != Py_None && !rows(a[7], N, d, type, ry)) ||
-        !PyLong_Check(a[3]) || !integer(a[4], step) || !integer(a[6], base) || !integer(a[9], site) || site != static_cast<int>(site) ||
-        step < 0 || !PyFloat_Check(a[8]))
+        !PyLong_Check(a[3]) || !integer(a[4], step) || !integer(a[6], base) || !integer(a[9], site) ||
+        site != static_cast<int>(site) || step < 0 || !PyFloat_Check(a[8]))
       return ordinary();
     const uint64_t seed = PyLong_AsUnsignedLongLongMask(a[3]);
     PyObject* y = a[7];
