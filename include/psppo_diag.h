@@ -39,6 +39,14 @@ int ps_diag_choose_splitk(int64_t M, int64_t N, int num_kb, int narrow_too, int 
                           int* ranks, int* halves);
 
 /*
+ * Bytes of partial tiles that the feed-forward block's grouped products write into the workspace behind its header, as they
+ * are cut for a call of these sizes: Y of ps_gated_ffn_fwd (products 0), or those of ps_gated_ffn_bwd whose outputs are asked
+ * for (1: dX, 2: dWg and dWu, 4: dWd, added up). f32: the outputs' type. The workspace sizes that psppo.h's functions give
+ * hold them for any fewer rows too. Host only.
+ */
+size_t ps_diag_gated_ffn_partial_bytes(int64_t N, int d, int F, int products, int f32);
+
+/*
  * Launch one CTA that waits on a shared-memory barrier that nothing ever completes,
  * using the same bounded wait as the GEMM pipeline. After about timeout_ns
  * (<= 10 s) the wait gives up and sets PS_DEV_TIMEOUT in the workspace status word;

@@ -34,7 +34,8 @@ EXPORTS = [
     "ps_lmhead_ppo_fwd_from_stats_workspace_size", "ps_lmhead_ppo_fwd_from_stats", "ps_lmhead_ppo_bwd_vocab_shard",
     "ps_lmhead_logit_store_size", "ps_lmhead_ppo_fwd_store", "ps_lmhead_ppo_bwd_from_store_workspace_size",
     "ps_lmhead_ppo_bwd_from_store", "ps_lmhead_logit_stats_store", "ps_lmhead_ppo_bwd_vocab_shard_from_store",
-    "ps_diag_gemm_bf16", "ps_diag_choose_splitk", "ps_diag_wait_timeout", "ps_lmhead_ppo_fwd_noalloc",
+    "ps_diag_gemm_bf16", "ps_diag_choose_splitk", "ps_diag_gated_ffn_partial_bytes", "ps_diag_wait_timeout",
+    "ps_lmhead_ppo_fwd_noalloc",
     "ps_lmhead_score_proxy_workspace_size", "ps_lmhead_score_proxy",
     "ps_design_cutoffs_workspace_size", "ps_design_cutoffs",
     "ps_reward_uncertainty_workspace_size", "ps_reward_uncertainty", "ps_binarize_rewards",
@@ -104,6 +105,7 @@ _SIGS = {
     "ps_diag_gemm_bf16": (_i32, [_i32, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _vp, _sz,
                                  _vp]),
     "ps_diag_choose_splitk": (_i32, [_i64, _i64, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp]),
+    "ps_diag_gated_ffn_partial_bytes": (_sz, [_i64, _i32, _i32, _i32, _i32]),
     "ps_diag_wait_timeout": (_i32, [_u64, _vp, _sz, _vp]),
     "ps_lmhead_score_proxy_workspace_size": (_sz, [_i64, _i32, _i32, _i32, _i32]),
     "ps_lmhead_score_proxy": (_i32, [_i64, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _sz,
@@ -483,6 +485,11 @@ def ps_diag_choose_splitk(M, N, num_kb, narrow_too, sms, at_once):
                                      ctypes.byref(halves))
     _check(rc, "ps_diag_choose_splitk")
     return ranks.value, halves.value
+
+
+def ps_diag_gated_ffn_partial_bytes(N, d, F, products, f32) -> int:
+    """Bytes of partial tiles of the feed-forward block's grouped products (0: Y; 1: dX, 2: dWg and dWu, 4: dWd)."""
+    return lib().ps_diag_gated_ffn_partial_bytes(N, d, F, products, int(f32))
 
 
 def ps_diag_wait_timeout(timeout_ns, ws, stream=None):

@@ -19,6 +19,7 @@
 
 #include "internal.h"
 #include "ps_nvtx.h"
+#include "psppo_diag.h"
 #include "umma_group.cuh"
 #include "umma_host.cuh"
 
@@ -774,15 +775,18 @@ static GroupPlan plan_group(const Product* p, int count) {
 }
 
 // Bytes that hold the partial tiles of these products or of any some of them, and of as many with fewer rows: a share has
-// at least kLeastKb k blocks, and there are at most two tiles of at most 256 x 256 per SM (or 512 x 256 per pair).
+// at least kLeastKb k blocks, and a K loop is cut only into shares of at most two tiles of at most 256 x 256 per SM (or
+// 512 x 256 per pair); outputs in two parts (fold) have a plane of every tile also where nothing is cut.
 static size_t part_bytes(const Product* p, int count) {
   size_t sum = 0;
   for (int t = 0; t < count; ++t) {
     const size_t shares = static_cast<size_t>(kb_of(p[t])) / kLeastKb + 1;
     if (shares < 2 && !p[t].fold) continue;
-    const size_t all = shares * ((p[t].M + 4 * kBM - 1) / (4 * kBM) * (4 * kBM)) * p[t].N * 4;
+    const size_t plane = static_cast<size_t>((p[t].M + 4 * kBM - 1) / (4 * kBM) * (4 * kBM)) * p[t].N * 4;
     const size_t most = static_cast<size_t>(2 * kPlanSms) * 2 * kBM * kBN * 4;
-    sum += ((all < most ? all : most) + 255) / 256 * 256;
+    size_t bytes = shares * plane < most ? shares * plane : most;
+    if (p[t].fold && plane > bytes) bytes = plane;
+    sum += (bytes + 255) / 256 * 256;
   }
   return sum;
 }
@@ -804,9 +808,8 @@ static int launch_group(const GroupArgs& g, uint32_t* status, cudaStream_t s) {
   return PS_ERR_CUDA;
 }
 
-// The products p[0 .. count), cut as plan_group says, partial tiles at `part`.
-static int run_group(const Product* p, int count, void* part, uint32_t* status, cudaStream_t s) {
-  const GroupPlan plan = plan_group(p, count);
+// The products p[0 .. count), cut as `plan` (plan_group's of them) says, its partial tiles at `part`.
+static int run_group(const GroupPlan& plan, const Product* p, int count, void* part, uint32_t* status, cudaStream_t s) {
   GroupArgs g;
   SumArgs sums;
   sums.count = 0;
@@ -869,12 +872,13 @@ static int run_group(const Product* p, int count, void* part, uint32_t* status, 
 static Product down_product(int64_t N, int d, int F, const void* A, const void* Wd, void* Y, int64_t ldy) {
   return {N, d, F, false, false, false, A, nullptr, Wd, nullptr, F, F, Y, ldy, kOutBf16};
 }
-static int ffn_down(int64_t N, int d, int F, const void* A, const void* Wd, void* Y, int64_t ldy, void* part,
-                    uint32_t* status, cudaStream_t s) {
+// rows that go by the grouped kernel: as `plan` cuts down_product()
+static int ffn_down(int64_t N, int d, int F, const void* A, const void* Wd, void* Y, int64_t ldy, const GroupPlan& plan,
+                    void* part, uint32_t* status, cudaStream_t s) {
   const FewKept kept = {nullptr, nullptr, nullptr, kept_parts(N, F)};
   if (N <= kFewRows) return ffn_few<kFewDown, PS_ACT_SILU, false>(N, d, F, A, F, Wd, Wd, Y, ldy, kept, status, s);
   const Product p = down_product(N, d, F, A, Wd, Y, ldy);
-  return run_group(&p, 1, part, status, s);
+  return run_group(plan, &p, 1, part, status, s);
 }
 static size_t down_part_bytes(int64_t N, int d, int F) {
   const Product p = down_product(N, d, F, nullptr, nullptr, nullptr, d);
@@ -945,9 +949,17 @@ int ps_gated_ffn_fwd(int64_t N, int d, int F, int dtype, int act, const void* X,
   uint32_t* status = static_cast<uint32_t*>(ws);
   FfnStore f = ffn_store(store, N, F);
   uint8_t* scratch = static_cast<uint8_t*>(ws) + kWsHeader;
+  size_t left = ws_bytes - kWsHeader;
   if (!store) {
     f.A = reinterpret_cast<uint16_t*>(scratch);
     scratch += plane_bytes(N * kept_parts(N, F), F);
+    left -= plane_bytes(N * kept_parts(N, F), F);
+  }
+  GroupPlan plan = {};
+  if (N > kFewRows) {
+    const Product p = down_product(N, d, F, f.A, Wd, Y, ldy);
+    plan = plan_group(&p, 1);
+    if (plan.bytes > left) return refused(PS_ERR_WORKSPACE, ws, s);   // (the size function and the plan are two formulas)
   }
   if (act == PS_ACT_SILU)
     rc = store ? ffn_up<PS_ACT_SILU, true>(N, d, F, X, ldx, Wg, Wu, f, status, s)
@@ -956,7 +968,7 @@ int ps_gated_ffn_fwd(int64_t N, int d, int F, int dtype, int act, const void* X,
     rc = store ? ffn_up<PS_ACT_GELU, true>(N, d, F, X, ldx, Wg, Wu, f, status, s)
                : ffn_up<PS_ACT_GELU, false>(N, d, F, X, ldx, Wg, Wu, f, status, s);
   if (rc != PS_OK) return refused(rc, ws, s);
-  return ffn_down(N, d, F, f.A, Wd, Y, ldy, scratch, status, s);
+  return ffn_down(N, d, F, f.A, Wd, Y, ldy, plan, scratch, status, s);
 }
 
 size_t ps_gated_ffn_bwd_workspace_size(int64_t N, int d, int F) {
@@ -970,6 +982,23 @@ size_t ps_gated_ffn_bwd_workspace_size(int64_t N, int d, int F) {
   };
   const size_t all = parts(N), few = parts(N < kPartsRows ? N : kPartsRows);   // (any fewer rows too)
   return kWsHeader + (all > few ? all : few);
+}
+
+size_t ps_diag_gated_ffn_partial_bytes(int64_t N, int d, int F, int products, int f32) {
+  if (!sizes_ok(N, d, F) || !sizes_fit(N, d, F) || N == 0 || products < 0 || products > 7) return 0;
+  void* some = reinterpret_cast<void*>(16);   // (not read)
+  Product p[kGroupMost];
+  int n = 1;
+  if (products == 0) {
+    if (N <= kFewRows) return 0;
+    p[0] = down_product(N, d, F, nullptr, nullptr, nullptr, d);
+  } else {
+    void *dX = products & 1 ? some : nullptr, *dWgu = products & 2 ? some : nullptr, *dWd = products & 4 ? some : nullptr;
+    const int kind = f32 ? kOutF32 : kOutBf16;
+    n = grad_products(p, N, d, F, ffn_store(nullptr, N, F), nullptr, d, nullptr, d, nullptr, nullptr, dX, d, kind, dWgu, dWgu,
+                      dWd, kind);
+  }
+  return plan_group(p, n).bytes;
 }
 
 int ps_gated_ffn_bwd(int64_t N, int d, int F, int dtype, const void* dY, int64_t lddy, const void* X, int64_t ldx,
@@ -1006,13 +1035,16 @@ int ps_gated_ffn_bwd(int64_t N, int d, int F, int dtype, const void* dY, int64_t
     return PS_OK;
   }
   const FfnStore f = ffn_store(store, N, F);
-  rc = ffn_da(N, d, F, dY, lddy, Wd, f, status, s);
-  if (rc != PS_OK) return refused(rc, ws, s);
   auto kind = [](int dtype, int acc) { return dtype == PS_DTYPE_BF16 ? kOutBf16 : acc ? kOutF32Add : kOutF32; };
   Product p[kGroupMost];
   const int n = grad_products(p, N, d, F, f, dY, lddy, X, ldx, Wg, Wu, dX, lddx, kind(dx_dtype, dx_acc), dWg, dWu, dWd,
                               kind(dw_dtype, dw_acc));
-  return n == 0 ? PS_OK : run_group(p, n, static_cast<uint8_t*>(ws) + kWsHeader, status, s);
+  GroupPlan plan = {};
+  if (n > 0) plan = plan_group(p, n);
+  if (plan.bytes > ws_bytes - kWsHeader) return refused(PS_ERR_WORKSPACE, ws, s);   // (before the store is consumed)
+  rc = ffn_da(N, d, F, dY, lddy, Wd, f, status, s);
+  if (rc != PS_OK) return refused(rc, ws, s);
+  return n == 0 ? PS_OK : run_group(plan, p, n, static_cast<uint8_t*>(ws) + kWsHeader, status, s);
 }
 
 }  // extern "C"
