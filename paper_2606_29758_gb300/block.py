@@ -17,36 +17,48 @@ from . import _binding as B
 
 # the current stream's raw handle; the tensors that a call was given are on the device already, so torch is set up
 _raw_stream, _device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
-_stream = (lambda: _raw_stream(_device())) if _raw_stream and _device else B._stream
+_device = _device or torch.cuda.current_device
+_stream = (lambda: _raw_stream(_device())) if _raw_stream else B._stream
 
 _CODE = {torch.bfloat16: B.PS_DTYPE_BF16, torch.float32: B.PS_DTYPE_F32}
 
 
 # The checks of a call's ordinary way, before a pointer is taken: one comparison of what a right call has, and the reason after
-# it fails. (Calls in order go by B.calls(), which compares the same on the tensors themselves.)
-def _pitch(name: str, t: torch.Tensor, n: int, cols: int, dtype: torch.dtype) -> int:
+# it fails. (Calls in order go by B.calls(), which compares the same on the tensors themselves.) `at`: the device that the
+# call's buffers, and so its launches, are on.
+def _pitch(name: str, t: torch.Tensor, n: int, cols: int, dtype: torch.dtype, at: torch.device) -> int:
     """The row pitch of a tensor of n rows of cols elements that lie side by side."""
     st = t.stride()
-    if t.shape != (n, cols) or t.dtype is not dtype or not t.is_cuda or (st[1] != 1 and cols > 1 and n > 0):
+    if t.shape != (n, cols) or t.dtype is not dtype or not t.is_cuda or t.device != at or (st[1] != 1 and cols > 1 and n > 0):
         if t.dim() != 2 or t.shape != (n, cols):
             raise ValueError(f"{name}: need [{n}][{cols}], got {tuple(t.shape)}")
-        if t.dtype is not dtype:
-            raise TypeError(f"{name}: need {dtype}, got {t.dtype}")
-        if not t.is_cuda:
-            raise ValueError(f"{name}: not on a GPU ({t.device})")
+        _placed(name, t, dtype, at)
         raise ValueError(f"{name}: the elements of a row must lie side by side (stride {st[1]})")
     return st[0] if n > 1 else cols      # (a single row's stride says nothing)
 
 
-def _whole(name: str, t: torch.Tensor, shape, dtype: torch.dtype) -> int:
+def _whole(name: str, t: torch.Tensor, shape, dtype: torch.dtype, at: torch.device) -> int:
     """The address of a contiguous tensor."""
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-        if t.dtype is not dtype:
-            raise TypeError(f"{name}: need {dtype}, got {t.dtype}")
-        if not t.is_cuda:
-            raise ValueError(f"{name}: not on a GPU ({t.device})")
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or t.device != at or not t.is_contiguous():
+        _placed(name, t, dtype, at)
         raise ValueError(f"{name}: need a contiguous {tuple(shape)}, got {tuple(t.shape)}, strides {t.stride()}")
     return t.data_ptr()
+
+
+def _placed(name: str, t: torch.Tensor, dtype: torch.dtype, at: torch.device):
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: need {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: not on a GPU ({t.device})")
+    if t.device != at:
+        raise ValueError(f"{name}: on {t.device}, the call's other buffers are on {at}")
+
+
+def _launched_on(at: torch.device):
+    """The current stream, which has to be one of the call's device."""
+    if _device() != at.index:
+        raise ValueError(f"the call's buffers are on {at}, the current device is cuda:{_device()}")
+    return _stream()
 
 
 def _row_count(name: str, t: torch.Tensor, most: int) -> int:
@@ -57,6 +69,10 @@ def _row_count(name: str, t: torch.Tensor, most: int) -> int:
 
 def _first(t: torch.Tensor, n: int) -> torch.Tensor:
     return t if t.shape[0] == n else t[:n]
+
+
+def _index(at: torch.device) -> int:
+    return -1 if at.index is None else at.index
 
 
 def _status(what: str, ws):
@@ -87,6 +103,7 @@ class GatedFFN:
         bf16 = dict(dtype=torch.bfloat16, device=device)
         u8 = dict(dtype=torch.uint8, device=device)   # zeroed: a status word never written reads clear
         self.Y = torch.empty(s.rows, s.d, **bf16)
+        self._at = self.Y.device
         self.ws_fwd = torch.zeros(B.ps_gated_ffn_fwd_workspace_size(s.rows, s.d, s.F, s.train), **u8)
         self._fwd_tail = (None, 0, self.ws_fwd.data_ptr(), self.ws_fwd.numel())
         self.store = self.ws_bwd = None
@@ -110,12 +127,12 @@ class GatedFFN:
         grads = (self.dX, self.dWg, self.dWu, self.dWd) if s.train else [None] * 4
         self._plan = calls.ffn_plan(s.rows, s.d, s.F, s.act, *(self._bwd_tail[4], self._bwd_tail[8]) if s.train else (0, 0),
                                     *map(at, (self.Y, self.store, self.ws_fwd, self.ws_bwd, *grads)),
-                                    *map(size, (self.store, self.ws_fwd, self.ws_bwd)))
+                                    *map(size, (self.store, self.ws_fwd, self.ws_bwd)), _index(self._at))
 
     def _inputs(self, X, Wg, Wu, Wd):
-        N, t = X.shape[0], torch.bfloat16
-        return (X.data_ptr(), _pitch("X", X, N, self.s.d, t), _whole("Wg", Wg, self._w1, t),
-                _whole("Wu", Wu, self._w1, t), _whole("Wd", Wd, self._w2, t))
+        N, t, at = X.shape[0], torch.bfloat16, self._at
+        return (X.data_ptr(), _pitch("X", X, N, self.s.d, t, at), _whole("Wg", Wg, self._w1, t, at),
+                _whole("Wu", Wu, self._w1, t, at), _whole("Wd", Wd, self._w2, t, at))
 
     def forward(self, X, Wg, Wu, Wd, out=None):
         """Y [N][d] (in `out` if given)."""
@@ -126,7 +143,8 @@ class GatedFFN:
         if rc is None:
             inputs = self._inputs(X, Wg, Wu, Wd)
             rc = self._fwd(N, s.d, s.F, B.PS_DTYPE_BF16, s.act, *inputs, Y.data_ptr(),
-                           s.d if out is None else _pitch("out", out, N, s.d, torch.bfloat16), *self._fwd_tail, _stream())
+                           s.d if out is None else _pitch("out", out, N, s.d, torch.bfloat16, self._at), *self._fwd_tail,
+                           _launched_on(self._at))
         self.stored = N if s.train and rc == B.PS_OK else -1
         if rc:
             B._check(rc, "ps_gated_ffn_fwd")
@@ -143,8 +161,9 @@ class GatedFFN:
         rc = self._fast_bwd(self._plan, dY, X, Wg, Wu, Wd, dw_accumulate)
         if rc is None:
             inputs = self._inputs(X, Wg, Wu, Wd)
-            rc = self._bwd(N, s.d, s.F, B.PS_DTYPE_BF16, dY.data_ptr(), _pitch("dY", dY, N, s.d, torch.bfloat16), *inputs,
-                           *self._bwd_tail, B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._bwd_ws, _stream())
+            rc = self._bwd(N, s.d, s.F, B.PS_DTYPE_BF16, dY.data_ptr(), _pitch("dY", dY, N, s.d, torch.bfloat16, self._at),
+                           *inputs, *self._bwd_tail, B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._bwd_ws,
+                           _launched_on(self._at))
         self.stored = -1
         if rc:
             B._check(rc, "ps_gated_ffn_bwd")
@@ -187,7 +206,7 @@ class QKNormRope:
         if s.R > 0:
             if table is None or table.dim() != 3:
                 raise ValueError("a table [T][R/2][2] is needed (rope_table)")
-            _whole("table", table, (table.shape[0], s.R // 2, 2), torch.float32)
+            _whole("table", table, (table.shape[0], s.R // 2, 2), torch.float32, torch.empty(0, device=device).device)
         self.s, self.table, self.device = s, table if s.R > 0 else None, device
         L = B.lib()
         self._fwd, self._bwd = L.ps_qk_norm_rope_fwd, L.ps_qk_norm_rope_bwd
@@ -197,6 +216,7 @@ class QKNormRope:
         self._wq, self._wk = s.Hq * s.D, s.Hk * s.D
         t = dict(dtype=s.dtype, device=device)
         self.q, self.k = torch.empty(s.rows, self._wq, **t), torch.empty(s.rows, self._wk, **t)
+        self._at = self.q.device
         size = B.ps_qk_norm_rope_workspace_size(s.D) if s.train else 256
         self.ws = torch.zeros(max(size, 256), dtype=torch.uint8, device=device)
         self._ws = (self.ws.data_ptr(), self.ws.numel())
@@ -210,14 +230,14 @@ class QKNormRope:
         self._fast_fwd, self._fast_bwd = calls.qk_fwd, calls.qk_bwd
         grads = [t.data_ptr() for t in (self.dq, self.dk, self.dgq, self.dgk)] if s.train else [0] * 4
         self._plan = calls.qk_plan(s.rows, *self._head, self._table[0], s.eps, self._table[1] or 0, self.q.data_ptr(),
-                                   self.k.data_ptr(), *self._ws, *grads)
+                                   self.k.data_ptr(), *self._ws, *grads, _index(self._at))
 
     def _inputs(self, N, q, k, gq, gk, pos, pos_base):
         s = self.s
-        t, gain = s.dtype, (s.D,)
-        return (q.data_ptr(), _pitch("q", q, N, self._wq, t), k.data_ptr(), _pitch("k", k, N, self._wk, t),
-                None if gq is None else _whole("gq", gq, gain, t), None if gk is None else _whole("gk", gk, gain, t),
-                s.eps, _whole("pos", pos, (N,), torch.int32) if s.R > 0 else None, pos_base, *self._table)
+        t, gain, at = s.dtype, (s.D,), self._at
+        return (q.data_ptr(), _pitch("q", q, N, self._wq, t, at), k.data_ptr(), _pitch("k", k, N, self._wk, t, at),
+                None if gq is None else _whole("gq", gq, gain, t, at), None if gk is None else _whole("gk", gk, gain, t, at),
+                s.eps, _whole("pos", pos, (N,), torch.int32, at) if s.R > 0 else None, pos_base, *self._table)
 
     def forward(self, q, k, gq, gk, pos, pos_base: int = 1, in_place: bool = False):
         """(q, k) normed and rotated; in_place writes over the inputs (serving: no backward follows)."""
@@ -225,7 +245,8 @@ class QKNormRope:
         N = _row_count("q", q, self.s.rows)
         if rc is None:
             inputs = self._inputs(N, q, k, gq, gk, pos, pos_base)
-            rc = self._fwd(N, *self._head, *inputs, *(inputs[:4] if in_place else self._out), *self._ws, _stream())
+            rc = self._fwd(N, *self._head, *inputs, *(inputs[:4] if in_place else self._out), *self._ws,
+                           _launched_on(self._at))
         if rc:
             B._check(rc, "ps_qk_norm_rope_fwd")
         return (q, k) if in_place else (_first(self.q, N), _first(self.k, N))
@@ -238,10 +259,10 @@ class QKNormRope:
         if rc is None:
             if not s.train:
                 raise RuntimeError("built without a backward (train=False)")
-            rc = self._bwd(N, *self._head, dq_out.data_ptr(), _pitch("dq_out", dq_out, N, self._wq, s.dtype),
-                           dk_out.data_ptr(), _pitch("dk_out", dk_out, N, self._wk, s.dtype),
+            rc = self._bwd(N, *self._head, dq_out.data_ptr(), _pitch("dq_out", dq_out, N, self._wq, s.dtype, self._at),
+                           dk_out.data_ptr(), _pitch("dk_out", dk_out, N, self._wk, s.dtype, self._at),
                            *self._inputs(N, q, k, gq, gk, pos, pos_base), *self._grads,
-                           B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._ws, _stream())
+                           B.PS_DW_ACCUMULATE if dw_accumulate else 0, *self._ws, _launched_on(self._at))
         if rc:
             B._check(rc, "ps_qk_norm_rope_bwd")
         return _first(self.dq, N), _first(self.dk, N), self.dgq, self.dgk
@@ -266,14 +287,15 @@ class RowDropout:
                 B._check(y, "ps_dropout_rows")
             return y
         N, d = x.shape
-        t = x.dtype
-        pitch = _pitch("x", x, N, d, t)
+        t, at = x.dtype, x.device
+        pitch = _pitch("x", x, N, d, t, at)
         y = torch.empty_like(x) if out is None else out
         rc = self._call(N, d, _CODE[t] if t in _CODE else B.dtype_code(x), x.data_ptr(), pitch,
-                        None if res is None else res.data_ptr(), 0 if res is None else _pitch("res", res, N, d, t), _whole("row_traj", row_traj, (N,), torch.int32),
-                        _whole("row_pos", row_pos, (N,), torch.int32), traj_base, self.p, seed & (2**64 - 1),
-                        step & (2**64 - 1), self.site, y.data_ptr(), d if out is None else _pitch("out", out, N, d, t),
-                        _stream())
+                        None if res is None else res.data_ptr(), 0 if res is None else _pitch("res", res, N, d, t, at),
+                        _whole("row_traj", row_traj, (N,), torch.int32, at),
+                        _whole("row_pos", row_pos, (N,), torch.int32, at), traj_base, self.p, seed & (2**64 - 1),
+                        step & (2**64 - 1), self.site, y.data_ptr(), d if out is None else _pitch("out", out, N, d, t, at),
+                        _launched_on(at))
         B._check(rc, "ps_dropout_rows")
         return y
 

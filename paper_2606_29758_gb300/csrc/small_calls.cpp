@@ -6,6 +6,7 @@
 #include <Python.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -23,19 +24,21 @@ decltype(&ps_gated_ffn_bwd) ffn_bwd_fn = nullptr;
 
 ps_stream_t stream() { return reinterpret_cast<ps_stream_t>(c10::cuda::getCurrentCUDAStream().stream()); }
 
-const at::Tensor* tensor(PyObject* o) {
+// `device`: the one that the call launches on, the current one; a plan's buffers are on it, and so has every tensor to be.
+const at::Tensor* tensor(PyObject* o, int device) {
   if (!THPVariable_Check(o)) return nullptr;
   const at::Tensor& t = THPVariable_Unpack(o);
-  return t.defined() && t.layout() == at::kStrided && t.is_cuda() ? &t : nullptr;
+  return t.defined() && t.layout() == at::kStrided && t.is_cuda() && t.get_device() == device ? &t : nullptr;
 }
+int current_device() { return static_cast<int>(c10::cuda::current_device()); }
 
 struct Rows {
   void* at = nullptr;
   int64_t ld = 0;
 };
 // N rows of cols elements that lie side by side.
-bool rows(PyObject* o, int64_t N, int64_t cols, at::ScalarType type, Rows& r) {
-  const at::Tensor* t = tensor(o);
+bool rows(PyObject* o, int device, int64_t N, int64_t cols, at::ScalarType type, Rows& r) {
+  const at::Tensor* t = tensor(o, device);
   if (!t || t->dim() != 2 || t->size(0) != N || t->size(1) != cols || t->scalar_type() != type) return false;
   if (t->stride(1) != 1 && cols > 1 && N > 0) return false;
   r.at = t->data_ptr();
@@ -43,8 +46,8 @@ bool rows(PyObject* o, int64_t N, int64_t cols, at::ScalarType type, Rows& r) {
   return true;
 }
 // n contiguous elements.
-bool whole(PyObject* o, int64_t n, at::ScalarType type, const void** at) {
-  const at::Tensor* t = tensor(o);
+bool whole(PyObject* o, int device, int64_t n, at::ScalarType type, const void** at) {
+  const at::Tensor* t = tensor(o, device);
   if (!t || t->dim() != 1 || t->size(0) != n || t->scalar_type() != type || !t->is_contiguous()) return false;
   *at = t->data_ptr();
   return true;
@@ -71,7 +74,9 @@ PyObject* guarded(F&& f) {   // (no C++ exception passes into the interpreter)
 // (x, row_traj, row_pos, seed, step, res or None, traj_base, out or None, p, site) -> output, status or None
 PyObject* dropout_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    const at::Tensor* x = n == 10 ? tensor(a[0]) : nullptr;
+    if (n != 10 || !THPVariable_Check(a[0])) return ordinary();
+    const int dev = current_device();
+    const at::Tensor* x = tensor(a[0], dev);
     if (!x || x->dim() != 2) return ordinary();
     const at::ScalarType type = x->scalar_type();
     if (type != at::kBFloat16 && type != at::kFloat) return ordinary();
@@ -79,8 +84,9 @@ PyObject* dropout_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Rows rx, rr, ry;
     const void *traj, *pos;
     int64_t step, base, site;
-    if (d > INT32_MAX || !rows(a[0], N, d, type, rx) || !whole(a[1], N, at::kInt, &traj) || !whole(a[2], N, at::kInt, &pos) ||
-        (a[5] != Py_None && !rows(a[5], N, d, type, rr)) || (a[7] != Py_None && !rows(a[7], N, d, type, ry)) ||
+    if (d > INT32_MAX || !rows(a[0], dev, N, d, type, rx) || !whole(a[1], dev, N, at::kInt, &traj) ||
+        !whole(a[2], dev, N, at::kInt, &pos) || (a[5] != Py_None && !rows(a[5], dev, N, d, type, rr)) ||
+        (a[7] != Py_None && !rows(a[7], dev, N, d, type, ry)) ||
         !PyLong_Check(a[3]) || !integer(a[4], step) || !integer(a[6], base) || !integer(a[9], site) ||
         site != static_cast<int>(site) || step < 0 || !PyFloat_Check(a[8]))
       return ordinary();
@@ -105,7 +111,8 @@ PyObject* dropout_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// A plan in a capsule: what stays the same over a holder's calls (the holder keeps the buffers).
+// A plan in a capsule: what stays the same over a holder's calls (the holder keeps the buffers). device: theirs; a plan made
+// without one takes no call.
 template <class P>
 PyObject* capsule(const P& p) {
   P* own = new (std::nothrow) P(p);
@@ -114,9 +121,11 @@ PyObject* capsule(const P& p) {
   if (!c) delete own;
   return c;
 }
+// The plan of a call that launches on its device.
 template <class P>
 const P* plan_of(PyObject* o) {
-  return static_cast<const P*>(PyCapsule_GetPointer(o, P::kName));
+  const P* p = static_cast<const P*>(PyCapsule_GetPointer(o, P::kName));
+  return p && p->device >= 0 && p->device == current_device() ? p : nullptr;
 }
 
 struct QkPlan {
@@ -128,6 +137,7 @@ struct QkPlan {
   void *q, *k, *ws, *dq, *dk;
   float *dgq, *dgk;
   size_t ws_bytes;
+  int device = -1;
   at::ScalarType type() const { return dtype == PS_DTYPE_F32 ? at::kFloat : at::kBFloat16; }
   int64_t wq() const { return static_cast<int64_t>(Hq) * D; }
   int64_t wk() const { return static_cast<int64_t>(Hk) * D; }
@@ -137,8 +147,8 @@ PyObject* qk_plan(PyObject*, PyObject* args) {
   QkPlan p;
   unsigned long long ptr[8], ws_bytes;
   long long rows_;
-  if (!PyArg_ParseTuple(args, "LiiiiiiidKKKKKKKKK", &rows_, &p.Hq, &p.Hk, &p.D, &p.R, &p.dtype, &p.layout, &p.T, &p.eps, &ptr[0],
-                        &ptr[1], &ptr[2], &ptr[3], &ws_bytes, &ptr[4], &ptr[5], &ptr[6], &ptr[7]))
+  if (!PyArg_ParseTuple(args, "LiiiiiiidKKKKKKKKK|i", &rows_, &p.Hq, &p.Hk, &p.D, &p.R, &p.dtype, &p.layout, &p.T, &p.eps,
+                        &ptr[0], &ptr[1], &ptr[2], &ptr[3], &ws_bytes, &ptr[4], &ptr[5], &ptr[6], &ptr[7], &p.device))
     return nullptr;
   p.rows = rows_;
   p.ws_bytes = static_cast<size_t>(ws_bytes);
@@ -161,12 +171,15 @@ struct QkIn {
   int64_t base;
 };
 bool qk_inputs(const QkPlan& p, PyObject* const* a, QkIn& in) {
-  const at::Tensor* q = tensor(a[0]);
+  const int dev = p.device;
+  const at::Tensor* q = tensor(a[0], dev);
   if (!q || q->dim() != 2) return false;
   in.N = q->size(0);
-  return in.N <= p.rows && rows(a[0], in.N, p.wq(), p.type(), in.q) && rows(a[1], in.N, p.wk(), p.type(), in.k) &&
-         (a[2] == Py_None || whole(a[2], p.D, p.type(), &in.gq)) && (a[3] == Py_None || whole(a[3], p.D, p.type(), &in.gk)) &&
-         (p.R == 0 || whole(a[4], in.N, at::kInt, &in.pos)) && integer(a[5], in.base) && in.base == static_cast<int>(in.base);
+  return in.N <= p.rows && rows(a[0], dev, in.N, p.wq(), p.type(), in.q) && rows(a[1], dev, in.N, p.wk(), p.type(), in.k) &&
+         (a[2] == Py_None || whole(a[2], dev, p.D, p.type(), &in.gq)) &&
+         (a[3] == Py_None || whole(a[3], dev, p.D, p.type(), &in.gk)) &&
+         (p.R == 0 || whole(a[4], dev, in.N, at::kInt, &in.pos)) && integer(a[5], in.base) &&
+         in.base == static_cast<int>(in.base);
 }
 
 // (plan, q, k, gq, gk, pos, pos_base, in_place) -> status or None
@@ -189,8 +202,8 @@ PyObject* qk_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const QkPlan* p = n == 10 ? plan_of<QkPlan>(a[0]) : nullptr;
     QkIn in;
     Rows dq, dk;
-    if (!p || !p->dgq || !qk_inputs(*p, a + 3, in) || !rows(a[1], in.N, p->wq(), p->type(), dq) ||
-        !rows(a[2], in.N, p->wk(), p->type(), dk) || !PyBool_Check(a[9]))
+    if (!p || !p->dgq || !qk_inputs(*p, a + 3, in) || !rows(a[1], p->device, in.N, p->wq(), p->type(), dq) ||
+        !rows(a[2], p->device, in.N, p->wk(), p->type(), dk) || !PyBool_Check(a[9]))
       return ordinary();
     return PyLong_FromLong(qk_bwd_fn(in.N, p->Hq, p->Hk, p->D, p->R, p->dtype, p->layout, dq.at, dq.ld, dk.at, dk.ld, in.q.at, in.q.ld,
                                      in.k.at, in.k.ld, in.gq, in.gk, p->eps, static_cast<const int32_t*>(in.pos),
@@ -205,14 +218,15 @@ struct FfnPlan {
   int d, F, act, dx_dtype, dw_dtype;
   void *Y, *store, *ws_fwd, *ws_bwd, *dX, *dWg, *dWu, *dWd;
   size_t store_bytes, ws_fwd_bytes, ws_bwd_bytes;
+  int device = -1;
 };
 
 PyObject* ffn_plan(PyObject*, PyObject* args) {
   FfnPlan p;
   unsigned long long v[11];
   long long rows_;
-  if (!PyArg_ParseTuple(args, "LiiiiiKKKKKKKKKKK", &rows_, &p.d, &p.F, &p.act, &p.dx_dtype, &p.dw_dtype, &v[0], &v[1], &v[2], &v[3],
-                        &v[4], &v[5], &v[6], &v[7], &v[8], &v[9], &v[10]))
+  if (!PyArg_ParseTuple(args, "LiiiiiKKKKKKKKKKK|i", &rows_, &p.d, &p.F, &p.act, &p.dx_dtype, &p.dw_dtype, &v[0], &v[1], &v[2],
+                        &v[3], &v[4], &v[5], &v[6], &v[7], &v[8], &v[9], &v[10], &p.device))
     return nullptr;
   p.rows = rows_;
   void** const to[8] = {&p.Y, &p.store, &p.ws_fwd, &p.ws_bwd, &p.dX, &p.dWg, &p.dWu, &p.dWd};
@@ -230,12 +244,12 @@ struct FfnIn {
   const void* w[3];
 };
 bool ffn_inputs(const FfnPlan& p, PyObject* const* a, FfnIn& in) {
-  const at::Tensor* X = tensor(a[0]);
+  const at::Tensor* X = tensor(a[0], p.device);
   if (!X || X->dim() != 2) return false;
   in.N = X->size(0);
-  if (in.N > p.rows || !rows(a[0], in.N, p.d, at::kBFloat16, in.X)) return false;
+  if (in.N > p.rows || !rows(a[0], p.device, in.N, p.d, at::kBFloat16, in.X)) return false;
   for (int i = 0; i < 3; ++i) {
-    const at::Tensor* w = tensor(a[1 + i]);
+    const at::Tensor* w = tensor(a[1 + i], p.device);
     if (!w || w->dim() != 2 || w->size(0) != (i < 2 ? p.F : p.d) || w->size(1) != (i < 2 ? p.d : p.F) ||
         w->scalar_type() != at::kBFloat16 || !w->is_contiguous())
       return false;
@@ -254,7 +268,7 @@ PyObject* ffn_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (a[5] == Py_None) {
       Y.at = p->Y;
       Y.ld = p->d;
-    } else if (!rows(a[5], in.N, p->d, at::kBFloat16, Y)) {
+    } else if (!rows(a[5], p->device, in.N, p->d, at::kBFloat16, Y)) {
       return ordinary();
     }
     return PyLong_FromLong(ffn_fwd_fn(in.N, p->d, p->F, PS_DTYPE_BF16, p->act, in.X.at, in.X.ld, in.w[0], in.w[1], in.w[2], Y.at,
@@ -268,7 +282,8 @@ PyObject* ffn_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const FfnPlan* p = n == 7 ? plan_of<FfnPlan>(a[0]) : nullptr;
     FfnIn in;
     Rows dY;
-    if (!p || !p->store || !ffn_inputs(*p, a + 2, in) || !rows(a[1], in.N, p->d, at::kBFloat16, dY) || !PyBool_Check(a[6]))
+    if (!p || !p->store || !ffn_inputs(*p, a + 2, in) || !rows(a[1], p->device, in.N, p->d, at::kBFloat16, dY) ||
+        !PyBool_Check(a[6]))
       return ordinary();
     return PyLong_FromLong(ffn_bwd_fn(in.N, p->d, p->F, PS_DTYPE_BF16, dY.at, dY.ld, in.X.at, in.X.ld, in.w[0], in.w[1], in.w[2],
                                       p->store, p->store_bytes, p->dX, p->d, p->dx_dtype, p->dWg, p->dWu, p->dWd, p->dw_dtype,
