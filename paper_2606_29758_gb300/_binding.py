@@ -8,6 +8,8 @@ no fallback, and importing this module without the built library raises.
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import threading
 import os
 from typing import Optional
@@ -158,11 +160,13 @@ def calls():
     """The module of the block operators' small calls (csrc/small_calls.cpp), bound to the library."""
     global _calls
     if _calls is None:
-        L = lib()
-        try:
-            from . import _calls as module
-        except ImportError as e:
-            raise ImportError("_calls.so is not built or not for this torch; run __graft_entry__.build()") from e
+        from . import _build
+        L, path = lib(), _build.calls_path()
+        if not os.path.exists(path):
+            raise ImportError(f"the module of small calls is not built for this torch ({path}); run __graft_entry__.build()")
+        loader = importlib.machinery.ExtensionFileLoader(__package__ + "._calls", path)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader(loader.name, loader))
+        loader.exec_module(module)
         module.bind(*(ctypes.cast(f, _vp).value for f in (L.ps_dropout_rows, L.ps_qk_norm_rope_fwd, L.ps_qk_norm_rope_bwd,
                                                           L.ps_gated_ffn_fwd, L.ps_gated_ffn_bwd)))
         _calls = module

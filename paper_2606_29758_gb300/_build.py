@@ -1,9 +1,10 @@
-"""Build libpsppo.so (nvcc, sm_103a only) and _calls.so (the host compiler) in place.
+"""Build libpsppo.so (nvcc, sm_103a only) and the module of small calls (the host compiler) in place.
 
 Each translation unit compiles in parallel; the objects link into
 paper_2606_29758_gb300/libpsppo.so with the CUDA runtime linked statically, so the
-library needs only the driver at run time. _calls.so is a Python module over torch's
-headers that makes the block operators' small calls; nothing in libpsppo.so depends on it.
+library needs only the driver at run time. The other is a Python module over torch's headers
+that makes the block operators' small calls; nothing in libpsppo.so depends on it. Its file's
+name says which torch and which Python it was compiled for.
 No cmake, no torch extension machinery.
 """
 from __future__ import annotations
@@ -21,7 +22,6 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libpsppo.so")
-CALLS = os.path.join(PKG, "_calls.so")
 SOURCES = ["psppo_api.cu", "lmhead_bf16.cu", "lmhead_f32.cu", "fwd_static_scratch.cu", "design.cu", "ffn.cu", "block_ops.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
@@ -47,12 +47,20 @@ def _compile(src: str, verbose_ptxas: bool) -> str:
     return obj
 
 
+def calls_path() -> str:
+    """The module of small calls for the running torch and Python."""
+    import torch
+    return os.path.join(PKG, f"_calls-{torch.__version__}-{(torch.version.git_version or '')[:12]}-"
+                             f"{sysconfig.get_config_var('SOABI')}.so")
+
+
 def _build_calls() -> None:
     import torch
+    out = calls_path()
     base = os.path.dirname(torch.__file__)
     dirs = [INCLUDE, os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"),
             sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(nvcc())), "include")]
-    tmp = CALLS + f".tmp{os.getpid()}"
+    tmp = out + f".tmp{os.getpid()}"
     cmd = [shutil.which("g++") or "c++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-I{d}" for d in dirs),
            os.path.join(CSRC, "small_calls.cpp"), "-o", tmp, "-L" + os.path.join(base, "lib"),
@@ -60,13 +68,13 @@ def _build_calls() -> None:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"{cmd[0]} failed for small_calls.cpp:\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, CALLS)
+    os.replace(tmp, out)
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(CALLS):
+    if not os.path.exists(LIB) or not os.path.exists(calls_path()):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
+    t = min(os.path.getmtime(LIB), os.path.getmtime(calls_path()))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + \
         [os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE)] + [os.path.abspath(__file__)]
     return any(os.path.getmtime(p) > t for p in deps)
