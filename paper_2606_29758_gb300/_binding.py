@@ -156,14 +156,21 @@ def lib() -> ctypes.CDLL:
 _calls = None
 
 
+class _Ordinary:
+    """In the place of the module of small calls: every call is left to the holder's ordinary way, through ctypes."""
+    qk_plan = ffn_plan = dropout_rows = qk_fwd = qk_bwd = ffn_fwd = ffn_bwd = staticmethod(lambda *a: None)
+
+
 def calls():
-    """The module of the block operators' small calls (csrc/small_calls.cpp), bound to the library."""
+    """The module of the block operators' small calls (csrc/small_calls.cpp), bound to the library; without it (see
+    _build.build) what leaves them to the ordinary way."""
     global _calls
     if _calls is None:
         from . import _build
         L, path = lib(), _build.calls_path()
         if not os.path.exists(path):
-            raise ImportError(f"the module of small calls is not built for this torch ({path}); run __graft_entry__.build()")
+            _calls = _Ordinary
+            return _calls
         loader = importlib.machinery.ExtensionFileLoader(__package__ + "._calls", path)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader(loader.name, loader))
         loader.exec_module(module)
