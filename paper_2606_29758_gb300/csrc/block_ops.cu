@@ -155,8 +155,9 @@ static __device__ __forceinline__ void store_pairs(T* lo, T* hi, const F2 (&a)[4
 // the row and their gains for the side; the arithmetic is on pairs of f32 (two to an instruction). The heads come through a
 // ring in shared memory of the warp's own, filled by its lanes' copies some steps ahead. us forward / backward, before from
 // bulk copies (bf16, from 4 steps a row on) or registers a step ahead: bf16, 106k rows of 28 + 4 heads of 128 270 / 421 (6.4 and
-// 6.2 TB/s; 282 / 452); 20k of 40 + 8 of 256 160 / 232 (182 / 237); 100k of 6 + 2 of 96 91 / 143 (100 / 153), of 64 57 / 86 (68 /
-// 103); 4000 of 28 + 4 18 / 31; f32, 50k of 28 + 4 253 / 366 (259 / 380), 100k of 6 + 2 of 64 78 / 124 (93 / 146).
+// 6.2 TB/s; 282 / 452); 20k of 40 + 8 of 256, half of it rotated, 169 / 240 (182 / 237); 100k of 6 + 2 of 96, half rotated, 96 / 148
+// (100 / 153), of 64 57 / 86 (68 / 103); 4000 of 28 + 4 18 / 31; f32, 50k of 28 + 4 253 / 366 (259 / 380), 100k of 6 + 2 of 64
+// 78 / 124 (93 / 146).
 constexpr int kQkThreads = 128;
 constexpr int kQkWarps = kQkThreads / 32;
 template <class T, bool BWD>
@@ -212,7 +213,10 @@ static __device__ __forceinline__ float group_sum(float v, int G) {
   return v;
 }
 
-template <class T, bool EVEN, bool BWD>
+// ALL: every dim is rotated (R = D). Else the lanes of the others take their values as they are: by a cosine of 1 and a sine of
+// 0 an infinity would reach the value beside it as 0 inf. (The selects cost 3-5% of many bf16 rows, 28 + 4 heads of 128, 64 of
+// them rotated, 106k rows: 283 / 448 us instead of 270 / 432; a branch of the lanes 9% and every call.)
+template <class T, bool EVEN, bool BWD, bool ALL>
 __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD>::kBlocks)) qk_kernel(const QkArgs a) {
   using Cfg = QkCfg<T, BWD>;
   constexpr int ST = Cfg::kStages;
@@ -407,8 +411,9 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD>::kBlocks)) qk_kerne
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const F2 na = mul2(mul2(xa[j], r2), ga[j]), nb = mul2(mul2(xb[j], r2), gb[j]);
-          ya[j] = fma2(minus2, mul2(nb, sn[j]), mul2(na, cs[j]));
-          yb[j] = fma2(na, sn[j], mul2(nb, cs[j]));
+          const F2 ta = fma2(minus2, mul2(nb, sn[j]), mul2(na, cs[j])), tb = fma2(na, sn[j], mul2(nb, cs[j]));
+          ya[j] = ALL || rotated ? ta : na;
+          yb[j] = ALL || rotated ? tb : nb;
         }
       } else {
         // With n = x r: dg += dn n, dx = r (g dn - n mean(g dn n)). bf16: the two sums over the head go side by side, the
@@ -424,7 +429,8 @@ __global__ void __launch_bounds__(kQkThreads, (QkCfg<T, BWD>::kBlocks)) qk_kerne
         F2 r2 = pair2(r, r), dot = zero2;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const F2 da = fma2(yb[j], sn[j], mul2(ya[j], cs[j])), db = fma2(minus2, mul2(ya[j], sn[j]), mul2(yb[j], cs[j]));
+          const F2 ta = fma2(yb[j], sn[j], mul2(ya[j], cs[j])), tb = fma2(minus2, mul2(ya[j], sn[j]), mul2(yb[j], cs[j]));
+          const F2 da = ALL || rotated ? ta : ya[j], db = ALL || rotated ? tb : yb[j];
           if (kBoth) {
             ya[j] = da;
             yb[j] = db;
@@ -750,7 +756,7 @@ static bool qk_sizes_ok(int64_t N, int Hq, int Hk, int D, int R, int dtype, int 
   return (dtype == PS_DTYPE_BF16 || dtype == PS_DTYPE_F32) && (layout == PS_ROPE_HALF || layout == PS_ROPE_EVEN);
 }
 
-template <class T, bool BWD>
+template <class T, bool BWD, bool ALL>
 static int launch_qk(const QkArgs& a, int layout, cudaStream_t s) {
   using Cfg = QkCfg<T, BWD>;
   // resident blocks take their units in turn
@@ -760,7 +766,7 @@ static int launch_qk(const QkArgs& a, int layout, cudaStream_t s) {
   if (most > kQkMaxBlocks) most = kQkMaxBlocks;
   const unsigned grid = static_cast<unsigned>(want < most ? want : most);
   const size_t smem = kQkWarps * Cfg::kWarp + 2 * sizeof(float) * a.D;
-  auto kern = layout == PS_ROPE_EVEN ? qk_kernel<T, true, BWD> : qk_kernel<T, false, BWD>;
+  auto kern = layout == PS_ROPE_EVEN ? qk_kernel<T, true, BWD, ALL> : qk_kernel<T, false, BWD, ALL>;
   if (smem > 32 * 1024 &&
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
     return refused(PS_ERR_CUDA, a.status, s);
@@ -778,7 +784,9 @@ static int run_qk(QkArgs a, int dtype, int layout, cudaStream_t s) {
   a.G = lanes_for(a.D / 16);
   const int at_once = 32 / a.G;
   a.parts = parts_for(a.N, static_cast<int64_t>(num_sms_current()) * 2 * kQkWarps, (a.Hq + a.Hk + at_once - 1) / at_once);
-  return dtype == PS_DTYPE_F32 ? launch_qk<float, BWD>(a, layout, s) : launch_qk<Bf16, BWD>(a, layout, s);
+  if (a.R == a.D)
+    return dtype == PS_DTYPE_F32 ? launch_qk<float, BWD, true>(a, layout, s) : launch_qk<Bf16, BWD, true>(a, layout, s);
+  return dtype == PS_DTYPE_F32 ? launch_qk<float, BWD, false>(a, layout, s) : launch_qk<Bf16, BWD, false>(a, layout, s);
 }
 
 }  // namespace psk
