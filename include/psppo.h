@@ -456,8 +456,12 @@ int ps_lmhead_ppo_fwd_noalloc(int64_t N, int d, int V, int dtype, const void* Hp
  *   dWu = dU^T X, dWd = dY^T A.
  * X, Y, dY [N][d] bf16, Wg, Wu [F][d] and Wd [d][F] bf16, contiguous (the halves of one
  * [2F][d] buffer will do); f32 accumulation. A, dG and dU are rounded to bf16 between the
- * products; up to 64 rows with F <= 2048 they are kept in two bf16 parts, the second what the first
- * one's rounding left. PS_DTYPE_F32 returns PS_ERR_UNSUPPORTED.
+ * products, 2^-8 of a value at most; up to 64 rows with F <= 2048 they are kept in two bf16 parts,
+ * the second what the first one's rounding left (2^-17). So the last bits of a row's outputs depend
+ * on how many rows its call has: a row of a narrow block differs by up to that rounding between a
+ * call of 64 rows and one of 65. (With two parts an infinite X, dY or weight may also give NaN where
+ * one part gives an infinity: the parts' products with it need not have one sign.)
+ * PS_DTYPE_F32 returns PS_ERR_UNSUPPORTED.
  * store: NULL (no backward follows; A lies in the workspace), or ps_gated_ffn_store_size(N, F)
  *   bytes, 16-byte aligned, that the forward fills and the backward of the same N, F, X and
  *   weights consumes: A [N][F] bf16, then, each from the next 256-byte boundary, P = U s'(G)

@@ -467,11 +467,13 @@ struct FfnStore {
 };
 static size_t plane_bytes(int64_t N, int F) { return (static_cast<size_t>(N) * F * 2 + 255) / 256 * 256; }
 // Few rows of a narrow block have A, dG and dU in two parts, each of N rows: the bf16 values, and in bf16 what their
-// rounding left, which the products that read them add up. Over few values the errors do not average out: with one part
-// an output was up to 1.8 times as far off as its own rounding alone leaves it (d = 100, F = 300; 1.55 at 300, 1000; from
-// d = 1000, F = 3000 on 1.41, the two roundings' mean). One part / two, forward and backward, us: 8 rows, d = 304,
-// F = 1000 24.7 / 25.5; 16, 600, 2000 30.4 / 31.7; 64, 304, 1000 34 / 37; beyond, where it would give little: 32, 1000,
-// 4000 37.8 / 41.8; 1, 3584, 16384 206 / 237.
+// rounding left, which the products that read them add up. An element's error from one part is the same for any N and d
+// (2^-8 of a term at most, over K = F terms of Y, 2 F of dX and N of dW); but outputs over few values do not average it
+// out: in 2-norm they were up to 1.8 times as far off as their own rounding alone leaves them (d = 100, F = 300; 1.55 at 300,
+// 1000; from d = 1000, F = 3000 on 1.41, the two roundings' mean). The rule's edges are what it costs: calls this small are
+// launches rather than products. One part / two, forward and backward, us: 8 rows, d = 304, F = 1000 24.7 / 25.5; 16, 600, 2000
+// 30.4 / 31.7; 64, 304, 1000 34 / 37; beyond: 32, 1000, 4000 37.8 / 41.8; 1, 3584, 16384 206 / 237. From 65 rows on the general
+// kernels have no second plane to write.
 constexpr int kPartsRows = 64, kPartsF = 2048;
 static int kept_parts(int64_t N, int F) { return N <= kPartsRows && F <= kPartsF ? 2 : 1; }
 static FfnStore ffn_store(void* base, int64_t N, int F) {
