@@ -555,9 +555,12 @@ static int ffn_few(int64_t N, int C, int64_t K, const void* X, int64_t ldx, cons
 }
 
 // Whether gate and up of these rows go by the kernel for few rows: always up to 64; from there to 128 unless the general
-// kernel's CTA pairs come in one round that is enough to stream the weights, or the weights are small. Measured at 128 rows,
-// us few / pairs (both products, nothing kept): d = 3584, F = 16384 71 / 77; 2048, 3000 23 / 28; 1536, 8192 32 / 30; 3000, 9000
-// 55 / 50; 768, 2048 17.9 / 17.6 (kept: 21 / 19).
+// kernel's CTA pairs come in one round that is enough to stream the weights, or the weights are small. Both products, nothing
+// kept, us few / pairs at 65, 96 and 128 rows: d = 3584, F = 16384 68 / 75, 70 / 76, 72 / 78; 3584, 4096 22 / 32, 24 / 33, 27 / 35; 2048,
+// 6144 22 / 25, 24 / 26, 27 / 28; 2048, 3000 18 / 23, 19 / 24, 21 / 25; 512, 16384 25 / 31, 26 / 31, 27 / 29; 3000, 9000 45 / 43, 49 / 44,
+// 52 / 48; 1536, 8192 22.6 / 24.2, 24.4 / 25.1, 27.2 / 26.1; 1000, 3000 17.4 / 18.7, 18.8 / 19.8, 21.2 / 21.5; 768, 2048 14.9 / 15.5,
+// 16.3 / 16.1, 18.4 / 16.9; 392, 1048 15.2 / 15.1, 16.8 / 16.1, 19.2 / 17.5 (kept: 23 / 19 at 128). Where the rule takes the slower one
+// it is by 10% at most (1000, 3000 at 65 rows, kept: 18.4 / 20.2).
 static bool few_up(int64_t N, int d, int F) {
   const int tiles = (F + 127) / 128;
   return N <= 64 || (N <= kFewRows && (tiles > kPlanSms / 2 || (tiles < kPlanSms / 3 && d >= 1024)));
@@ -566,8 +569,6 @@ static bool few_up(int64_t N, int d, int F) {
 template <int ACT, bool KEEP>
 static int ffn_up(int64_t N, int d, int F, const void* X, int64_t ldx, const void* Wg, const void* Wu,
                   const FfnStore& f, uint32_t* status, cudaStream_t s) {
-  using Epi = FfnUpEpi<ACT, KEEP, 2>;
-  using PairEpi = FfnUpEpi<ACT, KEEP, 4>;
   const FewKept kept = {f.P, f.Q, f.scale, kept_parts(N, F)};
   if (few_up(N, d, F)) return ffn_few<kFewUp, ACT, KEEP>(N, F, d, X, ldx, Wg, Wu, f.A, F, kept, status, s);
   TwoMaps m;

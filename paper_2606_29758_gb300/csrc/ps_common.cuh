@@ -42,13 +42,13 @@ __device__ __forceinline__ uint32_t smem_addr(const void* p) {
 // The kernels of one library call after its first are launched programmatically (launch_after): their CTAs may be set
 // up while the kernel before them drains, and wait here, before they read or write anything of the call's, until it
 // has completed and its writes are visible. (In a kernel launched plainly the wait returns at once.) A call's first
-// kernel is launched plainly, so nothing before the call is overlapped (two operators differ, see below). Passes of the Tiny workload take 80 instead of
-// 90 us, of a small bf16 head 87 instead of 95; with the kernels also letting the next one's CTAs in from their start
-// (griddepcontrol.launch_dependents), 82 and 89, and the 8k-row 7B-shaped step was 3% slower. The feed-forward block's
-// kernels, whose CTAs fill an SM, do let the next one's in once they have waited themselves, and its calls' first kernels
-// are launched programmatically and wait before anything else: forward and backward of 571 rows at d = 392, F = 1048 43.4
-// instead of 47.9 us, 1000, 1000, 3000 85.7 instead of 90.7, 6030, 1536, 8192 838 instead of 857. So do row dropout's (the
-// q/k norms', whose gain sum would take slots early, do not: 4000 rows, both ways, 48 and 53 us).
+// kernel is launched plainly, so nothing before the call is overlapped (two operators differ, see below). Passes of the
+// Tiny workload take 80 instead of 90 us, of a small bf16 head 87 instead of 95; with the kernels also letting the next one's
+// CTAs in from their start (griddepcontrol.launch_dependents), 82 and 89, and the 8k-row 7B-shaped step was 3% slower. The
+// feed-forward block's kernels, whose CTAs fill an SM, do let the next one's in once they have waited themselves, and its
+// calls' first kernels are launched programmatically and wait before anything else: forward and backward of 571 rows at d =
+// 392, F = 1048 43.4 instead of 47.9 us, 1000, 1000, 3000 85.7 instead of 90.7, 6030, 1536, 8192 838 instead of 857. So do row
+// dropout's (the q/k norms', whose gain sum would take slots early, do not: 4000 rows, both ways, 48 and 53 us).
 __device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // The next kernel's CTAs may be set up from here on, where this one leaves SMs or drains (they wait as above).
 __device__ __forceinline__ void let_next_kernel_in() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

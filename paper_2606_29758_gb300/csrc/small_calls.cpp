@@ -1,6 +1,6 @@
 // Calls of the block operators from Python without the interpreter's share: a token's rows take the GPU 3 us, and attribute
-// by attribute through Python and ctypes a call cost the host 8 to 13 (q/k norms 8.2 and 12.5, row dropout 12, now 2.8, 4.2
-// and 3.0). The checks are those of the holders (block.py), made on the tensors themselves. A call that is not exactly in
+// by attribute through Python and ctypes a call cost the host 8 to 13 (q/k norms 8.2 and 12.5, row dropout 12, now 2.9, 4.5
+// and 3.1). The checks are those of the holders (block.py), made on the tensors themselves. A call that is not exactly in
 // order returns None: the holder then goes its ordinary way, which says what is wrong. Otherwise the library's status
 // comes back, or the output.
 #include <Python.h>
