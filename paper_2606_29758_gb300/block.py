@@ -4,6 +4,7 @@ GatedFFN, QKNormRope and RowDropout run the library's calls of the same names on
 rows are those of a packed batch (UpdatePass.pack: src_row, row_traj, row_pos, cu_seqlens), so they carry the
 head's dH into the policy's body and prepare its rows for the head. Each call takes the first N = x.shape[0] rows
 of the buffers it was built for; the tensors it returns are views of those buffers, overwritten by its next call.
+Every tensor of a call is on the current device, where the holder's buffers are.
 """
 from __future__ import annotations
 
