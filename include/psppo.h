@@ -60,7 +60,8 @@ enum { PS_DW_OVERWRITE = 0, PS_DW_ACCUMULATE = 1, PS_DH_ACCUMULATE = 2 };
 enum {
   PS_DEV_BAD_PMF = 1, PS_DEV_BAD_LENGTH = 2, PS_DEV_CAPACITY = 4,
   PS_DEV_BAD_TOKEN = 8, PS_DEV_TIMEOUT = 16,
-  PS_DEV_NONFINITE = 32   /* ps_design_cutoffs: a timestep weight gamma_bar * u is NaN or infinite */
+  PS_DEV_NONFINITE = 32,  /* ps_design_cutoffs: a timestep weight gamma_bar * u is NaN or infinite */
+  PS_DEV_BAD_PAGE = 64    /* a page that a sequence needs is outside the cache */
 };
 
 /* Static string for a ps_status value. */
@@ -553,6 +554,77 @@ int ps_dropout_rows(int64_t N, int d, int dtype, const void* x, int64_t ldx, con
                     int64_t ldr, const int32_t* row_traj, const int32_t* row_pos,
                     int64_t traj_base, double p, uint64_t seed, uint64_t step, int site,
                     void* y, int64_t ldy, ps_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * ps_residual_norm_fwd / ps_residual_norm_bwd -- the norm after a branch, its gate, the scaled residual sum and the norm
+ * before the next branch, in one pass.
+ *
+ *   n = y r_y gy, r_y = (mean over the row of y^2 + eps)^(-1/2) with PS_NORM_BRANCH, else 1;
+ *   h = res_scale x + branch_scale gate_i n;  with PS_NORM_OUT o = h r_h go, r_h = (mean h^2 + eps)^(-1/2), taken from h
+ *   before it is rounded to the rows' type. y NULL: no branch, h = x whatever res_scale is (not written), o its norm.
+ *   Backward: dH = dh + r_h (go do - h r_h^2 mean(go do h)), dx = res_scale dH, dn = branch_scale gate_i dH,
+ *   dy = r_y (gy dn - y r_y^2 mean(gy dn y)) or gy dn, dgy = sum over rows of dn y r_y, dgo = sum of do h r_h,
+ *   dgate_i = branch_scale sum over columns of dH n.
+ * x, y, h, o [N][d], bf16 or f32, any pitch >= d and any alignment of whole elements (16-byte rows of whole blocks of 8
+ *   are fastest). gy, go [d] in the rows' type, NULL: 1; gy without PS_NORM_BRANCH scales the branch per column. gate
+ *   [N] f32 or NULL (1): a gate of 0 leaves the branch out whatever it holds (NaN and infinities too; dy is then 0).
+ *   norms: PS_NORM_BRANCH | PS_NORM_OUT; without a branch PS_NORM_OUT alone, without PS_NORM_OUT o and go are not used.
+ * Backward: dout the gradient of o (read with PS_NORM_OUT), dh that of h (NULL: 0), h the forward's h as it is held (x
+ *   where there was no branch; read with PS_NORM_OUT), y, gy, go and gate as the forward's. dx, dy in the rows' type
+ *   (dy not used without a branch); dgy, dgo [d] f32 or NULL (PS_DW_ACCUMULATE adds to them; summed in a fixed order,
+ *   reruns are bit-identical); dgate [N] f32 or NULL. N = 0 zeroes dgy and dgo.
+ * Outputs may be inputs (same pointer and pitch), else must not overlap them or each other.
+ * Workspace: none for the forward; 256 bytes for a backward without gain gradients, else
+ *   ps_residual_norm_workspace_size(d).
+ * Limits: 1 <= d, rows of at most 32768 bytes (16384 bf16 or 8192 f32 columns), finite scales, eps >= 0.
+ * ------------------------------------------------------------------------- */
+enum { PS_NORM_BRANCH = 1, PS_NORM_OUT = 2 };
+int ps_residual_norm_fwd(int64_t N, int d, int dtype, int norms, const void* x, int64_t ldx,
+                         const void* y, int64_t ldy, const void* gy, const void* go, const float* gate,
+                         double res_scale, double branch_scale, double eps, void* h, int64_t ldh,
+                         void* o, int64_t ldo, ps_stream_t stream);
+size_t ps_residual_norm_workspace_size(int d);
+int ps_residual_norm_bwd(int64_t N, int d, int dtype, int norms, const void* dout, int64_t lddo,
+                         const void* dh, int64_t lddh, const void* h, int64_t ldh, const void* y, int64_t ldy,
+                         const void* gy, const void* go, const float* gate, double res_scale,
+                         double branch_scale, double eps, void* dx, int64_t lddx, void* dy, int64_t lddy,
+                         float* dgy, float* dgo, float* dgate, int flags, void* ws, size_t ws_bytes,
+                         ps_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * A paged cache of keys and values (one layer's) in sampling, and attention of one new token a sequence over it.
+ *
+ * k_cache, v_cache [pages][Hk][page][D], bf16 or f32, contiguous; table [seqs][ldt] int32 names the pages of each sequence in
+ * order: position p (from 0) is slot p mod page of page table[seq][p / page]. Pages may serve several sequences (the
+ * completions of a prompt share its pages). page is a power of two up to 65536, ldt page < 2^31 - 64 page.
+ * ps_paged_append: row i of k and v [N][Hk D] (row pitches ldk, ldv of whole 16 bytes, so they may lie in one projection's
+ *   rows) is copied to position row_pos[i] - pos_base of sequence row_seq[i] (of ps_pack_prefixes' rows: row_traj and row_pos
+ *   with pos_base = 1). A row with row_seq = -1 is passed by. A sequence outside [0, seqs) or a position outside the
+ *   table sets PS_DEV_BAD_LENGTH, a page id outside [0, pages) PS_DEV_BAD_PAGE; such rows are not written. No two rows of
+ *   a call may go to one place (which of them stays is not defined), and no row to a page that another sequence still
+ *   reads. Workspace: 256 bytes.
+ * ps_paged_decode: for each sequence b and query head h, with the key head h / (Hq / Hk) and s_j = scale q.k_j over
+ *   the last `window` (0: all) of the positions below lengths[b], o = sum_j softmax(s)_j v_j and lse = log sum_j e^s_j. The
+ *   new token's own key and value are in the cache (ps_paged_append comes first). A length of 0 gives o = 0, lse =
+ *   -inf. q, o [seqs][Hq D] (pitches of whole 16 bytes), in the cache's type; o may be q (same pointer
+ *   and pitch); lse [seqs][Hq] f32 or NULL. Table entries behind a sequence's last page are not read, nor are
+ *   slots behind its length. A length outside [0, ldt page] sets PS_DEV_BAD_LENGTH, a page id outside
+ *   [0, pages) PS_DEV_BAD_PAGE; those sequences' outputs (the page's key heads') are NaN. Sums and weights are f32 (the
+ *   weights as operands of the tensor cores in two bf16 parts, 2^-17, so that an infinite value may give NaN where one
+ *   part would give an infinity); a fixed order, reruns are bit-identical; the
+ *   order depends on the lengths of all sequences of the call.
+ *   Workspace: ps_paged_decode_workspace_size(D).
+ * Limits: 16 <= D <= 256, a multiple of 16, Hk <= Hq <= 65536, a multiple, pages >= 1, 16-byte aligned pointers.
+ * ------------------------------------------------------------------------- */
+int ps_paged_append(int64_t N, int seqs, int Hk, int D, int dtype, const void* k, int64_t ldk,
+                    const void* v, int64_t ldv, const int32_t* row_seq, const int32_t* row_pos, int pos_base,
+                    const int32_t* table, int64_t ldt, int pages, int page, void* k_cache, void* v_cache,
+                    void* ws, size_t ws_bytes, ps_stream_t stream);
+size_t ps_paged_decode_workspace_size(int D);
+int ps_paged_decode(int seqs, int Hq, int Hk, int D, int dtype, const void* q, int64_t ldq,
+                    const void* k_cache, const void* v_cache, int pages, int page, const int32_t* table,
+                    int64_t ldt, const int32_t* lengths, int window, double scale, void* o, int64_t ldo,
+                    float* lse, void* ws, size_t ws_bytes, ps_stream_t stream);
 
 #ifdef __cplusplus
 }

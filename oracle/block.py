@@ -2,6 +2,8 @@
 
   ffn_*      G = X Wg^T, U = X Wu^T, A = s(G) U, Y = A Wd^T and the gradients of sum(Y * dY)
   qk_*       root-mean-square norms per head and rotary positions, forward and backward
+  norm_*     h = a x + b gate n(y), o = n(h) and the gradients of sum(h * dh) + sum(o * do)
+  attend     attention of one query per head over keys and values
   keep_mask  the kept elements of a dropout whose 16-bit uniforms come from Philox4x32-10
              (Salmon et al., SC'11)
 """
@@ -62,6 +64,53 @@ def qk_backward(dy, x, gain, eps, cos, sin, interleaved):
     dgain = np.sum(dn * x * r, axis=(0, 1))
     dn = dn * gain
     return r * (dn - x * r * r * np.mean(dn * x, axis=-1, keepdims=True)), dgain
+
+
+def _rms(x, eps):
+    return 1.0 / np.sqrt(np.mean(x * x, axis=-1, keepdims=True) + eps)
+
+
+def norm_forward(x, y, gy, go, gate, a, b, eps, post):
+    """h and o of rows x and, if y is not None, a branch y; gate [N] (0: the branch is left out)."""
+    h = x
+    if y is not None:
+        shut = gate == 0
+        n = np.where(shut[:, None], 0.0, y)
+        n = n * (_rms(n, eps) if post else 1.0) * gy
+        h = a * x + b * gate[:, None] * n
+    return h, h * _rms(h, eps) * go
+
+
+def norm_backward(do, dh, h, y, gy, go, gate, a, b, eps, post):
+    """dx, dy, dgy, dgo, dgate; do or dh may be 0 (a scalar), y None."""
+    r = _rms(h, eps)
+    g = go * do
+    dH = dh + r * (g - h * r * r * np.mean(g * h, axis=-1, keepdims=True))
+    dgo = np.sum(do * h * r, axis=0)
+    if y is None:
+        return dH, None, None, dgo, None
+    ry = _rms(y, eps) if post else np.ones((len(y), 1))
+    dgate = b * np.sum(dH * y * ry * gy, axis=-1)      # (of a shut gate too)
+    y = np.where((gate == 0)[:, None], 0.0, y)
+    ry = _rms(y, eps) if post else ry
+    dn = b * gate[:, None] * dH
+    dy = gy * dn
+    if post:
+        dy = ry * (dy - y * ry * ry * np.mean(dy * y, axis=-1, keepdims=True))
+    return a * dH, dy, np.sum(dn * y * ry, axis=0), dgo, dgate
+
+
+def attend(q, k, v, scale):
+    """q [Hq][D], k and v [n][Hk][D] -> o [Hq][D] and lse [Hq]; no keys: zeros and -inf."""
+    Hq, Hk = q.shape[0], k.shape[1]
+    if len(k) == 0:
+        return np.zeros_like(q), np.full(Hq, -np.inf)
+    of = np.arange(Hq) // (Hq // Hk)
+    s = scale * np.einsum("hd,jhd->hj", q, k[:, of])
+    top = s.max(axis=1, keepdims=True)
+    e = np.exp(s - top)
+    total = e.sum(axis=1, keepdims=True)
+    return np.einsum("hj,jhd->hd", e / total, v[:, of]), (top + np.log(total))[:, 0]
 
 
 def philox4x32_10(counter, key):

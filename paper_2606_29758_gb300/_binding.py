@@ -25,6 +25,7 @@ PS_ADV_CENTERED, PS_ADV_GROUP_NORM = 0, 1
 PS_DW_OVERWRITE, PS_DW_ACCUMULATE, PS_DH_ACCUMULATE = 0, 1, 2
 PS_DEV_BAD_PMF, PS_DEV_BAD_LENGTH, PS_DEV_CAPACITY, PS_DEV_BAD_TOKEN, PS_DEV_TIMEOUT, PS_DEV_NONFINITE = \
     1, 2, 4, 8, 16, 32
+PS_DEV_BAD_PAGE = 64
 
 EXPORTS = [
     "ps_status_string", "ps_version", "ps_workspace_status",
@@ -44,10 +45,13 @@ EXPORTS = [
     "ps_gated_ffn_store_size", "ps_gated_ffn_fwd_workspace_size", "ps_gated_ffn_fwd",
     "ps_gated_ffn_bwd_workspace_size", "ps_gated_ffn_bwd",
     "ps_rope_table", "ps_qk_norm_rope_workspace_size", "ps_qk_norm_rope_fwd", "ps_qk_norm_rope_bwd", "ps_dropout_rows",
+    "ps_residual_norm_fwd", "ps_residual_norm_workspace_size", "ps_residual_norm_bwd",
+    "ps_paged_append", "ps_paged_decode_workspace_size", "ps_paged_decode",
 ]
 PS_DESIGN_OPTIMIZED, PS_DESIGN_HEURISTIC, PS_DESIGN_UNIFORM, PS_DESIGN_TIME_PRIOR, PS_DESIGN_FIXED = range(5)
 PS_ACT_SILU, PS_ACT_GELU = 0, 1
 PS_ROPE_HALF, PS_ROPE_EVEN = 0, 1
+PS_NORM_BRANCH, PS_NORM_OUT = 1, 2
 
 
 __all__ = EXPORTS + [
@@ -58,6 +62,7 @@ __all__ = EXPORTS + [
     "PS_DW_ACCUMULATE", "PS_DH_ACCUMULATE", "PS_DEV_BAD_PMF", "PS_DEV_BAD_LENGTH", "PS_DEV_CAPACITY", "PS_DEV_BAD_TOKEN",
     "PS_DEV_TIMEOUT", "PS_DEV_NONFINITE", "PS_DESIGN_OPTIMIZED", "PS_DESIGN_HEURISTIC", "PS_DESIGN_UNIFORM",
     "PS_DESIGN_TIME_PRIOR", "PS_DESIGN_FIXED", "PS_ACT_SILU", "PS_ACT_GELU", "PS_ROPE_HALF", "PS_ROPE_EVEN",
+    "PS_NORM_BRANCH", "PS_NORM_OUT", "PS_DEV_BAD_PAGE",
 ]
 
 
@@ -135,6 +140,16 @@ _SIGS = {
                                    _vp]),
     "ps_dropout_rows": (_i32, [_i64, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _f64, _u64, _u64, _i32, _vp,
                                _i64, _vp]),
+    "ps_residual_norm_fwd": (_i32, [_i64, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _f64, _f64, _f64, _vp, _i64,
+                                    _vp, _i64, _vp]),
+    "ps_residual_norm_workspace_size": (_sz, [_i32]),
+    "ps_residual_norm_bwd": (_i32, [_i64, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _f64,
+                                    _f64, _f64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i32, _vp, _sz, _vp]),
+    "ps_paged_append": (_i32, [_i64, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _i32, _vp, _i64, _i32, _i32, _vp,
+                               _vp, _vp, _sz, _vp]),
+    "ps_paged_decode_workspace_size": (_sz, [_i32]),
+    "ps_paged_decode": (_i32, [_i32, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _i32, _i32, _vp, _i64, _vp, _i32, _f64, _vp,
+                               _i64, _vp, _vp, _sz, _vp]),
 }
 
 
@@ -480,6 +495,47 @@ def ps_dropout_rows(N, d, dtype, x, res, row_traj, row_pos, traj_base, p, seed, 
                                traj_base, float(p), seed & (2**64 - 1), step & (2**64 - 1), site, _ptr(y), _ld(y),
                                _stream(stream))
     _check(rc, "ps_dropout_rows")
+
+
+def ps_residual_norm_fwd(N, d, dtype, norms, x, y, gy, go, gate, res_scale, branch_scale, eps, h, o, stream=None):
+    """x, y, h and o: 2-D tensors whose row pitch is taken from the tensor."""
+    rc = lib().ps_residual_norm_fwd(N, d, dtype, norms, _ptr(x), _ld(x), _ptr(y), _ld(y), _ptr(gy), _ptr(go), _ptr(gate),
+                                    float(res_scale), float(branch_scale), float(eps), _ptr(h), _ld(h), _ptr(o), _ld(o),
+                                    _stream(stream))
+    _check(rc, "ps_residual_norm_fwd")
+
+
+def ps_residual_norm_workspace_size(d: int) -> int:
+    return lib().ps_residual_norm_workspace_size(d)
+
+
+def ps_residual_norm_bwd(N, d, dtype, norms, dout, dh, h, y, gy, go, gate, res_scale, branch_scale, eps, dx, dy, dgy, dgo,
+                         dgate, flags, ws, stream=None):
+    rc = lib().ps_residual_norm_bwd(N, d, dtype, norms, _ptr(dout), _ld(dout), _ptr(dh), _ld(dh), _ptr(h), _ld(h), _ptr(y),
+                                    _ld(y), _ptr(gy), _ptr(go), _ptr(gate), float(res_scale), float(branch_scale), float(eps),
+                                    _ptr(dx), _ld(dx), _ptr(dy), _ld(dy), _ptr(dgy), _ptr(dgo), _ptr(dgate), flags, _ptr(ws),
+                                    _nbytes(ws), _stream(stream))
+    _check(rc, "ps_residual_norm_bwd")
+
+
+def ps_paged_append(N, seqs, Hk, D, dtype, k, v, row_seq, row_pos, pos_base, table, pages, page, k_cache, v_cache, ws,
+                    stream=None):
+    rc = lib().ps_paged_append(N, seqs, Hk, D, dtype, _ptr(k), _ld(k), _ptr(v), _ld(v), _ptr(row_seq), _ptr(row_pos), pos_base,
+                               _ptr(table), table.stride(0) if table.shape[0] > 1 else table.shape[1], pages, page,
+                               _ptr(k_cache), _ptr(v_cache), _ptr(ws), _nbytes(ws), _stream(stream))
+    _check(rc, "ps_paged_append")
+
+
+def ps_paged_decode_workspace_size(D: int) -> int:
+    return lib().ps_paged_decode_workspace_size(D)
+
+
+def ps_paged_decode(seqs, Hq, Hk, D, dtype, q, k_cache, v_cache, pages, page, table, lengths, window, scale, o, lse, ws,
+                    stream=None):
+    rc = lib().ps_paged_decode(seqs, Hq, Hk, D, dtype, _ptr(q), _ld(q), _ptr(k_cache), _ptr(v_cache), pages, page, _ptr(table),
+                               table.stride(0) if table.shape[0] > 1 else table.shape[1], _ptr(lengths), window, float(scale),
+                               _ptr(o), _ld(o), _ptr(lse), _ptr(ws), _nbytes(ws), _stream(stream))
+    _check(rc, "ps_paged_decode")
 
 
 def ps_diag_gemm_bf16(M, N, K, a_mn_major, b_mn_major, A, lda, B, ldb, C, ldc, accumulate, ws, variant=0,

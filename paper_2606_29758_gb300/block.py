@@ -1,6 +1,6 @@
 """Row-wise operators of a policy block over packed rows, with buffers held in torch.
 
-GatedFFN, QKNormRope and RowDropout run the library's calls of the same names on the current stream. Their
+GatedFFN, QKNormRope, RowDropout and ResidualNorm run the library's calls of the same names on the current stream. Their
 rows are those of a packed batch (UpdatePass.pack: src_row, row_traj, row_pos, cu_seqlens), so they carry the
 head's dH into the policy's body and prepare its rows for the head. Each call takes the first N = x.shape[0] rows
 of the buffers it was built for; the tensors it returns are views of those buffers, overwritten by its next call.
@@ -307,3 +307,92 @@ class RowDropout:
     def backward(self, dy, row_traj, row_pos, seed: int, step: int, traj_base: int = 0, out=None):
         """The gradient of x (that of res is dy itself)."""
         return self._run(dy, row_traj, row_pos, seed, step, None, traj_base, out)
+
+
+@dataclass
+class NormShape:
+    rows: int
+    d: int
+    dtype: torch.dtype = torch.bfloat16
+    post: bool = True             # a norm of the branch before its gate (else its gain alone scales the branch's columns)
+    pre: bool = True              # the normed output (else the residual sum alone)
+    eps: float = 1e-6
+    res_scale: float = 1.0
+    branch_scale: float = 1.0
+    train: bool = True
+
+
+class ResidualNorm:
+    """h = res_scale x + branch_scale gate n(y) and o = n(h), the norms before and after a branch with its gate and the residual
+    sum in one pass, and the gradients (ps_residual_norm_fwd, ps_residual_norm_bwd). Rows may have any pitch."""
+
+    def __init__(self, shape: NormShape, device: str = "cuda"):
+        s = shape
+        self.s, self.device = s, device
+        L = B.lib()
+        self._fwd, self._bwd = L.ps_residual_norm_fwd, L.ps_residual_norm_bwd
+        t, f32 = dict(dtype=s.dtype, device=device), dict(dtype=torch.float32, device=device)
+        code = B.dtype_code(torch.empty(0, dtype=s.dtype))
+        self.h = torch.empty(s.rows, s.d, **t)
+        self.o = torch.empty(s.rows, s.d, **t) if s.pre else None
+        self._at = self.h.device
+        self._scales = (s.res_scale, s.branch_scale, s.eps)
+        out = B.PS_NORM_OUT if s.pre else 0
+        self._with, self._alone = (s.d, code, out | (B.PS_NORM_BRANCH if s.post else 0)), (s.d, code, out)
+        self.ws = None
+        if s.train:
+            self.dx, self.dy = torch.empty(s.rows, s.d, **t), torch.empty(s.rows, s.d, **t)
+            self.dgy, self.dgo = torch.empty(s.d, **f32), torch.empty(s.d, **f32)
+            self.dgate = torch.empty(s.rows, **f32)
+            self.ws = torch.zeros(B.ps_residual_norm_workspace_size(s.d), dtype=torch.uint8, device=device)
+
+    def _row(self, name, t, N):
+        """Address and pitch of rows; (None, 0) of none."""
+        return (None, 0) if t is None else (t.data_ptr(), _pitch(name, t, N, self.s.d, self.s.dtype, self._at))
+
+    def _gain(self, name, t):
+        return None if t is None else _whole(name, t, (self.s.d,), self.s.dtype, self._at)
+
+    def _gate(self, gate, N):
+        return None if gate is None else _whole("gate", gate, (N,), torch.float32, self._at)
+
+    def forward(self, x, y=None, gy=None, go=None, gate=None, out=None):
+        """(h, o), o None without the output's norm; h in `out` if given (it may be x or y). Without a branch h is x itself."""
+        s = self.s
+        N = _row_count("x", x, s.rows)
+        h = x if y is None else _first(self.h, N) if out is None else out
+        o = _first(self.o, N) if s.pre else None
+        if y is None and (gy is not None or gate is not None or out is not None):
+            raise ValueError("a branch's gain, its gate or a place for the sum without a branch")
+        rc = self._fwd(N, *(self._alone if y is None else self._with), *self._row("x", x, N), *self._row("y", y, N),
+                       self._gain("gy", gy), self._gain("go", go), self._gate(gate, N), *self._scales, *self._row("out", h, N),
+                       *((None, 0) if o is None else (o.data_ptr(), s.d)), _launched_on(self._at))
+        if rc:
+            B._check(rc, "ps_residual_norm_fwd")
+        return h, o
+
+    def backward(self, do, dh, h, y=None, gy=None, go=None, gate=None, dw_accumulate: bool = False):
+        """(dx, dy, dgy, dgo, dgate) from the gradients of o (None without the output's norm) and of h (None: 0), the forward's h
+        and the branch; what the forward did not have is None."""
+        s = self.s
+        if not s.train:
+            raise RuntimeError("built without a backward (train=False)")
+        if (do is None) == s.pre:
+            raise ValueError("do: the gradient of the normed output, given exactly where there is one")
+        if do is None and dh is None:
+            raise ValueError("neither output has a gradient")
+        if y is None and (gy is not None or gate is not None):
+            raise ValueError("a branch's gain or its gate without a branch")
+        N = _row_count("dh" if do is None else "do", dh if do is None else do, s.rows)
+        dx, dy = _first(self.dx, N), None if y is None else _first(self.dy, N)
+        dgy, dgo, dgate = (None if y is None else self.dgy), (self.dgo if s.pre else None), None
+        if gate is not None:
+            dgate = _first(self.dgate, N)
+        rc = self._bwd(N, *(self._alone if y is None else self._with), *self._row("do", do, N), *self._row("dh", dh, N),
+                       *self._row("h", h if s.pre else None, N), *self._row("y", y, N), self._gain("gy", gy), self._gain("go", go),
+                       self._gate(gate, N), *self._scales, dx.data_ptr(), s.d, *((None, 0) if dy is None else (dy.data_ptr(), s.d)),
+                       *(None if t is None else t.data_ptr() for t in (dgy, dgo, dgate)),
+                       B.PS_DW_ACCUMULATE if dw_accumulate else 0, self.ws.data_ptr(), self.ws.numel(), _launched_on(self._at))
+        if rc:
+            B._check(rc, "ps_residual_norm_bwd")
+        return dx, dy, dgy, dgo, dgate

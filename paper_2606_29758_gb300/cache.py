@@ -1,0 +1,182 @@
+"""Keys and values of a policy block in sampling, in pages, and the attention of a new token over them.
+
+PagedCache holds the pages of every layer, the table that says which pages a sequence has, and the sequences' lengths;
+DecodeAttention runs one new token a sequence over a layer of it. A step of sampling is, per layer: the new rows' q, k
+and v (QKNormRope in place), PagedCache.append, DecodeAttention.forward; and PagedCache.lengths counts the new tokens
+before the first layer's attention. All of that is ordered on the current stream and may be captured in a CUDA graph;
+reserve, share and release, which hand out pages, run between the steps.
+"""
+from __future__ import annotations
+
+from dataclasses import dataclass
+from typing import Optional
+
+import torch
+
+from . import _binding as B
+from .block import _first, _launched_on, _pitch, _row_count, _status, _whole
+
+
+@dataclass
+class CacheShape:
+    seqs: int                     # sequences (completions) at a time
+    pages: int                    # pages of a layer
+    page: int                     # positions a page, a power of two
+    Hk: int
+    D: int
+    max_len: int                  # longest sequence that the table can name
+    layers: int = 1
+    dtype: torch.dtype = torch.bfloat16
+
+
+class PagedCache:
+    """k and v [layers][pages][Hk][page][D], table [seqs][max_len / page] and lengths [seqs] on the device (ps_paged_append).
+
+    The table and the lengths may be written by the caller; or reserve() gives sequences pages, share() lets completions
+    have their prompt's pages without a copy, and release() takes a finished sequence's back."""
+
+    def __init__(self, shape: CacheShape, device: str = "cuda"):
+        s = shape
+        if s.page < 1 or s.page & (s.page - 1):
+            raise ValueError(f"page: a power of two, got {s.page}")
+        self.s, self.device = s, device
+        self.width = -(-s.max_len // s.page)
+        t, i32 = dict(dtype=s.dtype, device=device), dict(dtype=torch.int32, device=device)
+        self.k, self.v = (torch.empty(s.layers, s.pages, s.Hk, s.page, s.D, **t) for _ in range(2))
+        self.table = torch.full((s.seqs, self.width), -1, **i32)
+        self.lengths = torch.zeros(s.seqs, **i32)
+        self.ws = torch.zeros(256, dtype=torch.uint8, device=device)
+        self._at = self.k.device
+        self._layers = [(k.data_ptr(), v.data_ptr()) for k, v in zip(self.k, self.v)]
+        self._append = B.lib().ps_paged_append
+        self._code = B.dtype_code(self.k)
+        self._free = list(range(s.pages - 1, -1, -1))
+        self._users = [0] * s.pages          # sequences that have a page
+        self._own = [[] for _ in range(s.seqs)]
+
+    def _layer(self, layer: int):
+        if not 0 <= layer < self.s.layers:
+            raise IndexError(f"layer {layer} of {self.s.layers}")
+        return self._layers[layer]
+
+    def append(self, layer: int, k, v, row_seq, row_pos, pos_base: int = 1):
+        """Rows of k and v [N][Hk * D] to positions row_pos - pos_base of sequences row_seq (-1: the row is passed by)."""
+        s, at = self.s, self._at
+        if k.dim() != 2:
+            raise ValueError(f"k: need [N][{s.Hk * s.D}], got {tuple(k.shape)}")
+        N, w = k.shape[0], s.Hk * s.D
+        rc = self._append(N, s.seqs, s.Hk, s.D, self._code, k.data_ptr(), _pitch("k", k, N, w, s.dtype, at), v.data_ptr(),
+                          _pitch("v", v, N, w, s.dtype, at), _whole("row_seq", row_seq, (N,), torch.int32, at),
+                          _whole("row_pos", row_pos, (N,), torch.int32, at), pos_base, self.table.data_ptr(), self.width, s.pages,
+                          s.page, *self._layer(layer), self.ws.data_ptr(), self.ws.numel(), _launched_on(at))
+        if rc:
+            B._check(rc, "ps_paged_append")
+
+    # ------------------------------------------------------------------ pages
+    def _publish(self, seqs):
+        rows = torch.full((len(seqs), self.width), -1, dtype=torch.int32)
+        for i, b in enumerate(seqs):
+            rows[i, :len(self._own[b])] = torch.tensor(self._own[b], dtype=torch.int32)
+        self.table[torch.tensor(seqs, device=self.device)] = rows.to(self.device)
+
+    def reserve(self, seq: int, n: int):
+        """Pages for the first n positions of a sequence (those it has stay)."""
+        s = self.s
+        need = -(-n // s.page)
+        if need > self.width:
+            raise ValueError(f"{n} positions, built for {s.max_len}")
+        own = self._own[seq]
+        if need - len(own) > len(self._free):
+            raise B.PsppoError(B.PS_ERR_CAPACITY, f"PagedCache.reserve: {need - len(own)} pages wanted, {len(self._free)} free")
+        if need > len(own):
+            for _ in range(need - len(own)):
+                own.append(self._free.pop())
+                self._users[own[-1]] = 1
+            self._publish([seq])
+
+    def share(self, src: int, dst, n: int):
+        """The first n positions of `src` for the sequences `dst`, which have none: whole pages are shared, a begun one is copied."""
+        s, whole = self.s, n // self.s.page
+        dst = [int(b) for b in dst]
+        if any(self._own[b] for b in dst) or src in dst or len(set(dst)) != len(dst):
+            raise ValueError("share: the sequences must be different ones without pages")
+        if n > len(self._own[src]) * s.page:
+            raise ValueError(f"share: sequence {src} has pages for {len(self._own[src]) * s.page} positions, not {n}")
+        begun = n % s.page != 0
+        if begun and len(dst) > len(self._free):
+            raise B.PsppoError(B.PS_ERR_CAPACITY, f"PagedCache.share: {len(dst)} pages wanted, {len(self._free)} free")
+        for b in dst:
+            self._own[b] = self._own[src][:whole]
+            for p in self._own[b]:
+                self._users[p] += 1
+            if begun:
+                p = self._free.pop()
+                self._users[p] = 1
+                self._own[b].append(p)
+                for c in (self.k, self.v):
+                    c[:, p].copy_(c[:, self._own[src][whole]])
+        if dst:
+            self._publish(dst)
+
+    def release(self, seq: int):
+        """A sequence's pages back, except those that others still have; its length becomes 0."""
+        for p in reversed(self._own[seq]):
+            self._users[p] -= 1
+            if self._users[p] == 0:
+                self._free.append(p)
+        self._own[seq] = []
+        self._publish([seq])
+        self.lengths[seq] = 0
+
+    def check_status(self):
+        """Raise PsppoError if the last append reports a device-side error."""
+        _status("append", self.ws)
+
+
+@dataclass
+class DecodeShape:
+    seqs: int
+    Hq: int
+    Hk: int
+    D: int
+    dtype: torch.dtype = torch.bfloat16
+    window: int = 0               # a query sees the last `window` keys (0: all)
+    scale: Optional[float] = None  # D ** -0.5
+
+
+class DecodeAttention:
+    """Attention of one new token a sequence over a layer of a PagedCache (ps_paged_decode): row b of q is sequence b's, whose
+    length counts the new token. One holder serves all layers of a policy, one call after another."""
+
+    def __init__(self, shape: DecodeShape, device: str = "cuda"):
+        s = shape
+        self.s, self.device = s, device
+        self._call = B.lib().ps_paged_decode
+        self._scale = s.D ** -0.5 if s.scale is None else float(s.scale)
+        self.o = torch.empty(s.seqs, s.Hq * s.D, dtype=s.dtype, device=device)
+        self._at = self.o.device
+        self._code = B.dtype_code(self.o)
+        self.ws = torch.zeros(max(256, B.ps_paged_decode_workspace_size(s.D)), dtype=torch.uint8, device=device)
+
+    def forward(self, q, cache: PagedCache, layer: int = 0, out=None, lse=None):
+        """o [n][Hq * D] (in `out` if given; it may be q) of the first n = q.shape[0] sequences; lse f32 [n][Hq] is written if
+        given. A sequence of length 0 gives zeros."""
+        s, c, at = self.s, cache.s, self._at
+        if (c.Hk, c.D, c.dtype) != (s.Hk, s.D, s.dtype):
+            raise ValueError(f"the cache holds {c.Hk} heads of {c.D} in {c.dtype}, built for {s.Hk} of {s.D} in {s.dtype}")
+        if cache._at != at:
+            raise ValueError(f"the cache is on {cache._at}, the call's other buffers are on {at}")
+        n, w = _row_count("q", q, min(s.seqs, c.seqs)), s.Hq * s.D
+        o = _first(self.o, n) if out is None else out
+        rc = self._call(n, s.Hq, s.Hk, s.D, self._code, q.data_ptr(), _pitch("q", q, n, w, s.dtype, at), *cache._layer(layer),
+                        c.pages, c.page, cache.table.data_ptr(), cache.width, cache.lengths.data_ptr(), s.window, self._scale,
+                        o.data_ptr(), w if out is None else _pitch("out", out, n, w, s.dtype, at),
+                        None if lse is None else _whole("lse", lse, (n, s.Hq), torch.float32, at), self.ws.data_ptr(),
+                        self.ws.numel(), _launched_on(at))
+        if rc:
+            B._check(rc, "ps_paged_decode")
+        return o
+
+    def check_status(self):
+        """Raise PsppoError if the last call reports a device-side error."""
+        _status("decode", self.ws)

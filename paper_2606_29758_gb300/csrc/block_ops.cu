@@ -10,66 +10,9 @@
 #include "internal.h"
 #include "ps_common.cuh"
 #include "ps_nvtx.h"
+#include "row_elems.cuh"
 
 namespace psk {
-
-// ================================================================== elements
-struct Bf16 {
-  uint16_t v;
-};
-template <class T>
-struct Elem;
-template <>
-struct Elem<Bf16> {
-  static __device__ __forceinline__ float get(Bf16 x) { return __uint_as_float(static_cast<uint32_t>(x.v) << 16); }
-  static __device__ __forceinline__ Bf16 put(float x) {
-    return Bf16{static_cast<uint16_t>(pack_bf16x2(x, 0.f) & 0xffffu)};
-  }
-};
-template <>
-struct Elem<float> {
-  static __device__ __forceinline__ float get(float x) { return x; }
-  static __device__ __forceinline__ float put(float x) { return x; }
-};
-
-// Eight consecutive elements at a 16-byte boundary, as they are loaded and as floats.
-template <class T>
-struct Raw8;
-template <>
-struct Raw8<Bf16> {
-  uint4 v;
-  __device__ __forceinline__ void load(const Bf16* p) { v = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ void get(float* f) const {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = __uint_as_float(w[i] << 16);
-      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ void store(Bf16* p, const float* f) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]),
-                                              pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
-  }
-};
-template <>
-struct Raw8<float> {
-  float4 a, b;
-  __device__ __forceinline__ void load(const float* p) {
-    a = reinterpret_cast<const float4*>(p)[0];
-    b = reinterpret_cast<const float4*>(p)[1];
-  }
-  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
-  __device__ __forceinline__ void get(float* f) const {
-    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w;
-    f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
-  }
-  static __device__ __forceinline__ void store(float* p, const float* f) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
-  }
-};
 
 // Two f32 in one register pair: an instruction for both.
 struct F2 {
@@ -179,11 +122,6 @@ static_assert(QkCfg<uint16_t, true>::kWarp >= 2 * 512 * 4, "a warp's gain gradie
 // The status is cleared by a memset before the launch, as any block may set it early; of fewer rows the first block looks at
 // every position and sets the word alone (a token's call takes one launch, 6.3 -> 4 us on the device).
 constexpr int kQkCheckRows = 2048;
-
-// 16 bytes global -> shared.
-static __device__ __forceinline__ void lane_copy(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
 
 struct QkArgs {
   int64_t N;
@@ -731,8 +669,6 @@ __global__ void __launch_bounds__(kDropThreads, sizeof(T) == 4 || ROWS != kWhole
 }
 
 // ================================================================== host side
-static bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-static int elem_bytes(int dtype) { return dtype == PS_DTYPE_BF16 ? 2 : 4; }
 static int lanes_for(int chunks) {
   int g = 1;
   while (g < chunks && g < 32) g *= 2;

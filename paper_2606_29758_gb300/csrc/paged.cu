@@ -1,0 +1,886 @@
+// A paged cache of keys and values in sampling: new tokens' rows written into their pages, and attention of one new token
+// a sequence over the pages, split over all keys and joined.
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <climits>
+
+#include "internal.h"
+#include "ps_common.cuh"
+#include "ps_nvtx.h"
+#include "row_elems.cuh"
+
+namespace psk {
+
+// The cache of one layer: keys and values [pages][Hk][page][D]; the table [seqs][ldt] names the pages of a sequence in order.
+struct PagesOf {
+  const int32_t* table;
+  int64_t ldt;                // pages a row of the table holds
+  int pages, page_log2, page;
+  int Hk, D;
+};
+
+// ================================================================== append
+struct AppendArgs {
+  int64_t N;
+  PagesOf c;
+  int seqs;
+  const void *k, *v;
+  int64_t ldk, ldv;
+  const int32_t *seq, *pos;
+  int pos_base;
+  void *kc, *vc;
+  int pieces, head_pieces;    // 16-byte pieces of a row, of a head
+  int parts;                  // warps that share a row
+  int checked;                // the first block looks at every row and writes the status alone
+  uint32_t* status;
+};
+constexpr int kAppendThreads = 128;
+constexpr int kAppendCheckRows = 2048;
+
+// Where row i goes, or what is wrong with it: 0 and its page and slot, -1 for a row without a sequence, else status bits.
+static __device__ __forceinline__ int append_place(const AppendArgs& a, int64_t row, int& page_id, int& in_page) {
+  const int seq = __ldg(a.seq + row);
+  if (seq == -1) return -1;
+  const int64_t p = static_cast<int64_t>(__ldg(a.pos + row)) - a.pos_base;
+  if (seq < 0 || seq >= a.seqs || p < 0 || (p >> a.c.page_log2) >= a.c.ldt) return PS_DEV_BAD_LENGTH;
+  page_id = __ldg(a.c.table + seq * a.c.ldt + (p >> a.c.page_log2));
+  in_page = static_cast<int>(p & (a.c.page - 1));
+  return page_id < 0 || page_id >= a.c.pages ? PS_DEV_BAD_PAGE : 0;
+}
+
+// Each row is read once and written once: HBM, or the latency of three dependent loads (sequence and position, page, row).
+__global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs a) {
+  const int lane = threadIdx.x & 31;
+  const int64_t units = a.N * a.parts, stride = static_cast<int64_t>(gridDim.x) * (kAppendThreads / 32);
+  wait_for_previous_kernel();
+  let_next_kernel_in();
+  if (a.checked && blockIdx.x == 0) {
+    int bad = 0, id, at;
+    for (int64_t i = threadIdx.x; i < a.N; i += kAppendThreads) bad |= max(0, append_place(a, i, id, at));
+    const int len = __syncthreads_or(bad & PS_DEV_BAD_LENGTH), page = __syncthreads_or(bad & PS_DEV_BAD_PAGE);
+    if (threadIdx.x == 0) {
+      a.status[1] = 0u;
+      a.status[0] = (len ? PS_DEV_BAD_LENGTH : 0) | (page ? PS_DEV_BAD_PAGE : 0);
+    }
+  }
+  for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kAppendThreads / 32) + (threadIdx.x >> 5); u < units; u += stride) {
+    const int64_t row = a.parts == 1 ? u : u / a.parts;
+    const int part = static_cast<int>(u - row * a.parts);
+    int id = 0, slot = 0;
+    const int bad = append_place(a, row, id, slot);
+    if (bad) {
+      if (bad > 0 && !a.checked && lane == 0) raise_status(a.status, bad);
+      continue;
+    }
+    const uint4* ks = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.k) + row * a.ldk);
+    const uint4* vs = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.v) + row * a.ldv);
+    const int64_t first = static_cast<int64_t>(id) * a.c.Hk;
+    const int p1 = static_cast<int>(static_cast<int64_t>(a.pieces) * (part + 1) / a.parts);
+    for (int p0 = static_cast<int>(static_cast<int64_t>(a.pieces) * part / a.parts); p0 < p1; p0 += 64) {
+      uint4 kv[2], vv[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int p = p0 + h * 32 + lane;
+        if (p < p1) kv[h] = __ldg(ks + p), vv[h] = __ldg(vs + p);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int p = p0 + h * 32 + lane;
+        if (p >= p1) continue;
+        const int head = p / a.head_pieces;
+        const int64_t to = (((first + head) << a.c.page_log2) + slot) * a.head_pieces + (p - head * a.head_pieces);
+        static_cast<uint4*>(a.kc)[to] = kv[h];
+        static_cast<uint4*>(a.vc)[to] = vv[h];
+      }
+    }
+  }
+}
+
+// ================================================================== decode
+//   x_j = c q.k_j (c = scale log2 e) over a sequence's keys j, m = max x_j, l = sum 2^(x_j - m), o = sum 2^(x_j - m) v_j / l;
+//   parts of a sequence join by m = max m_i, l = sum l_i 2^(m_i - m), o likewise.
+// HBM-bound: every key and value is read once, for all query heads that share it. The work is a list of tiles of 64 keys of
+// one key head of one sequence (a unit: its query heads, up to 8 NB of them); each CTA takes an equal run of the list,
+// whatever the lengths are. Its four warps take 16 keys of a tile each, through rings of their own in shared memory that
+// their lanes' copies fill some tiles ahead, across units; within a unit nothing crosses warps. What a CTA has
+// of a unit that it does not hold whole goes to the workspace (two slots a CTA), and decode_join_kernel adds those up.
+// bf16: products by mma.sync with the keys (S^T = K Q^T, 16 keys x 8 heads) and the values' dims (O^T = V^T P^T, 16 dims x 8
+// heads) as rows, so that eight heads fill a product's columns; P in two bf16 parts (2^-17 of a weight), so that a
+// short sequence's outputs are rounded once. The rows of tcgen05 products would be 64 or more of one operand in
+// shared memory and accumulators in TMEM, whose round trips a chunk of 16 keys would wait for, and these
+// products are a few per cent of what mma.sync does.
+constexpr int kDecWarps = 4;
+constexpr int kDecThreads = 32 * kDecWarps;
+constexpr int kChunk = 16;                        // keys of a warp's share of a tile
+constexpr int kTile = kChunk * kDecWarps;
+
+struct DecodeArgs {
+  int B, Hq, group, blocks;     // sequences, query heads, query heads a key head, units a key head
+  PagesOf c;
+  const int32_t* lens;
+  int window;                   // 0: all keys
+  float scale2;                 // scale log2 e
+  const void* q;
+  int64_t ldq;
+  const void *kc, *vc;
+  void* o;
+  int64_t ldo;
+  float* lse;                   // [B][Hq] or nullptr
+  uint32_t* status;
+  int4* seg;                    // [CTAs] status bits, unit that begins here and goes on (sequence or -1, block), what slot 0 holds
+  float2* ml;                   // [2 CTAs][heads of a unit] (m, l)
+  float* part;                  // [2 CTAs][heads of a unit][DP]
+};
+enum { kSlotNone = 0, kSlotEnds = 1, kSlotGoesOn = 2 };
+
+static __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+static __device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+static __device__ __forceinline__ uint32_t transposed(uint32_t x) {   // an 8 x 8 matrix of 16-bit elements over the warp
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+static __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 16 bytes global -> shared, or zeros.
+static __device__ __forceinline__ void lane_copy_or_zero(uint32_t dst, const void* src, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+}
+
+// A warp's part of a unit: m, l and o of its query heads over the keys that it has seen.
+//   load    the unit's queries
+//   chunk   16 keys and values in shared memory, the first nv of them (rows behind are zeros), 16-byte piece p of row r at p ^ (r & 7)
+//   put_ml  m and l to shared memory
+//   add_o   o times a head's factor, to or added to what shared memory [heads][DP + 4] holds
+template <class T, int DP, int NB>
+struct DecodeMath;
+
+template <int DP, int NB>
+struct DecodeMath<Bf16, DP, NB> {
+  static constexpr int kHeads = 8 * NB, kRow = DP * 2, kQBytes = 0;
+  uint32_t q[NB][DP / 16][2];
+  float o[NB][DP / 16][4];      // o[dim lane / 4 (+ 8)][head 2 (lane % 4) (+ 1)]
+  float m[NB][2], l[NB][2];     // of heads 2 (lane % 4) and the next; l of this lane's keys
+
+  __device__ __forceinline__ void load(const Bf16* qs, int heads, int D, uint8_t*, int lane) {
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      const int head = n * 8 + lane / 4;
+#pragma unroll
+      for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int at = k * 16 + i * 8 + 2 * (lane & 3);
+          q[n][k][i] = head < heads && at < D ? *reinterpret_cast<const uint32_t*>(qs + head * D + at) : 0u;
+        }
+#pragma unroll
+      for (int t = 0; t < DP / 16; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n][t][i] = 0.f;
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.f;
+    }
+  }
+  __device__ __forceinline__ void poison() {
+#pragma unroll
+    for (int n = 0; n < NB; ++n) l[n][0] = l[n][1] = __int_as_float(0x7fffffff);
+  }
+  __device__ __forceinline__ void chunk(uint32_t ks, uint32_t vs, int nv, float scale2, const uint8_t*, float*, int lane) {
+    const int r = lane & 15, hi = lane >> 4;
+    float s[NB][4];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+    // rows: keys 0-7 and 8-15 by the lanes' first 16 addresses, then the next eight dims
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k) {
+      uint32_t a[4];
+      ldsm4(a, ks + r * kRow + (((2 * k + hi) ^ (r & 7)) << 4));
+#pragma unroll
+      for (int n = 0; n < NB; ++n) mma_bf16(s[n], a, q[n][k][0], q[n][k][1]);
+    }
+    const int key = lane / 4;
+    uint32_t ph[NB][2], pl[NB][2];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      float x[4], top[2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = key + (i & 2 ? 8 : 0) < nv ? s[n][i] * scale2 : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float v = fmaxf(x[i], x[i + 2]);
+        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+        top[i] = fmaxf(m[n][i], v);
+      }
+      if (__any_sync(0xffffffffu, top[0] != m[n][0] || top[1] != m[n][1])) {
+        float f[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          f[i] = m[n][i] == top[i] ? 1.f : ex2_ftz(m[n][i] - top[i]);
+          m[n][i] = top[i];
+          l[n][i] *= f[i];
+        }
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[n][t][i] *= f[i & 1];
+      }
+      float p[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[i] = ex2_ftz(x[i] - (m[n][i & 1] == -INFINITY ? 0.f : m[n][i & 1]));
+        l[n][i & 1] += p[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t h = pack_bf16x2(p[2 * i], p[2 * i + 1]);
+        const uint32_t w = pack_bf16x2(p[2 * i] - __uint_as_float(h << 16), p[2 * i + 1] - __uint_as_float(h & 0xffff0000u));
+        ph[n][i] = transposed(h);
+        pl[n][i] = transposed(w);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < DP / 16; ++t) {
+      uint32_t a[4];   // dims 0-7 and 8-15 of keys 0-7, then of keys 8-15
+      const int row = (lane & 7) + (hi << 3);
+      ldsm4_t(a, vs + row * kRow + (((2 * t + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        mma_bf16(o[n][t], a, ph[n][0], ph[n][1]);
+        mma_bf16(o[n][t], a, pl[n][0], pl[n][1]);
+      }
+    }
+  }
+  __device__ __forceinline__ void put_ml(float2* ml, int lane) {
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float v = l[n][i];
+        v += __shfl_xor_sync(0xffffffffu, v, 4);
+        v += __shfl_xor_sync(0xffffffffu, v, 8);
+        v += __shfl_xor_sync(0xffffffffu, v, 16);
+        if (lane < 4) ml[n * 8 + 2 * lane + i] = make_float2(m[n][i], v);
+      }
+  }
+  template <class F>
+  __device__ __forceinline__ void add_o(float* to, F&& factor, bool first, int lane) {
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int head = n * 8 + 2 * (lane & 3) + i;
+        const float f = factor(head);
+        float* at = to + head * (DP + 4) + lane / 4;
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t) {
+          const float v = f == 0.f ? 0.f : o[n][t][i] * f, w = f == 0.f ? 0.f : o[n][t][i + 2] * f;
+          at[t * 16] = first ? v : at[t * 16] + v;
+          at[t * 16 + 8] = first ? w : at[t * 16 + 8] + w;
+        }
+      }
+  }
+};
+
+template <int DP, int NB>
+struct DecodeMath<float, DP, NB> {   // on the f32 pipe: a lane has half of a key's dims, then four dims of all keys' values
+  static_assert(NB == 1, "eight heads at a time");
+  static constexpr int kHeads = 8, kRow = DP * 4, kHalf = DP / 2 + 4, kQBytes = kHeads * 2 * kHalf * 4;
+  static constexpr int kOwn = (DP + 127) / 128;   // pieces of four dims a lane has
+  float o[kHeads][kOwn][4];
+  float m[kHeads], l[kHeads];                     // the same in all lanes
+
+  __device__ __forceinline__ void load(const float* qs, int heads, int D, uint8_t* mem, int lane) {
+    float* q = reinterpret_cast<float*>(mem);
+    __syncwarp();
+    for (int i = lane; i < kHeads * DP; i += 32) {
+      const int head = i / DP, at = i % DP;
+      q[(head * 2 + at / (DP / 2)) * kHalf + at % (DP / 2)] = head < heads && at < D ? qs[head * D + at] : 0.f;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+      m[h] = -INFINITY;
+      l[h] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kOwn; ++w)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[h][w][i] = 0.f;
+    }
+  }
+  __device__ __forceinline__ void poison() {
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) l[h] = __int_as_float(0x7fffffff);
+  }
+  __device__ __forceinline__ float4 at(uint32_t base, int r, int p) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(base + r * kRow + ((p ^ (r & 7)) << 4))
+                 : "memory");
+    return v;
+  }
+  __device__ __forceinline__ void chunk(uint32_t ks, uint32_t vs, int nv, float scale2, const uint8_t* mem, float* ps, int lane) {
+    const int key = lane & 15, half = lane >> 4;
+    const float* q = reinterpret_cast<const float*>(mem) + half * kHalf;
+    float s[kHeads];
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) s[h] = 0.f;
+#pragma unroll 4
+    for (int p = 0; p < DP / 8; ++p) {
+      const float4 k = at(ks, key, half * (DP / 8) + p);
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h) {
+        const float4 w = *reinterpret_cast<const float4*>(q + h * 2 * kHalf + 4 * p);
+        s[h] = fmaf(k.x, w.x, fmaf(k.y, w.y, fmaf(k.z, w.z, fmaf(k.w, w.w, s[h]))));
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+      s[h] += __shfl_xor_sync(0xffffffffu, s[h], 16);
+      const float x = key < nv ? s[h] * scale2 : -INFINITY;
+      float v = x;
+#pragma unroll
+      for (int i = 8; i >= 1; i >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, i));
+      const float top = fmaxf(m[h], v);
+      if (top != m[h]) {
+        const float f = ex2_ftz(m[h] - top);
+        m[h] = top;
+        l[h] *= f;
+#pragma unroll
+        for (int w = 0; w < kOwn; ++w)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[h][w][i] *= f;
+      }
+      const float p = ex2_ftz(x - (m[h] == -INFINITY ? 0.f : m[h]));
+      float t = p;
+#pragma unroll
+      for (int i = 8; i >= 1; i >>= 1) t += __shfl_xor_sync(0xffffffffu, t, i);
+      l[h] += t;
+      if (h / 4 == half) ps[h * kChunk + key] = p;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int r = 0; r < kChunk; r += 4) {
+      if (r >= nv) break;
+      float4 v[kOwn][4];
+#pragma unroll
+      for (int w = 0; w < kOwn; ++w)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          v[w][i] = w * 32 + lane < DP / 4 ? at(vs, r + i, w * 32 + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h) {
+        const float4 p = *reinterpret_cast<const float4*>(ps + h * kChunk + r);
+        const float pv[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+        for (int w = 0; w < kOwn; ++w)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            o[h][w][0] = fmaf(pv[i], v[w][i].x, o[h][w][0]);
+            o[h][w][1] = fmaf(pv[i], v[w][i].y, o[h][w][1]);
+            o[h][w][2] = fmaf(pv[i], v[w][i].z, o[h][w][2]);
+            o[h][w][3] = fmaf(pv[i], v[w][i].w, o[h][w][3]);
+          }
+      }
+    }
+    __syncwarp();
+  }
+  __device__ __forceinline__ void put_ml(float2* ml, int lane) {
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h)
+      if (lane == h) ml[h] = make_float2(m[h], l[h]);
+  }
+  template <class F>
+  __device__ __forceinline__ void add_o(float* to, F&& factor, bool first, int lane) {
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+      const float f = factor(h);
+#pragma unroll
+      for (int w = 0; w < kOwn; ++w) {
+        if (w * 32 + lane >= DP / 4) continue;
+        float4& at = *reinterpret_cast<float4*>(to + h * (DP + 4) + (w * 32 + lane) * 4);
+        float4 v = first ? make_float4(0.f, 0.f, 0.f, 0.f) : at;
+        if (f != 0.f) {
+          v.x += o[h][w][0] * f;
+          v.y += o[h][w][1] * f;
+          v.z += o[h][w][2] * f;
+          v.w += o[h][w][3] * f;
+        }
+        at = v;
+      }
+    }
+  }
+};
+
+template <class T, int DP, int NB>
+struct DecodeCfg {
+  using Math = DecodeMath<T, DP, NB>;
+  static constexpr int kChunkBytes = kChunk * DP * static_cast<int>(sizeof(T));   // of keys, and of values
+  static constexpr int kStages = kChunkBytes >= 16384 ? 1 : kChunkBytes >= 4096 ? 3 : 4;
+  static constexpr int kRing = kStages * 2 * kChunkBytes;
+  static constexpr int kPs = sizeof(T) == 4 ? Math::kHeads * kChunk * 4 : 0;
+  static constexpr int kWarp = kRing + Math::kQBytes + kPs;
+  static constexpr int kOuts = NB == 1 ? 2 : 1;                                   // where the warps' o are added up
+  static constexpr int kOut = Math::kHeads * (DP + 4) * 4;
+  static constexpr int kSmem = kDecWarps * kWarp + kOuts * kOut;
+  static constexpr int kBlocks = kSmem <= 112 * 1024 ? 2 : 1;                     // per SM
+  static_assert(kSmem <= 226 * 1024, "an SM's shared memory");
+};
+
+// A sequence's keys: the last `window` of its length, or all.
+struct Keys {
+  int first, end;
+  bool bad;
+  __device__ __forceinline__ int tiles() const { return (end - first + kTile - 1) / kTile; }
+};
+static __device__ __forceinline__ Keys keys_of(const DecodeArgs& a, int b) {
+  const int len = __ldg(a.lens + b);
+  if (len < 0 || len > (a.c.ldt << a.c.page_log2)) return {0, 0, true};
+  return {a.window > 0 && len > a.window ? len - a.window : 0, len, false};
+}
+
+template <class T, int DP, int NB>
+__global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) decode_kernel(const DecodeArgs a) {
+  using Cfg = DecodeCfg<T, DP, NB>;
+  using Math = typename Cfg::Math;
+  constexpr int ST = Cfg::kStages, E = 16 / static_cast<int>(sizeof(T)), PR = DP / E, H = Math::kHeads;
+  extern __shared__ __align__(128) uint8_t dec_smem[];
+  __shared__ float2 ml_s[kDecWarps][H];
+  __shared__ int64_t scan_s[kDecWarps], start_s;
+  __shared__ int b_s, bad_s;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  uint8_t* const mine = dec_smem + warp * Cfg::kWarp;
+  const uint32_t ring = smem_addr(mine);
+  float* const out_s = reinterpret_cast<float*>(dec_smem + kDecWarps * Cfg::kWarp);
+  uint8_t* const q_s = mine + Cfg::kRing;
+  float* const p_s = reinterpret_cast<float*>(q_s + Math::kQBytes);
+  const int per_head = a.blocks, HM = a.c.Hk * per_head;    // units a sequence
+
+  // dims behind D stay zeros in every stage
+  if (a.c.D < DP)
+    for (int i = lane; i < ST * 2 * kChunk * PR; i += 32) *reinterpret_cast<uint4*>(mine + i * 16) = make_uint4(0, 0, 0, 0);
+  if (tid == 0) bad_s = 0, b_s = a.B;
+  __syncthreads();
+  wait_for_previous_kernel();
+  let_next_kernel_in();
+
+  // the list's length, and the sequence in which this CTA's run begins
+  const int per = (a.B + kDecThreads - 1) / kDecThreads, b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
+  int64_t sum = 0;
+  for (int b = b0; b < b1; ++b) sum += keys_of(a, b).tiles();
+  int64_t upto = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += v;
+  }
+  if (lane == 31) scan_s[warp] = upto;
+  __syncthreads();
+  int64_t before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kDecWarps; ++w) {
+    if (w < warp) before += scan_s[w];
+    total += scan_s[w];
+  }
+  upto += before;
+  const int64_t list = total * HM;
+  // (of a list with fewer tiles than CTAs the first ones have one each, so that a unit's parts are its CTAs' in a row)
+  const int64_t takers = min(static_cast<int64_t>(gridDim.x), list), me = min(static_cast<int64_t>(blockIdx.x), takers);
+  const int64_t t0 = me < takers ? list * me / takers : list, t1 = me < takers ? list * (me + 1) / takers : list;
+  if (t0 < t1 && (upto - sum) * HM <= t0 && t0 < upto * HM) {
+    int64_t at = upto - sum;
+    int b = b0;
+    for (; b < b1; ++b) {
+      const int n = keys_of(a, b).tiles();
+      if (t0 < (at + n) * HM) break;
+      at += n;
+    }
+    b_s = b;
+    start_s = at * HM;
+  }
+  // sequences without keys
+  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+    const Keys k = keys_of(a, b);
+    if (k.end > 0) continue;
+    if (k.bad && tid == 0) bad_s = PS_DEV_BAD_LENGTH;
+    for (int i = tid; i < a.Hq * a.c.D; i += kDecThreads)
+      static_cast<T*>(a.o)[b * a.ldo + i] = Elem<T>::put(k.bad ? __int_as_float(0x7fffffff) : 0.f);
+    if (a.lse)
+      for (int i = tid; i < a.Hq; i += kDecThreads) a.lse[static_cast<int64_t>(b) * a.Hq + i] = k.bad ? __int_as_float(0x7fffffff) : -INFINITY;
+  }
+  __syncthreads();
+
+  // A place in the list: tile `tile` of `tiles` of unit hm of sequence b.
+  struct Place {
+    int64_t t;
+    int b, hm, tile, tiles, first, end;
+  };
+  auto enter = [&](Place& p) {   // the sequence's keys
+    const Keys k = keys_of(a, p.b);
+    p.first = k.first;
+    p.end = k.end;
+    p.tiles = k.tiles();
+  };
+  auto next = [&](Place& p) {
+    if (++p.t >= t1) return;
+    if (++p.tile < p.tiles) return;
+    p.tile = 0;
+    if (++p.hm < HM) return;
+    p.hm = 0;
+    do {
+      ++p.b;
+      enter(p);
+    } while (p.tiles == 0);
+  };
+  // the page of this lane's key (row lane % 16 of the warp's chunk) at a place: -1 behind the end
+  auto page_at = [&](const Place& p) {
+    const int key = p.first + p.tile * kTile + warp * kChunk + (lane & 15);
+    return p.t < t1 && key < p.end ? __ldg(a.c.table + p.b * a.c.ldt + (key >> a.c.page_log2)) : -1;
+  };
+  uint32_t bad_stages = 0;
+  auto issue = [&](const Place& p, int id, int st) {
+    const int k0 = p.first + p.tile * kTile + warp * kChunk;
+    bad_stages &= ~(1u << st);
+    if (p.t < t1 && k0 < p.end) {
+      const bool in = k0 + (lane & 15) < p.end, good = in && id >= 0 && id < a.c.pages;
+      if (__any_sync(0xffffffffu, in && !good)) bad_stages |= 1u << st;
+      const int valid_id = good ? id : -1;
+      const int hk = per_head == 1 ? p.hm : p.hm / per_head;
+      const uint32_t to = ring + st * 2 * Cfg::kChunkBytes;
+#pragma unroll
+      for (int i = 0; i < kChunk * PR / 32; ++i) {
+        const int idx = i * 32 + lane, r = idx / PR, pc = idx % PR;
+        const int pid = __shfl_sync(0xffffffffu, valid_id, r);
+        const int64_t row = ((static_cast<int64_t>(max(pid, 0)) * a.c.Hk + hk) << a.c.page_log2) + ((k0 + r) & (a.c.page - 1));
+        const int64_t off = row * a.c.D + pc * E;
+        const uint32_t at = to + (r * PR + (pc ^ (r & 7))) * 16;
+        if (pc * E < a.c.D) {
+          lane_copy_or_zero(at, static_cast<const T*>(a.kc) + off, pid >= 0);
+          lane_copy_or_zero(at + Cfg::kChunkBytes, static_cast<const T*>(a.vc) + off, pid >= 0);
+        }
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+
+  int4 seg = make_int4(0, -1, 0, kSlotNone);
+  if (t0 < t1) {
+    Place t, n;
+    t.b = b_s;
+    t.t = t0;
+    enter(t);
+    const int64_t in_seq = t0 - start_s;
+    t.hm = static_cast<int>(in_seq / t.tiles);
+    t.tile = static_cast<int>(in_seq - static_cast<int64_t>(t.hm) * t.tiles);
+    n = t;
+    int id = page_at(n);
+#pragma unroll
+    for (int s = 0; s < ST; ++s) {
+      const Place now = n;
+      const int now_id = id;
+      next(n);
+      id = page_at(n);
+      issue(now, now_id, s);
+    }
+    int st = 0, bad = 0;
+    Math math;
+    while (t.t < t1) {
+      const int b = t.b, hm = t.hm, tile0 = t.tile;
+      const int hk = per_head == 1 ? hm : hm / per_head, h0 = hk * a.group + (hm - hk * per_head) * H;
+      const int heads = min(H, (hk + 1) * a.group - h0);
+      const int tile1 = static_cast<int>(min(static_cast<int64_t>(t.tiles), tile0 + (t1 - t.t)));
+      const bool whole = tile0 == 0 && tile1 == t.tiles, ends = tile1 == t.tiles;
+      math.load(static_cast<const T*>(a.q) + b * a.ldq + static_cast<int64_t>(h0) * a.c.D, heads, a.c.D, q_s, lane);
+      for (int tile = tile0; tile < tile1; ++tile) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
+        __syncwarp();
+        const int nv = t.end - (t.first + tile * kTile + warp * kChunk);
+        const uint32_t from = ring + st * 2 * Cfg::kChunkBytes;
+        if (nv > 0) math.chunk(from, from + Cfg::kChunkBytes, min(nv, kChunk), a.scale2, q_s, p_s, lane);
+        if (bad_stages >> st & 1u) {
+          math.poison();
+          bad = PS_DEV_BAD_PAGE;
+        }
+        __syncwarp();   // the stage has been read
+        const Place now = n;
+        const int now_id = id;
+        next(n);
+        id = page_at(n);
+        issue(now, now_id, st);
+        st = st + 1 == ST ? 0 : st + 1;
+        next(t);
+      }
+      // the warps' parts together
+      math.put_ml(ml_s[warp], lane);
+      __syncthreads();
+      auto top_of = [&](int h) {
+        float top = ml_s[0][h].x;
+#pragma unroll
+        for (int w = 1; w < kDecWarps; ++w) top = fmaxf(top, ml_s[w][h].x);
+        return top;
+      };
+      constexpr int OUTS = Cfg::kOuts, OUT = Cfg::kOut / 4;
+#pragma unroll
+      for (int k = 0; k < kDecWarps / OUTS; ++k) {
+        if (warp / OUTS == k)
+          math.add_o(out_s + warp % OUTS * OUT, [&](int h) {
+            const float top = top_of(h);
+            return top == -INFINITY ? 1.f : ex2_ftz(ml_s[warp][h].x - top);   // (0 where this warp had no keys)
+          }, k == 0, lane);
+        __syncthreads();
+      }
+      const int slot = 2 * blockIdx.x + (tile0 == 0 ? 1 : 0);
+      for (int i = tid; i < heads * DP; i += kDecThreads) {
+        const int h = i / DP, c = i % DP;
+        const float top = top_of(h);
+        float l = 0.f, v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kDecWarps; ++w) l += ml_s[w][h].x == top ? ml_s[w][h].y : ml_s[w][h].y * ex2_ftz(ml_s[w][h].x - top);
+#pragma unroll
+        for (int k = 0; k < OUTS; ++k) v += out_s[k * OUT + h * (DP + 4) + c];
+        if (whole) {
+          if (c < a.c.D) static_cast<T*>(a.o)[b * a.ldo + static_cast<int64_t>(h0 + h) * a.c.D + c] = Elem<T>::put(v / l);
+          if (c == 0 && a.lse) a.lse[static_cast<int64_t>(b) * a.Hq + h0 + h] = (top + log2f(l)) * kLn2;
+        } else {
+          a.part[(static_cast<int64_t>(slot) * H + h) * DP + c] = v;
+          if (c == 0) a.ml[slot * H + h] = make_float2(top, l);
+        }
+      }
+      if (!whole) {
+        if (tile0 == 0) seg.y = b, seg.z = hm;
+        else seg.w = ends ? kSlotEnds : kSlotGoesOn;
+      }
+      __syncthreads();
+    }
+    if (bad) atomicOr(&bad_s, bad);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    seg.x = bad_s;
+    a.seg[blockIdx.x] = seg;
+  }
+}
+
+// The units that several CTAs had parts of, by the CTA where one begins; and the call's status.
+constexpr int kJoinThreads = 256;
+template <class T, int DP, int H>
+__global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecodeArgs a, int ctas) {
+  __shared__ float top_s[kJoinThreads / 32], l_s[kJoinThreads / 32];
+  __shared__ float o_s[kJoinThreads / 32][DP];
+  __shared__ int last_s;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = kJoinThreads / 32;
+  const int i = blockIdx.x, h = blockIdx.y;
+  wait_for_previous_kernel();
+  if (i == 0 && h == 0) {
+    int bits = 0;
+    for (int j = tid; j < ctas; j += kJoinThreads) bits |= a.seg[j].x;
+    const int len = __syncthreads_or(bits & PS_DEV_BAD_LENGTH), page = __syncthreads_or(bits & PS_DEV_BAD_PAGE);
+    if (tid == 0) {
+      a.status[1] = 0u;
+      a.status[0] = (len ? PS_DEV_BAD_LENGTH : 0) | (page ? PS_DEV_BAD_PAGE : 0);
+    }
+  }
+  const int4 seg = a.seg[i];
+  if (seg.y < 0) return;
+  const int hk = seg.z / a.blocks, h0 = hk * a.group + (seg.z - hk * a.blocks) * H;
+  if (h >= min(H, (hk + 1) * a.group - h0)) return;
+  // the CTA where it ends
+  if (tid == 0) last_s = ctas - 1;
+  __syncthreads();
+  for (int j0 = i + 1; j0 < ctas; j0 += kJoinThreads) {
+    const int j = j0 + tid;
+    const bool ends = j < ctas && a.seg[j].w == kSlotEnds;
+    if (ends) atomicMin(&last_s, j);
+    if (__syncthreads_or(ends)) break;
+  }
+  __syncthreads();
+  const int parts = last_s - i + 1;
+  auto slot = [&](int k) { return (k == 0 ? 2 * i + 1 : 2 * (i + k)) * H + h; };
+  float top = -INFINITY;
+  for (int k = tid; k < parts; k += kJoinThreads) top = fmaxf(top, a.ml[slot(k)].x);
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (lane == 0) top_s[warp] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < W; ++w) top = fmaxf(top, top_s[w]);
+  constexpr int C = (DP + 127) / 128;
+  float4 v[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) v[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+  float l = 0.f;
+#pragma unroll 4
+  for (int k = warp; k < parts; k += W) {
+    const float2 ml = a.ml[slot(k)];
+    const float f = ml.x == top ? 1.f : ex2_ftz(ml.x - top);
+    l = fmaf(ml.y, f, l);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int at = (c * 32 + lane) * 4;
+      if (at >= DP || f == 0.f) continue;
+      const float4 p = *reinterpret_cast<const float4*>(a.part + static_cast<int64_t>(slot(k)) * DP + at);
+      v[c].x = fmaf(p.x, f, v[c].x);
+      v[c].y = fmaf(p.y, f, v[c].y);
+      v[c].z = fmaf(p.z, f, v[c].z);
+      v[c].w = fmaf(p.w, f, v[c].w);
+    }
+  }
+  if (lane == 0) l_s[warp] = l;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+    if ((c * 32 + lane) * 4 < DP) *reinterpret_cast<float4*>(&o_s[warp][(c * 32 + lane) * 4]) = v[c];
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int w = 0; w < W; ++w) l += l_s[w];
+  for (int c = tid; c < a.c.D; c += kJoinThreads) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) s += o_s[w][c];
+    static_cast<T*>(a.o)[seg.y * a.ldo + static_cast<int64_t>(h0 + h) * a.c.D + c] = Elem<T>::put(s / l);
+  }
+  if (tid == 0 && a.lse) a.lse[static_cast<int64_t>(seg.y) * a.Hq + h0 + h] = (top + log2f(l)) * kLn2;
+}
+
+// ================================================================== host side
+constexpr int kDecMaxCtas = 304;
+constexpr int kDecMaxHeads = 16, kDecMaxDim = 256;
+constexpr size_t kDecSeg = sizeof(int4) * kDecMaxCtas, kDecMl = sizeof(float2) * 2 * kDecMaxCtas * kDecMaxHeads;
+
+static bool pages_ok(int seqs, int Hk, int D, int dtype, int pages, int page, int64_t ldt) {
+  return seqs >= 0 && Hk >= 1 && Hk <= 65536 && D >= 16 && D <= kDecMaxDim && D % 16 == 0 &&
+         (dtype == PS_DTYPE_BF16 || dtype == PS_DTYPE_F32) && pages >= 1 && page >= 1 && page <= 65536 && !(page & (page - 1)) &&
+         ldt >= 1 && ldt <= INT32_MAX / page - 64;
+}
+static int log2_of(int v) {
+  int n = 0;
+  while ((1 << n) < v) ++n;
+  return n;
+}
+static PagesOf pages_of(const int32_t* table, int64_t ldt, int pages, int page, int Hk, int D) {
+  PagesOf c;
+  c.table = table, c.ldt = ldt, c.pages = pages, c.page = page, c.page_log2 = log2_of(page), c.Hk = Hk, c.D = D;
+  return c;
+}
+
+template <class T, int DP, int NB>
+static int launch_decode(DecodeArgs a, cudaStream_t s) {
+  using Cfg = DecodeCfg<T, DP, NB>;
+  auto kern = decode_kernel<T, DP, NB>;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem) != cudaSuccess) return PS_ERR_CUDA;
+  constexpr int H = Cfg::Math::kHeads;
+  a.blocks = (a.group + H - 1) / H;
+  int ctas = num_sms_current() * Cfg::kBlocks;
+  if (ctas > kDecMaxCtas) ctas = kDecMaxCtas;
+  // no more than the tiles that the table can name
+  const int64_t most = static_cast<int64_t>(a.B) * a.c.Hk * a.blocks * (((a.c.ldt << a.c.page_log2) + kTile - 1) / kTile);
+  if (ctas > most) ctas = static_cast<int>(most);
+  if (launch_after(kern, dim3(static_cast<unsigned>(ctas)), kDecThreads, Cfg::kSmem, s, 1, 1, true, a) != cudaSuccess)
+    return PS_ERR_CUDA;
+  return launch_after(decode_join_kernel<T, DP, H>, dim3(static_cast<unsigned>(ctas), H), kJoinThreads, 0, s, 1, 1, true, a, ctas) ==
+                 cudaSuccess
+             ? PS_OK
+             : PS_ERR_CUDA;
+}
+
+}  // namespace psk
+
+using namespace psk;
+
+extern "C" {
+
+int ps_paged_append(int64_t N, int seqs, int Hk, int D, int dtype, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                    const int32_t* row_seq, const int32_t* row_pos, int pos_base, const int32_t* table, int64_t ldt, int pages,
+                    int page, void* k_cache, void* v_cache, void* ws, size_t ws_bytes, ps_stream_t stream) {
+  NvtxRange nvtx_range("ps_paged_append");
+  if (N < 0 || !pages_ok(seqs, Hk, D, dtype, pages, page, ldt)) return PS_ERR_INVALID_ARG;
+  const int e = elem_bytes(dtype);
+  const int64_t cols = static_cast<int64_t>(Hk) * D;
+  auto rows_ok = [&](const void* p, int64_t ld) { return p && al16(p) && ld >= cols && ld * e % 16 == 0; };
+  if (N > 0 && (!rows_ok(k, ldk) || !rows_ok(v, ldv) || !row_seq || !row_pos || !table || !k_cache || !v_cache || !al16(k_cache) ||
+                !al16(v_cache)))
+    return PS_ERR_INVALID_ARG;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const int rc = check_ws(ws, ws_bytes, kWsHeader);
+  if (rc != PS_OK) return rc;
+  if (N == 0) return refused(PS_OK, ws, s);
+  AppendArgs a = {};
+  a.N = N, a.seqs = seqs, a.c = pages_of(table, ldt, pages, page, Hk, D);
+  a.k = k, a.v = v, a.ldk = ldk * e, a.ldv = ldv * e, a.seq = row_seq, a.pos = row_pos, a.pos_base = pos_base;
+  a.kc = k_cache, a.vc = v_cache;
+  a.pieces = static_cast<int>(cols * e / 16), a.head_pieces = D * e / 16;
+  const int64_t want = static_cast<int64_t>(num_sms_current()) * 16;
+  const int steps = (a.pieces + 63) / 64;
+  a.parts = N >= want ? 1 : static_cast<int>(want / N < steps ? want / N : steps);
+  a.checked = N <= kAppendCheckRows;
+  a.status = static_cast<uint32_t*>(ws);
+  if (!a.checked && cudaMemsetAsync(ws, 0, kWsHeader, s) != cudaSuccess) return PS_ERR_CUDA;
+  const int64_t blocks = (N * a.parts + kAppendThreads / 32 - 1) / (kAppendThreads / 32), most = want;
+  const int rc2 = launch_after(append_kernel, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), kAppendThreads, 0, s, 1, 1,
+                               true, a) == cudaSuccess
+                      ? PS_OK
+                      : PS_ERR_CUDA;
+  return rc2 == PS_OK ? rc2 : refused(rc2, ws, s);
+}
+
+size_t ps_paged_decode_workspace_size(int D) {
+  if (D < 16 || D > kDecMaxDim || D % 16) return 0;
+  const int DP = D <= 64 ? 64 : D <= 128 ? 128 : 256;
+  return kWsHeader + kDecSeg + kDecMl + sizeof(float) * 2 * kDecMaxCtas * kDecMaxHeads * DP;
+}
+
+int ps_paged_decode(int seqs, int Hq, int Hk, int D, int dtype, const void* q, int64_t ldq, const void* k_cache,
+                    const void* v_cache, int pages, int page, const int32_t* table, int64_t ldt, const int32_t* lengths, int window,
+                    double scale, void* o, int64_t ldo, float* lse, void* ws, size_t ws_bytes, ps_stream_t stream) {
+  NvtxRange nvtx_range("ps_paged_decode");
+  if (!pages_ok(seqs, Hk, D, dtype, pages, page, ldt) || Hq < Hk || Hq > 65536 || Hq % Hk || window < 0 || !isfinite(scale))
+    return PS_ERR_INVALID_ARG;
+  const int e = elem_bytes(dtype);
+  const int64_t cols = static_cast<int64_t>(Hq) * D;
+  auto rows_ok = [&](const void* p, int64_t ld) { return p && al16(p) && ld >= cols && ld * e % 16 == 0; };
+  if (seqs > 0 && (!rows_ok(q, ldq) || !rows_ok(o, ldo) || !k_cache || !v_cache || !al16(k_cache) || !al16(v_cache) || !table ||
+                   !lengths))
+    return PS_ERR_INVALID_ARG;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const int rc = check_ws(ws, ws_bytes, ps_paged_decode_workspace_size(D));
+  if (rc != PS_OK) return rc;
+  if (seqs == 0) return refused(PS_OK, ws, s);
+  DecodeArgs a = {};
+  a.B = seqs, a.Hq = Hq, a.group = Hq / Hk, a.c = pages_of(table, ldt, pages, page, Hk, D);
+  a.lens = lengths, a.window = window, a.scale2 = static_cast<float>(scale * 1.4426950408889634);
+  a.q = q, a.ldq = ldq, a.kc = k_cache, a.vc = v_cache, a.o = o, a.ldo = ldo, a.lse = lse;
+  uint8_t* w = static_cast<uint8_t*>(ws);
+  a.status = reinterpret_cast<uint32_t*>(w);
+  a.seg = reinterpret_cast<int4*>(w + kWsHeader);
+  a.ml = reinterpret_cast<float2*>(w + kWsHeader + kDecSeg);
+  a.part = reinterpret_cast<float*>(w + kWsHeader + kDecSeg + kDecMl);
+  int out;
+  if (dtype == PS_DTYPE_F32)
+    out = D <= 128 ? launch_decode<float, 128, 1>(a, s) : launch_decode<float, 256, 1>(a, s);
+  else if (D <= 64)
+    out = a.group <= 8 ? launch_decode<Bf16, 64, 1>(a, s) : launch_decode<Bf16, 64, 2>(a, s);
+  else if (D <= 128)
+    out = a.group <= 8 ? launch_decode<Bf16, 128, 1>(a, s) : launch_decode<Bf16, 128, 2>(a, s);
+  else
+    out = launch_decode<Bf16, 256, 1>(a, s);
+  return out == PS_OK ? out : refused(out, ws, s);
+}
+
+}  // extern "C"
