@@ -565,10 +565,11 @@ int ps_dropout_rows(int64_t N, int d, int dtype, const void* x, int64_t ldx, con
  *   Backward: dH = dh + r_h (go do - h r_h^2 mean(go do h)), dx = res_scale dH, dn = branch_scale gate_i dH,
  *   dy = r_y (gy dn - y r_y^2 mean(gy dn y)) or gy dn, dgy = sum over rows of dn y r_y, dgo = sum of do h r_h,
  *   dgate_i = branch_scale sum over columns of dH n.
- * x, y, h, o [N][d], bf16 or f32, any pitch >= d and any alignment of whole elements (16-byte rows of whole blocks of 8
- *   are fastest). gy, go [d] in the rows' type, NULL: 1; gy without PS_NORM_BRANCH scales the branch per column. gate
- *   [N] f32 or NULL (1): a gate of 0 leaves the branch out whatever it holds (NaN and infinities too; dy is then 0).
- *   norms: PS_NORM_BRANCH | PS_NORM_OUT; without a branch PS_NORM_OUT alone, without PS_NORM_OUT o and go are not used.
+ * x, y, h, o [N][d], bf16 or f32, any pitch >= d and any alignment of whole elements (rows of whole 16 bytes at
+ *   16-byte boundaries are fastest, then rows that all lie alike; the order of a row's sums, and so its last bits, goes by how they lie).
+ *   gy, go [d] in the rows' type, NULL: 1; gy without PS_NORM_BRANCH scales the branch per column. gate [N] f32 or NULL
+ *   (1): a gate of 0 leaves the branch out whatever it holds (NaN and infinities too; dy is then 0). norms:
+ *   PS_NORM_BRANCH | PS_NORM_OUT; without a branch PS_NORM_OUT alone, without PS_NORM_OUT o and go are not used.
  * Backward: dout the gradient of o (read with PS_NORM_OUT), dh that of h (NULL: 0), h the forward's h as it is held (x
  *   where there was no branch; read with PS_NORM_OUT), y, gy, go and gate as the forward's. dx, dy in the rows' type
  *   (dy not used without a branch); dgy, dgo [d] f32 or NULL (PS_DW_ACCUMULATE adds to them; summed in a fixed order,
@@ -576,7 +577,8 @@ int ps_dropout_rows(int64_t N, int d, int dtype, const void* x, int64_t ldx, con
  * Outputs may be inputs (same pointer and pitch), else must not overlap them or each other.
  * Workspace: none for the forward; 256 bytes for a backward without gain gradients, else
  *   ps_residual_norm_workspace_size(d).
- * Limits: 1 <= d, rows of at most 32768 bytes (16384 bf16 or 8192 f32 columns), finite scales, eps >= 0.
+ * Limits: 1 <= d, rows of at most 32768 bytes (16384 bf16 or 8192 f32 columns; of rows that are not whole 16 bytes at
+ *   16-byte boundaries 16370 and 8186, else PS_ERR_UNSUPPORTED), finite scales, eps >= 0.
  * ------------------------------------------------------------------------- */
 enum { PS_NORM_BRANCH = 1, PS_NORM_OUT = 2 };
 int ps_residual_norm_fwd(int64_t N, int d, int dtype, int norms, const void* x, int64_t ldx,

@@ -14,29 +14,6 @@
 
 namespace psk {
 
-// Two f32 in one register pair: an instruction for both.
-struct F2 {
-  unsigned long long v;
-};
-static __device__ __forceinline__ F2 pair2(float x, float y) {
-  F2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
-  return r;
-}
-static __device__ __forceinline__ void split2(F2 a, float& x, float& y) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(a.v));
-}
-static __device__ __forceinline__ F2 mul2(F2 a, F2 b) {
-  F2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-static __device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-  F2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
-
 // The 16 values of a lane as eight pairs to be turned together: a[j] holds the first members of pairs 2 j and 2 j + 1, b[j]
 // the second ones. Half: the pairs are (lo[i], hi[i]) of the lane's two runs of eight; even: (v[2 i], v[2 i + 1]).
 template <bool EVEN>

@@ -13,23 +13,32 @@ namespace psk {
 
 //   n = y r_y gy (r_y = (mean y^2 + eps)^(-1/2); without the branch's norm y gy), h = a x + b gate n, o = h r_h go.
 //   backward: dH = dh + r_h (go do - h r_h^2 mean(go do h)), dx = a dH, dn = b gate dH, dgy = sum dn y r_y,
-//   dgo = sum do h r_h, dy = r_y (gy dn - y r_y^2 mean(gy dn y)), dgate = b sum dH n = b r_y sum gy dH y: the
-//   row's sums are two rounds, three sums (h^2, go do h, y^2) and then one (gy dH y), which dy's mean and dgate share.
+//   dgo = sum do h r_h, dy = r_y (gy dn - y r_y^2 mean(gy dn y)), dgate = b sum dH n = b r_y sum gy dH y. That last sum, which
+//   dy's mean and dgate share, is sum gy y dh + r_h (sum gy y go do - r_h^2 mean(go do h) sum gy y h), so that all of a
+//   backward row's sums are one round of six. (The forward's are two: h's squares from sums over x and y would cancel.)
 // HBM-bound: each input is read once and each output written once. A row lies on a team of threads (part of a warp, a
-// warp, or some), CH chunks of eight values each, the same columns of every row, so that the gains' gradients stay in its
-// registers over all rows. Rows come through a ring in shared memory that a thread's own copies fill ST rows ahead: what a
-// thread reads is what it copied, so only the sums cross threads.
+// warp, or some), CH chunks of 16 bytes each, the same columns of every row, so that the gains and their gradients stay
+// in its registers over all rows. Rows come through a ring in shared memory that a thread's own copies fill some rows
+// ahead: what a thread reads is what it copied, so only the sums cross threads; a row's first sums are taken beside the
+// outputs of the row before it, so that their way through the team is hidden.
+// Rows that do not start at 16-byte boundaries or have no whole chunks (SHIFT): a chunk is the columns from one
+// 16-byte boundary to the next, so the first and last chunks reach over the row's ends; a thread keeps its columns as its rows are
+// a multiple of eight apart, whose starts lie alike.
 constexpr int kNormThreads = 512;   // at most
 __host__ __device__ constexpr int norm_arrays(bool bwd) { return bwd ? 4 : 2; }   // h, y, do, dh; x, y
-// Rows ahead: as many as lie in shared memory beside what the registers allow of threads.
-__host__ __device__ constexpr int norm_stages(int e, int ch, bool bwd, bool vec) { return !vec ? 1 : ch * e <= 4 ? 3 : bwd ? 1 : 2; }
+// Rows in shared memory: as many as fit beside what the registers allow of threads.
+__host__ __device__ constexpr int norm_stages(int ch, bool bwd) { return ch <= 2 ? 3 : bwd ? 1 : 2; }
 
 struct NormArgs {
   int64_t N;
-  int d, chunks;                  // chunks of eight columns
+  int d, chunks;                  // chunks of 16 bytes a row
   int team, teams;                // threads per row, and teams of a block
   const void *in[4];              // forward: x, y; backward: h, y, do, dh (nullptr: absent)
   int64_t ld[4];
+  int copied;                     // bits of the arrays whose rows come by copies: those there are, but `apart`
+  int apart;                      // SHIFT: bits of the arrays (inputs, then outputs from bit 4) whose rows lie otherwise
+  const void* like;               // SHIFT: the array that the others lie like, and its pitch
+  int64_t ld_like;
   const void *gy, *go;            // gains [d], nullptr: 1
   const float* gate;              // [N], nullptr: 1
   int post, pre;                  // a norm of the branch; a normed output (or its gradient)
@@ -41,287 +50,459 @@ struct NormArgs {
   float* part;                    // backward: [blocks][2][d] partial gain gradients (dgy, dgo), nullptr without
 };
 
-template <class T, int CH, bool BWD, bool VEC>
-__global__ void __launch_bounds__(kNormThreads, BWD ? 1 : 2) norm_kernel(const NormArgs a) {
-  constexpr int A = norm_arrays(BWD), ST = norm_stages(sizeof(T), CH, BWD, VEC);
-  constexpr int P = VEC ? sizeof(T) / 2 : 1;      // 16-byte pieces of a chunk
+// Two columns: in the forward the two f32 of one instruction (60000 rows of 3584 bf16, post norm and gate, 306 -> 295 us), in the
+// backward plain ones, whose registers the packed ones' pairs would overrun (515 / 537 us).
+struct Plain2 {
+  float x, y;
+};
+static __device__ __forceinline__ Plain2 mul2(Plain2 a, Plain2 b) { return {a.x * b.x, a.y * b.y}; }
+static __device__ __forceinline__ Plain2 fma2(Plain2 a, Plain2 b, Plain2 c) { return {fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)}; }
+static __device__ __forceinline__ void split2(Plain2 a, float& x, float& y) { x = a.x, y = a.y; }
+template <bool PACKED>
+struct PairOf;
+template <>
+struct PairOf<true> {
+  using type = F2;
+  static __device__ __forceinline__ F2 two(float x, float y) { return pair2(x, y); }
+};
+template <>
+struct PairOf<false> {
+  using type = Plain2;
+  static __device__ __forceinline__ Plain2 two(float x, float y) { return {x, y}; }
+};
+template <int E, class P2>
+struct Vals {   // a chunk's columns
+  P2 p[E / 2];
+};
+template <class P2>
+static __device__ __forceinline__ float sum2(P2 v) {
+  float x, y;
+  split2(v, x, y);
+  return x + y;
+}
+
+// Bytes of a thread in a stage. (A piece's threads lie side by side: a warp's copies to places apart are fetched a piece at a
+// time, half a sector each, 147 instead of 125 us for a backward of 12000 rows of 3584 bf16.)
+__host__ __device__ constexpr int norm_thread_bytes(int ch, bool bwd) { return norm_arrays(bwd) * ch * 16; }   // (and 4 for the row's gate)
+
+template <class T, int CH, bool BWD, bool SHIFT>
+__global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a) {
+  constexpr int A = norm_arrays(BWD), ST = norm_stages(CH, BWD), BYTES = norm_thread_bytes(CH, BWD);
+  constexpr int E = 16 / static_cast<int>(sizeof(T));             // columns of a chunk
+  using P2 = typename PairOf<!BWD>::type;
+  using V8 = Vals<E, P2>;
+  auto two = [](float x, float y) { return PairOf<!BWD>::two(x, y); };
+  constexpr bool PIPE = ST > 1;   // the next row's first sums are taken beside a row's outputs
+  constexpr bool kHeld = CH <= 2;                                          // gains in registers
+  constexpr int K = BWD ? 6 : 1;                                           // sums of a first round
   extern __shared__ __align__(128) uint8_t norm_smem[];
-  __shared__ float4 red[2][kNormThreads / 32];
-  const int threads = blockDim.x, tid = threadIdx.x;
+  __shared__ __align__(16) float red[2][2][kNormThreads / 32 * 8];
+  const int threads = blockDim.x, tid = threadIdx.x, lane = tid & 31;
   const int unit_threads = a.team > 32 ? a.team : 32;             // what goes through the rows together
   const int unit_in = tid / unit_threads, units_here = threads / unit_threads;
-  const int t = tid % a.team, sub = a.team < 32 ? (tid & 31) / a.team : 0;
+  const int t = tid % a.team, sub = a.team < 32 ? lane / a.team : 0;
   const int rows_a_unit = a.team < 32 ? 32 / a.team : 1;
   const int64_t units = (a.N + rows_a_unit - 1) / rows_a_unit, stride = static_cast<int64_t>(gridDim.x) * units_here;
-  int parity = 0;
+  const int64_t u0 = static_cast<int64_t>(blockIdx.x) * units_here + unit_in;
+  const int stage_bytes = threads * BYTES;
+  const int step = threads * 16;   // from one of a thread's pieces to the next
+  uint8_t* const mine = norm_smem + tid * 16;
+  const P2 zero2 = two(0.f, 0.f);
+  auto row_of = [&](int64_t u) { return u * rows_a_unit + sub; };
 
-  // the sums of K values over a team, the same bits in each of its threads
-  auto team_sum = [&](auto& v) {
-    constexpr int K = sizeof(v) / sizeof(float);
+  // this thread's columns: chunk j begins at col(j)
+  int shift = 0;
+  if (SHIFT)
+    shift = static_cast<int>((reinterpret_cast<uintptr_t>(a.like) + static_cast<uint64_t>(row_of(u0)) * a.ld_like * sizeof(T)) & 15) /
+            static_cast<int>(sizeof(T));
+  auto col = [&](int j) { return E * (j * a.team + t) - shift; };
+  auto some = [&](int j) { return SHIFT ? col(j) < a.d : j * a.team + t < a.chunks; };
+  auto all = [&](int j) { return SHIFT ? col(j) >= 0 && col(j) + E <= a.d : some(j); };
+  const int apart_j = E * a.team;   // columns from a chunk to the next
+
+  // A round of sums over a team, the same bits in each of its threads: publish() by all, sync(), then totals(). Two rounds that
+  // follow each other have different places (which, parity). Six sums: a warp's lanes first share the values out among them,
+  // four lanes a value, which takes 9 exchanges instead of 30.
+  const int warps = a.team / 32, w0 = unit_in * (a.team > 256 ? 16 : 8);
+  auto publish = [&](float (&v)[K], int which, int parity) {
+    if (K > 1 && a.team >= 32) {
+      float x[8];
 #pragma unroll
-    for (int o = 16; o >= 1; o >>= 1)
-      if (a.team > o)
+      for (int i = 0; i < 8; ++i) x[i] = i < K ? v[i < K ? i : 0] : 0.f;
 #pragma unroll
-        for (int i = 0; i < K; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-    if (a.team > 32) {
-      const int w0 = unit_in * (a.team / 32);
-      if ((tid & 31) == 0) red[parity][tid >> 5] = make_float4(v[0], K > 1 ? v[K > 1 ? 1 : 0] : 0.f, K > 2 ? v[K > 2 ? 2 : 0] : 0.f, 0.f);
-      asm volatile("bar.sync %0, %1;" ::"r"(unit_in + 1), "r"(a.team) : "memory");
-      float s[3] = {0.f, 0.f, 0.f};
-      for (int w = 0; w < a.team / 32; ++w) {
-        const float4 r = red[parity][w0 + w];
-        s[0] += r.x, s[1] += r.y, s[2] += r.z;
+      for (int o = 4; o >= 1; o >>= 1) {
+        const bool up = lane & (4 * o);
+#pragma unroll
+        for (int i = 0; i < o; ++i) x[i] = (up ? x[i + o] : x[i]) + __shfl_xor_sync(0xffffffffu, up ? x[i] : x[i + o], 4 * o);
+      }
+      x[0] += __shfl_xor_sync(0xffffffffu, x[0], 2);
+      x[0] += __shfl_xor_sync(0xffffffffu, x[0], 1);
+      v[0] = x[0];   // of value lane / 4
+      if (a.team > 32 && (lane & 3) == 0) red[which][parity][(unit_in * warps + t / 32) * 8 + lane / 4] = x[0];
+    } else {
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1)
+        if (a.team > o)
+#pragma unroll
+          for (int i = 0; i < K; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+      if (K == 1 && a.team > 32 && lane == 0) red[which][parity][w0 + t / 32] = v[0];
+    }
+  };
+  auto sync = [&]() {
+    if (a.team > 32) asm volatile("bar.sync %0, %1;" ::"r"(unit_in + 1), "r"(a.team) : "memory");
+  };
+  auto totals = [&](float (&v)[K], int which, int parity) {
+    if (K > 1) {
+      if (a.team < 32) return;
+      float x = v[0];
+      int at = 4;                                 // lanes from a value to the next
+      if (a.team > 32) {
+        const int w = lane >> 3;
+        const float* from = red[which][parity] + (unit_in * warps + w) * 8 + (lane & 7);
+        x = w < warps ? from[0] : 0.f;
+#pragma unroll
+        for (int k = 1; k < 4; ++k)
+          if (4 * k < warps) x += w + 4 * k < warps ? from[32 * k] : 0.f;
+        x += __shfl_xor_sync(0xffffffffu, x, 8);
+        x += __shfl_xor_sync(0xffffffffu, x, 16);
+        at = 1;
       }
 #pragma unroll
-      for (int i = 0; i < K; ++i) v[i] = s[i];
-      parity ^= 1;   // (the next sum's barrier lies between this one's reads and the sum after it)
+      for (int i = 0; i < K; ++i) v[i] = __shfl_sync(0xffffffffu, x, i * at);
+    } else if (a.team > 32) {
+      const float4* from = reinterpret_cast<const float4*>(red[which][parity] + w0);   // (zeros behind the last warp)
+      const float4 x = from[0], y = from[1];
+      v[0] = ((x.x + x.y) + (x.z + x.w)) + ((y.x + y.y) + (y.z + y.w));
+      if (a.team > 256) {
+        const float4 z = from[2], w = from[3];
+        v[0] += ((z.x + z.y) + (z.z + z.w)) + ((w.x + w.y) + (w.z + w.w));
+      }
     }
   };
 
-  auto slot = [&](int st, int arr, int j, int p) {   // VEC: this thread's piece
-    return norm_smem + ((((st * A + arr) * CH + j) * P + p) * threads + tid) * 16;
+  // chunk j of an array's row in a stage
+  auto slot = [&](int st, int arr, int j) { return mine + st * stage_bytes + (arr * CH + j) * step; };
+  auto get = [&](int st, int arr, int j) {
+    V8 v;
+    const uint4 w = *reinterpret_cast<const uint4*>(slot(st, arr, j));
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i)
+      v.p[i] = E == 8 ? two(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u))
+                      : two(__uint_as_float(x[2 * i & 3]), __uint_as_float(x[(2 * i + 1) & 3]));
+    return v;
   };
-  auto cell = [&](int arr, int e) {                  // else: its element e = 8 j + i of the row
-    return reinterpret_cast<T*>(norm_smem) + (arr * CH * 8 + e) * threads + tid;
+  // what no copy reaches (absent arrays, chunks behind the row) reads as zeros
+  auto clear_row = [&](int st) {
+#pragma unroll 1
+    for (int i = 0; i < A * CH; ++i) *reinterpret_cast<uint4*>(mine + st * stage_bytes + i * step) = make_uint4(0, 0, 0, 0);
   };
-  auto column = [&](int j, int i) { return VEC ? (j * a.team + t) * 8 + i : (j * 8 + i) * a.team + t; };
-  auto in_chunk = [&](int j) { return VEC ? j * a.team + t < a.chunks : true; };
-  // the copies of a unit's row into a stage; a group for each, be it empty
+  // the row's gate, beside its pieces (loaded ahead into a register it is waited for where the loop hands it on: 346 instead of
+  // 271 us for a forward of 60000 rows of 3584 bf16)
+  float* const gates = reinterpret_cast<float*>(norm_smem + ST * stage_bytes) + tid;
+  for (int s = 0; s < ST; ++s) {
+    clear_row(s);
+    gates[s * threads] = 1.f;
+  }
+  if (!BWD) {
+    for (int i = tid; i < 4 * kNormThreads / 32 * 8; i += threads) (&red[0][0][0])[i] = 0.f;
+    __syncthreads();
+  }
+  // The copies of a unit's row into a stage; a group for each, be it empty.
   auto issue = [&](int64_t u, int st) {
-    const int64_t row = u * rows_a_unit + sub;
-    if (VEC) {
-      if (u < units && row < a.N) {
-#pragma unroll
-        for (int arr = 0; arr < A; ++arr) {
-          if (!a.in[arr]) continue;
-          const T* from = static_cast<const T*>(a.in[arr]) + row * a.ld[arr];
-#pragma unroll
-          for (int j = 0; j < CH; ++j) {
-            if (!in_chunk(j)) continue;
-#pragma unroll
-            for (int p = 0; p < P; ++p) lane_copy(smem_addr(slot(st, arr, j, p)), from + column(j, 0) + p * (16 / sizeof(T)));
-          }
-        }
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-  };
-  auto arrive = [&](int64_t row, bool live) {
-    if (VEC) {
-      asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
-    } else if (live) {
-      T v[A][CH * 8];
+    const int64_t row = row_of(u);
+    if (row < a.N) {
+      if (a.gate)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_addr(gates + st * threads)), "l"(a.gate + row) : "memory");
 #pragma unroll
       for (int arr = 0; arr < A; ++arr) {
-        const T* from = static_cast<const T*>(a.in[arr]) + row * a.ld[arr];
+        const T* from = static_cast<const T*>(a.in[arr]) + row * a.ld[arr] + (E * t - shift);
 #pragma unroll
-        for (int e = 0; e < CH * 8; ++e)
-          if (a.in[arr] && e * a.team + t < a.d) v[arr][e] = from[e * a.team + t];
-      }
-#pragma unroll
-      for (int arr = 0; arr < A; ++arr)
-#pragma unroll
-        for (int e = 0; e < CH * 8; ++e)
-          if (a.in[arr] && e * a.team + t < a.d) *cell(arr, e) = v[arr][e];
-    }
-  };
-  // eight values of an array's row, zeros where there is none
-  auto get = [&](int st, int arr, int j, bool live, float (&f)[8]) {
-    if (VEC) {
-      if (live && a.in[arr] && in_chunk(j)) {
-        if (sizeof(T) == 2) {
-          Raw8<Bf16> r;
-          r.load(reinterpret_cast<const Bf16*>(slot(st, arr, j, 0)));
-          r.get(f);
-        } else {
-          const float4 u = *reinterpret_cast<const float4*>(slot(st, arr, j, 0));
-          const float4 v = *reinterpret_cast<const float4*>(slot(st, arr, j, P - 1));
-          f[0] = u.x, f[1] = u.y, f[2] = u.z, f[3] = u.w;
-          f[4] = v.x, f[5] = v.y, f[6] = v.z, f[7] = v.w;
+        for (int j = 0; j < CH; ++j) {
+          const int c = col(j);
+          // a chunk with some of the row; beyond the first row's start and the last one's end it goes element by element
+          if (SHIFT ? c + E <= 0 || c >= a.d || (c < 0 && row == 0) || (c + E > a.d && row == a.N - 1) : !some(j)) continue;
+          if (a.copied >> arr & 1) lane_copy(smem_addr(slot(st, arr, j)), from + j * apart_j);
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = 0.f;
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = live && a.in[arr] && column(j, i) < a.d ? Elem<T>::get(*cell(arr, j * 8 + i)) : 0.f;
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // chunk j of a row, element by element: what its copies left out
+  auto load_plainly = [&](int64_t row, int st, int j) {
+#pragma unroll 1
+    for (int arr = 0; arr < A; ++arr) {
+      if (!a.in[arr] || ((a.copied >> arr & 1) && all(j))) continue;
+      const T* at = static_cast<const T*>(a.in[arr]) + row * a.ld[arr];
+#pragma unroll 1
+      for (int i = 0; i < E; ++i)
+        if (col(j) + i >= 0 && col(j) + i < a.d) reinterpret_cast<T*>(slot(st, arr, j))[i] = at[col(j) + i];
     }
   };
-  auto gains = [&](const void* g, int j, float (&f)[8]) {
-    const T* from = static_cast<const T*>(g);
-    if (VEC && g && in_chunk(j)) {
+  // a unit's row in its stage: the stages after it may still be under way
+  auto arrive = [&](int64_t row, int st, bool first) {
+    if (first || !PIPE)
+      asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
+    else
+      asm volatile("cp.async.wait_group %0;" ::"n"(PIPE ? ST - 2 : 0) : "memory");
+    if (row >= a.N) clear_row(st);
+    if (SHIFT && row < a.N) {
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        if (some(j) && ((a.apart & 15) || ((row == 0 || row == a.N - 1) && !all(j)))) load_plainly(row, st, j);
+        if (!some(j) || all(j)) continue;
+        uint32_t keep[4];   // of the row's end only its columns
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int c = col(j) + w * E / 4;
+          keep[w] = E == 8 ? (c >= 0 && c < a.d ? 0xffffu : 0u) | (c + 1 >= 0 && c + 1 < a.d ? 0xffff0000u : 0u)
+                           : c >= 0 && c < a.d ? 0xffffffffu : 0u;
+        }
+#pragma unroll
+        for (int arr = 0; arr < A; ++arr) {
+          uint4& v = *reinterpret_cast<uint4*>(slot(st, arr, j));
+          v = make_uint4(v.x & keep[0], v.y & keep[1], v.z & keep[2], v.w & keep[3]);
+        }
+      }
+    }
+  };
+  auto gains_at = [&](const void* g, int j) {
+    const T* at = static_cast<const T*>(g);
+    float f[8];
+    if (!SHIFT && g && E == 8 && all(j)) {
       Raw8<T> r;
-      r.load(from + column(j, 0));
+      r.load(at + col(j));
       r.get(f);
-    } else {
+    } else
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = !VEC && g && column(j, i) < a.d ? Elem<T>::get(from[column(j, i)]) : 1.f;
+    for (int i = 0; i < E; ++i) f[i] = g && col(j) + i >= 0 && col(j) + i < a.d ? Elem<T>::get(at[col(j) + i]) : 1.f;
+    V8 v;
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) v.p[i] = two(f[2 * i], f[2 * i + 1]);
+    return v;
+  };
+  auto put = [&](int which, int64_t row, int j, const V8& v) {
+    T* at = static_cast<T*>(which ? a.out1 : a.out0) + row * (which ? a.ldo1 : a.ldo0) + col(j);
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) split2(v.p[i], f[2 * i], f[2 * i + 1]);
+    if (all(j) && !(SHIFT && (a.apart >> (4 + which) & 1))) {
+      *reinterpret_cast<uint4*>(at) =
+          E == 8 ? make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4 % E], f[5 % E]),
+                              pack_bf16x2(f[6 % E], f[7 % E]))
+                 : make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    } else if (SHIFT && some(j)) {
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (col(j) + i >= 0 && col(j) + i < a.d) at[i] = Elem<T>::put(f[i]);
     }
   };
-  auto put = [&](void* base, int64_t ld, int64_t row, int j, const float (&f)[8]) {
-    T* to = static_cast<T*>(base) + row * ld;
-    if (VEC) {
-      if (in_chunk(j)) Raw8<T>::store(to + column(j, 0), f);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (column(j, i) < a.d) to[column(j, i)] = Elem<T>::put(f[i]);
-    }
-  };
-
-  float accy[BWD ? CH : 1][8], acco[BWD ? CH : 1][8];
-  if (BWD)
-#pragma unroll
-    for (int j = 0; j < CH; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) accy[j][i] = acco[j][i] = 0.f;
 
   wait_for_previous_kernel();
   let_next_kernel_in();
   if (BWD && a.status && blockIdx.x == 0 && tid == 0) clear_status(a.status);
-  const int64_t u0 = static_cast<int64_t>(blockIdx.x) * units_here + unit_in;
 #pragma unroll
   for (int s = 0; s < ST; ++s) issue(u0 + s * stride, s);
-  int st = 0;
-  for (int64_t u = u0; u < units; u += stride) {
-    const int64_t row = u * rows_a_unit + sub;
-    const bool live = row < a.N;
-    const float gate = live && a.gate ? __ldg(a.gate + row) : 1.f;
-    const bool open = live && a.in[1] && gate != 0.f;   // (a closed gate leaves the branch out whatever it holds)
-    arrive(row, live);
-    if (!BWD) {
-      float ry = 1.f;
-      if (a.post) {
-        float s[1] = {0.f};
+
+  V8 gy_r[kHeld ? CH : 1], go_r[kHeld ? CH : 1];
+  if (kHeld)
 #pragma unroll
-        for (int j = 0; j < CH; ++j) {
-          float y[8];
-          get(st, 1, j, live, y);
+    for (int j = 0; j < CH; ++j) {
+      gy_r[j] = gains_at(a.gy, j);
+      go_r[j] = gains_at(a.go, j);
+    }
+  auto gain_y = [&](int j) { return kHeld ? gy_r[kHeld ? j : 0] : gains_at(a.gy, j); };
+  auto gain_o = [&](int j) { return kHeld ? go_r[kHeld ? j : 0] : gains_at(a.go, j); };
+  V8 accy[BWD ? CH : 1], acco[BWD ? CH : 1];
+  if (BWD)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) s[0] = fmaf(y[i], y[i], s[0]);
-        }
-        team_sum(s);
-        ry = rsqrtf(fmaf(s[0], a.inv_d, a.eps));
-      }
-      const float w = a.b * gate * ry;
-      float h[CH][8], s[1] = {0.f};
+    for (int j = 0; j < CH; ++j)
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) accy[j].p[i] = acco[j].p[i] = zero2;
+
+  // the sums over a row as it comes in
+  auto first_sums = [&](int st, float (&s)[K]) {
+    if (BWD) {
+      P2 q2[6] = {zero2, zero2, zero2, zero2, zero2, zero2};
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
-        get(st, 0, j, live, h[j]);
-        if (a.in[1]) {
-          float y[8], g[8];
-          get(st, 1, j, open, y);
-          gains(a.gy, j, g);
+        const V8 h = get(st, 0, j), y = get(st, 1, j), q = get(st, BWD ? 2 : 0, j), dh = get(st, BWD ? 3 : 0, j);
+        const V8 gy = gain_y(j), go = gain_o(j);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) h[j][i] = fmaf(a.a, h[j][i], open ? w * (y[i] * g[i]) : 0.f);
-          if (live) put(a.out0, a.ldo0, row, j, h[j]);
+        for (int i = 0; i < E / 2; ++i) {
+          const P2 gq = mul2(go.p[i], q.p[i]), yg = mul2(gy.p[i], y.p[i]);
+          q2[0] = fma2(h.p[i], h.p[i], q2[0]);
+          q2[1] = fma2(gq, h.p[i], q2[1]);
+          q2[2] = fma2(y.p[i], y.p[i], q2[2]);
+          q2[3] = fma2(yg, dh.p[i], q2[3]);
+          q2[4] = fma2(yg, gq, q2[4]);
+          q2[5] = fma2(yg, h.p[i], q2[5]);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[0] = fmaf(h[j][i], h[j][i], s[0]);
       }
-      if (a.pre) {
-        team_sum(s);
-        const float rh = rsqrtf(fmaf(s[0], a.inv_d, a.eps));
+#pragma unroll
+      for (int i = 0; i < K; ++i) s[i] = sum2(q2[i]);
+    } else {
+      P2 q2 = zero2;
+      if (a.post)
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
-          float g[8];
-          gains(a.go, j, g);
+          const V8 y = get(st, 1, j);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) g[i] *= h[j][i] * rh;
-          if (live) put(a.out1, a.ldo1, row, j, g);
+          for (int i = 0; i < E / 2; ++i) q2 = fma2(y.p[i], y.p[i], q2);
+        }
+      s[0] = sum2(q2);
+    }
+  };
+
+  float s[K];
+  int st = 0, parity = 0;
+  if (u0 < units) {
+    arrive(row_of(u0), 0, true);
+    first_sums(0, s);
+    publish(s, 0, 0);
+    sync();
+    totals(s, 0, 0);
+  }
+  for (int64_t u = u0; u < units; u += stride) {
+    const int64_t row = row_of(u);
+    const bool live = row < a.N, more = u + stride < units;
+    const float gate = gates[st * threads];
+    const bool open = live && a.in[1] && gate != 0.f;   // (a closed gate leaves the branch out whatever it holds)
+    const int st_next = st + 1 == ST ? 0 : st + 1;
+    float s_next[K];
+    parity ^= 1;
+    if (PIPE && more) {
+      arrive(row_of(u + stride), st_next, false);
+      first_sums(st_next, s_next);
+      publish(s_next, 0, parity);
+    }
+    if (!BWD) {
+      const float ry = a.post ? rsqrtf(fmaf(s[0], a.inv_d, a.eps)) : 1.f;
+      const P2 w2 = two(a.b * gate * ry, a.b * gate * ry), a2 = two(a.a, a.a);
+      V8 h[CH];
+      P2 q = zero2;
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        h[j] = get(st, 0, j);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) h[j].p[i] = mul2(h[j].p[i], a2);
+        if (open) {
+          const V8 y = get(st, 1, j), g = gain_y(j);
+#pragma unroll
+          for (int i = 0; i < E / 2; ++i) h[j].p[i] = fma2(mul2(y.p[i], w2), g.p[i], h[j].p[i]);
+        }
+        if (live && a.in[1]) put(0, row, j, h[j]);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) q = fma2(h[j].p[i], h[j].p[i], q);
+      }
+      float sh[K] = {sum2(q)};
+      publish(sh, 1, parity);
+      issue(u + ST * stride, st);   // (the stage has been read: its values went into what was published)
+      sync();
+      if (a.pre) {
+        totals(sh, 1, parity);
+        const float rh = rsqrtf(fmaf(sh[0], a.inv_d, a.eps));
+        const P2 r2 = two(rh, rh);
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+          const V8 g = gain_o(j);
+          V8 o;
+#pragma unroll
+          for (int i = 0; i < E / 2; ++i) o.p[i] = mul2(mul2(h[j].p[i], r2), g.p[i]);
+          if (live) put(1, row, j, o);
         }
       }
     } else {
-      float s[3] = {0.f, 0.f, 0.f};
-      if (a.pre || a.post) {
-#pragma unroll
-        for (int j = 0; j < CH; ++j) {
-          float h[8], y[8], q[8], g[8];
-          get(st, 0, j, live, h);
-          get(st, 1, j, live, y);
-          get(st, 2, j, live, q);
-          gains(a.go, j, g);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            s[0] = fmaf(h[i], h[i], s[0]);
-            s[1] = fmaf(g[i] * q[i], h[i], s[1]);
-            s[2] = fmaf(y[i], y[i], s[2]);
-          }
-        }
-        team_sum(s);
-      }
-      const float rh = a.pre ? rsqrtf(fmaf(s[0], a.inv_d, a.eps)) : 0.f, m = s[1] * a.inv_d * rh * rh;
-      const float ry = a.post ? rsqrtf(fmaf(s[2], a.inv_d, a.eps)) : 1.f;
-      float dH[CH][8], dot[1] = {0.f};
+      const float rh = a.pre ? rsqrtf(fmaf(s[0], a.inv_d, a.eps)) : 0.f, m = -s[K > 1 ? 1 : 0] * a.inv_d * rh * rh;
+      const float ry = a.post ? rsqrtf(fmaf(s[K > 2 ? 2 : 0], a.inv_d, a.eps)) : 1.f;
+      const float dot = s[K > 3 ? 3 : 0] + rh * fmaf(m, s[K > 5 ? 5 : 0], s[K > 4 ? 4 : 0]);   // of gy dH y
+      const float w = a.b * gate * ry, k = a.post ? -dot * a.inv_d * ry * ry * w : 0.f;
+      const P2 r2 = two(rh, rh), m2 = two(m, m), a2 = two(a.a, a.a), w2 = two(w, w), k2 = two(k, k);
+      if (a.dgate && live && t == 0) a.dgate[row] = a.b * ry * dot;
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
-        get(st, 3, j, live, dH[j]);
-        if (a.pre) {
-          float h[8], q[8], g[8];
-          get(st, 0, j, live, h);
-          get(st, 2, j, live, q);
-          gains(a.go, j, g);
+        V8 dH = get(st, BWD ? 3 : 0, j);
+        {
+          const V8 h = get(st, 0, j), q = get(st, BWD ? 2 : 0, j), g = gain_o(j);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            dH[j][i] = fmaf(rh, fmaf(h[i], -m, g[i] * q[i]), dH[j][i]);
-            acco[j][i] += live ? q[i] * (h[i] * rh) : 0.f;
+          for (int i = 0; i < E / 2; ++i) {
+            dH.p[i] = fma2(r2, fma2(h.p[i], m2, mul2(g.p[i], q.p[i])), dH.p[i]);
+            acco[BWD ? j : 0].p[i] = fma2(q.p[i], mul2(h.p[i], r2), acco[BWD ? j : 0].p[i]);
           }
         }
-        if (a.dgate || a.post) {
-          float y[8], g[8];
-          get(st, 1, j, live, y);
-          gains(a.gy, j, g);
+        V8 v;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) dot[0] = fmaf(g[i] * dH[j][i], y[i], dot[0]);
-        }
-        float v[8];
+        for (int i = 0; i < E / 2; ++i) v.p[i] = mul2(a2, dH.p[i]);
+        if (live) put(0, row, j, v);
+        if (open) {
+          const V8 y = get(st, 1, j), g = gain_y(j);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = a.a * dH[j][i];
-        if (live) put(a.out0, a.ldo0, row, j, v);
-      }
-      if (a.in[1]) {
-        if (a.dgate || a.post) team_sum(dot);
-        if (a.dgate && live && t == 0) a.dgate[row] = a.b * ry * dot[0];
-        const float w = a.b * gate * ry, k = a.post ? dot[0] * a.inv_d * ry * ry : 0.f;
-#pragma unroll
-        for (int j = 0; j < CH; ++j) {
-          float y[8], g[8];
-          get(st, 1, j, open, y);
-          gains(a.gy, j, g);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            accy[j][i] += open ? w * dH[j][i] * y[i] : 0.f;
-            y[i] = open ? w * fmaf(y[i], -k, g[i] * dH[j][i]) : 0.f;
+          for (int i = 0; i < E / 2; ++i) {
+            const P2 dn = mul2(w2, dH.p[i]);
+            accy[BWD ? j : 0].p[i] = fma2(dn, y.p[i], accy[BWD ? j : 0].p[i]);
+            v.p[i] = fma2(k2, y.p[i], mul2(g.p[i], dn));
           }
-          if (live) put(a.out1, a.ldo1, row, j, y);
+          put(1, row, j, v);
+        } else if (live && a.in[1]) {
+#pragma unroll
+          for (int i = 0; i < E / 2; ++i) v.p[i] = zero2;
+          put(1, row, j, v);
         }
       }
+      issue(u + ST * stride, st);   // (the stage has been read: its values went into what was stored)
+      if (PIPE) sync();
     }
-    issue(u + ST * stride, st);   // (the stage has been read: its values went into what was stored)
-    st = st + 1 == ST ? 0 : st + 1;
+    if (more) {
+      if (!PIPE) {
+        arrive(row_of(u + stride), st_next, false);
+        first_sums(st_next, s_next);
+        publish(s_next, 0, parity);
+        sync();
+      }
+      totals(s_next, 0, parity);
+#pragma unroll
+      for (int i = 0; i < K; ++i) s[i] = s_next[i];
+    }
+    st = st_next;
   }
   if (!BWD || a.part == nullptr) return;
 
   // gain gradients: over a warp's rows, then the block's units in order; norm_gain_sum_kernel adds the blocks'
   asm volatile("cp.async.wait_group 0;" ::: "memory");
   __syncthreads();
-  float* mine = reinterpret_cast<float*>(norm_smem) + static_cast<size_t>(unit_in) * 2 * a.d;
+  float* sums = reinterpret_cast<float*>(norm_smem) + static_cast<size_t>(unit_in) * 2 * a.d;
+  if (SHIFT) {   // (a warp's rows may have different columns; those without a row have none)
+    for (int c = tid % unit_threads; c < 2 * a.d; c += unit_threads) sums[c] = 0.f;
+    __syncthreads();
+  }
+  for (int k = 0; k < (SHIFT ? rows_a_unit : 1); ++k) {
+    if (!SHIFT || sub == k)
 #pragma unroll
-  for (int j = 0; j < CH; ++j)
+      for (int j = 0; j < CH; ++j)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float v = accy[BWD ? j : 0][i], w = acco[BWD ? j : 0][i];
-      for (int o = 16; o >= a.team; o >>= 1) {
-        v += __shfl_xor_sync(0xffffffffu, v, o);
-        w += __shfl_xor_sync(0xffffffffu, w, o);
-      }
-      const int c = column(j, i);
-      if (sub == 0 && c < a.d) {
-        mine[c] = v;
-        mine[a.d + c] = w;
-      }
-    }
+        for (int i = 0; i < E; ++i) {
+          float v[2], w[2];
+          split2(accy[BWD ? j : 0].p[i / 2], v[0], v[1]);
+          split2(acco[BWD ? j : 0].p[i / 2], w[0], w[1]);
+          const int c = col(j) + i;
+          if (SHIFT) {
+            if (c >= 0 && c < a.d) {
+              sums[c] += v[i & 1];
+              sums[a.d + c] += w[i & 1];
+            }
+          } else {
+            for (int o = 16; o >= a.team; o >>= 1) {
+              v[i & 1] += __shfl_xor_sync(0xffffffffu, v[i & 1], o);
+              w[i & 1] += __shfl_xor_sync(0xffffffffu, w[i & 1], o);
+            }
+            if (sub == 0 && c < a.d) {
+              sums[c] = v[i & 1];
+              sums[a.d + c] = w[i & 1];
+            }
+          }
+        }
+    if (SHIFT) __syncwarp();
+  }
   __syncthreads();
   float* part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.d;
   for (int c = tid; c < 2 * a.d; c += threads) {
@@ -362,11 +543,10 @@ struct NormPlan {
   int ch, team, teams, threads, blocks_a_sm;
   size_t smem;
 };
-// Threads of 32 bytes of a row each, up to 512 to a row, then more bytes each.
-static NormPlan norm_plan(int d, int e, bool bwd, bool vec) {
+// Threads of two chunks of a row each (of few chunks: one), up to 512 to a row, then four each.
+static NormPlan norm_plan(int chunks, int d, bool bwd) {
   NormPlan p;
-  const int chunks = (d + 7) / 8, unit = 32 / (8 * e) > 0 ? 32 / (8 * e) : 1;   // bf16 2, f32 1
-  p.ch = chunks <= 32 ? 1 : unit;
+  p.ch = chunks <= 32 ? 1 : 2;
   while ((chunks + p.ch - 1) / p.ch > kNormThreads) p.ch *= 2;
   const int need = (chunks + p.ch - 1) / p.ch;
   if (need <= 32) {
@@ -378,45 +558,52 @@ static NormPlan norm_plan(int d, int e, bool bwd, bool vec) {
   const int unit_threads = p.team > 32 ? p.team : 32;
   p.teams = 256 / unit_threads > 1 ? 256 / unit_threads : 1;
   p.threads = p.teams * unit_threads;
-  p.smem = static_cast<size_t>(norm_stages(e, p.ch, bwd, vec)) * norm_arrays(bwd) * p.ch * 8 * e * p.threads;
+  p.smem = static_cast<size_t>(norm_stages(p.ch, bwd)) * (norm_thread_bytes(p.ch, bwd) + 4) * p.threads;
   const size_t sums = bwd ? static_cast<size_t>(p.teams) * 2 * d * sizeof(float) : 0;
   if (p.smem < sums) p.smem = sums;
-  p.blocks_a_sm = (bwd ? 512 : 1024) / p.threads;
+  p.blocks_a_sm = 512 / p.threads;
   const int fit = static_cast<int>(kSmemOfSm / (p.smem + 2048));
   if (p.blocks_a_sm > fit) p.blocks_a_sm = fit;
   if (p.blocks_a_sm < 1) p.blocks_a_sm = 1;
   return p;
 }
 
-template <class T, int CH, bool BWD, bool VEC>
+template <class T, int CH, bool BWD, bool SHIFT>
 static int launch_norm(NormArgs& a, const NormPlan& p, int& grid, cudaStream_t s) {
-  auto kern = norm_kernel<T, CH, BWD, VEC>;
+  auto kern = norm_kernel<T, CH, BWD, SHIFT>;
   if (p.smem > 40 * 1024 &&   // (beside the block's own)
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(p.smem)) != cudaSuccess)
     return PS_ERR_CUDA;
   const int rows_a_unit = a.team < 32 ? 32 / a.team : 1;
-  const int64_t units = (a.N + rows_a_unit - 1) / rows_a_unit, want = (units + p.teams - 1) / p.teams;
-  int64_t most = static_cast<int64_t>(num_sms_current()) * p.blocks_a_sm;
+  const int64_t units = (a.N + rows_a_unit - 1) / rows_a_unit;
+  int64_t want = (units + p.teams - 1) / p.teams, most = static_cast<int64_t>(num_sms_current()) * p.blocks_a_sm;
   if (BWD && most > kNormMaxBlocks) most = kNormMaxBlocks;
+  if (SHIFT) {   // units a multiple of eight, so that a thread's rows start alike
+    want = (want + 7) / 8 * 8;
+    most = most > 8 ? most / 8 * 8 : 8;
+  }
   grid = static_cast<int>(want < most ? want : most);
+  a.copied = 0;
+  for (int i = 0; i < 4; ++i)
+    if (a.in[i] && !(SHIFT && (a.apart >> i & 1))) a.copied |= 1 << i;
   return launch_after(kern, dim3(static_cast<unsigned>(grid)), static_cast<unsigned>(p.threads), p.smem, s, 1, 1, true, a) ==
                  cudaSuccess
              ? PS_OK
              : PS_ERR_CUDA;
 }
 template <class T, bool BWD>
-static int run_norm(NormArgs a, bool vec, int& grid, cudaStream_t s) {
-  const NormPlan p = norm_plan(a.d, sizeof(T), BWD, vec);
-  a.chunks = (a.d + 7) / 8, a.team = p.team, a.teams = p.teams;
+static int run_norm(NormArgs a, bool shift, int& grid, cudaStream_t s) {
+  constexpr int E = 16 / static_cast<int>(sizeof(T));
+  a.chunks = shift ? (a.d + 2 * E - 2) / E : a.d / E;   // at the largest shift
+  if (a.chunks > 4 * kNormThreads) return PS_ERR_UNSUPPORTED;
+  const NormPlan p = norm_plan(a.chunks, a.d, BWD);
+  a.team = p.team, a.teams = p.teams;
   a.inv_d = 1.f / static_cast<float>(a.d);
   switch (p.ch) {
-    case 1: return vec ? launch_norm<T, 1, BWD, true>(a, p, grid, s) : launch_norm<T, 1, BWD, false>(a, p, grid, s);
-    case 2: return vec ? launch_norm<T, 2, BWD, true>(a, p, grid, s) : launch_norm<T, 2, BWD, false>(a, p, grid, s);
-    default: break;
+    case 1: return shift ? launch_norm<T, 1, BWD, true>(a, p, grid, s) : launch_norm<T, 1, BWD, false>(a, p, grid, s);
+    case 2: return shift ? launch_norm<T, 2, BWD, true>(a, p, grid, s) : launch_norm<T, 2, BWD, false>(a, p, grid, s);
+    default: return shift ? launch_norm<T, 4, BWD, true>(a, p, grid, s) : launch_norm<T, 4, BWD, false>(a, p, grid, s);
   }
-  if constexpr (sizeof(T) == 2)   // (f32 rows of 8192 columns take two chunks)
-    return vec ? launch_norm<T, 4, BWD, true>(a, p, grid, s) : launch_norm<T, 4, BWD, false>(a, p, grid, s);
-  return PS_ERR_UNSUPPORTED;
 }
 
 }  // namespace psk
@@ -429,18 +616,30 @@ bool norm_sizes_ok(int64_t N, int d, int dtype, int norms, double a, double b, d
   return N >= 0 && d >= 1 && (dtype == PS_DTYPE_BF16 || dtype == PS_DTYPE_F32) && d <= kNormMaxBytes / elem_bytes(dtype) &&
          !(norms & ~(PS_NORM_BRANCH | PS_NORM_OUT)) && isfinite(a) && isfinite(b) && eps >= 0.0 && isfinite(eps);
 }
-struct NormRows {   // the tensors of a call: placed on their elements, and all rows on 16-byte boundaries or not
-  int e, d;
-  bool ok = true, vec;
-  NormRows(int d_, int dtype) : e(elem_bytes(dtype)), d(d_), vec(d_ % 8 == 0) {}
-  void rows(const void* p, int64_t ld) {
+// The tensors of a call: on their elements' boundaries, and whether all rows lie on 16-byte boundaries, or like each other.
+struct NormRows {
+  const int64_t N;
+  const int e, d;
+  bool ok = true, whole;
+  const void* like = nullptr;
+  int64_t ld_like = 0;
+  int apart = 0;
+  NormRows(int64_t N_, int d_, int dtype) : N(N_), e(elem_bytes(dtype)), d(d_), whole(d_ * e % 16 == 0) {}
+  void rows(const void* p, int64_t ld, int bit) {
     ok = ok && p && ld >= d && reinterpret_cast<uintptr_t>(p) % e == 0;
-    vec = vec && al16(p) && ld * e % 16 == 0;
+    whole = whole && al16(p) && (N == 1 || ld * e % 16 == 0);
+    if (!like) like = p, ld_like = ld;
+    auto start = [&](const void* v, int64_t l, int64_t row) {
+      return (reinterpret_cast<uintptr_t>(v) + static_cast<uint64_t>(row) * static_cast<uint64_t>(l) * e) % 16;
+    };
+    // the first two rows decide all
+    if (start(p, ld, 0) != start(like, ld_like, 0) || (N > 1 && start(p, ld, 1) != start(like, ld_like, 1))) apart |= 1 << bit;
   }
   void gains(const void* p) {
     ok = ok && reinterpret_cast<uintptr_t>(p) % e == 0;
-    vec = vec && al16(p);
+    whole = whole && al16(p);
   }
+  void into(NormArgs& a) const { a.apart = apart, a.like = like, a.ld_like = ld_like; }
 };
 
 }  // namespace
@@ -455,15 +654,15 @@ int ps_residual_norm_fwd(int64_t N, int d, int dtype, int norms, const void* x, 
   if (N == 0) return PS_OK;
   const bool out = norms & PS_NORM_OUT;
   if (!y && ((norms & PS_NORM_BRANCH) || gate || !out)) return PS_ERR_INVALID_ARG;   // a branch's norm or gate without one
-  NormRows r(d, dtype);
-  r.rows(x, ldx);
+  NormRows r(N, d, dtype);
+  r.rows(x, ldx, 0);
   if (y) {
-    r.rows(y, ldy);
-    r.rows(h, ldh);
+    r.rows(y, ldy, 1);
+    r.rows(h, ldh, 4);
     r.gains(gy);
   }
   if (out) {
-    r.rows(o, ldo);
+    r.rows(o, ldo, 5);
     r.gains(go);
   }
   if (!r.ok || reinterpret_cast<uintptr_t>(gate) % 4) return PS_ERR_INVALID_ARG;
@@ -472,11 +671,12 @@ int ps_residual_norm_fwd(int64_t N, int d, int dtype, int norms, const void* x, 
   a.in[0] = x, a.in[1] = y, a.ld[0] = ldx, a.ld[1] = ldy;
   a.gy = gy, a.go = go, a.gate = gate;
   a.post = (norms & PS_NORM_BRANCH) ? 1 : 0, a.pre = out ? 1 : 0;
-  a.a = static_cast<float>(res_scale), a.b = static_cast<float>(branch_scale), a.eps = static_cast<float>(eps);
+  r.into(a);
+  a.a = y ? static_cast<float>(res_scale) : 1.f, a.b = static_cast<float>(branch_scale), a.eps = static_cast<float>(eps);
   a.out0 = h, a.out1 = o, a.ldo0 = ldh, a.ldo1 = ldo;
   int grid;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  return dtype == PS_DTYPE_F32 ? run_norm<float, false>(a, r.vec, grid, s) : run_norm<Bf16, false>(a, r.vec, grid, s);
+  return dtype == PS_DTYPE_F32 ? run_norm<float, false>(a, !r.whole, grid, s) : run_norm<Bf16, false>(a, !r.whole, grid, s);
 }
 
 size_t ps_residual_norm_workspace_size(int d) {
@@ -498,19 +698,19 @@ int ps_residual_norm_bwd(int64_t N, int d, int dtype, int norms, const void* dou
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   auto aligned4 = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; };
   if (!aligned4(gate) || !aligned4(dgate) || !aligned4(dgy) || !aligned4(dgo)) return PS_ERR_INVALID_ARG;
-  NormRows r(d, dtype);
+  NormRows r(N, d, dtype);
   if (N > 0) {
     if (!out && !dh) return PS_ERR_INVALID_ARG;   // no gradient comes in
-    r.rows(dx, lddx);
+    r.rows(dx, lddx, 4);
     if (out) {
-      r.rows(dout, lddo);
-      r.rows(h, ldh);
+      r.rows(dout, lddo, 2);
+      r.rows(h, ldh, 0);
       r.gains(go);
     }
-    if (dh) r.rows(dh, lddh);
+    if (dh) r.rows(dh, lddh, 3);
     if (y) {
-      r.rows(y, ldy);
-      r.rows(dy, lddy);
+      r.rows(y, ldy, 1);
+      r.rows(dy, lddy, 5);
       r.gains(gy);
     }
     if (!r.ok) return PS_ERR_INVALID_ARG;
@@ -530,13 +730,14 @@ int ps_residual_norm_bwd(int64_t N, int d, int dtype, int norms, const void* dou
   a.gy = gy, a.go = go, a.gate = gate;
   a.post = (norms & PS_NORM_BRANCH) ? 1 : 0, a.pre = out ? 1 : 0;
   // without a branch the stream is x itself, whatever the scales
+  r.into(a);
   a.a = y ? static_cast<float>(res_scale) : 1.f, a.b = static_cast<float>(branch_scale), a.eps = static_cast<float>(eps);
   a.out0 = dx, a.out1 = dy, a.ldo0 = lddx, a.ldo1 = lddy;
   a.dgate = dgate;
   a.status = static_cast<uint32_t*>(ws);
   a.part = gains ? reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + kWsHeader) : nullptr;
   int grid = 0;
-  rc = dtype == PS_DTYPE_F32 ? run_norm<float, true>(a, r.vec, grid, s) : run_norm<Bf16, true>(a, r.vec, grid, s);
+  rc = dtype == PS_DTYPE_F32 ? run_norm<float, true>(a, !r.whole, grid, s) : run_norm<Bf16, true>(a, !r.whole, grid, s);
   if (rc != PS_OK) return refused(rc, ws, s);
   if (!gains) return PS_OK;
   return launch_after(norm_gain_sum_kernel, dim3(static_cast<unsigned>((2 * d + 7) / 8)), 256, 0, s, 1, 1, true, d, grid, a.part,
