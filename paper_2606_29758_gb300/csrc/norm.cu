@@ -24,6 +24,10 @@ namespace psk {
 // Rows that do not start at 16-byte boundaries or have no whole chunks (SHIFT): a chunk is the columns from one
 // 16-byte boundary to the next, so the first and last chunks reach over the row's ends; a thread keeps its columns as its rows are
 // a multiple of eight apart, whose starts lie alike.
+// EXACT (bf16 forwards with the branch's norm of up to kExactValues values): h is the nearest f32 of the sum rounded to bf16, whatever the order of the
+// row's sums: y gy is exact in f32, the root and the scales are kept in two f32 each, and a value whose f32 sum lies next to the
+// middle of two bf16 values is settled by the roundings that it left. Otherwise a few of 10^5 values are rounded to the other
+// neighbour, which in sums over few rows of the backward (dgo) shows as ten times f32's error.
 constexpr int kNormThreads = 512;   // at most
 __host__ __device__ constexpr int norm_arrays(bool bwd) { return bwd ? 4 : 2; }   // h, y, do, dh; x, y
 // Rows in shared memory: as many as fit beside what the registers allow of threads.
@@ -43,6 +47,7 @@ struct NormArgs {
   const float* gate;              // [N], nullptr: 1
   int post, pre;                  // a norm of the branch; a normed output (or its gradient)
   float a, b, eps, inv_d;
+  float a_lo, b_lo, eps_lo, inv_d_lo;   // EXACT: what f32 leaves of them
   void *out0, *out1;              // forward: h, o; backward: dx, dy
   int64_t ldo0, ldo1;
   float* dgate;
@@ -58,6 +63,13 @@ struct Plain2 {
 static __device__ __forceinline__ Plain2 mul2(Plain2 a, Plain2 b) { return {a.x * b.x, a.y * b.y}; }
 static __device__ __forceinline__ Plain2 fma2(Plain2 a, Plain2 b, Plain2 c) { return {fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)}; }
 static __device__ __forceinline__ void split2(Plain2 a, float& x, float& y) { x = a.x, y = a.y; }
+static __device__ __forceinline__ Plain2 add2(Plain2 a, Plain2 b) { return {__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y)}; }
+static __device__ __forceinline__ F2 add2(F2 a, F2 b) {   // (a packed addition after a packed product would be taken as one fma)
+  float x, y, u, v;
+  split2(a, x, y);
+  split2(b, u, v);
+  return pair2(__fadd_rn(x, u), __fadd_rn(y, v));
+}
 template <bool PACKED>
 struct PairOf;
 template <>
@@ -85,7 +97,25 @@ static __device__ __forceinline__ float sum2(P2 v) {
 // time, half a sector each, 147 instead of 125 us for a backward of 12000 rows of 3584 bf16.)
 __host__ __device__ constexpr int norm_thread_bytes(int ch, bool bwd) { return norm_arrays(bwd) * ch * 16; }   // (and 4 for the row's gate)
 
-template <class T, int CH, bool BWD, bool SHIFT>
+// h + l of two f32: with h' + l' (the sums' lower parts added plainly).
+static __device__ __forceinline__ void add_two(float& h, float& l, float h2, float l2) {
+  const float s = h + h2, b = s - h;
+  l = (l + l2) + ((h - (s - b)) + (h2 - b));
+  h = s;
+}
+// a x + w n to the nearest f32: a and w of two parts each, the sum's and the products' roundings taken back.
+static __device__ __forceinline__ float settled(float a, float a_lo, float x, float w, float w_lo, float n) {
+  const float ax = __fmul_rn(a, x), p = __fmul_rn(w, n), s = __fadd_rn(ax, p), b = s - ax;
+  const float left = ((ax - (s - b)) + (p - b)) + (fmaf(w, n, -p) + fmaf(a, x, -ax) + fmaf(w_lo, n, a_lo * x));
+  return s + left;
+}
+// Whether v, of |a x| and a like share, lies within their roundings of the middle of two bf16 values.
+static __device__ __forceinline__ bool in_the_middle(float v, float ax) {
+  const float m = __uint_as_float((__float_as_uint(v) & 0xffff0000u) | 0x8000u);
+  return fabsf(v - m) <= 2.4e-7f * (fabsf(v) + fabsf(ax));   // 2^-22
+}
+
+template <class T, int CH, bool BWD, bool SHIFT, bool EXACT>
 __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a) {
   constexpr int A = norm_arrays(BWD), ST = norm_stages(CH, BWD), BYTES = norm_thread_bytes(CH, BWD);
   constexpr int E = 16 / static_cast<int>(sizeof(T));             // columns of a chunk
@@ -94,7 +124,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
   auto two = [](float x, float y) { return PairOf<!BWD>::two(x, y); };
   constexpr bool PIPE = ST > 1;   // the next row's first sums are taken beside a row's outputs
   constexpr bool kHeld = CH <= 2;                                          // gains in registers
-  constexpr int K = BWD ? 6 : 1;                                           // sums of a first round
+  constexpr int K = BWD ? 6 : EXACT ? 2 : 1;                               // sums of a first round
   extern __shared__ __align__(128) uint8_t norm_smem[];
   __shared__ __align__(16) float red[2][2][kNormThreads / 32 * 8];
   const int threads = blockDim.x, tid = threadIdx.x, lane = tid & 31;
@@ -125,7 +155,15 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
   // four lanes a value, which takes 9 exchanges instead of 30.
   const int warps = a.team / 32, w0 = unit_in * (a.team > 256 ? 16 : 8);
   auto publish = [&](float (&v)[K], int which, int parity) {
-    if (K > 1 && a.team >= 32) {
+    if (EXACT) {
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1)
+        if (a.team > o) add_two(v[0], v[K - 1], __shfl_xor_sync(0xffffffffu, v[0], o), __shfl_xor_sync(0xffffffffu, v[K - 1], o));
+      if (a.team > 32 && lane == 0) {
+        red[which][parity][2 * (w0 + t / 32)] = v[0];
+        red[which][parity][2 * (w0 + t / 32) + 1] = v[K - 1];
+      }
+    } else if (BWD && a.team >= 32) {
       float x[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = i < K ? v[i < K ? i : 0] : 0.f;
@@ -145,14 +183,27 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
         if (a.team > o)
 #pragma unroll
           for (int i = 0; i < K; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-      if (K == 1 && a.team > 32 && lane == 0) red[which][parity][w0 + t / 32] = v[0];
+      if (!BWD && a.team > 32 && lane == 0) red[which][parity][w0 + t / 32] = v[0];
     }
   };
   auto sync = [&]() {
     if (a.team > 32) asm volatile("bar.sync %0, %1;" ::"r"(unit_in + 1), "r"(a.team) : "memory");
   };
   auto totals = [&](float (&v)[K], int which, int parity) {
-    if (K > 1) {
+    if (EXACT) {
+      if (a.team <= 32) return;
+      const float4* from = reinterpret_cast<const float4*>(red[which][parity] + 2 * w0);   // (zeros behind the last warp)
+      float4 x = from[0];
+      v[0] = x.x, v[K - 1] = x.y;
+      add_two(v[0], v[K - 1], x.z, x.w);
+#pragma unroll
+      for (int i = 1; i < 8; ++i) {
+        if (i >= 4 && a.team <= 256) break;
+        x = from[i];
+        add_two(v[0], v[K - 1], x.x, x.y);
+        add_two(v[0], v[K - 1], x.z, x.w);
+      }
+    } else if (BWD) {
       if (a.team < 32) return;
       float x = v[0];
       int at = 4;                                 // lanes from a value to the next
@@ -343,6 +394,22 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
       for (int i = 0; i < K; ++i) s[i] = sum2(q2[i]);
     } else {
       P2 q2 = zero2;
+      if (EXACT) {
+        s[0] = s[K - 1] = 0.f;
+        if (a.post)
+#pragma unroll
+          for (int j = 0; j < CH; ++j) {
+            const V8 y = get(st, 1, j);
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+              float u, v;
+              split2(y.p[i], u, v);
+              add_two(s[0], s[K - 1], u * u, 0.f);   // (a square of eight bits is exact)
+              add_two(s[0], s[K - 1], v * v, 0.f);
+            }
+          }
+        return;
+      }
       if (a.post)
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
@@ -377,25 +444,63 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
       publish(s_next, 0, parity);
     }
     if (!BWD) {
-      const float ry = a.post ? rsqrtf(fmaf(s[0], a.inv_d, a.eps)) : 1.f;
-      const P2 w2 = two(a.b * gate * ry, a.b * gate * ry), a2 = two(a.a, a.a);
+      float ry = 1.f, w = a.b * gate, w_lo = 0.f;
+      if (!EXACT) {
+        ry = a.post ? rsqrtf(fmaf(s[0], a.inv_d, a.eps)) : 1.f;
+        w *= ry;
+      } else {
+        w_lo = fmaf(a.b, gate, -w) + a.b_lo * gate;
+        if (a.post) {
+          // the mean and eps, the inverse root by a step from its approximation r (1 - v r^2 without cancelling), times the scales
+          float v = s[0] * a.inv_d, v_lo = fmaf(s[0], a.inv_d, -v) + (s[0] * a.inv_d_lo + s[K - 1] * a.inv_d);
+          add_two(v, v_lo, a.eps, a.eps_lo);
+          ry = rsqrtf(v);
+          const float q = ry * ry;
+          const float left = fmaf(-v, q, 1.f) - fmaf(v, fmaf(ry, ry, -q), v_lo * q);
+          const float r_lo = 0.5f * ry * left, wr = w * ry;
+          w_lo = fmaf(w, ry, -wr) + fmaf(w, r_lo, w_lo * ry);
+          w = wr;
+        }
+      }
+      const P2 w2 = two(w, w), a2 = two(a.a, a.a);
       V8 h[CH];
       P2 q = zero2;
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
-        h[j] = get(st, 0, j);
+        const V8 x = get(st, 0, j);
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) h[j].p[i] = mul2(h[j].p[i], a2);
+        for (int i = 0; i < E / 2; ++i) h[j].p[i] = mul2(x.p[i], a2);
         if (open) {
           const V8 y = get(st, 1, j), g = gain_y(j);
 #pragma unroll
-          for (int i = 0; i < E / 2; ++i) h[j].p[i] = fma2(mul2(y.p[i], w2), g.p[i], h[j].p[i]);
+          // (the product rounded before the sum: scales like 0.7 then give sums of few bits what they give in decimals)
+          for (int i = 0; i < E / 2; ++i) h[j].p[i] = add2(h[j].p[i], mul2(mul2(y.p[i], g.p[i]), w2));
+          if (EXACT) {
+            bool near = false;
+            float hv[E], xv[E], nv[E];
+#pragma unroll
+            for (int i = 0; i < E / 2; ++i) {
+              split2(h[j].p[i], hv[2 * i], hv[2 * i + 1]);
+              split2(x.p[i], xv[2 * i], xv[2 * i + 1]);
+              near |= in_the_middle(hv[2 * i], a.a * xv[2 * i]) || in_the_middle(hv[2 * i + 1], a.a * xv[2 * i + 1]);
+            }
+            if (near) {
+#pragma unroll
+              for (int i = 0; i < E / 2; ++i) {
+                split2(mul2(y.p[i], g.p[i]), nv[2 * i], nv[2 * i + 1]);
+#pragma unroll
+                for (int k = 2 * i; k < 2 * i + 2; ++k)
+                  if (in_the_middle(hv[k], a.a * xv[k])) hv[k] = settled(a.a, a.a_lo, xv[k], w, w_lo, nv[k]);
+                h[j].p[i] = two(hv[2 * i], hv[2 * i + 1]);
+              }
+            }
+          }
         }
         if (live && a.in[1]) put(0, row, j, h[j]);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) q = fma2(h[j].p[i], h[j].p[i], q);
       }
-      float sh[K] = {sum2(q)};
+      float sh[K] = {sum2(q)};   // (EXACT: the second part 0)
       publish(sh, 1, parity);
       issue(u + ST * stride, st);   // (the stage has been read: its values went into what was published)
       sync();
@@ -568,9 +673,9 @@ static NormPlan norm_plan(int chunks, int d, bool bwd) {
   return p;
 }
 
-template <class T, int CH, bool BWD, bool SHIFT>
-static int launch_norm(NormArgs& a, const NormPlan& p, int& grid, cudaStream_t s) {
-  auto kern = norm_kernel<T, CH, BWD, SHIFT>;
+template <class T, int CH, bool BWD, bool SHIFT, bool EXACT>
+static int launch_as(NormArgs& a, const NormPlan& p, int& grid, cudaStream_t s) {
+  auto kern = norm_kernel<T, CH, BWD, SHIFT, EXACT>;
   if (p.smem > 40 * 1024 &&   // (beside the block's own)
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(p.smem)) != cudaSuccess)
     return PS_ERR_CUDA;
@@ -591,6 +696,14 @@ static int launch_norm(NormArgs& a, const NormPlan& p, int& grid, cudaStream_t s
              ? PS_OK
              : PS_ERR_CUDA;
 }
+// Up to here the forward's sums are exact (EXACT above).
+constexpr int64_t kExactValues = 1 << 25;
+template <class T, int CH, bool BWD, bool SHIFT>
+static int launch_norm(NormArgs& a, const NormPlan& p, int& grid, cudaStream_t s) {
+  if constexpr (!BWD && sizeof(T) == 2)
+    if (a.in[1] && a.post && a.N <= kExactValues / a.d) return launch_as<T, CH, BWD, SHIFT, true>(a, p, grid, s);
+  return launch_as<T, CH, BWD, SHIFT, false>(a, p, grid, s);
+}
 template <class T, bool BWD>
 static int run_norm(NormArgs a, bool shift, int& grid, cudaStream_t s) {
   constexpr int E = 16 / static_cast<int>(sizeof(T));
@@ -598,7 +711,8 @@ static int run_norm(NormArgs a, bool shift, int& grid, cudaStream_t s) {
   if (a.chunks > 4 * kNormThreads) return PS_ERR_UNSUPPORTED;
   const NormPlan p = norm_plan(a.chunks, a.d, BWD);
   a.team = p.team, a.teams = p.teams;
-  a.inv_d = 1.f / static_cast<float>(a.d);
+  a.inv_d = static_cast<float>(1.0 / a.d);
+  a.inv_d_lo = static_cast<float>(1.0 / a.d - a.inv_d);
   switch (p.ch) {
     case 1: return shift ? launch_norm<T, 1, BWD, true>(a, p, grid, s) : launch_norm<T, 1, BWD, false>(a, p, grid, s);
     case 2: return shift ? launch_norm<T, 2, BWD, true>(a, p, grid, s) : launch_norm<T, 2, BWD, false>(a, p, grid, s);
@@ -673,6 +787,8 @@ int ps_residual_norm_fwd(int64_t N, int d, int dtype, int norms, const void* x, 
   a.post = (norms & PS_NORM_BRANCH) ? 1 : 0, a.pre = out ? 1 : 0;
   r.into(a);
   a.a = y ? static_cast<float>(res_scale) : 1.f, a.b = static_cast<float>(branch_scale), a.eps = static_cast<float>(eps);
+  a.a_lo = y ? static_cast<float>(res_scale - a.a) : 0.f;
+  a.b_lo = static_cast<float>(branch_scale - a.b), a.eps_lo = static_cast<float>(eps - a.eps);
   a.out0 = h, a.out1 = o, a.ldo0 = ldh, a.ldo1 = ldo;
   int grid;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
