@@ -174,6 +174,7 @@ _calls = None
 class _Ordinary:
     """In the place of the module of small calls: every call is left to the holder's ordinary way, through ctypes."""
     qk_plan = ffn_plan = dropout_rows = qk_fwd = qk_bwd = ffn_fwd = ffn_bwd = staticmethod(lambda *a: None)
+    norm_plan = norm_fwd = norm_bwd = cache_plan = append = decode_plan = decode = staticmethod(lambda *a: None)
 
 
 def calls():
@@ -191,6 +192,8 @@ def calls():
         loader.exec_module(module)
         module.bind(*(ctypes.cast(f, _vp).value for f in (L.ps_dropout_rows, L.ps_qk_norm_rope_fwd, L.ps_qk_norm_rope_bwd,
                                                           L.ps_gated_ffn_fwd, L.ps_gated_ffn_bwd)))
+        module.bind_more(*(ctypes.cast(f, _vp).value for f in (L.ps_residual_norm_fwd, L.ps_residual_norm_bwd, L.ps_paged_append,
+                                                               L.ps_paged_decode)))
         _calls = module
     return _calls
 

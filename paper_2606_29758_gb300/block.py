@@ -345,6 +345,12 @@ class ResidualNorm:
             self.dgy, self.dgo = torch.empty(s.d, **f32), torch.empty(s.d, **f32)
             self.dgate = torch.empty(s.rows, **f32)
             self.ws = torch.zeros(B.ps_residual_norm_workspace_size(s.d), dtype=torch.uint8, device=device)
+        calls = B.calls()
+        self._fast_fwd, self._fast_bwd = calls.norm_fwd, calls.norm_bwd
+        kept = [self.h, self.o] + ([self.dx, self.dy, self.dgy, self.dgo, self.dgate, self.ws] if s.train else [None] * 6)
+        self._plan = calls.norm_plan(s.rows, s.d, code, self._with[2], self._alone[2], *self._scales,
+                                     *(0 if t is None else t.data_ptr() for t in kept), 0 if self.ws is None else self.ws.numel(),
+                                     _index(self._at))
 
     def _row(self, name, t, N):
         """Address and pitch of rows; (None, 0) of none."""
@@ -359,21 +365,37 @@ class ResidualNorm:
     def forward(self, x, y=None, gy=None, go=None, gate=None, out=None):
         """(h, o), o None without the output's norm; h in `out` if given (it may be x or y). Without a branch h is x itself."""
         s = self.s
+        rc = self._fast_fwd(self._plan, x, y, gy, go, gate, out)
         N = _row_count("x", x, s.rows)
         h = x if y is None else _first(self.h, N) if out is None else out
         o = _first(self.o, N) if s.pre else None
-        if y is None and (gy is not None or gate is not None or out is not None):
-            raise ValueError("a branch's gain, its gate or a place for the sum without a branch")
-        rc = self._fwd(N, *(self._alone if y is None else self._with), *self._row("x", x, N), *self._row("y", y, N),
-                       self._gain("gy", gy), self._gain("go", go), self._gate(gate, N), *self._scales, *self._row("out", h, N),
-                       *((None, 0) if o is None else (o.data_ptr(), s.d)), _launched_on(self._at))
+        if rc is None:
+            rc = self._forward(N, x, y, gy, go, gate, out, h, o)
         if rc:
             B._check(rc, "ps_residual_norm_fwd")
         return h, o
 
+    def _forward(self, N, x, y, gy, go, gate, out, h, o):
+        if y is None and (gy is not None or gate is not None or out is not None):
+            raise ValueError("a branch's gain, its gate or a place for the sum without a branch")
+        return self._fwd(N, *(self._alone if y is None else self._with), *self._row("x", x, N), *self._row("y", y, N),
+                         self._gain("gy", gy), self._gain("go", go), self._gate(gate, N), *self._scales, *self._row("out", h, N),
+                         *((None, 0) if o is None else (o.data_ptr(), self.s.d)), _launched_on(self._at))
+
     def backward(self, do, dh, h, y=None, gy=None, go=None, gate=None, dw_accumulate: bool = False):
         """(dx, dy, dgy, dgo, dgate) from the gradients of o (None without the output's norm) and of h (None: 0), the forward's h
         and the branch; what the forward did not have is None."""
+        s = self.s
+        rc = self._fast_bwd(self._plan, do, dh, h, y, gy, go, gate, dw_accumulate)
+        if rc is None:
+            rc = self._backward(do, dh, h, y, gy, go, gate, dw_accumulate)
+        if rc:
+            B._check(rc, "ps_residual_norm_bwd")
+        N = (dh if do is None else do).shape[0]
+        return (_first(self.dx, N), None if y is None else _first(self.dy, N), None if y is None else self.dgy,
+                self.dgo if s.pre else None, None if gate is None else _first(self.dgate, N))
+
+    def _backward(self, do, dh, h, y, gy, go, gate, dw_accumulate):
         s = self.s
         if not s.train:
             raise RuntimeError("built without a backward (train=False)")
@@ -384,15 +406,16 @@ class ResidualNorm:
         if y is None and (gy is not None or gate is not None):
             raise ValueError("a branch's gain or its gate without a branch")
         N = _row_count("dh" if do is None else "do", dh if do is None else do, s.rows)
-        dx, dy = _first(self.dx, N), None if y is None else _first(self.dy, N)
-        dgy, dgo, dgate = (None if y is None else self.dgy), (self.dgo if s.pre else None), None
-        if gate is not None:
-            dgate = _first(self.dgate, N)
-        rc = self._bwd(N, *(self._alone if y is None else self._with), *self._row("do", do, N), *self._row("dh", dh, N),
-                       *self._row("h", h if s.pre else None, N), *self._row("y", y, N), self._gain("gy", gy), self._gain("go", go),
-                       self._gate(gate, N), *self._scales, dx.data_ptr(), s.d, *((None, 0) if dy is None else (dy.data_ptr(), s.d)),
-                       *(None if t is None else t.data_ptr() for t in (dgy, dgo, dgate)),
-                       B.PS_DW_ACCUMULATE if dw_accumulate else 0, self.ws.data_ptr(), self.ws.numel(), _launched_on(self._at))
-        if rc:
-            B._check(rc, "ps_residual_norm_bwd")
-        return dx, dy, dgy, dgo, dgate
+        at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        branch = y is not None
+        return self._bwd(N, *(self._with if branch else self._alone), *self._row("do", do, N), *self._row("dh", dh, N),
+                         *self._row("h", h if s.pre else None, N), *self._row("y", y, N), self._gain("gy", gy),
+                         self._gain("go", go), self._gate(gate, N), *self._scales, at(self.dx), s.d,
+                         *((at(self.dy), s.d) if branch else (None, 0)), at(self.dgy) if branch else None,
+                         at(self.dgo) if s.pre else None, None if gate is None else at(self.dgate),
+                         B.PS_DW_ACCUMULATE if dw_accumulate else 0, self.ws.data_ptr(), self.ws.numel(), _launched_on(self._at))
+
+    def check_status(self):
+        """Raise PsppoError if the backward's workspace reports a device-side error."""
+        if self.ws is not None:
+            _status("residual norm", self.ws)

@@ -14,7 +14,7 @@ from typing import Optional
 import torch
 
 from . import _binding as B
-from .block import _first, _launched_on, _pitch, _row_count, _status, _whole
+from .block import _first, _index, _launched_on, _pitch, _row_count, _status, _whole
 
 
 @dataclass
@@ -32,7 +32,7 @@ class CacheShape:
 class PagedCache:
     """k and v [layers][pages][Hk][page][D], table [seqs][max_len / page] and lengths [seqs] on the device (ps_paged_append).
 
-    The table and the lengths may be written by the caller; or reserve() gives sequences pages, share() lets completions
+    The table and the lengths may be written by the caller, in place; or reserve() gives sequences pages, share() lets completions
     have their prompt's pages without a copy, and release() takes a finished sequence's back."""
 
     def __init__(self, shape: CacheShape, device: str = "cuda"):
@@ -42,9 +42,9 @@ class PagedCache:
         self.s, self.device = s, device
         self.width = -(-s.max_len // s.page)
         t, i32 = dict(dtype=s.dtype, device=device), dict(dtype=torch.int32, device=device)
-        self.k, self.v = (torch.empty(s.layers, s.pages, s.Hk, s.page, s.D, **t) for _ in range(2))
-        self.table = torch.full((s.seqs, self.width), -1, **i32)
-        self.lengths = torch.zeros(s.seqs, **i32)
+        self._k, self._v = (torch.empty(s.layers, s.pages, s.Hk, s.page, s.D, **t) for _ in range(2))
+        self._table = torch.full((s.seqs, self.width), -1, **i32)
+        self._lengths = torch.zeros(s.seqs, **i32)
         self.ws = torch.zeros(256, dtype=torch.uint8, device=device)
         self._at = self.k.device
         self._layers = [(k.data_ptr(), v.data_ptr()) for k, v in zip(self.k, self.v)]
@@ -53,6 +53,18 @@ class PagedCache:
         self._free = list(range(s.pages - 1, -1, -1))
         self._users = [0] * s.pages          # sequences that have a page
         self._own = [[] for _ in range(s.seqs)]
+        calls = B.calls()
+        self._fast = calls.append
+        self._plan = calls.cache_plan(s.seqs, s.Hk, s.D, self._code, s.layers, s.pages, s.page, self.width,
+                                      self.k.stride(0) * self.k.element_size(),
+                                      *(t.data_ptr() for t in (self.k, self.v, self.table, self.lengths, self.ws)),
+                                      self.ws.numel(), _index(self._at))
+
+    # (written in place: the calls have their addresses)
+    k = property(lambda self: self._k)
+    v = property(lambda self: self._v)
+    table = property(lambda self: self._table)
+    lengths = property(lambda self: self._lengths)
 
     def _layer(self, layer: int):
         if not 0 <= layer < self.s.layers:
@@ -61,14 +73,16 @@ class PagedCache:
 
     def append(self, layer: int, k, v, row_seq, row_pos, pos_base: int = 1):
         """Rows of k and v [N][Hk * D] to positions row_pos - pos_base of sequences row_seq (-1: the row is passed by)."""
-        s, at = self.s, self._at
-        if k.dim() != 2:
-            raise ValueError(f"k: need [N][{s.Hk * s.D}], got {tuple(k.shape)}")
-        N, w = k.shape[0], s.Hk * s.D
-        rc = self._append(N, s.seqs, s.Hk, s.D, self._code, k.data_ptr(), _pitch("k", k, N, w, s.dtype, at), v.data_ptr(),
-                          _pitch("v", v, N, w, s.dtype, at), _whole("row_seq", row_seq, (N,), torch.int32, at),
-                          _whole("row_pos", row_pos, (N,), torch.int32, at), pos_base, self.table.data_ptr(), self.width, s.pages,
-                          s.page, *self._layer(layer), self.ws.data_ptr(), self.ws.numel(), _launched_on(at))
+        rc = self._fast(self._plan, layer, k, v, row_seq, row_pos, pos_base)
+        if rc is None:
+            s, at = self.s, self._at
+            if k.dim() != 2:
+                raise ValueError(f"k: need [N][{s.Hk * s.D}], got {tuple(k.shape)}")
+            N, w = k.shape[0], s.Hk * s.D
+            rc = self._append(N, s.seqs, s.Hk, s.D, self._code, k.data_ptr(), _pitch("k", k, N, w, s.dtype, at), v.data_ptr(),
+                              _pitch("v", v, N, w, s.dtype, at), _whole("row_seq", row_seq, (N,), torch.int32, at),
+                              _whole("row_pos", row_pos, (N,), torch.int32, at), pos_base, self.table.data_ptr(), self.width,
+                              s.pages, s.page, *self._layer(layer), self.ws.data_ptr(), self.ws.numel(), _launched_on(at))
         if rc:
             B._check(rc, "ps_paged_append")
 
@@ -157,10 +171,22 @@ class DecodeAttention:
         self._at = self.o.device
         self._code = B.dtype_code(self.o)
         self.ws = torch.zeros(max(256, B.ps_paged_decode_workspace_size(s.D)), dtype=torch.uint8, device=device)
+        calls = B.calls()
+        self._fast = calls.decode
+        self._plan = calls.decode_plan(s.seqs, s.Hq, s.Hk, s.D, self._code, s.window, self._scale, self.o.data_ptr(),
+                                       self.ws.data_ptr(), self.ws.numel(), _index(self._at))
 
     def forward(self, q, cache: PagedCache, layer: int = 0, out=None, lse=None):
         """o [n][Hq * D] (in `out` if given; it may be q) of the first n = q.shape[0] sequences; lse f32 [n][Hq] is written if
         given. A sequence of length 0 gives zeros."""
+        rc = self._fast(self._plan, cache._plan, layer, q, out, lse)
+        if rc is None:
+            rc = self._forward(q, cache, layer, out, lse)
+        if rc:
+            B._check(rc, "ps_paged_decode")
+        return _first(self.o, q.shape[0]) if out is None else out
+
+    def _forward(self, q, cache, layer, out, lse):
         s, c, at = self.s, cache.s, self._at
         if (c.Hk, c.D, c.dtype) != (s.Hk, s.D, s.dtype):
             raise ValueError(f"the cache holds {c.Hk} heads of {c.D} in {c.dtype}, built for {s.Hk} of {s.D} in {s.dtype}")
@@ -168,14 +194,11 @@ class DecodeAttention:
             raise ValueError(f"the cache is on {cache._at}, the call's other buffers are on {at}")
         n, w = _row_count("q", q, min(s.seqs, c.seqs)), s.Hq * s.D
         o = _first(self.o, n) if out is None else out
-        rc = self._call(n, s.Hq, s.Hk, s.D, self._code, q.data_ptr(), _pitch("q", q, n, w, s.dtype, at), *cache._layer(layer),
-                        c.pages, c.page, cache.table.data_ptr(), cache.width, cache.lengths.data_ptr(), s.window, self._scale,
-                        o.data_ptr(), w if out is None else _pitch("out", out, n, w, s.dtype, at),
-                        None if lse is None else _whole("lse", lse, (n, s.Hq), torch.float32, at), self.ws.data_ptr(),
-                        self.ws.numel(), _launched_on(at))
-        if rc:
-            B._check(rc, "ps_paged_decode")
-        return o
+        return self._call(n, s.Hq, s.Hk, s.D, self._code, q.data_ptr(), _pitch("q", q, n, w, s.dtype, at), *cache._layer(layer),
+                          c.pages, c.page, cache.table.data_ptr(), cache.width, cache.lengths.data_ptr(), s.window, self._scale,
+                          o.data_ptr(), w if out is None else _pitch("out", out, n, w, s.dtype, at),
+                          None if lse is None else _whole("lse", lse, (n, s.Hq), torch.float32, at), self.ws.data_ptr(),
+                          self.ws.numel(), _launched_on(at))
 
     def check_status(self):
         """Raise PsppoError if the last call reports a device-side error."""

@@ -21,6 +21,10 @@ decltype(&ps_qk_norm_rope_fwd) qk_fwd_fn = nullptr;
 decltype(&ps_qk_norm_rope_bwd) qk_bwd_fn = nullptr;
 decltype(&ps_gated_ffn_fwd) ffn_fwd_fn = nullptr;
 decltype(&ps_gated_ffn_bwd) ffn_bwd_fn = nullptr;
+decltype(&ps_residual_norm_fwd) norm_fwd_fn = nullptr;
+decltype(&ps_residual_norm_bwd) norm_bwd_fn = nullptr;
+decltype(&ps_paged_append) append_fn = nullptr;
+decltype(&ps_paged_decode) decode_fn = nullptr;
 
 ps_stream_t stream() { return reinterpret_cast<ps_stream_t>(c10::cuda::getCurrentCUDAStream().stream()); }
 
@@ -291,6 +295,201 @@ PyObject* ffn_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+struct NormPlan {
+  static constexpr char kName[] = "psppo.norm_plan";
+  int64_t rows;
+  int d, dtype, with, alone;      // `with` a branch and without one: the call's norms
+  double res_scale, branch_scale, eps;
+  void *h, *o, *dx, *dy, *ws;
+  float *dgy, *dgo, *dgate;
+  size_t ws_bytes;
+  int device = -1;
+  at::ScalarType type() const { return dtype == PS_DTYPE_F32 ? at::kFloat : at::kBFloat16; }
+};
+
+PyObject* norm_plan(PyObject*, PyObject* args) {
+  NormPlan p;
+  unsigned long long v[9];
+  long long rows_;
+  if (!PyArg_ParseTuple(args, "LiiiidddKKKKKKKKK|i", &rows_, &p.d, &p.dtype, &p.with, &p.alone, &p.res_scale, &p.branch_scale, &p.eps,
+                        &v[0], &v[1], &v[2], &v[3], &v[4], &v[5], &v[6], &v[7], &v[8], &p.device))
+    return nullptr;
+  p.rows = rows_;
+  void** const to[8] = {&p.h, &p.o, &p.dx, &p.dy, reinterpret_cast<void**>(&p.dgy), reinterpret_cast<void**>(&p.dgo),
+                        reinterpret_cast<void**>(&p.dgate), &p.ws};
+  for (int i = 0; i < 8; ++i) *to[i] = reinterpret_cast<void*>(v[i]);
+  p.ws_bytes = static_cast<size_t>(v[8]);
+  return capsule(p);
+}
+
+// Rows, or none of them.
+bool maybe_rows(PyObject* o, const NormPlan& p, int64_t N, Rows& r) { return o == Py_None || rows(o, p.device, N, p.d, p.type(), r); }
+// a[0..2] = gy, go, gate (None: 1).
+bool norm_gains(const NormPlan& p, PyObject* const* a, int64_t N, const void* (&g)[3]) {
+  for (int i = 0; i < 3; ++i) {
+    g[i] = nullptr;
+    if (a[i] != Py_None && !(i < 2 ? whole(a[i], p.device, p.d, p.type(), &g[i]) : whole(a[i], p.device, N, at::kFloat, &g[i])))
+      return false;
+  }
+  return true;
+}
+
+// (plan, x, y, gy, go, gate, out), all but x None where absent -> status or None
+PyObject* norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    const NormPlan* p = n == 7 ? plan_of<NormPlan>(a[0]) : nullptr;
+    const at::Tensor* x = p ? tensor(a[1], p->device) : nullptr;
+    if (!x || x->dim() != 2 || x->size(0) > p->rows) return ordinary();
+    const int64_t N = x->size(0);
+    const bool branch = a[2] != Py_None;
+    Rows rx, ry, rh;
+    const void* g[3];
+    if (!rows(a[1], p->device, N, p->d, p->type(), rx) || !maybe_rows(a[2], *p, N, ry) || !norm_gains(*p, a + 3, N, g) ||
+        (!branch && (g[0] || g[2] || a[6] != Py_None)) || !maybe_rows(a[6], *p, N, rh))
+      return ordinary();
+    if (a[6] == Py_None) {
+      rh.at = branch ? p->h : rx.at;
+      rh.ld = branch ? p->d : rx.ld;
+    }
+    return PyLong_FromLong(norm_fwd_fn(N, p->d, p->dtype, branch ? p->with : p->alone, rx.at, rx.ld, ry.at, ry.ld, g[0], g[1],
+                                       static_cast<const float*>(g[2]), p->res_scale, p->branch_scale, p->eps, rh.at, rh.ld, p->o,
+                                       p->o ? p->d : 0, stream()));
+  });
+}
+
+// (plan, do, dh, h, y, gy, go, gate, dw_accumulate), None where absent -> status or None
+PyObject* norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    const NormPlan* p = n == 9 ? plan_of<NormPlan>(a[0]) : nullptr;
+    if (!p || !p->dx || (a[1] == Py_None) != (p->o == nullptr) || (a[1] == Py_None && a[2] == Py_None)) return ordinary();
+    const at::Tensor* first = tensor(a[1] == Py_None ? a[2] : a[1], p->device);
+    if (!first || first->dim() != 2 || first->size(0) > p->rows || !PyBool_Check(a[8])) return ordinary();
+    const int64_t N = first->size(0);
+    const bool branch = a[4] != Py_None;
+    Rows rdo, rdh, rh, ry;
+    const void* g[3];
+    if (!maybe_rows(a[1], *p, N, rdo) || !maybe_rows(a[2], *p, N, rdh) || (p->o && !rows(a[3], p->device, N, p->d, p->type(), rh)) ||
+        !maybe_rows(a[4], *p, N, ry) || !norm_gains(*p, a + 5, N, g) || (!branch && (g[0] || g[2])))
+      return ordinary();
+    return PyLong_FromLong(norm_bwd_fn(N, p->d, p->dtype, branch ? p->with : p->alone, rdo.at, rdo.ld, rdh.at, rdh.ld, rh.at, rh.ld,
+                                       ry.at, ry.ld, g[0], g[1], static_cast<const float*>(g[2]), p->res_scale, p->branch_scale,
+                                       p->eps, p->dx, p->d, branch ? p->dy : nullptr, branch ? p->d : 0, branch ? p->dgy : nullptr,
+                                       p->o ? p->dgo : nullptr, g[2] ? p->dgate : nullptr, a[8] == Py_True ? PS_DW_ACCUMULATE : 0,
+                                       p->ws, p->ws_bytes, stream()));
+  });
+}
+
+struct CachePlan {
+  static constexpr char kName[] = "psppo.cache_plan";
+  int seqs, Hk, D, dtype, layers, pages, page;
+  int64_t width, layer_bytes;
+  char *k, *v;
+  const int32_t *table, *lengths;
+  void* ws;
+  size_t ws_bytes;
+  int device = -1;
+  at::ScalarType type() const { return dtype == PS_DTYPE_F32 ? at::kFloat : at::kBFloat16; }
+};
+
+PyObject* cache_plan(PyObject*, PyObject* args) {
+  CachePlan p;
+  unsigned long long v[6];
+  long long width, layer_bytes;
+  if (!PyArg_ParseTuple(args, "iiiiiiiLLKKKKKK|i", &p.seqs, &p.Hk, &p.D, &p.dtype, &p.layers, &p.pages, &p.page, &width, &layer_bytes,
+                        &v[0], &v[1], &v[2], &v[3], &v[4], &v[5], &p.device))
+    return nullptr;
+  p.width = width;
+  p.layer_bytes = layer_bytes;
+  p.k = reinterpret_cast<char*>(v[0]);
+  p.v = reinterpret_cast<char*>(v[1]);
+  p.table = reinterpret_cast<const int32_t*>(v[2]);
+  p.lengths = reinterpret_cast<const int32_t*>(v[3]);
+  p.ws = reinterpret_cast<void*>(v[4]);
+  p.ws_bytes = static_cast<size_t>(v[5]);
+  return capsule(p);
+}
+
+// (plan, layer, k, v, row_seq, row_pos, pos_base) -> status or None
+PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    const CachePlan* p = n == 7 ? plan_of<CachePlan>(a[0]) : nullptr;
+    const at::Tensor* k = p ? tensor(a[2], p->device) : nullptr;
+    if (!k || k->dim() != 2) return ordinary();
+    const int64_t N = k->size(0), w = static_cast<int64_t>(p->Hk) * p->D;
+    Rows rk, rv;
+    const void *seq, *pos;
+    int64_t layer, base;
+    if (!rows(a[2], p->device, N, w, p->type(), rk) || !rows(a[3], p->device, N, w, p->type(), rv) ||
+        !whole(a[4], p->device, N, at::kInt, &seq) || !whole(a[5], p->device, N, at::kInt, &pos) || !integer(a[1], layer) ||
+        layer < 0 || layer >= p->layers || !integer(a[6], base) || base != static_cast<int>(base))
+      return ordinary();
+    return PyLong_FromLong(append_fn(N, p->seqs, p->Hk, p->D, p->dtype, rk.at, rk.ld, rv.at, rv.ld, static_cast<const int32_t*>(seq),
+                                     static_cast<const int32_t*>(pos), static_cast<int>(base), p->table, p->width, p->pages, p->page,
+                                     p->k + layer * p->layer_bytes, p->v + layer * p->layer_bytes, p->ws, p->ws_bytes, stream()));
+  });
+}
+
+struct DecodePlan {
+  static constexpr char kName[] = "psppo.decode_plan";
+  int seqs, Hq, Hk, D, dtype, window;
+  double scale;
+  void *o, *ws;
+  size_t ws_bytes;
+  int device = -1;
+};
+
+PyObject* decode_plan(PyObject*, PyObject* args) {
+  DecodePlan p;
+  unsigned long long v[3];
+  if (!PyArg_ParseTuple(args, "iiiiiidKKK|i", &p.seqs, &p.Hq, &p.Hk, &p.D, &p.dtype, &p.window, &p.scale, &v[0], &v[1], &v[2], &p.device))
+    return nullptr;
+  p.o = reinterpret_cast<void*>(v[0]);
+  p.ws = reinterpret_cast<void*>(v[1]);
+  p.ws_bytes = static_cast<size_t>(v[2]);
+  return capsule(p);
+}
+
+// (plan, the cache's plan, layer, q, out or None, lse or None) -> status or None
+PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    const DecodePlan* p = n == 6 ? plan_of<DecodePlan>(a[0]) : nullptr;
+    const CachePlan* c = p ? plan_of<CachePlan>(a[1]) : nullptr;
+    const at::Tensor* q = c ? tensor(a[3], p->device) : nullptr;
+    if (!q || q->dim() != 2 || c->Hk != p->Hk || c->D != p->D || c->dtype != p->dtype) return ordinary();
+    const int64_t N = q->size(0), w = static_cast<int64_t>(p->Hq) * p->D;
+    Rows rq, ro;
+    int64_t layer;
+    if (N > p->seqs || N > c->seqs || !rows(a[3], p->device, N, w, c->type(), rq) || !integer(a[2], layer) || layer < 0 ||
+        layer >= c->layers || (a[4] != Py_None && !rows(a[4], p->device, N, w, c->type(), ro)))
+      return ordinary();
+    if (a[4] == Py_None) {
+      ro.at = p->o;
+      ro.ld = w;
+    }
+    float* lse = nullptr;
+    if (a[5] != Py_None) {
+      const at::Tensor* t = tensor(a[5], p->device);
+      if (!t || t->dim() != 2 || t->size(0) != N || t->size(1) != p->Hq || t->scalar_type() != at::kFloat || !t->is_contiguous())
+        return ordinary();
+      lse = static_cast<float*>(t->data_ptr());
+    }
+    return PyLong_FromLong(decode_fn(static_cast<int>(N), p->Hq, p->Hk, p->D, p->dtype, rq.at, rq.ld, c->k + layer * c->layer_bytes,
+                                     c->v + layer * c->layer_bytes, c->pages, c->page, c->table, c->width, c->lengths, p->window,
+                                     p->scale, ro.at, ro.ld, lse, p->ws, p->ws_bytes, stream()));
+  });
+}
+
+// The library's entries (addresses): ps_residual_norm_fwd and _bwd, ps_paged_append, ps_paged_decode.
+PyObject* bind_more(PyObject*, PyObject* args) {
+  unsigned long long f[4];
+  if (!PyArg_ParseTuple(args, "KKKK", &f[0], &f[1], &f[2], &f[3])) return nullptr;
+  norm_fwd_fn = reinterpret_cast<decltype(norm_fwd_fn)>(f[0]);
+  norm_bwd_fn = reinterpret_cast<decltype(norm_bwd_fn)>(f[1]);
+  append_fn = reinterpret_cast<decltype(append_fn)>(f[2]);
+  decode_fn = reinterpret_cast<decltype(decode_fn)>(f[3]);
+  Py_RETURN_NONE;
+}
+
 // The library's entries (addresses): ps_dropout_rows, ps_qk_norm_rope_fwd and _bwd, ps_gated_ffn_fwd and _bwd.
 PyObject* bind(PyObject*, PyObject* args) {
   unsigned long long f[5];
@@ -318,6 +517,14 @@ PyMODINIT_FUNC PyInit__calls() {
                                   {"ffn_plan", ffn_plan, METH_VARARGS, nullptr},
                                   {"ffn_fwd", fast(ffn_fwd), METH_FASTCALL, nullptr},
                                   {"ffn_bwd", fast(ffn_bwd), METH_FASTCALL, nullptr},
+                                  {"bind_more", bind_more, METH_VARARGS, nullptr},
+                                  {"norm_plan", norm_plan, METH_VARARGS, nullptr},
+                                  {"norm_fwd", fast(norm_fwd), METH_FASTCALL, nullptr},
+                                  {"norm_bwd", fast(norm_bwd), METH_FASTCALL, nullptr},
+                                  {"cache_plan", cache_plan, METH_VARARGS, nullptr},
+                                  {"append", fast(append), METH_FASTCALL, nullptr},
+                                  {"decode_plan", decode_plan, METH_VARARGS, nullptr},
+                                  {"decode", fast(decode), METH_FASTCALL, nullptr},
                                   {nullptr, nullptr, 0, nullptr}};
   static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods};
   return PyModule_Create(&module);
