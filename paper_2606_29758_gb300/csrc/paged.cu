@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
 //   x_j = c q.k_j (c = scale log2 e) over a sequence's keys j, m = max x_j, l = sum 2^(x_j - m), o = sum 2^(x_j - m) v_j / l;
 //   parts of a sequence join by m = max m_i, l = sum l_i 2^(m_i - m), o likewise.
 // HBM-bound: every key and value is read once, for all query heads that share it. The work is a list of tiles of 64 keys of
-// one key head of one sequence (a unit: its query heads, up to 8 NB of them); each CTA takes an equal run of the list,
+// one key head of one sequence (a unit: its query heads, up to 16 of them, in f32 8); each CTA takes an equal run of the list,
 // whatever the lengths are. Its four warps take 16 keys of a tile each, through rings of their own in shared memory that
 // their lanes' copies fill some tiles ahead, across units; within a unit nothing crosses warps. What a CTA has
 // of a unit that it does not hold whole goes to the workspace (two slots a CTA), and decode_join_kernel adds those up.
@@ -129,11 +129,11 @@ struct DecodeArgs {
   int64_t ldo;
   float* lse;                   // [B][Hq] or nullptr
   uint32_t* status;
-  int4* seg;                    // [CTAs] status bits, unit that begins here and goes on (sequence or -1, block), what slot 0 holds
+  int4* seg;                    // [CTAs] status bits, the unit that begins here and goes on (sequence or -1, block), the CTA where it ends
+  int2* unit;                   // [units] the CTAs where it begins and ends (-1: in one, or nothing of it), nullptr: by seg
   float2* ml;                   // [2 CTAs][heads of a unit] (m, l)
   float* part;                  // [2 CTAs][heads of a unit][DP]
 };
-enum { kSlotNone = 0, kSlotEnds = 1, kSlotGoesOn = 2 };
 
 static __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -299,9 +299,8 @@ struct DecodeMath<Bf16, DP, NB> {
 };
 
 template <int DP, int NB>
-struct DecodeMath<float, DP, NB> {   // on the f32 pipe: a lane has half of a key's dims, then four dims of all keys' values
-  static_assert(NB == 1, "eight heads at a time");
-  static constexpr int kHeads = 8, kRow = DP * 4, kHalf = DP / 2 + 4, kQBytes = kHeads * 2 * kHalf * 4;
+struct DecodeMath<float, DP, NB> {   // NB heads on the f32 pipe: a lane has half of a key's dims, then four dims of all keys' values
+  static constexpr int kHeads = NB, kRow = DP * 4, kHalf = DP / 2 + 4, kQBytes = kHeads * 2 * kHalf * 4;
   static constexpr int kOwn = (DP + 127) / 128;   // pieces of four dims a lane has
   float o[kHeads][kOwn][4];
   float m[kHeads], l[kHeads];                     // the same in all lanes
@@ -373,7 +372,7 @@ struct DecodeMath<float, DP, NB> {   // on the f32 pipe: a lane has half of a ke
 #pragma unroll
       for (int i = 8; i >= 1; i >>= 1) t += __shfl_xor_sync(0xffffffffu, t, i);
       l[h] += t;
-      if (h / 4 == half) ps[h * kChunk + key] = p;
+      if ((h * 2 >= kHeads) == half || kHeads == 1) ps[h * kChunk + key] = p;
     }
     __syncwarp();
 #pragma unroll
@@ -437,7 +436,7 @@ struct DecodeCfg {
   static constexpr int kRing = kStages * 2 * kChunkBytes;
   static constexpr int kPs = sizeof(T) == 4 ? Math::kHeads * kChunk * 4 : 0;
   static constexpr int kWarp = kRing + Math::kQBytes + kPs;
-  static constexpr int kOuts = NB == 1 ? 2 : 1;                                   // where the warps' o are added up
+  static constexpr int kOuts = sizeof(T) == 4 || NB == 1 ? 2 : 1;                 // where the warps' o are added up
   static constexpr int kOut = Math::kHeads * (DP + 4) * 4;
   static constexpr int kSmem = kDecWarps * kWarp + kOuts * kOut;
   static constexpr int kBlocks = kSmem <= 112 * 1024 ? 2 : 1;                     // per SM
@@ -483,8 +482,9 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
 
   // the list's length, and the sequence in which this CTA's run begins
   const int per = (a.B + kDecThreads - 1) / kDecThreads, b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
-  int64_t sum = 0;
-  for (int b = b0; b < b1; ++b) sum += keys_of(a, b).tiles();
+  const int tiles0 = b0 < b1 ? keys_of(a, b0).tiles() : 0;
+  int64_t sum = tiles0;
+  for (int b = b0 + 1; b < b1; ++b) sum += keys_of(a, b).tiles();
   int64_t upto = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -507,23 +507,12 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
   if (t0 < t1 && (upto - sum) * HM <= t0 && t0 < upto * HM) {
     int64_t at = upto - sum;
     int b = b0;
-    for (; b < b1; ++b) {
-      const int n = keys_of(a, b).tiles();
-      if (t0 < (at + n) * HM) break;
+    for (int n = tiles0; t0 >= (at + n) * HM; n = keys_of(a, b).tiles()) {
       at += n;
+      ++b;
     }
     b_s = b;
     start_s = at * HM;
-  }
-  // sequences without keys
-  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-    const Keys k = keys_of(a, b);
-    if (k.end > 0) continue;
-    if (k.bad && tid == 0) bad_s = PS_DEV_BAD_LENGTH;
-    for (int i = tid; i < a.Hq * a.c.D; i += kDecThreads)
-      static_cast<T*>(a.o)[b * a.ldo + i] = Elem<T>::put(k.bad ? __int_as_float(0x7fffffff) : 0.f);
-    if (a.lse)
-      for (int i = tid; i < a.Hq; i += kDecThreads) a.lse[static_cast<int64_t>(b) * a.Hq + i] = k.bad ? __int_as_float(0x7fffffff) : -INFINITY;
   }
   __syncthreads();
 
@@ -580,7 +569,7 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
 
-  int4 seg = make_int4(0, -1, 0, kSlotNone);
+  int4 seg = make_int4(0, -1, 0, 0);
   if (t0 < t1) {
     Place t, n;
     t.b = b_s;
@@ -606,7 +595,8 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
       const int hk = per_head == 1 ? hm : hm / per_head, h0 = hk * a.group + (hm - hk * per_head) * H;
       const int heads = min(H, (hk + 1) * a.group - h0);
       const int tile1 = static_cast<int>(min(static_cast<int64_t>(t.tiles), tile0 + (t1 - t.t)));
-      const bool whole = tile0 == 0 && tile1 == t.tiles, ends = tile1 == t.tiles;
+      const bool whole = tile0 == 0 && tile1 == t.tiles;
+      const int64_t end_tile = t.t - tile0 + t.tiles - 1;   // of the list
       math.load(static_cast<const T*>(a.q) + b * a.ldq + static_cast<int64_t>(h0) * a.c.D, heads, a.c.D, q_s, lane);
       for (int tile = tile0; tile < tile1; ++tile) {
         asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
@@ -664,12 +654,24 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
         }
       }
       if (!whole) {
-        if (tile0 == 0) seg.y = b, seg.z = hm;
-        else seg.w = ends ? kSlotEnds : kSlotGoesOn;
+        if (tile0 == 0) seg = make_int4(0, b, hm, static_cast<int>(((end_tile + 1) * takers - 1) / list));
       }
+      if (a.unit && tile0 == 0 && tid == 0) a.unit[b * HM + hm] = whole ? make_int2(-1, -1) : make_int2(blockIdx.x, seg.w);
       __syncthreads();
     }
     if (bad) atomicOr(&bad_s, bad);
+  }
+  // sequences without keys
+  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+    const Keys k = keys_of(a, b);
+    if (k.end > 0) continue;
+    if (k.bad && tid == 0) atomicOr(&bad_s, PS_DEV_BAD_LENGTH);
+    for (int i = tid; i < a.Hq * a.c.D; i += kDecThreads)
+      static_cast<T*>(a.o)[b * a.ldo + i] = Elem<T>::put(k.bad ? __int_as_float(0x7fffffff) : 0.f);
+    if (a.unit)
+      for (int i = tid; i < HM; i += kDecThreads) a.unit[b * HM + i] = make_int2(-1, -1);
+    if (a.lse)
+      for (int i = tid; i < a.Hq; i += kDecThreads) a.lse[static_cast<int64_t>(b) * a.Hq + i] = k.bad ? __int_as_float(0x7fffffff) : -INFINITY;
   }
   __syncthreads();
   if (tid == 0) {
@@ -678,17 +680,19 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
   }
 }
 
-// The units that several CTAs had parts of, by the CTA where one begins; and the call's status.
+// The units that several CTAs had parts of, and the call's status. BY_UNIT (fewer units than CTAs, so long ones): a block for
+// each head of each unit, whose warps share the parts; else a block for each CTA, which joins the unit that begins there and
+// goes on, a warp a head where the parts are few. What a block needs it finds by one load, then the parts and their m and l
+// come eight at a time. (A block for each head of each CTA that looks for its parts took 9 us, a third of it to start them.)
 constexpr int kJoinThreads = 256;
-template <class T, int DP, int H>
+template <class T, int DP, int H, bool BY_UNIT>
 __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecodeArgs a, int ctas) {
-  __shared__ float top_s[kJoinThreads / 32], l_s[kJoinThreads / 32];
-  __shared__ float o_s[kJoinThreads / 32][DP];
-  __shared__ int last_s;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = kJoinThreads / 32;
-  const int i = blockIdx.x, h = blockIdx.y;
+  constexpr int W = kJoinThreads / 32, C = (DP + 127) / 128, LD = 8 / C;
+  __shared__ float2 ml_s[W];
+  __shared__ float o_s[W][DP];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   wait_for_previous_kernel();
-  if (i == 0 && h == 0) {
+  if (blockIdx.x == 0 && blockIdx.y == 0) {
     int bits = 0;
     for (int j = tid; j < ctas; j += kJoinThreads) bits |= a.seg[j].x;
     const int len = __syncthreads_or(bits & PS_DEV_BAD_LENGTH), page = __syncthreads_or(bits & PS_DEV_BAD_PAGE);
@@ -697,72 +701,123 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecodeA
       a.status[0] = (len ? PS_DEV_BAD_LENGTH : 0) | (page ? PS_DEV_BAD_PAGE : 0);
     }
   }
-  const int4 seg = a.seg[i];
-  if (seg.y < 0) return;
-  const int hk = seg.z / a.blocks, h0 = hk * a.group + (seg.z - hk * a.blocks) * H;
-  if (h >= min(H, (hk + 1) * a.group - h0)) return;
-  // the CTA where it ends
-  if (tid == 0) last_s = ctas - 1;
-  __syncthreads();
-  for (int j0 = i + 1; j0 < ctas; j0 += kJoinThreads) {
-    const int j = j0 + tid;
-    const bool ends = j < ctas && a.seg[j].w == kSlotEnds;
-    if (ends) atomicMin(&last_s, j);
-    if (__syncthreads_or(ends)) break;
+  int i, last, b, hm;
+  if (BY_UNIT) {
+    const int2 at = a.unit[blockIdx.x];
+    i = at.x, last = at.y;
+    b = blockIdx.x / (a.c.Hk * a.blocks), hm = blockIdx.x - b * (a.c.Hk * a.blocks);
+    if (i < 0) return;
+  } else {
+    const int4 at = a.seg[blockIdx.x];
+    i = blockIdx.x, b = at.y, hm = at.z, last = at.w;
+    if (b < 0) return;
   }
-  __syncthreads();
-  const int parts = last_s - i + 1;
-  auto slot = [&](int k) { return (k == 0 ? 2 * i + 1 : 2 * (i + k)) * H + h; };
-  float top = -INFINITY;
-  for (int k = tid; k < parts; k += kJoinThreads) top = fmaxf(top, a.ml[slot(k)].x);
+  const int hk = hm / a.blocks, h0 = hk * a.group + (hm - hk * a.blocks) * H, heads = min(H, (hk + 1) * a.group - h0);
+  if (BY_UNIT && static_cast<int>(blockIdx.y) >= heads) return;
+  const int parts = last - i + 1;
+  auto slot = [&](int k, int h) { return (k == 0 ? 2 * i + 1 : 2 * (i + k)) * H + h; };
+  // parts first, first + every, ... of head h: m and l, in every lane, and this lane's dims of o
+  auto gather = [&](int h, int first, int every, float4 (&v)[C]) {
+    float top = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (lane == 0) top_s[warp] = top;
-  __syncthreads();
+    for (int c = 0; c < C; ++c) v[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = first; k0 < parts; k0 += LD * every) {
+      float2 ml[LD];
+      float4 p[LD][C];
 #pragma unroll
-  for (int w = 0; w < W; ++w) top = fmaxf(top, top_s[w]);
-  constexpr int C = (DP + 127) / 128;
-  float4 v[C];
+      for (int n = 0; n < LD; ++n) {
+        const int k = k0 + n * every;
+        ml[n] = make_float2(-INFINITY, 0.f);
+        if (k < parts) ml[n] = a.ml[slot(k, h)];
 #pragma unroll
-  for (int c = 0; c < C; ++c) v[c] = make_float4(0.f, 0.f, 0.f, 0.f);
-  float l = 0.f;
-#pragma unroll 4
-  for (int k = warp; k < parts; k += W) {
-    const float2 ml = a.ml[slot(k)];
-    const float f = ml.x == top ? 1.f : ex2_ftz(ml.x - top);
-    l = fmaf(ml.y, f, l);
+        for (int c = 0; c < C; ++c) {
+          p[n][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (k < parts && (c * 32 + lane) * 4 < DP)
+            p[n][c] = *reinterpret_cast<const float4*>(a.part + static_cast<int64_t>(slot(k, h)) * DP + (c * 32 + lane) * 4);
+        }
+      }
+      float up = top;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int at = (c * 32 + lane) * 4;
-      if (at >= DP || f == 0.f) continue;
-      const float4 p = *reinterpret_cast<const float4*>(a.part + static_cast<int64_t>(slot(k)) * DP + at);
-      v[c].x = fmaf(p.x, f, v[c].x);
-      v[c].y = fmaf(p.y, f, v[c].y);
-      v[c].z = fmaf(p.z, f, v[c].z);
-      v[c].w = fmaf(p.w, f, v[c].w);
+      for (int n = 0; n < LD; ++n) up = fmaxf(up, ml[n].x);
+      auto add = [&](float m, float lk, const float4 (&q)[C]) {
+        const float f = m == up ? 1.f : ex2_ftz(m - up);
+        l = fmaf(lk, f, l);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          v[c].x += f == 0.f ? 0.f : q[c].x * f;
+          v[c].y += f == 0.f ? 0.f : q[c].y * f;
+          v[c].z += f == 0.f ? 0.f : q[c].z * f;
+          v[c].w += f == 0.f ? 0.f : q[c].w * f;
+        }
+      };
+      if (up != top) {
+        float4 had[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          had[c] = v[c];
+          v[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        const float had_l = l;
+        l = 0.f;
+        add(top, had_l, had);
+        top = up;
+      }
+#pragma unroll
+      for (int n = 0; n < LD; ++n)
+        if (k0 + n * every < parts) add(ml[n].x, ml[n].y, p[n]);
     }
+    return make_float2(top, l);
+  };
+  auto put = [&](int h, int c, float v, float2 ml) {
+    static_cast<T*>(a.o)[b * a.ldo + static_cast<int64_t>(h0 + h) * a.c.D + c] = Elem<T>::put(v / ml.y);
+    if (c == 0 && a.lse) a.lse[static_cast<int64_t>(b) * a.Hq + h0 + h] = (ml.x + log2f(ml.y)) * kLn2;
+  };
+  float4 v[C];
+  if (!BY_UNIT && parts <= 2 * W) {
+    for (int h = warp; h < heads; h += W) {
+      const float2 ml = gather(h, 0, 1, v);
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int at = (c * 32 + lane) * 4;
+        if (at >= a.c.D) continue;
+        put(h, at, v[c].x, ml);
+        put(h, at + 1, v[c].y, ml);
+        put(h, at + 2, v[c].z, ml);
+        put(h, at + 3, v[c].w, ml);
+      }
+    }
+    return;
   }
-  if (lane == 0) l_s[warp] = l;
+  for (int h = BY_UNIT ? blockIdx.y : 0; h < (BY_UNIT ? static_cast<int>(blockIdx.y) + 1 : heads); ++h) {
+    const float2 mine = gather(h, warp, W, v);
+    if (lane == 0) ml_s[warp] = mine;
 #pragma unroll
-  for (int c = 0; c < C; ++c)
-    if ((c * 32 + lane) * 4 < DP) *reinterpret_cast<float4*>(&o_s[warp][(c * 32 + lane) * 4]) = v[c];
-  __syncthreads();
-  l = 0.f;
+    for (int c = 0; c < C; ++c)
+      if ((c * 32 + lane) * 4 < DP) *reinterpret_cast<float4*>(&o_s[warp][(c * 32 + lane) * 4]) = v[c];
+    __syncthreads();
+    float top = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int w = 0; w < W; ++w) l += l_s[w];
-  for (int c = tid; c < a.c.D; c += kJoinThreads) {
-    float s = 0.f;
+    for (int w = 0; w < W; ++w) top = fmaxf(top, ml_s[w].x);
+    float f[W];
 #pragma unroll
-    for (int w = 0; w < W; ++w) s += o_s[w][c];
-    static_cast<T*>(a.o)[seg.y * a.ldo + static_cast<int64_t>(h0 + h) * a.c.D + c] = Elem<T>::put(s / l);
+    for (int w = 0; w < W; ++w) {
+      f[w] = ml_s[w].x == top ? 1.f : ex2_ftz(ml_s[w].x - top);
+      l = fmaf(ml_s[w].y, f[w], l);
+    }
+    for (int c = tid; c < a.c.D; c += kJoinThreads) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) s += f[w] == 0.f ? 0.f : o_s[w][c] * f[w];
+      put(h, c, s, make_float2(top, l));
+    }
+    __syncthreads();
   }
-  if (tid == 0 && a.lse) a.lse[static_cast<int64_t>(seg.y) * a.Hq + h0 + h] = (top + log2f(l)) * kLn2;
 }
 
 // ================================================================== host side
 constexpr int kDecMaxCtas = 304;
 constexpr int kDecMaxHeads = 16, kDecMaxDim = 256;
-constexpr size_t kDecSeg = sizeof(int4) * kDecMaxCtas, kDecMl = sizeof(float2) * 2 * kDecMaxCtas * kDecMaxHeads;
+constexpr size_t kDecSeg = (sizeof(int4) + sizeof(int2)) * kDecMaxCtas, kDecMl = sizeof(float2) * 2 * kDecMaxCtas * kDecMaxHeads;
 
 static bool pages_ok(int seqs, int Hk, int D, int dtype, int pages, int page, int64_t ldt) {
   return seqs >= 0 && Hk >= 1 && Hk <= 65536 && D >= 16 && D <= kDecMaxDim && D % 16 == 0 &&
@@ -792,12 +847,15 @@ static int launch_decode(DecodeArgs a, cudaStream_t s) {
   // no more than the tiles that the table can name
   const int64_t most = static_cast<int64_t>(a.B) * a.c.Hk * a.blocks * (((a.c.ldt << a.c.page_log2) + kTile - 1) / kTile);
   if (ctas > most) ctas = static_cast<int>(most);
+  const int64_t units = static_cast<int64_t>(a.B) * a.c.Hk * a.blocks;
+  if (units >= ctas) a.unit = nullptr;
   if (launch_after(kern, dim3(static_cast<unsigned>(ctas)), kDecThreads, Cfg::kSmem, s, 1, 1, true, a) != cudaSuccess)
     return PS_ERR_CUDA;
-  return launch_after(decode_join_kernel<T, DP, H>, dim3(static_cast<unsigned>(ctas), H), kJoinThreads, 0, s, 1, 1, true, a, ctas) ==
-                 cudaSuccess
-             ? PS_OK
-             : PS_ERR_CUDA;
+  const cudaError_t e = a.unit ? launch_after(decode_join_kernel<T, DP, H, true>, dim3(static_cast<unsigned>(units), H), kJoinThreads, 0,
+                                                    s, 1, 1, true, a, ctas)
+                                     : launch_after(decode_join_kernel<T, DP, H, false>, dim3(static_cast<unsigned>(ctas)), kJoinThreads, 0,
+                                                    s, 1, 1, true, a, ctas);
+  return e == cudaSuccess ? PS_OK : PS_ERR_CUDA;
 }
 
 }  // namespace psk
@@ -869,11 +927,15 @@ int ps_paged_decode(int seqs, int Hq, int Hk, int D, int dtype, const void* q, i
   uint8_t* w = static_cast<uint8_t*>(ws);
   a.status = reinterpret_cast<uint32_t*>(w);
   a.seg = reinterpret_cast<int4*>(w + kWsHeader);
+  a.unit = reinterpret_cast<int2*>(a.seg + kDecMaxCtas);
   a.ml = reinterpret_cast<float2*>(w + kWsHeader + kDecSeg);
   a.part = reinterpret_cast<float*>(w + kWsHeader + kDecSeg + kDecMl);
   int out;
   if (dtype == PS_DTYPE_F32)
-    out = D <= 128 ? launch_decode<float, 128, 1>(a, s) : launch_decode<float, 256, 1>(a, s);
+    if (D <= 128)
+      out = a.group == 1 ? launch_decode<float, 128, 1>(a, s) : a.group <= 4 ? launch_decode<float, 128, 4>(a, s) : launch_decode<float, 128, 8>(a, s);
+    else
+      out = a.group == 1 ? launch_decode<float, 256, 1>(a, s) : a.group <= 4 ? launch_decode<float, 256, 4>(a, s) : launch_decode<float, 256, 8>(a, s);
   else if (D <= 64)
     out = a.group <= 8 ? launch_decode<Bf16, 64, 1>(a, s) : launch_decode<Bf16, 64, 2>(a, s);
   else if (D <= 128)
