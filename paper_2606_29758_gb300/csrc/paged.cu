@@ -68,23 +68,27 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
   for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kAppendThreads / 32) + (threadIdx.x >> 5); u < units; u += stride) {
     const int64_t row = a.parts == 1 ? u : u / a.parts;
     const int part = static_cast<int>(u - row * a.parts);
+    const uint4* ks = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.k) + row * a.ldk);
+    const uint4* vs = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.v) + row * a.ldv);
+    const int p1 = static_cast<int>(static_cast<int64_t>(a.pieces) * (part + 1) / a.parts);
+    int p0 = static_cast<int>(static_cast<int64_t>(a.pieces) * part / a.parts);
+    uint4 kv[2], vv[2];
+    auto read = [&]() {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int p = p0 + h * 32 + lane;
+        if (p < p1) kv[h] = __ldg(ks + p), vv[h] = __ldg(vs + p);
+      }
+    };
+    read();   // (the row is on its way while its place is looked up)
     int id = 0, slot = 0;
     const int bad = append_place(a, row, id, slot);
     if (bad) {
       if (bad > 0 && !a.checked && lane == 0) raise_status(a.status, bad);
       continue;
     }
-    const uint4* ks = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.k) + row * a.ldk);
-    const uint4* vs = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.v) + row * a.ldv);
     const int64_t first = static_cast<int64_t>(id) * a.c.Hk;
-    const int p1 = static_cast<int>(static_cast<int64_t>(a.pieces) * (part + 1) / a.parts);
-    for (int p0 = static_cast<int>(static_cast<int64_t>(a.pieces) * part / a.parts); p0 < p1; p0 += 64) {
-      uint4 kv[2], vv[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int p = p0 + h * 32 + lane;
-        if (p < p1) kv[h] = __ldg(ks + p), vv[h] = __ldg(vs + p);
-      }
+    while (true) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int p = p0 + h * 32 + lane;
@@ -94,6 +98,9 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
         static_cast<uint4*>(a.kc)[to] = kv[h];
         static_cast<uint4*>(a.vc)[to] = vv[h];
       }
+      p0 += 64;
+      if (p0 >= p1) break;
+      read();
     }
   }
 }
