@@ -5,11 +5,13 @@
 #include <stdint.h>
 
 #include <climits>
+#include <type_traits>
 
 #include "internal.h"
 #include "ps_common.cuh"
 #include "ps_nvtx.h"
 #include "row_elems.cuh"
+#include "umma_host.cuh"
 
 namespace psk {
 
@@ -122,6 +124,7 @@ constexpr int kDecWarps = 4;
 constexpr int kDecThreads = 32 * kDecWarps;
 constexpr int kChunk = 16;                        // keys of a warp's share of a tile
 constexpr int kTile = kChunk * kDecWarps;
+constexpr int kBoxBytes = kChunk * 128;
 
 struct DecodeArgs {
   int B, Hq, group, blocks;     // sequences, query heads, query heads a key head, units a key head
@@ -171,7 +174,8 @@ static __device__ __forceinline__ void lane_copy_or_zero(uint32_t dst, const voi
 
 // A warp's part of a unit: m, l and o of its query heads over the keys that it has seen.
 //   load    the unit's queries
-//   chunk   16 keys and values in shared memory, the first nv of them (rows behind are zeros), 16-byte piece p of row r at p ^ (r & 7)
+//   chunk   keys and values lo to nv of 16 in shared memory (the others' values are zeros). bf16: boxes of 64 dims, 128 bytes a
+//           row, 16-byte piece p of row r at p ^ (r & 7) (TMA's 128-byte swizzle); f32: whole rows, pieces likewise
 //   put_ml  m and l to shared memory
 //   add_o   o times a head's factor, to or added to what shared memory [heads][DP + 4] holds
 template <class T, int DP, int NB>
@@ -179,7 +183,7 @@ struct DecodeMath;
 
 template <int DP, int NB>
 struct DecodeMath<Bf16, DP, NB> {
-  static constexpr int kHeads = 8 * NB, kRow = DP * 2, kQBytes = 0;
+  static constexpr int kHeads = 8 * NB, kQBytes = 0;
   uint32_t q[NB][DP / 16][2];
   float o[NB][DP / 16][4];      // o[dim lane / 4 (+ 8)][head 2 (lane % 4) (+ 1)]
   float m[NB][2], l[NB][2];     // of heads 2 (lane % 4) and the next; l of this lane's keys
@@ -207,16 +211,17 @@ struct DecodeMath<Bf16, DP, NB> {
 #pragma unroll
     for (int n = 0; n < NB; ++n) l[n][0] = l[n][1] = __int_as_float(0x7fffffff);
   }
-  __device__ __forceinline__ void chunk(uint32_t ks, uint32_t vs, int nv, float scale2, const uint8_t*, float*, int lane) {
+  __device__ __forceinline__ void chunk(uint32_t ks, uint32_t vs, int lo, int nv, float scale2, const uint8_t*, float*, int lane) {
     const int r = lane & 15, hi = lane >> 4;
     float s[NB][4];
 #pragma unroll
     for (int n = 0; n < NB; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
     // rows: keys 0-7 and 8-15 by the lanes' first 16 addresses, then the next eight dims
+    const uint32_t ka = ks + r * 128 + ((hi ^ (r & 7)) << 4);
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k) {
       uint32_t a[4];
-      ldsm4(a, ks + r * kRow + (((2 * k + hi) ^ (r & 7)) << 4));
+      ldsm4(a, (ka ^ ((k & 3) * 32)) + (k >> 2) * kBoxBytes);
 #pragma unroll
       for (int n = 0; n < NB; ++n) mma_bf16(s[n], a, q[n][k][0], q[n][k][1]);
     }
@@ -226,7 +231,10 @@ struct DecodeMath<Bf16, DP, NB> {
     for (int n = 0; n < NB; ++n) {
       float x[4], top[2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = key + (i & 2 ? 8 : 0) < nv ? s[n][i] * scale2 : -INFINITY;
+      for (int i = 0; i < 4; ++i) {
+        const int at = key + (i & 2 ? 8 : 0);
+        x[i] = at >= lo && at < nv ? s[n][i] * scale2 : -INFINITY;
+      }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         float v = fmaxf(x[i], x[i + 2]);
@@ -262,11 +270,12 @@ struct DecodeMath<Bf16, DP, NB> {
         pl[n][i] = transposed(w);
       }
     }
+    const int row = (lane & 7) + (hi << 3);
+    const uint32_t va = vs + row * 128 + ((((lane >> 3) & 1) ^ (row & 7)) << 4);
 #pragma unroll
     for (int t = 0; t < DP / 16; ++t) {
       uint32_t a[4];   // dims 0-7 and 8-15 of keys 0-7, then of keys 8-15
-      const int row = (lane & 7) + (hi << 3);
-      ldsm4_t(a, vs + row * kRow + (((2 * t + ((lane >> 3) & 1)) ^ (row & 7)) << 4));
+      ldsm4_t(a, (va ^ ((t & 3) * 32)) + (t >> 2) * kBoxBytes);
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         mma_bf16(o[n][t], a, ph[n][0], ph[n][1]);
@@ -342,7 +351,7 @@ struct DecodeMath<float, DP, NB> {   // NB heads on the f32 pipe: a lane has hal
                  : "memory");
     return v;
   }
-  __device__ __forceinline__ void chunk(uint32_t ks, uint32_t vs, int nv, float scale2, const uint8_t* mem, float* ps, int lane) {
+  __device__ __forceinline__ void chunk(uint32_t ks, uint32_t vs, int lo, int nv, float scale2, const uint8_t* mem, float* ps, int lane) {
     const int key = lane & 15, half = lane >> 4;
     const float* q = reinterpret_cast<const float*>(mem) + half * kHalf;
     float s[kHeads];
@@ -360,7 +369,7 @@ struct DecodeMath<float, DP, NB> {   // NB heads on the f32 pipe: a lane has hal
 #pragma unroll
     for (int h = 0; h < kHeads; ++h) {
       s[h] += __shfl_xor_sync(0xffffffffu, s[h], 16);
-      const float x = key < nv ? s[h] * scale2 : -INFINITY;
+      const float x = key >= lo && key < nv ? s[h] * scale2 : -INFINITY;
       float v = x;
 #pragma unroll
       for (int i = 8; i >= 1; i >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, i));
@@ -450,24 +459,31 @@ struct DecodeCfg {
   static_assert(kSmem <= 226 * 1024, "an SM's shared memory");
 };
 
-// A sequence's keys: the last `window` of its length, or all.
+// A sequence's keys: the last `window` of its length, or all; in chunks, of TMA from a multiple of 16 on.
 struct Keys {
-  int first, end;
+  int first, base, end;
   bool bad;
-  __device__ __forceinline__ int tiles() const { return (end - first + kTile - 1) / kTile; }
+  __device__ __forceinline__ int tiles() const { return (end - base + kTile - 1) / kTile; }
 };
+template <bool TMA>
 static __device__ __forceinline__ Keys keys_of(const DecodeArgs& a, int b) {
   const int len = __ldg(a.lens + b);
-  if (len < 0 || len > (a.c.ldt << a.c.page_log2)) return {0, 0, true};
-  return {a.window > 0 && len > a.window ? len - a.window : 0, len, false};
+  if (len < 0 || len > (a.c.ldt << a.c.page_log2)) return {0, 0, 0, true};
+  const int first = a.window > 0 && len > a.window ? len - a.window : 0;
+  return {first, TMA ? first & ~(kChunk - 1) : first, len, false};
 }
 
-template <class T, int DP, int NB>
-__global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) decode_kernel(const DecodeArgs a) {
+// TMA (bf16, pages of 16 positions and more: a chunk lies in one page): one lane has a chunk's boxes copied, four instructions
+// of D = 128 in the place of 16 copies a lane with their addresses; an mbarrier a stage. Values behind a sequence's end, or
+// before its window, may be anything: they are zeroed in shared memory. Else the lanes copy, rows of any pages.
+template <class T, int DP, int NB, bool TMA>
+__global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks))
+    decode_kernel(const DecodeArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using Cfg = DecodeCfg<T, DP, NB>;
   using Math = typename Cfg::Math;
   constexpr int ST = Cfg::kStages, E = 16 / static_cast<int>(sizeof(T)), PR = DP / E, H = Math::kHeads;
-  extern __shared__ __align__(128) uint8_t dec_smem[];
+  extern __shared__ __align__(1024) uint8_t dec_smem[];
+  __shared__ __align__(8) uint64_t full[kDecWarps][ST];
   __shared__ float2 ml_s[kDecWarps][H];
   __shared__ int64_t scan_s[kDecWarps], start_s;
   __shared__ int b_s, bad_s;
@@ -479,9 +495,15 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
   float* const p_s = reinterpret_cast<float*>(q_s + Math::kQBytes);
   const int per_head = a.blocks, HM = a.c.Hk * per_head;    // units a sequence
 
-  // dims behind D stay zeros in every stage
-  if (a.c.D < DP)
+  // dims behind D stay zeros in every stage (TMA fills its last box itself)
+  if (a.c.D < DP && (!TMA || a.c.D <= DP - 64)) {
     for (int i = lane; i < ST * 2 * kChunk * PR; i += 32) *reinterpret_cast<uint4*>(mine + i * 16) = make_uint4(0, 0, 0, 0);
+    if (TMA) fence_proxy_async_smem();
+  }
+  if (TMA && lane == 0) {
+    for (int s = 0; s < ST; ++s) mbar_init(&full[warp][s], 1);
+    fence_mbar_init();
+  }
   if (tid == 0) bad_s = 0, b_s = a.B;
   __syncthreads();
   wait_for_previous_kernel();
@@ -489,9 +511,9 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
 
   // the list's length, and the sequence in which this CTA's run begins
   const int per = (a.B + kDecThreads - 1) / kDecThreads, b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
-  const int tiles0 = b0 < b1 ? keys_of(a, b0).tiles() : 0;
+  const int tiles0 = b0 < b1 ? keys_of<TMA>(a, b0).tiles() : 0;
   int64_t sum = tiles0;
-  for (int b = b0 + 1; b < b1; ++b) sum += keys_of(a, b).tiles();
+  for (int b = b0 + 1; b < b1; ++b) sum += keys_of<TMA>(a, b).tiles();
   int64_t upto = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -514,7 +536,7 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
   if (t0 < t1 && (upto - sum) * HM <= t0 && t0 < upto * HM) {
     int64_t at = upto - sum;
     int b = b0;
-    for (int n = tiles0; t0 >= (at + n) * HM; n = keys_of(a, b).tiles()) {
+    for (int n = tiles0; t0 >= (at + n) * HM; n = keys_of<TMA>(a, b).tiles()) {
       at += n;
       ++b;
     }
@@ -526,11 +548,12 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
   // A place in the list: tile `tile` of `tiles` of unit hm of sequence b.
   struct Place {
     int64_t t;
-    int b, hm, tile, tiles, first, end;
+    int b, hm, tile, tiles, first, base, end;
   };
   auto enter = [&](Place& p) {   // the sequence's keys
-    const Keys k = keys_of(a, p.b);
+    const Keys k = keys_of<TMA>(a, p.b);
     p.first = k.first;
+    p.base = k.base;
     p.end = k.end;
     p.tiles = k.tiles();
   };
@@ -545,35 +568,77 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
       enter(p);
     } while (p.tiles == 0);
   };
-  // the page of this lane's key (row lane % 16 of the warp's chunk) at a place: -1 behind the end
+  // The page of the warp's chunk at a place, or (lanes) of this lane's key, row lane % 16: -1 where there is no key.
   auto page_at = [&](const Place& p) {
-    const int key = p.first + p.tile * kTile + warp * kChunk + (lane & 15);
-    return p.t < t1 && key < p.end ? __ldg(a.c.table + p.b * a.c.ldt + (key >> a.c.page_log2)) : -1;
+    const int key = p.base + p.tile * kTile + warp * kChunk + (TMA ? 0 : lane & 15);
+    return p.t < t1 && key < p.end && (TMA || key >= p.first) ? __ldg(a.c.table + p.b * a.c.ldt + (key >> a.c.page_log2)) : -1;
   };
-  uint32_t bad_stages = 0;
+  uint32_t bad_stages = 0, phases = 0;
+  bool stuck = false;
   auto issue = [&](const Place& p, int id, int st) {
-    const int k0 = p.first + p.tile * kTile + warp * kChunk;
+    const int k0 = p.base + p.tile * kTile + warp * kChunk;
     bad_stages &= ~(1u << st);
-    if (p.t < t1 && k0 < p.end) {
-      const bool in = k0 + (lane & 15) < p.end, good = in && id >= 0 && id < a.c.pages;
-      if (__any_sync(0xffffffffu, in && !good)) bad_stages |= 1u << st;
-      const int valid_id = good ? id : -1;
+    if (p.t < t1 && k0 < p.end && !stuck) {
       const int hk = per_head == 1 ? p.hm : p.hm / per_head;
       const uint32_t to = ring + st * 2 * Cfg::kChunkBytes;
+      if (TMA) {
+        if (id < 0 || id >= a.c.pages) bad_stages |= 1u << st;
+        if (lane == 0) {
+          const int64_t row = ((static_cast<int64_t>(id < 0 || id >= a.c.pages ? 0 : id) * a.c.Hk + hk) << a.c.page_log2) + (k0 & (a.c.page - 1));
+          uint8_t* at = mine + st * 2 * Cfg::kChunkBytes;
+          const int boxes = (a.c.D + 63) / 64;
+          mbar_arrive_expect_tx(&full[warp][st], boxes * 2 * kBoxBytes);
 #pragma unroll
-      for (int i = 0; i < kChunk * PR / 32; ++i) {
-        const int idx = i * 32 + lane, r = idx / PR, pc = idx % PR;
-        const int pid = __shfl_sync(0xffffffffu, valid_id, r);
-        const int64_t row = ((static_cast<int64_t>(max(pid, 0)) * a.c.Hk + hk) << a.c.page_log2) + ((k0 + r) & (a.c.page - 1));
-        const int64_t off = row * a.c.D + pc * E;
-        const uint32_t at = to + (r * PR + (pc ^ (r & 7))) * 16;
-        if (pc * E < a.c.D) {
-          lane_copy_or_zero(at, static_cast<const T*>(a.kc) + off, pid >= 0);
-          lane_copy_or_zero(at + Cfg::kChunkBytes, static_cast<const T*>(a.vc) + off, pid >= 0);
+          for (int x = 0; x < DP / 64; ++x) {
+            if (x >= boxes) break;
+            tma_load_2d(at + x * kBoxBytes, &k_map, &full[warp][st], x * 64, static_cast<int>(row));
+            tma_load_2d(at + Cfg::kChunkBytes + x * kBoxBytes, &v_map, &full[warp][st], x * 64, static_cast<int>(row));
+          }
+        }
+      } else {
+        const int key = k0 + (lane & 15);
+        const bool in = key >= p.first && key < p.end, good = in && id >= 0 && id < a.c.pages;
+        if (__any_sync(0xffffffffu, in && !good)) bad_stages |= 1u << st;
+        const int valid_id = good ? id : -1;
+#pragma unroll
+        for (int i = 0; i < kChunk * PR / 32; ++i) {
+          const int idx = i * 32 + lane, r = idx / PR, pc = idx % PR;
+          const int pid = __shfl_sync(0xffffffffu, valid_id, r);
+          const int64_t row = ((static_cast<int64_t>(max(pid, 0)) * a.c.Hk + hk) << a.c.page_log2) + ((k0 + r) & (a.c.page - 1));
+          const int64_t off = row * a.c.D + pc * E;
+          const uint32_t at = to + (sizeof(T) == 2 ? (pc >> 3) * kBoxBytes + r * 128 + (((pc & 7) ^ (r & 7)) << 4)
+                                                   : (r * PR + (pc ^ (r & 7))) * 16);
+          if (pc * E < a.c.D) {
+            lane_copy_or_zero(at, static_cast<const T*>(a.kc) + off, pid >= 0);
+            lane_copy_or_zero(at + Cfg::kChunkBytes, static_cast<const T*>(a.vc) + off, pid >= 0);
+          }
         }
       }
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (!TMA) asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // The warp's keys lo to nv of a tile in their stage: false where it has none.
+  auto arrive = [&](const Place& p, int tile, int st, int& lo, int& nv) {
+    const int k0 = p.base + tile * kTile + warp * kChunk;
+    lo = max(0, p.first - k0);
+    nv = min(kChunk, p.end - k0);
+    if (!TMA) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
+      __syncwarp();
+      return nv > 0;
+    }
+    if (nv <= 0) return false;
+    if (stuck || !mbar_wait(&full[warp][st], phases >> st & 1u, kDefaultTimeoutNs, nullptr)) stuck = true;
+    stuck = __any_sync(0xffffffffu, stuck);
+    phases ^= 1u << st;
+    if (lo > 0 || nv < kChunk) {
+      uint8_t* v = mine + st * 2 * Cfg::kChunkBytes + Cfg::kChunkBytes;
+      for (int i = lane; i < kChunk * DP / 8; i += 32)
+        if (i / 8 % kChunk < lo || i / 8 % kChunk >= nv) reinterpret_cast<uint4*>(v)[i] = make_uint4(0, 0, 0, 0);
+      fence_proxy_async_smem();   // (before the stage's next copies)
+      __syncwarp();
+    }
+    return true;
   };
 
   int4 seg = make_int4(0, -1, 0, 0);
@@ -586,15 +651,17 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
     t.hm = static_cast<int>(in_seq / t.tiles);
     t.tile = static_cast<int>(in_seq - static_cast<int64_t>(t.hm) * t.tiles);
     n = t;
-    int id = page_at(n);
+    Place ahead[ST];   // (their pages are looked up side by side)
+    int ids[ST];
 #pragma unroll
     for (int s = 0; s < ST; ++s) {
-      const Place now = n;
-      const int now_id = id;
+      ahead[s] = n;
+      ids[s] = page_at(n);
       next(n);
-      id = page_at(n);
-      issue(now, now_id, s);
     }
+    int id = page_at(n);
+#pragma unroll
+    for (int s = 0; s < ST; ++s) issue(ahead[s], ids[s], s);
     int st = 0, bad = 0;
     Math math;
     while (t.t < t1) {
@@ -606,14 +673,12 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
       const int64_t end_tile = t.t - tile0 + t.tiles - 1;   // of the list
       math.load(static_cast<const T*>(a.q) + b * a.ldq + static_cast<int64_t>(h0) * a.c.D, heads, a.c.D, q_s, lane);
       for (int tile = tile0; tile < tile1; ++tile) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
-        __syncwarp();
-        const int nv = t.end - (t.first + tile * kTile + warp * kChunk);
+        int lo, nv;
         const uint32_t from = ring + st * 2 * Cfg::kChunkBytes;
-        if (nv > 0) math.chunk(from, from + Cfg::kChunkBytes, min(nv, kChunk), a.scale2, q_s, p_s, lane);
-        if (bad_stages >> st & 1u) {
+        if (arrive(t, tile, st, lo, nv)) math.chunk(from, from + Cfg::kChunkBytes, lo, nv, a.scale2, q_s, p_s, lane);
+        if ((bad_stages >> st & 1u) || stuck) {
           math.poison();
-          bad = PS_DEV_BAD_PAGE;
+          bad |= stuck ? PS_DEV_TIMEOUT : PS_DEV_BAD_PAGE;
         }
         __syncwarp();   // the stage has been read
         const Place now = n;
@@ -644,19 +709,29 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
         __syncthreads();
       }
       const int slot = 2 * blockIdx.x + (tile0 == 0 ? 1 : 0);
-      for (int i = tid; i < heads * DP; i += kDecThreads) {
-        const int h = i / DP, c = i % DP;
+      for (int i = tid; i < heads * (DP / 8); i += kDecThreads) {   // eight dims of a head
+        const int h = i / (DP / 8), c = i % (DP / 8) * 8;
         const float top = top_of(h);
-        float l = 0.f, v = 0.f;
+        float l = 0.f, v[8];
 #pragma unroll
         for (int w = 0; w < kDecWarps; ++w) l += ml_s[w][h].x == top ? ml_s[w][h].y : ml_s[w][h].y * ex2_ftz(ml_s[w][h].x - top);
 #pragma unroll
-        for (int k = 0; k < OUTS; ++k) v += out_s[k * OUT + h * (DP + 4) + c];
+        for (int j = 0; j < 8; j += 4) {
+          float4 x = *reinterpret_cast<const float4*>(out_s + h * (DP + 4) + c + j);
+          if (OUTS == 2) {
+            const float4 y = *reinterpret_cast<const float4*>(out_s + OUT + h * (DP + 4) + c + j);
+            x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+          }
+          v[j] = x.x, v[j + 1] = x.y, v[j + 2] = x.z, v[j + 3] = x.w;
+        }
         if (whole) {
-          if (c < a.c.D) static_cast<T*>(a.o)[b * a.ldo + static_cast<int64_t>(h0 + h) * a.c.D + c] = Elem<T>::put(v / l);
+          const float r = 1.f / l;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] *= r;
+          if (c < a.c.D) Raw8<T>::store(static_cast<T*>(a.o) + b * a.ldo + static_cast<int64_t>(h0 + h) * a.c.D + c, v);
           if (c == 0 && a.lse) a.lse[static_cast<int64_t>(b) * a.Hq + h0 + h] = (top + log2f(l)) * kLn2;
         } else {
-          a.part[(static_cast<int64_t>(slot) * H + h) * DP + c] = v;
+          Raw8<float>::store(a.part + (static_cast<int64_t>(slot) * H + h) * DP + c, v);
           if (c == 0) a.ml[slot * H + h] = make_float2(top, l);
         }
       }
@@ -667,10 +742,12 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks)) 
       __syncthreads();
     }
     if (bad) atomicOr(&bad_s, bad);
+    if (TMA && stuck)   // copies that may still come
+      for (int s = 0; s < ST; ++s) mbar_wait(&full[warp][s], phases >> s & 1u, kDefaultTimeoutNs, nullptr);
   }
   // sequences without keys
   for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-    const Keys k = keys_of(a, b);
+    const Keys k = keys_of<TMA>(a, b);
     if (k.end > 0) continue;
     if (k.bad && tid == 0) atomicOr(&bad_s, PS_DEV_BAD_LENGTH);
     for (int i = tid; i < a.Hq * a.c.D; i += kDecThreads)
@@ -703,9 +780,10 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecodeA
     int bits = 0;
     for (int j = tid; j < ctas; j += kJoinThreads) bits |= a.seg[j].x;
     const int len = __syncthreads_or(bits & PS_DEV_BAD_LENGTH), page = __syncthreads_or(bits & PS_DEV_BAD_PAGE);
+    const int time = __syncthreads_or(bits & PS_DEV_TIMEOUT);
     if (tid == 0) {
       a.status[1] = 0u;
-      a.status[0] = (len ? PS_DEV_BAD_LENGTH : 0) | (page ? PS_DEV_BAD_PAGE : 0);
+      a.status[0] = (len ? PS_DEV_BAD_LENGTH : 0) | (page ? PS_DEV_BAD_PAGE : 0) | (time ? PS_DEV_TIMEOUT : 0);
     }
   }
   int i, last, b, hm;
@@ -842,10 +920,15 @@ static PagesOf pages_of(const int32_t* table, int64_t ldt, int pages, int page, 
   return c;
 }
 
-template <class T, int DP, int NB>
+template <class T, int DP, int NB, bool TMA>
 static int launch_decode(DecodeArgs a, cudaStream_t s) {
   using Cfg = DecodeCfg<T, DP, NB>;
-  auto kern = decode_kernel<T, DP, NB>;
+  auto kern = decode_kernel<T, DP, NB, TMA>;
+  CUtensorMap maps[2] = {};
+  if (TMA)
+    for (int i = 0; i < 2; ++i)
+      if (!make_map(&maps[i], i ? a.vc : a.kc, a.c.D, static_cast<uint64_t>(a.c.pages) * a.c.Hk * a.c.page, a.c.D * 2, 64, kChunk))
+        return PS_ERR_CUDA;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem) != cudaSuccess) return PS_ERR_CUDA;
   constexpr int H = Cfg::Math::kHeads;
   a.blocks = (a.group + H - 1) / H;
@@ -856,7 +939,7 @@ static int launch_decode(DecodeArgs a, cudaStream_t s) {
   if (ctas > most) ctas = static_cast<int>(most);
   const int64_t units = static_cast<int64_t>(a.B) * a.c.Hk * a.blocks;
   if (units >= ctas) a.unit = nullptr;
-  if (launch_after(kern, dim3(static_cast<unsigned>(ctas)), kDecThreads, Cfg::kSmem, s, 1, 1, true, a) != cudaSuccess)
+  if (launch_after(kern, dim3(static_cast<unsigned>(ctas)), kDecThreads, Cfg::kSmem, s, 1, 1, true, a, maps[0], maps[1]) != cudaSuccess)
     return PS_ERR_CUDA;
   const cudaError_t e = a.unit ? launch_after(decode_join_kernel<T, DP, H, true>, dim3(static_cast<unsigned>(units), H), kJoinThreads, 0,
                                                     s, 1, 1, true, a, ctas)
@@ -937,18 +1020,31 @@ int ps_paged_decode(int seqs, int Hq, int Hk, int D, int dtype, const void* q, i
   a.unit = reinterpret_cast<int2*>(a.seg + kDecMaxCtas);
   a.ml = reinterpret_cast<float2*>(w + kWsHeader + kDecSeg);
   a.part = reinterpret_cast<float*>(w + kWsHeader + kDecSeg + kDecMl);
+  const bool tma = page >= kChunk && static_cast<int64_t>(pages) * Hk * page <= INT32_MAX - kChunk;   // (rows are counted in 32 bits)
+  auto bf16 = [&](auto DP, auto NB) {
+    return tma ? launch_decode<Bf16, decltype(DP)::value, decltype(NB)::value, true>(a, s)
+               : launch_decode<Bf16, decltype(DP)::value, decltype(NB)::value, false>(a, s);
+  };
+  auto f32 = [&](auto DP) {
+    constexpr int D_ = decltype(DP)::value;
+    return a.group == 1   ? launch_decode<float, D_, 1, false>(a, s)
+           : a.group <= 4 ? launch_decode<float, D_, 4, false>(a, s)
+                          : launch_decode<float, D_, 8, false>(a, s);
+  };
+  const std::integral_constant<int, 1> one;
+  const std::integral_constant<int, 2> two;
+  const std::integral_constant<int, 64> d64;
+  const std::integral_constant<int, 128> d128;
+  const std::integral_constant<int, 256> d256;
   int out;
   if (dtype == PS_DTYPE_F32)
-    if (D <= 128)
-      out = a.group == 1 ? launch_decode<float, 128, 1>(a, s) : a.group <= 4 ? launch_decode<float, 128, 4>(a, s) : launch_decode<float, 128, 8>(a, s);
-    else
-      out = a.group == 1 ? launch_decode<float, 256, 1>(a, s) : a.group <= 4 ? launch_decode<float, 256, 4>(a, s) : launch_decode<float, 256, 8>(a, s);
+    out = D <= 128 ? f32(d128) : f32(d256);
   else if (D <= 64)
-    out = a.group <= 8 ? launch_decode<Bf16, 64, 1>(a, s) : launch_decode<Bf16, 64, 2>(a, s);
+    out = a.group <= 8 ? bf16(d64, one) : bf16(d64, two);
   else if (D <= 128)
-    out = a.group <= 8 ? launch_decode<Bf16, 128, 1>(a, s) : launch_decode<Bf16, 128, 2>(a, s);
+    out = a.group <= 8 ? bf16(d128, one) : bf16(d128, two);
   else
-    out = launch_decode<Bf16, 256, 1>(a, s);
+    out = bf16(d256, one);
   return out == PS_OK ? out : refused(out, ws, s);
 }
 
