@@ -354,20 +354,22 @@ struct DecodeMath<float, DP, NB> {   // NB heads on the f32 pipe: a lane has hal
   __device__ __forceinline__ void chunk(uint32_t ks, uint32_t vs, int lo, int nv, float scale2, const uint8_t* mem, float* ps, int lane) {
     const int key = lane & 15, half = lane >> 4;
     const float* q = reinterpret_cast<const float*>(mem) + half * kHalf;
-    float s[kHeads];
+    float s[kHeads], u[kHeads];   // (two sums each, half as long)
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h) s[h] = 0.f;
+    for (int h = 0; h < kHeads; ++h) s[h] = u[h] = 0.f;
 #pragma unroll 4
     for (int p = 0; p < DP / 8; ++p) {
       const float4 k = at(ks, key, half * (DP / 8) + p);
 #pragma unroll
       for (int h = 0; h < kHeads; ++h) {
         const float4 w = *reinterpret_cast<const float4*>(q + h * 2 * kHalf + 4 * p);
-        s[h] = fmaf(k.x, w.x, fmaf(k.y, w.y, fmaf(k.z, w.z, fmaf(k.w, w.w, s[h]))));
+        s[h] = fmaf(k.x, w.x, fmaf(k.y, w.y, s[h]));
+        u[h] = fmaf(k.z, w.z, fmaf(k.w, w.w, u[h]));
       }
     }
 #pragma unroll
     for (int h = 0; h < kHeads; ++h) {
+      s[h] += u[h];
       s[h] += __shfl_xor_sync(0xffffffffu, s[h], 16);
       const float x = key >= lo && key < nv ? s[h] * scale2 : -INFINITY;
       float v = x;
@@ -383,7 +385,8 @@ struct DecodeMath<float, DP, NB> {   // NB heads on the f32 pipe: a lane has hal
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[h][w][i] *= f;
       }
-      const float p = ex2_ftz(x - (m[h] == -INFINITY ? 0.f : m[h]));
+      // (the scaled score is rounded with the difference only)
+      const float p = x == -INFINITY ? 0.f : ex2_ftz(fmaf(s[h], scale2, m[h] == -INFINITY ? 0.f : -m[h]));
       float t = p;
 #pragma unroll
       for (int i = 8; i >= 1; i >>= 1) t += __shfl_xor_sync(0xffffffffu, t, i);
