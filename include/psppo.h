@@ -578,7 +578,7 @@ int ps_dropout_rows(int64_t N, int d, int dtype, const void* x, int64_t ldx, con
  * Workspace: none for the forward; 256 bytes for a backward without gain gradients, else
  *   ps_residual_norm_workspace_size(d).
  * Limits: 1 <= d, rows of at most 32768 bytes (16384 bf16 or 8192 f32 columns; of rows that are not whole 16 bytes at
- *   16-byte boundaries 16370 and 8186, else PS_ERR_UNSUPPORTED), finite scales, eps >= 0.
+ *   16-byte boundaries 16377 and 8189, else PS_ERR_UNSUPPORTED), finite scales, eps >= 0.
  * ------------------------------------------------------------------------- */
 enum { PS_NORM_BRANCH = 1, PS_NORM_OUT = 2 };
 int ps_residual_norm_fwd(int64_t N, int d, int dtype, int norms, const void* x, int64_t ldx,

@@ -384,7 +384,8 @@ class ResidualNorm:
 
     def backward(self, do, dh, h, y=None, gy=None, go=None, gate=None, dw_accumulate: bool = False):
         """(dx, dy, dgy, dgo, dgate) from the gradients of o (None without the output's norm) and of h (None: 0), the forward's h
-        and the branch; what the forward did not have is None."""
+        and the branch. A gain that was not given is 1 and has a gradient; dgate is None without a gate, the branch's are without
+        a branch."""
         s = self.s
         rc = self._fast_bwd(self._plan, do, dh, h, y, gy, go, gate, dw_accumulate)
         if rc is None:

@@ -93,11 +93,16 @@ class PagedCache:
             rows[i, :len(self._own[b])] = torch.tensor(self._own[b], dtype=torch.int32)
         self.table[torch.tensor(seqs, device=self.device)] = rows.to(self.device)
 
+    def _seq(self, seq: int) -> int:
+        if not 0 <= seq < self.s.seqs:
+            raise IndexError(f"sequence {seq} of {self.s.seqs}")
+        return int(seq)
+
     def reserve(self, seq: int, n: int):
         """Pages for the first n positions of a sequence (those it has stay)."""
-        s = self.s
+        s, seq = self.s, self._seq(seq)
         need = -(-n // s.page)
-        if need > self.width:
+        if not 0 <= need <= self.width:
             raise ValueError(f"{n} positions, built for {s.max_len}")
         own = self._own[seq]
         if need - len(own) > len(self._free):
@@ -111,10 +116,10 @@ class PagedCache:
     def share(self, src: int, dst, n: int):
         """The first n positions of `src` for the sequences `dst`, which have none: whole pages are shared, a begun one is copied."""
         s, whole = self.s, n // self.s.page
-        dst = [int(b) for b in dst]
+        src, dst = self._seq(src), [self._seq(b) for b in dst]
         if any(self._own[b] for b in dst) or src in dst or len(set(dst)) != len(dst):
             raise ValueError("share: the sequences must be different ones without pages")
-        if n > len(self._own[src]) * s.page:
+        if not 0 <= n <= len(self._own[src]) * s.page:
             raise ValueError(f"share: sequence {src} has pages for {len(self._own[src]) * s.page} positions, not {n}")
         begun = n % s.page != 0
         if begun and len(dst) > len(self._free):
@@ -134,6 +139,7 @@ class PagedCache:
 
     def release(self, seq: int):
         """A sequence's pages back, except those that others still have; its length becomes 0."""
+        seq = self._seq(seq)
         for p in reversed(self._own[seq]):
             self._users[p] -= 1
             if self._users[p] == 0:

@@ -43,6 +43,7 @@ struct NormArgs {
   int apart;                      // SHIFT: bits of the arrays (inputs, then outputs from bit 4) whose rows lie otherwise
   const void* like;               // SHIFT: the array that the others lie like, and its pitch
   int64_t ld_like;
+  int edge;                       // SHIFT: rows at either end whose chunks may reach over the whole tensor's ends
   const void *gy, *go;            // gains [d], nullptr: 1
   const float* gate;              // [N], nullptr: 1
   int post, pre;                  // a norm of the branch; a normed output (or its gradient)
@@ -272,7 +273,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
         for (int j = 0; j < CH; ++j) {
           const int c = col(j);
           // a chunk with some of the row; beyond the first row's start and the last one's end it goes element by element
-          if (SHIFT ? c + E <= 0 || c >= a.d || (c < 0 && row == 0) || (c + E > a.d && row == a.N - 1) : !some(j)) continue;
+          if (SHIFT ? c + E <= 0 || c >= a.d || (c < 0 && row < a.edge) || (c + E > a.d && row >= a.N - a.edge) : !some(j)) continue;
           if (a.copied >> arr & 1) lane_copy(smem_addr(slot(st, arr, j)), from + j * apart_j);
         }
       }
@@ -300,7 +301,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
     if (SHIFT && row < a.N) {
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
-        if (some(j) && ((a.apart & 15) || ((row == 0 || row == a.N - 1) && !all(j)))) load_plainly(row, st, j);
+        if (some(j) && ((a.apart & 15) || ((row < a.edge || row >= a.N - a.edge) && !all(j)))) load_plainly(row, st, j);
         if (!some(j) || all(j)) continue;
         uint32_t keep[4];   // of the row's end only its columns
 #pragma unroll
@@ -724,6 +725,7 @@ static int run_norm(NormArgs a, bool shift, int& grid, cudaStream_t s) {
   if (a.chunks > 4 * kNormThreads) return PS_ERR_UNSUPPORTED;
   const NormPlan p = norm_plan(a.chunks, a.d, BWD);
   a.team = p.team, a.teams = p.teams;
+  a.edge = (E + a.d - 2) / a.d;                           // (a chunk reaches E - 1 columns over a row's end at most)
   a.inv_d = static_cast<float>(1.0 / a.d);
   a.inv_d_lo = static_cast<float>(1.0 / a.d - a.inv_d);
   switch (p.ch) {

@@ -455,7 +455,7 @@ PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const DecodePlan* p = n == 6 ? plan_of<DecodePlan>(a[0]) : nullptr;
     const CachePlan* c = p ? plan_of<CachePlan>(a[1]) : nullptr;
     const at::Tensor* q = c ? tensor(a[3], p->device) : nullptr;
-    if (!q || q->dim() != 2 || c->Hk != p->Hk || c->D != p->D || c->dtype != p->dtype) return ordinary();
+    if (!q || q->dim() != 2 || c->device != p->device || c->Hk != p->Hk || c->D != p->D || c->dtype != p->dtype) return ordinary();
     const int64_t N = q->size(0), w = static_cast<int64_t>(p->Hq) * p->D;
     Rows rq, ro;
     int64_t layer;
