@@ -97,7 +97,7 @@ def run(steps=24, prompts=3, K=4, d=256, F=520, V=1000, longest=40, capture=True
     graph, new = None, []
     for t in range(steps):
         noise = -torch.log(-torch.log(torch.rand(n, V, device="cuda", generator=g).clamp(1e-6, 1 - 1e-6)))
-        tokens = ((rows @ table.t()).float() / d ** 0.5 + noise).argmax(dim=1)
+        tokens = ((rows @ table.t()).float() / d + noise).argmax(dim=1)
         new.append(tokens)
         x.copy_(table[tokens])
         if graph is not None:

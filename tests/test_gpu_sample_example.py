@@ -50,6 +50,7 @@ def _last_row(block, x):
 def test_the_last_step(steps, prompts, K, capture):
     block, table, tokens, rows = _example().run(steps, prompts, K, capture=capture)
     assert len(tokens) == prompts * K and block.cache.lengths.tolist() == [len(t) for t in tokens]
+    assert len({tuple(t.tolist()) for t in tokens}) == len(tokens)        # (sampled: completions differ)
     for b, t in enumerate(tokens):
         want = _last_row(block, table[t].double())
         off = (torch.linalg.norm(rows[b].double() - want) / torch.linalg.norm(want)).item()
