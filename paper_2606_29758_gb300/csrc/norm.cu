@@ -98,6 +98,12 @@ static __device__ __forceinline__ float sum2(P2 v) {
 // time, half a sector each, 147 instead of 125 us for a backward of 12000 rows of 3584 bf16.)
 __host__ __device__ constexpr int norm_thread_bytes(int ch, bool bwd) { return norm_arrays(bwd) * ch * 16; }   // (and 4 for the row's gate)
 
+// The larger of the sizes of two pairs of bf16 (their signs are any).
+static __device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 // h + l of two f32: with h' + l' (the sums' lower parts added plainly).
 static __device__ __forceinline__ void add_two(float& h, float& l, float h2, float l2) {
   const float s = h + h2, b = s - h;
@@ -110,10 +116,26 @@ static __device__ __forceinline__ float settled(float a, float a_lo, float x, fl
   const float left = ((ax - (s - b)) + (p - b)) + (fmaf(w, n, -p) + fmaf(a, x, -ax) + fmaf(w_lo, n, a_lo * x));
   return s + left;
 }
-// Whether v, of |a x| and a like share, lies within their roundings of the middle of two bf16 values.
-static __device__ __forceinline__ bool in_the_middle(float v, float ax) {
-  const float m = __uint_as_float((__float_as_uint(v) & 0xffff0000u) | 0x8000u);
-  return fabsf(v - m) <= 2.4e-7f * (fabsf(v) + fabsf(ax));   // 2^-22
+// Whether v is the middle of two bf16 values or up to two f32 from it.
+static __device__ __forceinline__ bool in_the_middle(float v) { return (__float_as_uint(v) << 16) + 0x80020000u < 0x50000u; }
+// The sum over a warp of h + l, h >= 0 and |l| of up to 32 roundings of h, the same bits in any order: in units of four roundings
+// of the largest h (22 bits) and in 2^-18 of those, by integers. (Exchanges with a sum of two parts each took three times that.)
+static __device__ __forceinline__ void warp_sum_two(float& h, float& l) {
+  const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(h));
+  if (top >= 0x7f800000u) {   // infinite, or not a number
+    h = __uint_as_float(top);
+    l = 0.f;
+    return;
+  }
+  const uint32_t e = max(top >> 23, 48u);
+  const float g = __uint_as_float((e - 21) << 23), inv_g = __uint_as_float((275 - e) << 23), magic = 12582912.f;   // 1.5 2^23
+  const float big = fmaf(h, inv_g, magic);
+  const float rest = fmaf(-(big - magic), g, h) + l, small = fmaf(rest, inv_g * 262144.f, magic);
+  const int hs = __reduce_add_sync(0xffffffffu, __float_as_int(big) - 0x4b400000);
+  const int ls = __reduce_add_sync(0xffffffffu, __float_as_int(small) - 0x4b400000);
+  const float sum = static_cast<float>(hs & ~15) * g, left = static_cast<float>((hs & 15) * 262144 + ls) * (g * (1.f / 262144.f));
+  h = sum + left;
+  l = left - (h - sum);
 }
 
 template <class T, int CH, bool BWD, bool SHIFT, bool EXACT>
@@ -156,10 +178,14 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
   // four lanes a value, which takes 9 exchanges instead of 30.
   const int warps = a.team / 32, w0 = unit_in * (a.team > 256 ? 16 : 8);
   auto publish = [&](float (&v)[K], int which, int parity) {
-    if (EXACT) {
+    if (EXACT && which == 0) {
+      if (a.team < 32) {
 #pragma unroll
-      for (int o = 16; o >= 1; o >>= 1)
-        if (a.team > o) add_two(v[0], v[K - 1], __shfl_xor_sync(0xffffffffu, v[0], o), __shfl_xor_sync(0xffffffffu, v[K - 1], o));
+        for (int o = 8; o >= 1; o >>= 1)
+          if (a.team > o) add_two(v[0], v[K - 1], __shfl_xor_sync(0xffffffffu, v[0], o), __shfl_xor_sync(0xffffffffu, v[K - 1], o));
+      } else {
+        warp_sum_two(v[0], v[K - 1]);
+      }
       if (a.team > 32 && lane == 0) {
         red[which][parity][2 * (w0 + t / 32)] = v[0];
         red[which][parity][2 * (w0 + t / 32) + 1] = v[K - 1];
@@ -183,7 +209,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
       for (int o = 16; o >= 1; o >>= 1)
         if (a.team > o)
 #pragma unroll
-          for (int i = 0; i < K; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+          for (int i = 0; i < (BWD ? K : 1); ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
       if (!BWD && a.team > 32 && lane == 0) red[which][parity][w0 + t / 32] = v[0];
     }
   };
@@ -191,19 +217,11 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
     if (a.team > 32) asm volatile("bar.sync %0, %1;" ::"r"(unit_in + 1), "r"(a.team) : "memory");
   };
   auto totals = [&](float (&v)[K], int which, int parity) {
-    if (EXACT) {
+    if (EXACT && which == 0) {
       if (a.team <= 32) return;
-      const float4* from = reinterpret_cast<const float4*>(red[which][parity] + 2 * w0);   // (zeros behind the last warp)
-      float4 x = from[0];
+      const float2 x = lane < warps ? *reinterpret_cast<const float2*>(red[which][parity] + 2 * (w0 + lane)) : make_float2(0.f, 0.f);
       v[0] = x.x, v[K - 1] = x.y;
-      add_two(v[0], v[K - 1], x.z, x.w);
-#pragma unroll
-      for (int i = 1; i < 8; ++i) {
-        if (i >= 4 && a.team <= 256) break;
-        x = from[i];
-        add_two(v[0], v[K - 1], x.x, x.y);
-        add_two(v[0], v[K - 1], x.z, x.w);
-      }
+      warp_sum_two(v[0], v[K - 1]);
     } else if (BWD) {
       if (a.team < 32) return;
       float x = v[0];
@@ -396,19 +414,32 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
     } else {
       P2 q2 = zero2;
       if (EXACT) {
-        s[0] = s[K - 1] = 0.f;
-        if (a.post)
+        // A square of eight bits is exact. From the largest one on each sum is at most doubled, so that its difference to the sum
+        // before it is exact, and so is what it left out (four packed operations for two squares).
+        uint32_t m = 0;
 #pragma unroll
-          for (int j = 0; j < CH; ++j) {
-            const V8 y = get(st, 1, j);
+        for (int j = 0; j < CH; ++j) {
+          const uint4 w = *reinterpret_cast<const uint4*>(slot(st, 1, j));
+          m = max_abs2(max_abs2(m, w.x), max_abs2(w.y, max_abs2(w.z, w.w)));
+        }
+        const float most = fmaxf(__uint_as_float(m << 16 & 0x7fffffffu), __uint_as_float(m & 0x7fff0000u)), from = most * most;
+        const P2 minus = two(-1.f, -1.f), one = two(1.f, 1.f);
+        P2 hi = two(from, from), lo = zero2;
 #pragma unroll
-            for (int i = 0; i < E / 2; ++i) {
-              float u, v;
-              split2(y.p[i], u, v);
-              add_two(s[0], s[K - 1], u * u, 0.f);   // (a square of eight bits is exact)
-              add_two(s[0], s[K - 1], v * v, 0.f);
-            }
+        for (int j = 0; j < CH; ++j) {
+          const V8 y = get(st, 1, j);
+#pragma unroll
+          for (int i = 0; i < E / 2; ++i) {
+            const P2 sum = fma2(y.p[i], y.p[i], hi);
+            lo = fma2(fma2(y.p[i], y.p[i], fma2(sum, minus, hi)), one, lo);
+            hi = sum;
           }
+        }
+        float h2, l2;
+        split2(hi, s[0], h2);
+        split2(lo, s[K - 1], l2);
+        add_two(s[0], s[K - 1], h2, l2);
+        if (s[0] < INFINITY) add_two(s[0], s[K - 1], -2.f * from, 0.f);
         return;
       }
       if (a.post)
@@ -458,50 +489,60 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
           ry = rsqrtf(v);
           const float q = ry * ry;
           const float left = fmaf(-v, q, 1.f) - fmaf(v, fmaf(ry, ry, -q), v_lo * q);
-          const float r_lo = 0.5f * ry * left, wr = w * ry;
+          const float r_lo = v < INFINITY ? 0.5f * ry * left : 0.f, wr = w * ry;
           w_lo = fmaf(w, ry, -wr) + fmaf(w, r_lo, w_lo * ry);
           w = wr;
         }
       }
-      const P2 w2 = two(w, w), a2 = two(a.a, a.a);
+      const P2 w2 = two(w, w), a2 = two(a.a, a.a), wl2 = two(w_lo, w_lo), al2 = two(a.a_lo, a.a_lo), minus = two(-1.f, -1.f);
       V8 h[CH];
       P2 q = zero2;
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
         const V8 x = get(st, 0, j);
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i) h[j].p[i] = mul2(x.p[i], a2);
-        if (open) {
+        if (EXACT && open) {
           const V8 y = get(st, 1, j), g = gain_y(j);
+          V8 n;
+          bool near = false;
 #pragma unroll
-          // (the product rounded before the sum: scales like 0.7 then give sums of few bits what they give in decimals)
-          for (int i = 0; i < E / 2; ++i) h[j].p[i] = add2(h[j].p[i], mul2(mul2(y.p[i], g.p[i]), w2));
-          if (EXACT) {
-            bool near = false;
+          for (int i = 0; i < E / 2; ++i) {
+            n.p[i] = mul2(y.p[i], g.p[i]);   // (exact)
+            // a x + w n up to one f32 and a half: negated, and what its first parts left
+            const P2 ax = mul2(mul2(x.p[i], a2), minus);
+            const P2 left = fma2(wl2, n.p[i], fma2(x.p[i], al2, fma2(x.p[i], a2, ax)));
+            h[j].p[i] = fma2(fma2(mul2(w2, minus), n.p[i], ax), minus, left);
+            float u, v;
+            split2(h[j].p[i], u, v);
+            near |= in_the_middle(u) || in_the_middle(v);
+          }
+          if (near) {
             float hv[E], xv[E], nv[E];
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) {
               split2(h[j].p[i], hv[2 * i], hv[2 * i + 1]);
               split2(x.p[i], xv[2 * i], xv[2 * i + 1]);
-              near |= in_the_middle(hv[2 * i], a.a * xv[2 * i]) || in_the_middle(hv[2 * i + 1], a.a * xv[2 * i + 1]);
-            }
-            if (near) {
+              split2(n.p[i], nv[2 * i], nv[2 * i + 1]);
 #pragma unroll
-              for (int i = 0; i < E / 2; ++i) {
-                split2(mul2(y.p[i], g.p[i]), nv[2 * i], nv[2 * i + 1]);
-#pragma unroll
-                for (int k = 2 * i; k < 2 * i + 2; ++k)
-                  if (in_the_middle(hv[k], a.a * xv[k])) hv[k] = settled(a.a, a.a_lo, xv[k], w, w_lo, nv[k]);
-                h[j].p[i] = two(hv[2 * i], hv[2 * i + 1]);
-              }
+              for (int k = 2 * i; k < 2 * i + 2; ++k)
+                if (in_the_middle(hv[k])) hv[k] = settled(a.a, a.a_lo, xv[k], w, w_lo, nv[k]);
+              h[j].p[i] = two(hv[2 * i], hv[2 * i + 1]);
             }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < E / 2; ++i) h[j].p[i] = mul2(x.p[i], a2);
+          if (open) {
+            const V8 y = get(st, 1, j), g = gain_y(j);
+#pragma unroll
+            // (the product rounded before the sum: scales like 0.7 then give sums of few bits what they give in decimals)
+            for (int i = 0; i < E / 2; ++i) h[j].p[i] = add2(h[j].p[i], mul2(mul2(y.p[i], g.p[i]), w2));
           }
         }
         if (live && a.in[1]) put(0, row, j, h[j]);
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) q = fma2(h[j].p[i], h[j].p[i], q);
       }
-      float sh[K] = {sum2(q)};   // (EXACT: the second part 0)
+      float sh[K] = {sum2(q)};
       publish(sh, 1, parity);
       issue(u + ST * stride, st);   // (the stage has been read: its values went into what was published)
       sync();
