@@ -561,7 +561,9 @@ int ps_dropout_rows(int64_t N, int d, int dtype, const void* x, int64_t ldx, con
  *
  *   n = y r_y gy, r_y = (mean over the row of y^2 + eps)^(-1/2) with PS_NORM_BRANCH, else 1;
  *   h = res_scale x + branch_scale gate_i n;  with PS_NORM_OUT o = h r_h go, r_h = (mean h^2 + eps)^(-1/2), taken from h
- *   before it is rounded to the rows' type. y NULL: no branch, h = x whatever res_scale is (not written), o its norm.
+ *   before it is rounded to the rows' type. (bf16 h after the branch's norm, in calls of up to 2^25 values N d: the f32 nearest
+ *   to the sum, rounded, in whatever order the row is summed.) y NULL: no branch, h = x whatever res_scale is (not written),
+ *   o its norm.
  *   Backward: dH = dh + r_h (go do - h r_h^2 mean(go do h)), dx = res_scale dH, dn = branch_scale gate_i dH,
  *   dy = r_y (gy dn - y r_y^2 mean(gy dn y)) or gy dn, dgy = sum over rows of dn y r_y, dgo = sum of do h r_h,
  *   dgate_i = branch_scale sum over columns of dH n.
@@ -607,14 +609,14 @@ int ps_residual_norm_bwd(int64_t N, int d, int dtype, int norms, const void* dou
  *   reads. Workspace: 256 bytes.
  * ps_paged_decode: for each sequence b and query head h, with the key head h / (Hq / Hk) and s_j = scale q.k_j over
  *   the last `window` (0: all) of the positions below lengths[b], o = sum_j softmax(s)_j v_j and lse = log sum_j e^s_j. The
- *   new token's own key and value are in the cache (ps_paged_append comes first). A length of 0 gives o = 0, lse =
- *   -inf. q, o [seqs][Hq D] (pitches of whole 16 bytes), in the cache's type; o may be q (same pointer
- *   and pitch); lse [seqs][Hq] f32 or NULL. Table entries behind a sequence's last page are not read, nor are
- *   slots behind its length. A length outside [0, ldt page] sets PS_DEV_BAD_LENGTH, a page id outside
- *   [0, pages) PS_DEV_BAD_PAGE; those sequences' outputs (the page's key heads') are NaN. Sums and weights are f32 (the
- *   weights as operands of the tensor cores in two bf16 parts, 2^-17, so that an infinite value may give NaN where one
- *   part would give an infinity); a fixed order, reruns are bit-identical; the
- *   order depends on the lengths of all sequences of the call.
+ *   new token's own key and value are in the cache (ps_paged_append comes first). A length of 0 gives o = 0, lse = -inf; scores
+ *   that are all -inf give NaN and lse = -inf, as 0 / 0. q, o [seqs][Hq D] (pitches of whole 16 bytes), in the cache's type;
+ *   o may be q (same pointer and pitch); lse [seqs][Hq] f32 or NULL. Table entries behind a sequence's last page are not read;
+ *   slots behind its length may hold anything. A length outside [0, ldt page] sets PS_DEV_BAD_LENGTH, a page id outside
+ *   [0, pages) PS_DEV_BAD_PAGE; those sequences' outputs (the page's key heads') are NaN. Copies that never come set
+ *   PS_DEV_TIMEOUT. Sums and weights are f32 (the weights as operands of the tensor cores in two bf16 parts, 2^-17, so that an
+ *   infinite value may give NaN where one part would give an infinity); a fixed order, reruns are bit-identical; the order
+ *   depends on the lengths of all sequences of the call.
  *   Workspace: ps_paged_decode_workspace_size(D).
  * Limits: 16 <= D <= 256, a multiple of 16, Hk <= Hq <= 65536, a multiple, pages >= 1, 16-byte aligned pointers.
  * ------------------------------------------------------------------------- */

@@ -24,10 +24,14 @@ namespace psk {
 // Rows that do not start at 16-byte boundaries or have no whole chunks (SHIFT): a chunk is the columns from one
 // 16-byte boundary to the next, so the first and last chunks reach over the row's ends; a thread keeps its columns as its rows are
 // a multiple of eight apart, whose starts lie alike.
-// EXACT (bf16 forwards with the branch's norm of up to kExactValues values): h is the nearest f32 of the sum rounded to bf16, whatever the order of the
-// row's sums: y gy is exact in f32, the root and the scales are kept in two f32 each, and a value whose f32 sum lies next to the
-// middle of two bf16 values is settled by the roundings that it left. Otherwise a few of 10^5 values are rounded to the other
-// neighbour, which in sums over few rows of the backward (dgo) shows as ten times f32's error.
+// EXACT (bf16 forwards with the branch's norm of up to kExactValues values): h is the nearest f32 of the sum rounded to bf16,
+// whatever the order of the row's sums: the sum of squares, the root and the scales are kept in two f32 each (to 2^-36), y gy is exact in
+// f32, the sum over the streams is right up to an f32 and a half, and a value that lies so near to the middle of two bf16 values is
+// settled by the roundings that it left. Otherwise some 2 of 10^5 values are rounded to the other neighbour, and one of
+// those may show in dgo's sums over few rows as a hundred times f32's error.
+// Forward and backward of 60000 rows of 3584 bf16 with both norms and a gate 299 and 506 us (5.75 and 5.1 TB/s), without branch norm
+// and gate 265 and 496 (6.5 and 5.2); of 30000 f32 rows 289 and 387 (5.9 and 6.7); the backward is bound by issue and by its
+// sums' way through the team (14 warps an SM, 61 % of the issue slots).
 constexpr int kNormThreads = 512;   // at most
 __host__ __device__ constexpr int norm_arrays(bool bwd) { return bwd ? 4 : 2; }   // h, y, do, dh; x, y
 // Rows in shared memory: as many as fit beside what the registers allow of threads.
@@ -118,6 +122,14 @@ static __device__ __forceinline__ float settled(float a, float a_lo, float x, fl
 }
 // Whether v is the middle of two bf16 values or up to two f32 from it.
 static __device__ __forceinline__ bool in_the_middle(float v) { return (__float_as_uint(v) << 16) + 0x80020000u < 0x50000u; }
+// Smaller of l and the lower halves of u and v past two before the middle of two bf16 values, in 16 bits each.
+static __device__ __forceinline__ uint32_t low_min2(uint32_t l, float u, float v) {
+  uint32_t both;
+  asm("prmt.b32 %0, %1, %2, 0x5410;" : "=r"(both) : "r"(__float_as_uint(u)), "r"(__float_as_uint(v)));
+  asm("add.u16x2 %0, %0, %1;" : "+r"(both) : "r"(0x80028002u));
+  asm("min.u16x2 %0, %0, %1;" : "+r"(l) : "r"(both));
+  return l;
+}
 // The sum over a warp of h + l, h >= 0 and |l| of up to 32 roundings of h, the same bits in any order: in units of four roundings
 // of the largest h (22 bits) and in 2^-18 of those, by integers. (Exchanges with a sum of two parts each took three times that.)
 static __device__ __forceinline__ void warp_sum_two(float& h, float& l) {
@@ -495,6 +507,8 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
         }
       }
       const P2 w2 = two(w, w), a2 = two(a.a, a.a), wl2 = two(w_lo, w_lo), al2 = two(a.a_lo, a.a_lo), minus = two(-1.f, -1.f);
+      const P2 minus_a = mul2(a2, minus), minus_w = mul2(w2, minus);
+      const bool unit = a.a == 1.f && a.a_lo == 0.f;
       V8 h[CH];
       P2 q = zero2;
 #pragma unroll
@@ -503,19 +517,23 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
         if (EXACT && open) {
           const V8 y = get(st, 1, j), g = gain_y(j);
           V8 n;
-          bool near = false;
+          uint32_t lowest = 0xffffffffu;
 #pragma unroll
           for (int i = 0; i < E / 2; ++i) {
             n.p[i] = mul2(y.p[i], g.p[i]);   // (exact)
             // a x + w n up to one f32 and a half: negated, and what its first parts left
-            const P2 ax = mul2(mul2(x.p[i], a2), minus);
-            const P2 left = fma2(wl2, n.p[i], fma2(x.p[i], al2, fma2(x.p[i], a2, ax)));
-            h[j].p[i] = fma2(fma2(mul2(w2, minus), n.p[i], ax), minus, left);
+            if (unit) {
+              h[j].p[i] = fma2(wl2, n.p[i], fma2(w2, n.p[i], x.p[i]));
+            } else {
+              const P2 ax = mul2(x.p[i], minus_a);
+              const P2 left = fma2(wl2, n.p[i], fma2(x.p[i], al2, fma2(x.p[i], a2, ax)));
+              h[j].p[i] = fma2(fma2(minus_w, n.p[i], ax), minus, left);
+            }
             float u, v;
             split2(h[j].p[i], u, v);
-            near |= in_the_middle(u) || in_the_middle(v);
+            lowest = low_min2(lowest, u, v);
           }
-          if (near) {
+          if ((lowest & 0xffffu) <= 4u || lowest <= 0x4ffffu) {   // (as in_the_middle, for all at once)
             float hv[E], xv[E], nv[E];
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) {
@@ -751,7 +769,8 @@ static int launch_as(NormArgs& a, const NormPlan& p, int& grid, cudaStream_t s) 
              ? PS_OK
              : PS_ERR_CUDA;
 }
-// Up to here the forward's sums are exact (EXACT above).
+// Up to here a forward is EXACT (above), at 1.3 times the time (9000 rows of 3584: 60.7 against 46.7 us; 6030 of 1536: 16.8 against
+// 13.4; 200000 of 64: 26.4 against 19.8; 60000 of 3584 would take 380 instead of 280); sums over more rows smooth the others out.
 constexpr int64_t kExactValues = 1 << 25;
 template <class T, int CH, bool BWD, bool SHIFT>
 static int launch_norm(NormArgs& a, const NormPlan& p, int& grid, cudaStream_t s) {
