@@ -561,9 +561,8 @@ int ps_dropout_rows(int64_t N, int d, int dtype, const void* x, int64_t ldx, con
  *
  *   n = y r_y gy, r_y = (mean over the row of y^2 + eps)^(-1/2) with PS_NORM_BRANCH, else 1;
  *   h = res_scale x + branch_scale gate_i n;  with PS_NORM_OUT o = h r_h go, r_h = (mean h^2 + eps)^(-1/2), taken from h
- *   before it is rounded to the rows' type. (bf16 h after the branch's norm, in calls of up to 2^25 values N d: the f32 nearest
- *   to the sum, rounded, in whatever order the row is summed.) y NULL: no branch, h = x whatever res_scale is (not written),
- *   o its norm.
+ *   before it is rounded to the rows' type. (bf16 h after the branch's norm: the f32 nearest to the sum, rounded, in whatever
+ *   order the row is summed.) y NULL: no branch, h = x whatever res_scale is (not written), o its norm.
  *   Backward: dH = dh + r_h (go do - h r_h^2 mean(go do h)), dx = res_scale dH, dn = branch_scale gate_i dH,
  *   dy = r_y (gy dn - y r_y^2 mean(gy dn y)) or gy dn, dgy = sum over rows of dn y r_y, dgo = sum of do h r_h,
  *   dgate_i = branch_scale sum over columns of dH n.

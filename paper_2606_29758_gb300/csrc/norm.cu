@@ -24,14 +24,15 @@ namespace psk {
 // Rows that do not start at 16-byte boundaries or have no whole chunks (SHIFT): a chunk is the columns from one
 // 16-byte boundary to the next, so the first and last chunks reach over the row's ends; a thread keeps its columns as its rows are
 // a multiple of eight apart, whose starts lie alike.
-// EXACT (bf16 forwards with the branch's norm of up to kExactValues values): h is the nearest f32 of the sum rounded to bf16,
+// EXACT (bf16 forwards with the branch's norm): h is the nearest f32 of the sum rounded to bf16,
 // whatever the order of the row's sums: the sum of squares, the root and the scales are kept in two f32 each (to 2^-36), y gy is exact in
 // f32, the sum over the streams is right up to an f32 and a half, and a value that lies so near to the middle of two bf16 values is
 // settled by the roundings that it left. Otherwise some 2 of 10^5 values are rounded to the other neighbour, and one of
 // those may show in dgo's sums over few rows as a hundred times f32's error.
-// Forward and backward of 60000 rows of 3584 bf16 with both norms and a gate 299 and 506 us (5.75 and 5.1 TB/s), without branch norm
-// and gate 265 and 496 (6.5 and 5.2); of 30000 f32 rows 289 and 387 (5.9 and 6.7); the backward is bound by issue and by its
-// sums' way through the team (14 warps an SM, 61 % of the issue slots).
+// That takes a third of the time more (60000 rows of 3584 without a gate 280 -> 364 us, 6030 of 1536 13.4 -> 16.3).
+// Forward and backward of 60000 rows of 3584 bf16 with both norms and a gate 373 and 507 us (4.6 and 5.1 TB/s), without branch norm and
+// gate 258 and 497 (6.7 and 5.2); of 30000 f32 rows 275 and 388 (6.3 and 6.7). Both are bound by latency and issue at the 14 warps
+// of an SM that the registers allow (forward 50 % of the issue slots, backward 61 %), the lighter ones by HBM.
 constexpr int kNormThreads = 512;   // at most
 __host__ __device__ constexpr int norm_arrays(bool bwd) { return bwd ? 4 : 2; }   // h, y, do, dh; x, y
 // Rows in shared memory: as many as fit beside what the registers allow of threads.
@@ -169,8 +170,8 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
   const int rows_a_unit = a.team < 32 ? 32 / a.team : 1;
   const int64_t units = (a.N + rows_a_unit - 1) / rows_a_unit, stride = static_cast<int64_t>(gridDim.x) * units_here;
   const int64_t u0 = static_cast<int64_t>(blockIdx.x) * units_here + unit_in;
-  const int stage_bytes = threads * BYTES;
-  const int step = threads * 16;   // from one of a thread's pieces to the next
+  // from one of a thread's pieces to the next (the forward's in places that the compiler knows)
+  const int step = (BWD ? threads : kNormThreads) * 16, stage_bytes = step / 16 * BYTES;
   uint8_t* const mine = norm_smem + tid * 16;
   const P2 zero2 = two(0.f, 0.f);
   auto row_of = [&](int64_t u) { return u * rows_a_unit + sub; };
@@ -216,13 +217,16 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
       x[0] += __shfl_xor_sync(0xffffffffu, x[0], 1);
       v[0] = x[0];   // of value lane / 4
       if (a.team > 32 && (lane & 3) == 0) red[which][parity][(unit_in * warps + t / 32) * 8 + lane / 4] = x[0];
+    } else if (!BWD && a.team >= 32) {
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+      if (a.team > 32 && lane == 0) red[which][parity][w0 + t / 32] = v[0];
     } else {
 #pragma unroll
-      for (int o = 16; o >= 1; o >>= 1)
+      for (int o = 8; o >= 1; o >>= 1)
         if (a.team > o)
 #pragma unroll
           for (int i = 0; i < (BWD ? K : 1); ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-      if (!BWD && a.team > 32 && lane == 0) red[which][parity][w0 + t / 32] = v[0];
     }
   };
   auto sync = [&]() {
@@ -736,7 +740,7 @@ static NormPlan norm_plan(int chunks, int d, bool bwd) {
   for (int t = p.teams + 1; t * unit_threads <= kNormThreads; ++t)
     if (filled(t) > filled(p.teams)) p.teams = t;
   p.threads = p.teams * unit_threads;
-  p.smem = static_cast<size_t>(norm_stages(p.ch, bwd)) * (norm_thread_bytes(p.ch, bwd) + 4) * p.threads;
+  p.smem = static_cast<size_t>(norm_stages(p.ch, bwd)) * (norm_thread_bytes(p.ch, bwd) + 4) * (bwd ? p.threads : kNormThreads);
   const size_t sums = bwd ? static_cast<size_t>(p.teams) * 2 * d * sizeof(float) : 0;
   if (p.smem < sums) p.smem = sums;
   p.blocks_a_sm = 512 / p.threads;
@@ -769,13 +773,10 @@ static int launch_as(NormArgs& a, const NormPlan& p, int& grid, cudaStream_t s) 
              ? PS_OK
              : PS_ERR_CUDA;
 }
-// Up to here a forward is EXACT (above), at 1.3 times the time (9000 rows of 3584: 60.7 against 46.7 us; 6030 of 1536: 16.8 against
-// 13.4; 200000 of 64: 26.4 against 19.8; 60000 of 3584 would take 380 instead of 280); sums over more rows smooth the others out.
-constexpr int64_t kExactValues = 1 << 25;
 template <class T, int CH, bool BWD, bool SHIFT>
 static int launch_norm(NormArgs& a, const NormPlan& p, int& grid, cudaStream_t s) {
   if constexpr (!BWD && sizeof(T) == 2)
-    if (a.in[1] && a.post && a.N <= kExactValues / a.d) return launch_as<T, CH, BWD, SHIFT, true>(a, p, grid, s);
+    if (a.in[1] && a.post) return launch_as<T, CH, BWD, SHIFT, true>(a, p, grid, s);
   return launch_as<T, CH, BWD, SHIFT, false>(a, p, grid, s);
 }
 template <class T, bool BWD>
