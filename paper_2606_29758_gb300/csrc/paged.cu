@@ -123,7 +123,10 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
 // heads) as rows, so that eight heads fill a product's columns; P in two bf16 parts (2^-17 of a weight), so that a
 // short sequence's outputs are rounded once. The rows of tcgen05 products would be 64 or more of one operand in
 // shared memory and accumulators in TMEM, whose round trips a chunk of 16 keys would wait for, and these
-// products are a few per cent of what mma.sync does.
+// products are a few per cent of what mma.sync does. More than eight heads a key head: sixteen a unit (16 on one key head, 64
+// sequences of 2300 keys 25.8 us, eight a unit 27.0; 16 of 7 heads would take 59 -> 64).
+// 128 sequences of about 2300 keys, 28 / 4 heads of 128: 102 us, 6.0 TB/s; of 12400 keys 481 us, 6.8 TB/s; one of 16384 keys 13.6
+// us, of which the two launches, the lists and the join are 10: latency.
 constexpr int kDecWarps = 4;
 constexpr int kDecThreads = 32 * kDecWarps;
 constexpr int kChunk = 16;                        // keys of a warp's share of a tile
@@ -318,116 +321,142 @@ struct DecodeMath<Bf16, DP, NB> {
   }
 };
 
+// NB heads on the f32 pipe, two f32 an instruction. Scores: eight lanes (sixteen of 256 dims) a key, each with its share of the dims
+// of all heads' queries in registers; the lanes' sums are handed out so that a lane ends with one head's score (seven exchanges for
+// eight heads), and has that head's m and l. Outputs: a lane has four dims (or eight) of all heads, of every key or every second.
+// (With the queries in shared memory, half a key's dims a lane, a load came with every four products: 64 sequences of 2300 keys,
+// 28 query heads on 4 of 128 dims, 212 us instead of 131, 4.6 TB/s; 5 on one of 64 62 instead of 24.)
 template <int DP, int NB>
-struct DecodeMath<float, DP, NB> {   // NB heads on the f32 pipe: a lane has half of a key's dims, then four dims of all keys' values
-  static constexpr int kHeads = NB, kRow = DP * 4, kHalf = DP / 2 + 4, kQBytes = kHeads * 2 * kHalf * 4;
-  static constexpr int kOwn = (DP + 127) / 128;   // pieces of four dims a lane has
-  float o[kHeads][kOwn][4];
-  float m[kHeads], l[kHeads];                     // the same in all lanes
+struct DecodeMath<float, DP, NB> {
+  static constexpr int kHeads = NB, kRow = DP * 4, kQBytes = 0;
+  static constexpr int kLanes = DP > 128 ? 16 : 8, kKeys = 32 / kLanes, kRounds = kChunk / kKeys;   // lanes a key, keys at a time
+  static constexpr int kPieces = DP / 4 / kLanes;               // of four dims, a lane's of a key
+  static constexpr int kTurns = DP < 128 ? 2 : 1, kOwn = DP < 128 ? 1 : DP / 128;   // lanes that share dims of the outputs; pieces of those a lane
+  F2 q[kHeads][kPieces][2];
+  F2 o[kHeads][kOwn][2];
+  float m, l;                                                   // of this lane's head; l of its keys
 
-  __device__ __forceinline__ void load(const float* qs, int heads, int D, uint8_t* mem, int lane) {
-    float* q = reinterpret_cast<float*>(mem);
-    __syncwarp();
-    for (int i = lane; i < kHeads * DP; i += 32) {
-      const int head = i / DP, at = i % DP;
-      q[(head * 2 + at / (DP / 2)) * kHalf + at % (DP / 2)] = head < heads && at < D ? qs[head * D + at] : 0.f;
-    }
-    __syncwarp();
+  static __device__ __forceinline__ int head_of(int lane) { return (lane & (kLanes - 1)) / (kLanes / kHeads); }
+  static __device__ __forceinline__ int piece(int w, int lane) { return kTurns == 2 ? lane & 15 : w * 32 + lane; }
+
+  __device__ __forceinline__ void load(const float* qs, int heads, int D, uint8_t*, int lane) {
 #pragma unroll
     for (int h = 0; h < kHeads; ++h) {
-      m[h] = -INFINITY;
-      l[h] = 0.f;
 #pragma unroll
-      for (int w = 0; w < kOwn; ++w)
+      for (int i = 0; i < kPieces; ++i) {
+        const int at = 4 * ((lane & (kLanes - 1)) + kLanes * i);
+        const float4 v = h < heads && at < D ? *reinterpret_cast<const float4*>(qs + h * D + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+        q[h][i][0] = pair2(v.x, v.y);
+        q[h][i][1] = pair2(v.z, v.w);
+      }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[h][w][i] = 0.f;
+      for (int w = 0; w < kOwn; ++w) o[h][w][0] = o[h][w][1] = pair2(0.f, 0.f);
     }
+    m = -INFINITY;
+    l = 0.f;
   }
-  __device__ __forceinline__ void poison() {
+  __device__ __forceinline__ void poison() { l = __int_as_float(0x7fffffff); }
+  // piece p of row r
+  static __device__ __forceinline__ void at(uint32_t base, int r, int p, F2& a, F2& b) {
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a.v), "=l"(b.v) : "r"(base + r * kRow + ((p ^ (r & 7)) << 4)) : "memory");
+  }
+  __device__ __forceinline__ void chunk(uint32_t ks, uint32_t vs, int lo, int nv, float scale2, const uint8_t*, float* ps, int lane) {
+    const int g = lane & (kLanes - 1), sub = lane / kLanes;
+    float x[kRounds];   // of keys sub, kKeys + sub, ...
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h) l[h] = __int_as_float(0x7fffffff);
-  }
-  __device__ __forceinline__ float4 at(uint32_t base, int r, int p) {
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                 : "r"(base + r * kRow + ((p ^ (r & 7)) << 4))
-                 : "memory");
-    return v;
-  }
-  __device__ __forceinline__ void chunk(uint32_t ks, uint32_t vs, int lo, int nv, float scale2, const uint8_t* mem, float* ps, int lane) {
-    const int key = lane & 15, half = lane >> 4;
-    const float* q = reinterpret_cast<const float*>(mem) + half * kHalf;
-    float s[kHeads], u[kHeads];   // (two sums each, half as long)
+    for (int n = 0; n < kRounds; ++n) {
+      F2 s[kHeads];
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h) s[h] = u[h] = 0.f;
-#pragma unroll 4
-    for (int p = 0; p < DP / 8; ++p) {
-      const float4 k = at(ks, key, half * (DP / 8) + p);
+      for (int h = 0; h < kHeads; ++h) s[h] = pair2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        F2 a, b;
+        at(ks, n * kKeys + sub, g + kLanes * i, a, b);
+#pragma unroll
+        for (int h = 0; h < kHeads; ++h) s[h] = fma2(b, q[h][i][1], fma2(a, q[h][i][0], s[h]));
+      }
+      float v[kHeads];
 #pragma unroll
       for (int h = 0; h < kHeads; ++h) {
-        const float4 w = *reinterpret_cast<const float4*>(q + h * 2 * kHalf + 4 * p);
-        s[h] = fmaf(k.x, w.x, fmaf(k.y, w.y, s[h]));
-        u[h] = fmaf(k.z, w.z, fmaf(k.w, w.w, u[h]));
+        float b;
+        split2(s[h], v[h], b);
+        v[h] += b;
+      }
+#pragma unroll
+      for (int d = kLanes / 2; d >= 1; d >>= 1) {   // lane distance d: half of the values each, while there are several
+        const int left = kHeads * 2 * d / kLanes;
+        const bool up = lane & d;
+        if (left > 1) {
+#pragma unroll
+          for (int k = 0; k < left / 2; ++k)
+            v[k] = (up ? v[k + left / 2] : v[k]) + __shfl_xor_sync(0xffffffffu, up ? v[k] : v[k + left / 2], d);
+        } else {
+          v[0] += __shfl_xor_sync(0xffffffffu, v[0], d);
+        }
+      }
+      x[n] = v[0];
+    }
+    float top = m;
+#pragma unroll
+    for (int n = 0; n < kRounds; ++n)
+      if (n * kKeys + sub >= lo && n * kKeys + sub < nv) top = fmaxf(top, x[n] * scale2);
+    if (kLanes == 8) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+    if (__any_sync(0xffffffffu, top != m)) {
+      const float f = top == m ? 1.f : ex2_ftz(m - top);
+      m = top;
+      l *= f;
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h) {
+        const float fh = __shfl_sync(0xffffffffu, f, h * (kLanes / kHeads));
+        const F2 f2 = pair2(fh, fh);
+#pragma unroll
+        for (int w = 0; w < kOwn; ++w) {
+          o[h][w][0] = mul2(o[h][w][0], f2);
+          o[h][w][1] = mul2(o[h][w][1], f2);
+        }
       }
     }
 #pragma unroll
-    for (int h = 0; h < kHeads; ++h) {
-      s[h] += u[h];
-      s[h] += __shfl_xor_sync(0xffffffffu, s[h], 16);
-      const float x = key >= lo && key < nv ? s[h] * scale2 : -INFINITY;
-      float v = x;
-#pragma unroll
-      for (int i = 8; i >= 1; i >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, i));
-      const float top = fmaxf(m[h], v);
-      if (top != m[h]) {
-        const float f = ex2_ftz(m[h] - top);
-        m[h] = top;
-        l[h] *= f;
-#pragma unroll
-        for (int w = 0; w < kOwn; ++w)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[h][w][i] *= f;
-      }
+    for (int n = 0; n < kRounds; ++n) {
+      const int key = n * kKeys + sub;
+      const float scaled = key >= lo && key < nv ? x[n] * scale2 : -INFINITY;
       // (the scaled score is rounded with the difference only)
-      const float p = x == -INFINITY ? 0.f : ex2_ftz(fmaf(s[h], scale2, m[h] == -INFINITY ? 0.f : -m[h]));
-      float t = p;
-#pragma unroll
-      for (int i = 8; i >= 1; i >>= 1) t += __shfl_xor_sync(0xffffffffu, t, i);
-      l[h] += t;
-      if ((h * 2 >= kHeads) == half || kHeads == 1) ps[h * kChunk + key] = p;
+      const float p = scaled == -INFINITY ? 0.f : ex2_ftz(fmaf(x[n], scale2, m == -INFINITY ? 0.f : -m));
+      l += p;
+      ps[head_of(lane) * kChunk + key % kTurns * (kChunk / kTurns) + key / kTurns] = p;
     }
     __syncwarp();
+    const int turn = kTurns == 2 ? lane >> 4 : 0;
 #pragma unroll
-    for (int r = 0; r < kChunk; r += 4) {
+    for (int r = 0; r < kChunk; r += 4 * kTurns) {
       if (r >= nv) break;
-      float4 v[kOwn][4];
+      F2 v[kOwn][4][2];
 #pragma unroll
       for (int w = 0; w < kOwn; ++w)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          v[w][i] = w * 32 + lane < DP / 4 ? at(vs, r + i, w * 32 + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < 4; ++i) at(vs, r + i * kTurns + turn, piece(w, lane), v[w][i][0], v[w][i][1]);
 #pragma unroll
       for (int h = 0; h < kHeads; ++h) {
-        const float4 p = *reinterpret_cast<const float4*>(ps + h * kChunk + r);
+        const float4 p = *reinterpret_cast<const float4*>(ps + h * kChunk + turn * (kChunk / kTurns) + r / kTurns);
         const float pv[4] = {p.x, p.y, p.z, p.w};
 #pragma unroll
-        for (int w = 0; w < kOwn; ++w)
+        for (int i = 0; i < 4; ++i) {
+          const F2 p2 = pair2(pv[i], pv[i]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            o[h][w][0] = fmaf(pv[i], v[w][i].x, o[h][w][0]);
-            o[h][w][1] = fmaf(pv[i], v[w][i].y, o[h][w][1]);
-            o[h][w][2] = fmaf(pv[i], v[w][i].z, o[h][w][2]);
-            o[h][w][3] = fmaf(pv[i], v[w][i].w, o[h][w][3]);
+          for (int w = 0; w < kOwn; ++w) {
+            o[h][w][0] = fma2(p2, v[w][i][0], o[h][w][0]);
+            o[h][w][1] = fma2(p2, v[w][i][1], o[h][w][1]);
           }
+        }
       }
     }
     __syncwarp();
   }
   __device__ __forceinline__ void put_ml(float2* ml, int lane) {
-#pragma unroll
-    for (int h = 0; h < kHeads; ++h)
-      if (lane == h) ml[h] = make_float2(m[h], l[h]);
+    if (kLanes == 8) l += __shfl_xor_sync(0xffffffffu, l, 8);
+    l += __shfl_xor_sync(0xffffffffu, l, 16);
+    if (lane < kLanes) ml[head_of(lane)] = make_float2(m, l);   // (lanes of the same head have the same)
   }
   template <class F>
   __device__ __forceinline__ void add_o(float* to, F&& factor, bool first, int lane) {
@@ -436,14 +465,21 @@ struct DecodeMath<float, DP, NB> {   // NB heads on the f32 pipe: a lane has hal
       const float f = factor(h);
 #pragma unroll
       for (int w = 0; w < kOwn; ++w) {
-        if (w * 32 + lane >= DP / 4) continue;
-        float4& at = *reinterpret_cast<float4*>(to + h * (DP + 4) + (w * 32 + lane) * 4);
+        float x[4];
+        split2(o[h][w][0], x[0], x[1]);
+        split2(o[h][w][1], x[2], x[3]);
+        if (kTurns == 2) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], 16);
+          if (lane >= 16) continue;
+        }
+        float4& at = *reinterpret_cast<float4*>(to + h * (DP + 4) + piece(w, lane) * 4);
         float4 v = first ? make_float4(0.f, 0.f, 0.f, 0.f) : at;
         if (f != 0.f) {
-          v.x += o[h][w][0] * f;
-          v.y += o[h][w][1] * f;
-          v.z += o[h][w][2] * f;
-          v.w += o[h][w][3] * f;
+          v.x += x[0] * f;
+          v.y += x[1] * f;
+          v.z += x[2] * f;
+          v.w += x[3] * f;
         }
         at = v;
       }
@@ -455,7 +491,9 @@ template <class T, int DP, int NB>
 struct DecodeCfg {
   using Math = DecodeMath<T, DP, NB>;
   static constexpr int kChunkBytes = kChunk * DP * static_cast<int>(sizeof(T));   // of keys, and of values
-  static constexpr int kStages = kChunkBytes >= 16384 ? 1 : kChunkBytes >= 4096 ? 3 : 4;
+  // rows of 512 bytes: one stage and two blocks an SM rather than three and one (64 sequences of 2300 keys: f32, 28 / 4 heads of 128,
+  // 162 -> 131 us; bf16, 4 / 4 of 256, 103 -> 95.5)
+  static constexpr int kStages = kChunkBytes >= 8192 ? 1 : kChunkBytes >= 4096 ? 3 : 4;
   static constexpr int kRing = kStages * 2 * kChunkBytes;
   static constexpr int kPs = sizeof(T) == 4 ? Math::kHeads * kChunk * 4 : 0;
   static constexpr int kWarp = kRing + Math::kQBytes + kPs;
@@ -771,9 +809,9 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks))
   }
 }
 
-// The units that several CTAs had parts of, and the call's status. BY_UNIT (few units, so long ones): a block for each head of each unit, whose warps share the parts; else a block for each CTA, which joins the unit that begins there and
-// goes on, a warp a head where the parts are few. What a block needs it finds by one load, then the parts and their m and l
-// come eight at a time. (A block for each head of each CTA that looks for its parts took 9 us, a third of it to start them.)
+// The units that several CTAs had parts of, and the call's status. BY_UNIT (few units, so long ones): a block for each head of
+// each unit, whose warps share the parts; else a block for each CTA, which joins the unit that begins there and goes on, a warp a
+// head where the parts are few. What a block needs it finds by one load, then the parts and their m and l come eight at a time. (A block for each head of each CTA that looks for its parts took 9 us, a third of it to start them.)
 constexpr int kJoinThreads = 256;
 template <class T, int DP, int H, bool BY_UNIT>
 __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecodeArgs a, int ctas) {
@@ -1035,9 +1073,8 @@ int ps_paged_decode(int seqs, int Hq, int Hk, int D, int dtype, const void* q, i
   };
   auto f32 = [&](auto DP) {
     constexpr int D_ = decltype(DP)::value;
-    return a.group == 1   ? launch_decode<float, D_, 1, false>(a, s)
-           : a.group <= 4 ? launch_decode<float, D_, 4, false>(a, s)
-                          : launch_decode<float, D_, 8, false>(a, s);
+    if (a.group == 1) return launch_decode<float, D_, 1, false>(a, s);
+    return a.group > 4 ? launch_decode<float, D_, 8, false>(a, s) : launch_decode<float, D_, 4, false>(a, s);
   };
   const std::integral_constant<int, 1> one;
   const std::integral_constant<int, 2> two;
@@ -1046,7 +1083,7 @@ int ps_paged_decode(int seqs, int Hq, int Hk, int D, int dtype, const void* q, i
   const std::integral_constant<int, 256> d256;
   int out;
   if (dtype == PS_DTYPE_F32)
-    out = D <= 128 ? f32(d128) : f32(d256);
+    out = D <= 64 ? f32(d64) : D <= 128 ? f32(d128) : f32(d256);
   else if (D <= 64)
     out = a.group <= 8 ? bf16(d64, one) : bf16(d64, two);
   else if (D <= 128)
