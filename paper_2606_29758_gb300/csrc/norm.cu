@@ -438,7 +438,8 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
           const uint4 w = *reinterpret_cast<const uint4*>(slot(st, 1, j));
           m = max_abs2(max_abs2(m, w.x), max_abs2(w.y, max_abs2(w.z, w.w)));
         }
-        const float most = fmaxf(__uint_as_float(m << 16 & 0x7fffffffu), __uint_as_float(m & 0x7fff0000u)), from = most * most;
+        const float most = fmaxf(__uint_as_float(m << 16 & 0x7fffffffu), __uint_as_float(m & 0x7fff0000u));
+        const float from = most < 1e18f ? most * most : 0.f;   // (a sum near f32's range from 0 on)
         const P2 minus = two(-1.f, -1.f), one = two(1.f, 1.f);
         P2 hi = two(from, from), lo = zero2;
 #pragma unroll

@@ -69,6 +69,25 @@ def test_the_sum_is_rounded_alike_however_rows_lie(N, d):
         assert torch.equal(place[0], want), (off, pitch)
 
 
+@pytest.mark.parametrize("d", [40, 300, 3584])
+def test_sums_near_the_end_of_the_range(d):
+    """A row whose squares add up to 1.5e38 to 3e38, one with zeros alone, one with an infinity: the root's f32 error (d 2^-24) and the
+    sum's rounding to bf16. Behind the infinity the root is 0."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    x, y = _rows(g, 5, d), _rows(g, 5, d)
+    y[0, d // 2] = 1.22e19
+    y[1, 0], y[1, d - 1] = -1.22e19, 1.22e19
+    y[2] = 0
+    y[3, 3] = float("inf")
+    h, o = _norm(5, d, train=False).forward(x, y)
+    rows = [0, 1, 2, 4]
+    hw, _ = ob.norm_forward(*(t[rows].double().cpu().numpy() for t in (x, y)), np.ones(d), np.ones(d), np.ones(4), 1.0, 1.0, 1e-6, True)
+    got, size = h[rows].double().cpu().numpy(), np.abs(hw) + np.abs(x[rows].double().cpu().numpy())
+    assert (np.abs(got - hw) <= (2.0 ** -8 + d * 2.0 ** -24) * size).all()
+    rest = torch.arange(d, device="cuda") != 3
+    assert h[3, 3].isnan() and torch.equal(h[3][rest], x[3][rest]) and o[3].isnan().all()
+
+
 @pytest.mark.parametrize("dt,d", [(BF, 16377), (BF, 16384), (F32, 8189), (F32, 8192)])
 def test_the_widest_rows_of_all_alignments(dt, d):
     """Sums of d squares and products: d 2^-24 of the sums of their sizes at most, both ways, plus the output's rounding."""
