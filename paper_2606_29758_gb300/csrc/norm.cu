@@ -61,7 +61,7 @@ struct NormArgs {
   float* part;                    // backward: [blocks][2][d] partial gain gradients (dgy, dgo), nullptr without
 };
 
-// Two columns: in the forward the two f32 of one instruction (60000 rows of 3584 bf16, post norm and gate, 306 -> 295 us), in the
+// Two columns: in the forward the two f32 of one instruction (60000 rows of 3584 bf16, post norm and gate, sums in one f32, 306 -> 295 us), in the
 // backward plain ones, whose registers the packed ones' pairs would overrun (515 / 537 us).
 struct Plain2 {
   float x, y;
@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
     for (int i = 0; i < A * CH; ++i) *reinterpret_cast<uint4*>(mine + st * stage_bytes + i * step) = make_uint4(0, 0, 0, 0);
   };
   // the row's gate, beside its pieces (loaded ahead into a register it is waited for where the loop hands it on: 346 instead of
-  // 271 us for a forward of 60000 rows of 3584 bf16)
+  // 271 us for a forward of 60000 rows of 3584 bf16, sums in one f32)
   float* const gates = reinterpret_cast<float*>(norm_smem + ST * stage_bytes) + tid;
   for (int s = 0; s < ST; ++s) {
     clear_row(s);
@@ -721,10 +721,11 @@ struct NormPlan {
   int ch, team, teams, threads, blocks_a_sm;
   size_t smem;
 };
-// Threads of two chunks of a row each (of few chunks: one), up to 512 to a row, then four each.
+// Threads of two chunks of a row each, up to 512 to a row, then four each. (One chunk each: 183750 rows of 128 bf16 47 and 62 us
+// instead of 36 and 56; four: 100000 of 1536 321 instead of 234 forward.)
 static NormPlan norm_plan(int chunks, int d, bool bwd) {
   NormPlan p;
-  p.ch = chunks <= 32 ? 1 : 2;
+  p.ch = 2;
   while ((chunks + p.ch - 1) / p.ch > kNormThreads) p.ch *= 2;
   const int need = (chunks + p.ch - 1) / p.ch;
   if (need <= 32) {
@@ -791,7 +792,6 @@ static int run_norm(NormArgs a, bool shift, int& grid, cudaStream_t s) {
   a.inv_d = static_cast<float>(1.0 / a.d);
   a.inv_d_lo = static_cast<float>(1.0 / a.d - a.inv_d);
   switch (p.ch) {
-    case 1: return shift ? launch_norm<T, 1, BWD, true>(a, p, grid, s) : launch_norm<T, 1, BWD, false>(a, p, grid, s);
     case 2: return shift ? launch_norm<T, 2, BWD, true>(a, p, grid, s) : launch_norm<T, 2, BWD, false>(a, p, grid, s);
     default: return shift ? launch_norm<T, 4, BWD, true>(a, p, grid, s) : launch_norm<T, 4, BWD, false>(a, p, grid, s);
   }
