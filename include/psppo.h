@@ -613,9 +613,9 @@ int ps_residual_norm_bwd(int64_t N, int d, int dtype, int norms, const void* dou
  *   o may be q (same pointer and pitch); lse [seqs][Hq] f32 or NULL. Table entries behind a sequence's last page are not read;
  *   slots behind its length may hold anything. A length outside [0, ldt page] sets PS_DEV_BAD_LENGTH, a page id outside
  *   [0, pages) PS_DEV_BAD_PAGE; those sequences' outputs (the page's key heads') are NaN. Copies that never come set
- *   PS_DEV_TIMEOUT. Sums and weights are f32 (the weights as operands of the tensor cores in two bf16 parts, 2^-17, so that an
- *   infinite value may give NaN where one part would give an infinity); a fixed order, reruns are bit-identical; the order
- *   depends on the lengths of all sequences of the call.
+ *   PS_DEV_TIMEOUT. Sums and weights are f32 (of a bf16 cache the weights as operands of the tensor cores in three bf16 parts, all
+ *   of f32's bits, so that an infinite value may give NaN where one part would give an infinity); a fixed order, reruns are
+ *   bit-identical; the order depends on the lengths of all sequences of the call.
  *   Workspace: ps_paged_decode_workspace_size(D).
  * Limits: 16 <= D <= 256, a multiple of 16, Hk <= Hq <= 65536, a multiple, pages >= 1, 16-byte aligned pointers.
  * ------------------------------------------------------------------------- */

@@ -120,8 +120,11 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
 // their lanes' copies fill some tiles ahead, across units; within a unit nothing crosses warps. What a CTA has
 // of a unit that it does not hold whole goes to the workspace (two slots a CTA), and decode_join_kernel adds those up.
 // bf16: products by mma.sync with the keys (S^T = K Q^T, 16 keys x 8 heads) and the values' dims (O^T = V^T P^T, 16 dims x 8
-// heads) as rows, so that eight heads fill a product's columns; P in two bf16 parts (2^-17 of a weight), so that a
-// short sequence's outputs are rounded once. The rows of tcgen05 products would be 64 or more of one operand in
+// heads) as rows, so that eight heads fill a product's columns; P in three bf16 parts, which hold all 24 bits of a weight, and a
+// chunk's products in a sum of their own that an f32 addition joins to o, as the tensor cores cut what they add to a large
+// sum off at its last bit instead of rounding it. (Two parts, 2^-17 of a weight, and sums by the tensor cores over all chunks left
+// 0.15 to 0.3 % of the outputs at another bf16 than the nearest, f32 sums of the plain form 0.04 to 0.13 %, these 0.02 to 0.04 %; 128
+// sequences of 12400 keys 482 -> 489 us, one of 16384 keys 13.6 -> 14.5.) The rows of tcgen05 products would be 64 or more of one operand in
 // shared memory and accumulators in TMEM, whose round trips a chunk of 16 keys would wait for, and these
 // products are a few per cent of what mma.sync does. More than eight heads a key head: sixteen a unit (16 on one key head, 64
 // sequences of 2300 keys 25.8 us, eight a unit 27.0; 16 of 7 heads would take 59 -> 64).
@@ -173,6 +176,12 @@ static __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// A product of its own: c = a b.
+static __device__ __forceinline__ void mma_bf16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+               : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 // 16 bytes global -> shared, or zeros.
 static __device__ __forceinline__ void lane_copy_or_zero(uint32_t dst, const void* src, bool in) {
@@ -233,7 +242,7 @@ struct DecodeMath<Bf16, DP, NB> {
       for (int n = 0; n < NB; ++n) mma_bf16(s[n], a, q[n][k][0], q[n][k][1]);
     }
     const int key = lane / 4;
-    uint32_t ph[NB][2], pl[NB][2];
+    uint32_t w[3][NB][2];   // the weights' parts, the largest last
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       float x[4], top[2];
@@ -271,10 +280,14 @@ struct DecodeMath<Bf16, DP, NB> {
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint32_t h = pack_bf16x2(p[2 * i], p[2 * i + 1]);
-        const uint32_t w = pack_bf16x2(p[2 * i] - __uint_as_float(h << 16), p[2 * i + 1] - __uint_as_float(h & 0xffff0000u));
-        ph[n][i] = transposed(h);
-        pl[n][i] = transposed(w);
+        float u = p[2 * i], v = p[2 * i + 1];
+#pragma unroll
+        for (int k = 2; k >= 0; --k) {
+          const uint32_t part = pack_bf16x2(u, v);
+          u -= __uint_as_float(part << 16);
+          v -= __uint_as_float(part & 0xffff0000u);
+          w[k][n][i] = transposed(part);
+        }
       }
     }
     const int row = (lane & 7) + (hi << 3);
@@ -285,8 +298,12 @@ struct DecodeMath<Bf16, DP, NB> {
       ldsm4_t(a, (va ^ ((t & 3) * 32)) + (t >> 2) * kBoxBytes);
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        mma_bf16(o[n][t], a, ph[n][0], ph[n][1]);
-        mma_bf16(o[n][t], a, pl[n][0], pl[n][1]);
+        float c[4];
+        mma_bf16_first(c, a, w[0][n][0], w[0][n][1]);
+        mma_bf16(c, a, w[1][n][0], w[1][n][1]);
+        mma_bf16(c, a, w[2][n][0], w[2][n][1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n][t][i] += c[i];
       }
     }
   }
