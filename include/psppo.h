@@ -562,7 +562,7 @@ int ps_dropout_rows(int64_t N, int d, int dtype, const void* x, int64_t ldx, con
  *   n = y r_y gy, r_y = (mean over the row of y^2 + eps)^(-1/2) with PS_NORM_BRANCH, else 1;
  *   h = res_scale x + branch_scale gate_i n;  with PS_NORM_OUT o = h r_h go, r_h = (mean h^2 + eps)^(-1/2), taken from h
  *   before it is rounded to the rows' type. (bf16 h after the branch's norm: the f32 nearest to the sum, rounded, in whatever
- *   order the row is summed.) y NULL: no branch, h = x whatever res_scale is (not written), o its norm.
+ *   order the row is summed, of branch values below 1e18 and a mean square plus eps of 1e-36 and more.) y NULL: no branch, h = x whatever res_scale is (not written), o its norm.
  *   Backward: dH = dh + r_h (go do - h r_h^2 mean(go do h)), dx = res_scale dH, dn = branch_scale gate_i dH,
  *   dy = r_y (gy dn - y r_y^2 mean(gy dn y)) or gy dn, dgy = sum over rows of dn y r_y, dgo = sum of do h r_h,
  *   dgate_i = branch_scale sum over columns of dH n.
@@ -579,7 +579,9 @@ int ps_dropout_rows(int64_t N, int d, int dtype, const void* x, int64_t ldx, con
  * Workspace: none for the forward; 256 bytes for a backward without gain gradients, else
  *   ps_residual_norm_workspace_size(d).
  * Limits: 1 <= d, rows of at most 32768 bytes (16384 bf16 or 8192 f32 columns; of rows that are not whole 16 bytes at
- *   16-byte boundaries 16377 and 8189, else PS_ERR_UNSUPPORTED), finite scales, eps >= 0.
+ *   16-byte boundaries 16377 and 8189, else PS_ERR_UNSUPPORTED), finite scales, eps >= 0. Squares, their sums and the roots'
+ *   products are f32: a mean square plus eps below 1e-38 forward or 1e-32 backward loses bits (0 gives NaN or infinities, as
+ *   0 / 0), a sum of squares beyond 3e38 counts as infinite.
  * ------------------------------------------------------------------------- */
 enum { PS_NORM_BRANCH = 1, PS_NORM_OUT = 2 };
 int ps_residual_norm_fwd(int64_t N, int d, int dtype, int norms, const void* x, int64_t ldx,

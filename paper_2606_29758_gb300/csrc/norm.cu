@@ -132,7 +132,8 @@ static __device__ __forceinline__ uint32_t low_min2(uint32_t l, float u, float v
   return l;
 }
 // The sum over a warp of h + l, h >= 0 and |l| of up to 32 roundings of h, the same bits in any order: in units of four roundings
-// of the largest h (22 bits) and in 2^-18 of those, by integers. (Exchanges with a sum of two parts each took three times that.)
+// of the largest h (22 bits) and in 2^-18 of those, by integers. (Exchanges with a sum of two parts each took three times that; they
+// are left where the largest h is below 2^-79, whose units f32 would not hold.)
 static __device__ __forceinline__ void warp_sum_two(float& h, float& l) {
   const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(h));
   if (top >= 0x7f800000u) {   // infinite, or not a number
@@ -140,7 +141,12 @@ static __device__ __forceinline__ void warp_sum_two(float& h, float& l) {
     l = 0.f;
     return;
   }
-  const uint32_t e = max(top >> 23, 48u);
+  const uint32_t e = top >> 23;
+  if (e < 48u) {
+#pragma unroll 1
+    for (int o = 16; o >= 1; o >>= 1) add_two(h, l, __shfl_xor_sync(0xffffffffu, h, o), __shfl_xor_sync(0xffffffffu, l, o));
+    return;
+  }
   const float g = __uint_as_float((e - 21) << 23), inv_g = __uint_as_float((275 - e) << 23), magic = 12582912.f;   // 1.5 2^23
   const float big = fmaf(h, inv_g, magic);
   const float rest = fmaf(-(big - magic), g, h) + l, small = fmaf(rest, inv_g * 262144.f, magic);
@@ -506,7 +512,8 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
           ry = rsqrtf(v);
           const float q = ry * ry;
           const float left = fmaf(-v, q, 1.f) - fmaf(v, fmaf(ry, ry, -q), v_lo * q);
-          const float r_lo = v < INFINITY ? 0.5f * ry * left : 0.f, wr = w * ry;
+          // (no step from a root of 0, or from one whose square is beyond f32: v below 3e-39)
+          const float r_lo = fabsf(left) < 1.f ? 0.5f * ry * left : 0.f, wr = w * ry;
           w_lo = fmaf(w, ry, -wr) + fmaf(w, r_lo, w_lo * ry);
           w = wr;
         }

@@ -1,0 +1,38 @@
+"""Residual norms at the ends of their ranges, against float64 (oracle.block): eps of 0 with small rows, rows that are not there, gates of
+0 with scales that f32 rounds, infinities in the stream and in a gate.
+
+Tolerances: those of test_gpu_residual_norm.py hold, whose sums and roots are relative to the rows themselves. A square below f32's
+smallest normal number is off by 2^-150; at a mean square of 1e-38 that is 2^-23 of it at most."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block as ob
+from test_gpu_residual_norm import _case, _check, _n, _op
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _rounded(h):
+    """The f32 nearest to h, rounded to bf16."""
+    return torch.from_numpy(h).float().to(BF).cuda()
+
+
+@pytest.mark.parametrize("d", [40, 256, 300, 771, 3584, 16384])
+def test_small_rows_without_an_epsilon(d):
+    """bf16 rows of 1e-12 to 1e-19 of teams below a warp, of one and of several: h is the f32 nearest to the sum, rounded, while the
+    squares that count are exact in f32 (down to 1e-18); at 1e-19 it is near the sum."""
+    g = torch.Generator().manual_seed(d)
+    sizes = torch.tensor([1e-12, 1e-16, 1e-18, 3e-19, 1e-19, 1.0])[:, None]
+    N = len(sizes)
+    x, gy = torch.randn(N, d, generator=g).to(BF), (1 + 0.3 * torch.randn(d, generator=g)).to(BF)
+    y = (sizes.double() * torch.randn(N, d, generator=g).double()).to(BF)
+    for a, b in ((1.0, 1.0), (0.7, 1.1)):
+        h, o = _op(N, d, BF, eps=0.0, res_scale=a, branch_scale=b, train=False).forward(x.cuda(), y.cuda(), gy.cuda())
+        want, norm = ob.norm_forward(_n(x), _n(y), _n(gy), np.ones(d), np.ones(N), a, b, 0.0, True)
+        exact = [0, 1, 2, 5]
+        assert torch.equal(h[exact], _rounded(want[exact])), (a, b)
+        size = np.abs(a * _n(x)) + np.abs(want - a * _n(x))
+        assert (np.abs(_n(h) - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -18 * size).all()
+        assert (np.abs(_n(o) - norm) <= 2.0 ** -8 * np.abs(norm) + 2.0 ** -16 * (np.abs(norm) + size)).all()
