@@ -590,7 +590,8 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
         }
       }
     } else {
-      const float rh = a.pre ? rsqrtf(fmaf(s[0], a.inv_d, a.eps)) : 0.f, m = -s[K > 1 ? 1 : 0] * a.inv_d * rh * rh;
+      // (0 for rows that are not there: dgo's sums go over them)
+      const float rh = a.pre && live ? rsqrtf(fmaf(s[0], a.inv_d, a.eps)) : 0.f, m = -s[K > 1 ? 1 : 0] * a.inv_d * rh * rh;
       const float ry = a.post ? rsqrtf(fmaf(s[K > 2 ? 2 : 0], a.inv_d, a.eps)) : 1.f;
       const float dot = s[K > 3 ? 3 : 0] + rh * fmaf(m, s[K > 5 ? 5 : 0], s[K > 4 ? 4 : 0]);   // of gy dH y
       const float w = a.b * gate * ry, k = a.post ? -dot * a.inv_d * ry * ry * w : 0.f;

@@ -36,3 +36,25 @@ def test_small_rows_without_an_epsilon(d):
         size = np.abs(a * _n(x)) + np.abs(want - a * _n(x))
         assert (np.abs(_n(h) - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -18 * size).all()
         assert (np.abs(_n(o) - norm) <= 2.0 ** -8 * np.abs(norm) + 2.0 ** -16 * (np.abs(norm) + size)).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("N,d", [(1, 8), (3, 64), (1, 128), (3, 128), (5, 128), (1, 256), (5, 256), (3, 771), (2, 3584)])
+@pytest.mark.parametrize("size", [1.0, 1e-15])
+def test_both_ways_without_an_epsilon(size, N, d, dtype):
+    """Rows that no row lies beside in their warp, aligned and not: nothing of a row that is not there counts."""
+    for pitch, shift in ((None, 0), (d + 3, 1)):
+        c = _case(N, d, dtype, seed=5, pitch=pitch, shift=shift)
+        g = torch.Generator().manual_seed(d)
+        c["x"].copy_(torch.randn(N, d, generator=g).to(dtype))
+        c["y"].copy_((size * torch.randn(N, d, generator=g)).to(dtype))
+        c["gate"] = 0.5 + torch.rand(N, generator=g).cuda()
+        for post in (True, False):
+            m = _op(N, d, dtype, post=post, eps=0.0, res_scale=0.75, branch_scale=0.5)
+            h, o = m.forward(c["x"], c["y"], c["gy"], c["go"], gate=c["gate"])
+            got = m.backward(c["do"], c["dh"], h, c["y"], c["gy"], c["go"], gate=c["gate"])
+            _check(c, (h, o, *got), dtype, post, True, 0.75, 0.5, 0.0, N)
+        m, one = _op(N, d, dtype, eps=0.0), dict(c, gate=None)
+        one["x"].copy_((size * torch.randn(N, d, generator=g)).to(dtype))
+        h, o = m.forward(one["x"], go=c["go"])
+        _check(one, (h, o, *m.backward(c["do"], c["dh"], h, go=c["go"])), dtype, False, True, 1.0, 1.0, 0.0, N, branch=False)
