@@ -569,7 +569,8 @@ int ps_dropout_rows(int64_t N, int d, int dtype, const void* x, int64_t ldx, con
  * x, y, h, o [N][d], bf16 or f32, any pitch >= d and any alignment of whole elements (rows of whole 16 bytes at
  *   16-byte boundaries are fastest, then rows that all lie alike; the order of a row's sums, and so its last bits, goes by how they lie).
  *   gy, go [d] in the rows' type, NULL: 1; gy without PS_NORM_BRANCH scales the branch per column. gate [N] f32 or NULL
- *   (1): a gate of 0 leaves the branch out whatever it holds (NaN and infinities too; dy is then 0). norms:
+ *   (1): a gate of 0 leaves the branch out whatever it holds (NaN and infinities too; dy is then 0), an infinite one leaves
+ *   nothing of its row finite. norms:
  *   PS_NORM_BRANCH | PS_NORM_OUT; without a branch PS_NORM_OUT alone, without PS_NORM_OUT o and go are not used.
  * Backward: dout the gradient of o (read with PS_NORM_OUT), dh that of h (NULL: 0), h the forward's h as it is held (x
  *   where there was no branch; read with PS_NORM_OUT), y, gy, go and gate as the forward's. dx, dy in the rows' type

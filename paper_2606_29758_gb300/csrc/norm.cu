@@ -520,7 +520,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
       }
       const P2 w2 = two(w, w), a2 = two(a.a, a.a), wl2 = two(w_lo, w_lo), al2 = two(a.a_lo, a.a_lo), minus = two(-1.f, -1.f);
       const P2 minus_a = mul2(a2, minus), minus_w = mul2(w2, minus);
-      const bool unit = a.a == 1.f && a.a_lo == 0.f;
+      const bool unit = a.a == 1.f && a.a_lo < 1e-30f;
       V8 h[CH];
       P2 q = zero2;
 #pragma unroll
@@ -537,9 +537,9 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
             if (unit) {
               h[j].p[i] = fma2(wl2, n.p[i], fma2(w2, n.p[i], x.p[i]));
             } else {
-              const P2 ax = mul2(x.p[i], minus_a);
-              const P2 left = fma2(wl2, n.p[i], fma2(x.p[i], al2, fma2(x.p[i], a2, ax)));
-              h[j].p[i] = fma2(fma2(minus_w, n.p[i], ax), minus, left);
+              const P2 wn = mul2(n.p[i], minus_w);   // (of a x an infinity stays one in both parts)
+              const P2 left = fma2(x.p[i], al2, fma2(wl2, n.p[i], fma2(w2, n.p[i], wn)));
+              h[j].p[i] = fma2(fma2(x.p[i], minus_a, wn), minus, left);
             }
             float u, v;
             split2(h[j].p[i], u, v);
@@ -560,7 +560,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < E / 2; ++i) h[j].p[i] = mul2(x.p[i], a2);
+          for (int i = 0; i < E / 2; ++i) h[j].p[i] = mul2(x.p[i], two(a.a + a.a_lo, a.a + a.a_lo));
           if (open) {
             const V8 y = get(st, 1, j), g = gain_y(j);
 #pragma unroll
@@ -874,6 +874,12 @@ int ps_residual_norm_fwd(int64_t N, int d, int dtype, int norms, const void* x, 
   a.a = y ? static_cast<float>(res_scale) : 1.f, a.b = static_cast<float>(branch_scale), a.eps = static_cast<float>(eps);
   a.a_lo = y ? static_cast<float>(res_scale - a.a) : 0.f;
   a.b_lo = static_cast<float>(branch_scale - a.b), a.eps_lo = static_cast<float>(eps - a.eps);
+  if (y && dtype == PS_DTYPE_BF16 && (norms & PS_NORM_BRANCH) && fabsf(a.a) > 1e-30f) {
+    // EXACT: both parts of one sign and neither 0, so that the two products of an infinity add up to it.
+    if (fabs(static_cast<double>(a.a)) > fabs(res_scale)) a.a = nextafterf(a.a, 0.f);
+    a.a_lo = static_cast<float>(res_scale - a.a);
+    if (a.a_lo == 0.f) a.a_lo = copysignf(1e-45f, a.a);
+  }
   a.out0 = h, a.out1 = o, a.ldo0 = ldh, a.ldo1 = ldo;
   int grid;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);

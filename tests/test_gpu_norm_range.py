@@ -58,3 +58,34 @@ def test_both_ways_without_an_epsilon(size, N, d, dtype):
         one["x"].copy_((size * torch.randn(N, d, generator=g)).to(dtype))
         h, o = m.forward(one["x"], go=c["go"])
         _check(one, (h, o, *m.backward(c["do"], c["dh"], h, go=c["go"])), dtype, False, True, 1.0, 1.0, 0.0, N, branch=False)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [40, 771, 3584])
+@pytest.mark.parametrize("post", [True, False])
+@pytest.mark.parametrize("a", [1.0, 0.75, 2.0])
+def test_infinities_of_the_stream_and_of_a_gate(a, post, d, dtype):
+    """An infinity of x, one that a scale makes, a gate of 0 beside one: h as the sum has it, o 0 beside an infinity and NaN in its
+    place. An infinite gate leaves nothing finite."""
+    N, g = 5, torch.Generator().manual_seed(d)
+    x, y = (torch.randn(N, d, generator=g).to(dtype) for _ in range(2))
+    gate = torch.ones(N)
+    x[0, 3], x[0, d - 1] = float("inf"), float("-inf")
+    x[1, 5] = torch.finfo(dtype).max          # (2: beyond the range)
+    gate[2] = float("inf")
+    x[3, 0], gate[3] = float("inf"), 0.0
+    y = torch.where(y == 0, 1, y)
+    h, o = _op(N, d, dtype, post=post, res_scale=a, train=False).forward(x.cuda(), y.cuda(), gate=gate.cuda())
+    with np.errstate(invalid="ignore"):
+        want, norm = ob.norm_forward(_n(x), _n(y), np.ones(d), np.ones(d), _n(gate), a, 1.0, 1e-6, post)
+    want = torch.from_numpy(want).float().to(dtype)
+    assert not torch.isfinite(h[2]).any() and o[2].isnan().all()
+    want[2] = h[2] = 0.0
+    fine = torch.isfinite(want)
+    assert torch.equal(h.cpu()[~fine], want[~fine])
+    off = (h.cpu()[fine].double() - want[fine].double()).abs()      # (a rounding each, and some e of terms below 16)
+    assert (off <= 2.0 ** -7 * want[fine].double().abs() + 2.0 ** -15).all()
+    for i in (0, 3):
+        place = torch.isinf(want[i])
+        assert o.cpu()[i][place].isnan().all() and not o.cpu()[i][~place].any(), i
+    assert torch.isfinite(o[4]).all()
