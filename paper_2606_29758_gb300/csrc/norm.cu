@@ -560,7 +560,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_kernel(const NormArgs a)
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < E / 2; ++i) h[j].p[i] = mul2(x.p[i], two(a.a + a.a_lo, a.a + a.a_lo));
+          for (int i = 0; i < E / 2; ++i) h[j].p[i] = EXACT ? fma2(x.p[i], a2, mul2(x.p[i], al2)) : mul2(x.p[i], a2);
           if (open) {
             const V8 y = get(st, 1, j), g = gain_y(j);
 #pragma unroll

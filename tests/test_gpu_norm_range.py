@@ -89,3 +89,29 @@ def test_infinities_of_the_stream_and_of_a_gate(a, post, d, dtype):
         place = torch.isinf(want[i])
         assert o.cpu()[i][place].isnan().all() and not o.cpu()[i][~place].any(), i
     assert torch.isfinite(o[4]).all()
+
+
+@pytest.mark.parametrize("a", [0.53, 0.65, 1.05, 1.3, 0.7, 1.0])
+def test_shut_gates_and_scales_that_f32_rounds(a):
+    """bf16 after the branch's norm: a x alone is rounded like the sum, from the scale as it was given."""
+    for d in (64, 256, 1024):
+        powers = 2.0 ** (torch.arange(d // 64) - d // 128)
+        x = (torch.arange(128, 256).repeat(d // 64) * powers.repeat_interleave(128)).to(BF).view(2, d).repeat(2, 1)
+        g = torch.Generator().manual_seed(d)
+        y, gate = torch.randn(4, d, generator=g).to(BF), torch.tensor([0.0, 0.0, 1.0, 0.5])
+        h, _ = _op(4, d, BF, res_scale=a, train=False).forward(x.cuda(), y.cuda(), gate=gate.cuda())
+        want, _ = ob.norm_forward(_n(x), _n(y), np.ones(d), np.ones(d), _n(gate), a, 1.0, 1e-6, True)
+        assert torch.equal(h, _rounded(want)), d
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("post", [True, False])
+def test_shut_gates_and_gains_that_are_not_finite(post, dtype):
+    """The branch is left out whatever its gain holds."""
+    N, d, g = 6, 300, torch.Generator().manual_seed(0)
+    x, y = (torch.randn(N, d, generator=g).to(dtype).cuda() for _ in range(2))
+    gy, gate = torch.ones(d, dtype=dtype, device="cuda"), (torch.arange(N) % 2).float().cuda()
+    gy[5], gy[77], gy[299] = float("inf"), float("nan"), float("-inf")
+    h, o = _op(N, d, dtype, post=post, train=False).forward(x, y, gy, gate=gate)
+    assert torch.equal(h[::2], x[::2]) and torch.isfinite(o[::2]).all()
+    assert not torch.isfinite(h[1::2, [5, 77, 299]]).any()
