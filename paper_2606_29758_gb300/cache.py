@@ -87,11 +87,13 @@ class PagedCache:
             B._check(rc, "ps_paged_append")
 
     # ------------------------------------------------------------------ pages
-    def _publish(self, seqs):
-        rows = torch.full((len(seqs), self.width), -1, dtype=torch.int32)
-        for i, b in enumerate(seqs):
-            rows[i, :len(self._own[b])] = torch.tensor(self._own[b], dtype=torch.int32)
-        self.table[torch.tensor(seqs, device=self.device)] = rows.to(self.device)
+    def _publish(self, own):
+        """The pages own[b] of sequences b to the table, wherever it is (before they are taken or given back: a call that fails
+        here leaves the cache as it was)."""
+        rows = torch.full((len(own), self.width), -1, dtype=torch.int32)
+        for i, pages in enumerate(own.values()):
+            rows[i, :len(pages)] = torch.tensor(pages, dtype=torch.int32)
+        self.table[torch.tensor(list(own), device=self.table.device)] = rows.to(self.table.device)
 
     def _seq(self, seq: int) -> int:
         if not 0 <= seq < self.s.seqs:
@@ -107,11 +109,14 @@ class PagedCache:
         own = self._own[seq]
         if need - len(own) > len(self._free):
             raise B.PsppoError(B.PS_ERR_CAPACITY, f"PagedCache.reserve: {need - len(own)} pages wanted, {len(self._free)} free")
-        if need > len(own):
-            for _ in range(need - len(own)):
-                own.append(self._free.pop())
-                self._users[own[-1]] = 1
-            self._publish([seq])
+        more = need - len(own)
+        if more > 0:
+            new = self._free[:-more - 1:-1]
+            self._publish({seq: own + new})
+            del self._free[-more:]
+            for p in new:
+                self._users[p] = 1
+            own += new
 
     def share(self, src: int, dst, n: int):
         """The first n positions of `src` for the sequences `dst`, which have none: whole pages are shared, a begun one is copied."""
@@ -124,29 +129,32 @@ class PagedCache:
         begun = n % s.page != 0
         if begun and len(dst) > len(self._free):
             raise B.PsppoError(B.PS_ERR_CAPACITY, f"PagedCache.share: {len(dst)} pages wanted, {len(self._free)} free")
+        if not dst:
+            return
+        shared, new = self._own[src][:whole], self._free[:-len(dst) - 1:-1] if begun else []
+        for p in new:
+            for c in (self.k, self.v):
+                c[:, p].copy_(c[:, self._own[src][whole]])
+        own = {b: shared + new[i:i + 1] for i, b in enumerate(dst)}
+        self._publish(own)
+        del self._free[len(self._free) - len(new):]
+        for p in shared:
+            self._users[p] += len(dst)
+        for p in new:
+            self._users[p] = 1
         for b in dst:
-            self._own[b] = self._own[src][:whole]
-            for p in self._own[b]:
-                self._users[p] += 1
-            if begun:
-                p = self._free.pop()
-                self._users[p] = 1
-                self._own[b].append(p)
-                for c in (self.k, self.v):
-                    c[:, p].copy_(c[:, self._own[src][whole]])
-        if dst:
-            self._publish(dst)
+            self._own[b] = own[b]
 
     def release(self, seq: int):
         """A sequence's pages back, except those that others still have; its length becomes 0."""
         seq = self._seq(seq)
+        self._publish({seq: []})
+        self.lengths[seq] = 0
         for p in reversed(self._own[seq]):
             self._users[p] -= 1
             if self._users[p] == 0:
                 self._free.append(p)
         self._own[seq] = []
-        self._publish([seq])
-        self.lengths[seq] = 0
 
     def check_status(self):
         """Raise PsppoError if the last append reports a device-side error."""
