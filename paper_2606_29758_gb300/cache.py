@@ -75,6 +75,8 @@ class PagedCache:
         """Rows of k and v [N][Hk * D] to positions row_pos - pos_base of sequences row_seq (-1: the row is passed by)."""
         rc = self._fast(self._plan, layer, k, v, row_seq, row_pos, pos_base)
         if rc is None:
+            if not -2 ** 31 <= pos_base < 2 ** 31:
+                raise ValueError(f"pos_base: {pos_base}, beyond 32 bits")
             s, at = self.s, self._at
             if k.dim() != 2:
                 raise ValueError(f"k: need [N][{s.Hk * s.D}], got {tuple(k.shape)}")
