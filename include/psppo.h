@@ -580,7 +580,7 @@ int ps_dropout_rows(int64_t N, int d, int dtype, const void* x, int64_t ldx, con
  * Workspace: none for the forward; 256 bytes for a backward without gain gradients, else
  *   ps_residual_norm_workspace_size(d).
  * Limits: 1 <= d, rows of at most 32768 bytes (16384 bf16 or 8192 f32 columns; of rows that are not whole 16 bytes at
- *   16-byte boundaries 16377 and 8189, else PS_ERR_UNSUPPORTED), finite scales, eps >= 0. Squares, their sums and the roots'
+ *   16-byte boundaries 16377 and 8189, else PS_ERR_UNSUPPORTED), scales and eps finite in f32, eps >= 0. Squares, their sums and the roots'
  *   products are f32: a mean square plus eps below 1e-38 forward or 1e-32 backward loses bits (0 gives NaN or infinities, as
  *   0 / 0), a sum of squares beyond 3e38 counts as infinite.
  * ------------------------------------------------------------------------- */
@@ -620,7 +620,8 @@ int ps_residual_norm_bwd(int64_t N, int d, int dtype, int norms, const void* dou
  *   of f32's bits, so that an infinite value may give NaN where one part would give an infinity); a fixed order, reruns are
  *   bit-identical; the order depends on the lengths of all sequences of the call.
  *   Workspace: ps_paged_decode_workspace_size(D).
- * Limits: 16 <= D <= 256, a multiple of 16, Hk <= Hq <= 65536, a multiple, pages >= 1, 16-byte aligned pointers.
+ * Limits: 16 <= D <= 256, a multiple of 16, Hk <= Hq <= 65536, a multiple, pages >= 1, 16-byte aligned pointers, scale log2 e finite
+ *   in f32.
  * ------------------------------------------------------------------------- */
 int ps_paged_append(int64_t N, int seqs, int Hk, int D, int dtype, const void* k, int64_t ldk,
                     const void* v, int64_t ldv, const int32_t* row_seq, const int32_t* row_pos, int pos_base,

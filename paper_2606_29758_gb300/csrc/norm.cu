@@ -812,6 +812,7 @@ using namespace psk;
 namespace {
 
 bool norm_sizes_ok(int64_t N, int d, int dtype, int norms, double a, double b, double eps) {
+  auto isfinite = [](double v) { return ::isfinite(static_cast<float>(v)) != 0; };   // (as the kernels have them)
   return N >= 0 && d >= 1 && (dtype == PS_DTYPE_BF16 || dtype == PS_DTYPE_F32) && d <= kNormMaxBytes / elem_bytes(dtype) &&
          !(norms & ~(PS_NORM_BRANCH | PS_NORM_OUT)) && isfinite(a) && isfinite(b) && eps >= 0.0 && isfinite(eps);
 }

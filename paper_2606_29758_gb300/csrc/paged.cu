@@ -1061,7 +1061,8 @@ int ps_paged_decode(int seqs, int Hq, int Hk, int D, int dtype, const void* q, i
                     const void* v_cache, int pages, int page, const int32_t* table, int64_t ldt, const int32_t* lengths, int window,
                     double scale, void* o, int64_t ldo, float* lse, void* ws, size_t ws_bytes, ps_stream_t stream) {
   NvtxRange nvtx_range("ps_paged_decode");
-  if (!pages_ok(seqs, Hk, D, dtype, pages, page, ldt) || Hq < Hk || Hq > 65536 || Hq % Hk || window < 0 || !isfinite(scale))
+  if (!pages_ok(seqs, Hk, D, dtype, pages, page, ldt) || Hq < Hk || Hq > 65536 || Hq % Hk || window < 0 ||
+      !isfinite(static_cast<float>(scale * 1.4426950408889634)))
     return PS_ERR_INVALID_ARG;
   const int e = elem_bytes(dtype);
   const int64_t cols = static_cast<int64_t>(Hq) * D;
