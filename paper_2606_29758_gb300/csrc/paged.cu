@@ -199,12 +199,12 @@ struct DecodeMath;
 
 template <int DP, int NB>
 struct DecodeMath<Bf16, DP, NB> {
-  static constexpr int kHeads = 8 * NB, kQBytes = 0;
+  static constexpr int kHeads = 8 * NB;
   uint32_t q[NB][DP / 16][2];
   float o[NB][DP / 16][4];      // o[dim lane / 4 (+ 8)][head 2 (lane % 4) (+ 1)]
   float m[NB][2], l[NB][2];     // of heads 2 (lane % 4) and the next; l of this lane's keys
 
-  __device__ __forceinline__ void load(const Bf16* qs, int heads, int D, uint8_t*, int lane) {
+  __device__ __forceinline__ void load(const Bf16* qs, int heads, int D, int lane) {
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
       const int head = n * 8 + lane / 4;
@@ -227,7 +227,7 @@ struct DecodeMath<Bf16, DP, NB> {
 #pragma unroll
     for (int n = 0; n < NB; ++n) l[n][0] = l[n][1] = __int_as_float(0x7fffffff);
   }
-  __device__ __forceinline__ void chunk(uint32_t ks, uint32_t vs, int lo, int nv, float scale2, const uint8_t*, float*, int lane) {
+  __device__ __forceinline__ void chunk(uint32_t ks, uint32_t vs, int lo, int nv, float scale2, float*, int lane) {
     const int r = lane & 15, hi = lane >> 4;
     float s[NB][4];
 #pragma unroll
@@ -345,7 +345,7 @@ struct DecodeMath<Bf16, DP, NB> {
 // 28 query heads on 4 of 128 dims, 212 us instead of 131, 4.6 TB/s; 5 on one of 64 62 instead of 24.)
 template <int DP, int NB>
 struct DecodeMath<float, DP, NB> {
-  static constexpr int kHeads = NB, kRow = DP * 4, kQBytes = 0;
+  static constexpr int kHeads = NB, kRow = DP * 4;
   static constexpr int kLanes = DP > 128 ? 16 : 8, kKeys = 32 / kLanes, kRounds = kChunk / kKeys;   // lanes a key, keys at a time
   static constexpr int kPieces = DP / 4 / kLanes;               // of four dims, a lane's of a key
   static constexpr int kTurns = DP < 128 ? 2 : 1, kOwn = DP < 128 ? 1 : DP / 128;   // lanes that share dims of the outputs; pieces of those a lane
@@ -356,7 +356,7 @@ struct DecodeMath<float, DP, NB> {
   static __device__ __forceinline__ int head_of(int lane) { return (lane & (kLanes - 1)) / (kLanes / kHeads); }
   static __device__ __forceinline__ int piece(int w, int lane) { return kTurns == 2 ? lane & 15 : w * 32 + lane; }
 
-  __device__ __forceinline__ void load(const float* qs, int heads, int D, uint8_t*, int lane) {
+  __device__ __forceinline__ void load(const float* qs, int heads, int D, int lane) {
 #pragma unroll
     for (int h = 0; h < kHeads; ++h) {
 #pragma unroll
@@ -377,7 +377,7 @@ struct DecodeMath<float, DP, NB> {
   static __device__ __forceinline__ void at(uint32_t base, int r, int p, F2& a, F2& b) {
     asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a.v), "=l"(b.v) : "r"(base + r * kRow + ((p ^ (r & 7)) << 4)) : "memory");
   }
-  __device__ __forceinline__ void chunk(uint32_t ks, uint32_t vs, int lo, int nv, float scale2, const uint8_t*, float* ps, int lane) {
+  __device__ __forceinline__ void chunk(uint32_t ks, uint32_t vs, int lo, int nv, float scale2, float* ps, int lane) {
     const int g = lane & (kLanes - 1), sub = lane / kLanes;
     float x[kRounds];   // of keys sub, kKeys + sub, ...
 #pragma unroll
@@ -513,7 +513,7 @@ struct DecodeCfg {
   static constexpr int kStages = kChunkBytes >= 8192 ? 1 : kChunkBytes >= 4096 ? 3 : 4;
   static constexpr int kRing = kStages * 2 * kChunkBytes;
   static constexpr int kPs = sizeof(T) == 4 ? Math::kHeads * kChunk * 4 : 0;
-  static constexpr int kWarp = kRing + Math::kQBytes + kPs;
+  static constexpr int kWarp = kRing + kPs;
   static constexpr int kOuts = sizeof(T) == 4 || NB == 1 ? 2 : 1;                 // where the warps' o are added up
   static constexpr int kOut = Math::kHeads * (DP + 4) * 4;
   static constexpr int kSmem = kDecWarps * kWarp + kOuts * kOut;
@@ -553,8 +553,7 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks))
   uint8_t* const mine = dec_smem + warp * Cfg::kWarp;
   const uint32_t ring = smem_addr(mine);
   float* const out_s = reinterpret_cast<float*>(dec_smem + kDecWarps * Cfg::kWarp);
-  uint8_t* const q_s = mine + Cfg::kRing;
-  float* const p_s = reinterpret_cast<float*>(q_s + Math::kQBytes);
+  float* const p_s = reinterpret_cast<float*>(mine + Cfg::kRing);
   const int per_head = a.blocks, HM = a.c.Hk * per_head;    // units a sequence
 
   // dims behind D stay zeros in every stage (TMA fills its last box itself)
@@ -733,11 +732,11 @@ __global__ void __launch_bounds__(kDecThreads, (DecodeCfg<T, DP, NB>::kBlocks))
       const int tile1 = static_cast<int>(min(static_cast<int64_t>(t.tiles), tile0 + (t1 - t.t)));
       const bool whole = tile0 == 0 && tile1 == t.tiles;
       const int64_t end_tile = t.t - tile0 + t.tiles - 1;   // of the list
-      math.load(static_cast<const T*>(a.q) + b * a.ldq + static_cast<int64_t>(h0) * a.c.D, heads, a.c.D, q_s, lane);
+      math.load(static_cast<const T*>(a.q) + b * a.ldq + static_cast<int64_t>(h0) * a.c.D, heads, a.c.D, lane);
       for (int tile = tile0; tile < tile1; ++tile) {
         int lo, nv;
         const uint32_t from = ring + st * 2 * Cfg::kChunkBytes;
-        if (arrive(t, tile, st, lo, nv)) math.chunk(from, from + Cfg::kChunkBytes, lo, nv, a.scale2, q_s, p_s, lane);
+        if (arrive(t, tile, st, lo, nv)) math.chunk(from, from + Cfg::kChunkBytes, lo, nv, a.scale2, p_s, lane);
         if ((bad_stages >> st & 1u) || stuck) {
           math.poison();
           bad |= stuck ? PS_DEV_TIMEOUT : PS_DEV_BAD_PAGE;
