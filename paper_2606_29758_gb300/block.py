@@ -324,7 +324,8 @@ class NormShape:
 
 class ResidualNorm:
     """h = res_scale x + branch_scale gate n(y) and o = n(h), the norms before and after a branch with its gate and the residual
-    sum in one pass, and the gradients (ps_residual_norm_fwd, ps_residual_norm_bwd). Rows may have any pitch."""
+    sum in one pass, and the gradients (ps_residual_norm_fwd, ps_residual_norm_bwd). Rows may have any pitch. o is the norm of the sum
+    before h is rounded to the rows' type; the backward takes h as it is held."""
 
     def __init__(self, shape: NormShape, device: str = "cuda"):
         s = shape

@@ -29,10 +29,12 @@ namespace psk {
 // f32, the sum over the streams is right up to an f32 and a half, and a value that lies so near to the middle of two bf16 values is
 // settled by the roundings that it left. Otherwise some 2 of 10^5 values are rounded to the other neighbour, and one of
 // those may show in dgo's sums over few rows as a hundred times f32's error.
-// That takes a third of the time more (60000 rows of 3584 without a gate 280 -> 364 us, 6030 of 1536 13.4 -> 16.3).
-// Forward and backward of 60000 rows of 3584 bf16 with both norms and a gate 373 and 507 us (4.6 and 5.1 TB/s), without branch norm and
-// gate 258 and 497 (6.7 and 5.2); of 30000 f32 rows 275 and 388 (6.3 and 6.7). Both are bound by latency and issue at the 14 warps
-// of an SM that the registers allow (forward 50 % of the issue slots, backward 61 %), the lighter ones by HBM.
+// That takes a third of the time more (60000 rows of 3584 without a gate 280 -> 374 us, 6030 of 1536 13.4 -> 16.9).
+// Forward and backward of 60000 rows of 3584 bf16 with both norms and a gate 382 and 510 us (4.5 and 5.1 TB/s), without branch norm and
+// gate 258 and 500 (6.7 and 5.2); of 30000 f32 rows 275 and 386 (6.3 and 6.7). Both are bound by latency and issue at the 14 warps
+// of an SM that the registers allow (forward 52 % of the issue slots, backward 61 %), the lighter ones by HBM. Rows of more than 1024
+// chunks (four a thread): 30000 of 8192 bf16 415 and 545 us (4.7 and 5.4 TB/s), 13000 of 16384 400 and 690, 12000 of 8192 f32 283 and
+// 570 (5.5 and 4.1); rows of odd widths: 100000 of 771 bf16 232 and 318 (2.7 and 2.9), f32 268 and 395 (4.6 and 4.7).
 constexpr int kNormThreads = 512;   // at most
 __host__ __device__ constexpr int norm_arrays(bool bwd) { return bwd ? 4 : 2; }   // h, y, do, dh; x, y
 // Rows in shared memory: as many as fit beside what the registers allow of threads.

@@ -114,22 +114,23 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
 // ================================================================== decode
 //   x_j = c q.k_j (c = scale log2 e) over a sequence's keys j, m = max x_j, l = sum 2^(x_j - m), o = sum 2^(x_j - m) v_j / l;
 //   parts of a sequence join by m = max m_i, l = sum l_i 2^(m_i - m), o likewise.
-// HBM-bound: every key and value is read once, for all query heads that share it. The work is a list of tiles of 64 keys of
-// one key head of one sequence (a unit: its query heads, up to 16 of them, in f32 8); each CTA takes an equal run of the list,
-// whatever the lengths are. Its four warps take 16 keys of a tile each, through rings of their own in shared memory that
-// their lanes' copies fill some tiles ahead, across units; within a unit nothing crosses warps. What a CTA has
-// of a unit that it does not hold whole goes to the workspace (two slots a CTA), and decode_join_kernel adds those up.
+// HBM-bound: every key and value is read once for the query heads of a unit, which share it: up to 16 of a key head, in f32 and above
+// 128 dims up to 8 (a key head with more has several units, each of which reads its keys: 32 on one key head, 64 sequences of 2300 keys
+// of 128, bf16 38 us where its bytes take 11, f32 128 and 22). The work is a list of tiles of 64 keys of a unit; each CTA takes an
+// equal run of the list, whatever the lengths are. Its four warps take 16 keys of a tile each, through rings of their own in shared
+// memory that their lanes' copies fill some tiles ahead, across units; within a unit nothing crosses warps. What a CTA has of a unit that it does not hold whole goes to the workspace (two slots a CTA), and decode_join_kernel adds those up.
 // bf16: products by mma.sync with the keys (S^T = K Q^T, 16 keys x 8 heads) and the values' dims (O^T = V^T P^T, 16 dims x 8
 // heads) as rows, so that eight heads fill a product's columns; P in three bf16 parts, which hold all 24 bits of a weight, and a
 // chunk's products in a sum of their own that an f32 addition joins to o, as the tensor cores cut what they add to a large
 // sum off at its last bit instead of rounding it. (Two parts, 2^-17 of a weight, and sums by the tensor cores over all chunks left
 // 0.15 to 0.3 % of the outputs at another bf16 than the nearest, f32 sums of the plain form 0.04 to 0.13 %, these 0.02 to 0.04 %; 128
-// sequences of 12400 keys 482 -> 489 us, one of 16384 keys 13.6 -> 14.5.) The rows of tcgen05 products would be 64 or more of one operand in
-// shared memory and accumulators in TMEM, whose round trips a chunk of 16 keys would wait for, and these
-// products are a few per cent of what mma.sync does. More than eight heads a key head: sixteen a unit (16 on one key head, 64
-// sequences of 2300 keys 25.8 us, eight a unit 27.0; 16 of 7 heads would take 59 -> 64).
-// 128 sequences of about 2300 keys, 28 / 4 heads of 128: 102 us, 6.0 TB/s; of 12400 keys 481 us, 6.8 TB/s; one of 16384 keys 13.6
-// us, of which the two launches, the lists and the join are 10: latency.
+// sequences of 12400 keys 482 -> 489 us, one of 16384 keys 13.6 -> 14.5.) The rows of tcgen05 products would be 64 or more of one
+// operand in shared memory and accumulators in TMEM, whose round trips a chunk of 16 keys would wait for, and these
+// products are a few per cent of what mma.sync does. More than eight heads a key head: sixteen a unit (16 on one key head, 128
+// sequences of 12400 keys 139 us, eight a unit 251; 64 of 2300 27.5 and 26.2, 16 of 1000 11.5 and 10.2; 7 heads, 64 of 2300 55.4 and 57.6).
+// 128 sequences of about 2300 keys, 28 / 4 heads of 128: 103 us, 5.9 TB/s; of 12400 keys 489 us, 6.7 TB/s; one of 16384 keys 14.5
+// us, of which the two launches, the lists and the join are 10: latency. 256 sequences of 3 to 16 keys 14.5 us, f32 22 to 24: a chunk's
+// work for one warp of four, then the unit's join, in turn.
 constexpr int kDecWarps = 4;
 constexpr int kDecThreads = 32 * kDecWarps;
 constexpr int kChunk = 16;                        // keys of a warp's share of a tile
@@ -509,7 +510,8 @@ struct DecodeCfg {
   using Math = DecodeMath<T, DP, NB>;
   static constexpr int kChunkBytes = kChunk * DP * static_cast<int>(sizeof(T));   // of keys, and of values
   // rows of 512 bytes: one stage and two blocks an SM rather than three and one (64 sequences of 2300 keys: f32, 28 / 4 heads of 128,
-  // 162 -> 131 us; bf16, 4 / 4 of 256, 103 -> 95.5)
+  // 163 -> 131 us; bf16, 4 / 4 of 256, 100 -> 97). Of f32 rows of 1024 bytes no more than one stage and one block fit (28 / 4 heads of
+  // 256 441 us, 4 / 4 241, where the bytes take 178).
   static constexpr int kStages = kChunkBytes >= 8192 ? 1 : kChunkBytes >= 4096 ? 3 : 4;
   static constexpr int kRing = kStages * 2 * kChunkBytes;
   static constexpr int kPs = sizeof(T) == 4 ? Math::kHeads * kChunk * 4 : 0;
@@ -999,7 +1001,7 @@ static int launch_decode(DecodeArgs a, cudaStream_t s) {
   if (ctas > most) ctas = static_cast<int>(most);
   const int64_t units = static_cast<int64_t>(a.B) * a.c.Hk * a.blocks;
   // Units of more than four CTAs' runs are joined by unit, a block a head, else by CTA (one sequence of 16384 keys, 4 key heads:
-  // 13.5 us by unit, 26.7 by CTA; 8 of 4096 16.5 and 17.2; 32 of 2300 34.0 and 32.0; 64 of 2300 59.2 and 54.4).
+  // 14.2 us by unit, 27.3 by CTA; 8 of 4096 17.1 and 17.9; 32 of 2300 34.2 and 32.6; 64 of 2300 60.7 and 55.4).
   if (units * 4 > ctas) a.unit = nullptr;
   if (launch_after(kern, dim3(static_cast<unsigned>(ctas)), kDecThreads, Cfg::kSmem, s, 1, 1, true, a, maps[0], maps[1]) != cudaSuccess)
     return PS_ERR_CUDA;
@@ -1090,6 +1092,8 @@ int ps_paged_decode(int seqs, int Hq, int Hk, int D, int dtype, const void* q, i
   };
   auto f32 = [&](auto DP) {
     constexpr int D_ = decltype(DP)::value;
+    // (64 sequences of 2300 keys, 4 key heads of 128: one head each 97 us, by units of four 109; two 107, by units of one 182; four 106,
+    // of eight 130; five 130, of four 206. Of 64 and 256 dims likewise.)
     if (a.group == 1) return launch_decode<float, D_, 1, false>(a, s);
     return a.group > 4 ? launch_decode<float, D_, 8, false>(a, s) : launch_decode<float, D_, 4, false>(a, s);
   };
