@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
 // heads) as rows, so that eight heads fill a product's columns; P in three bf16 parts, which hold all 24 bits of a weight, and a
 // chunk's products in a sum of their own that an f32 addition joins to o, as the tensor cores cut what they add to a large
 // sum off at its last bit instead of rounding it. (Two parts, 2^-17 of a weight, and sums by the tensor cores over all chunks left
-// 0.15 to 0.3 % of the outputs at another bf16 than the nearest, f32 sums of the plain form 0.04 to 0.13 %, these 0.02 to 0.04 %; 128
+// 0.15 to 0.34 % of the outputs at another bf16 than the nearest, f32 sums of the plain form 0.04 to 0.13 %, these 0.02 to 0.06 %; 128
 // sequences of 12400 keys 482 -> 489 us, one of 16384 keys 13.6 -> 14.5.) The rows of tcgen05 products would be 64 or more of one
 // operand in shared memory and accumulators in TMEM, whose round trips a chunk of 16 keys would wait for, and these
 // products are a few per cent of what mma.sync does. More than eight heads a key head: sixteen a unit (16 on one key head, 128
